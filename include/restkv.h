@@ -262,6 +262,114 @@ int restkv_evict(const restkv_params* p, const void* q, const void* k, const voi
                  void* k_out, void* v_out, void* workspace, size_t workspace_bytes, restkv_stream_t stream);
 
 /*
+ * ---- Paged cache -------------------------------------------------------------
+ * What follows an eviction: the kept rows go into pages, decoding appends to them and attends to them, and the
+ * rows come back as dense tensors when the cache is evicted again:
+ *
+ *     restkv_evict -> restkv_append (k_out, v_out, no rotation)
+ *     each step:      restkv_append (new keys and values, rotated)  ->  restkv_attend
+ *     re-eviction:    restkv_attend (window queries) -> restkv_fetch -> restkv_score_from_attention -> ...
+ *
+ * Pages.  A page holds page_size cache positions; `table` names, for each sequence (and, if told so, each KV head), the
+ * page of positions 0 .. page_size-1, of the next page_size, and so on.  Keys and values lie in two arrays of rows, a
+ * row the d channels of one position of one KV head.  The row of position t is row
+ *     table[...][t / page_size] * page_stride + head * head_stride + (t % page_size) * token_stride .
+ * Formats of a row: RESTKV_F32 and RESTKV_BF16, d values of that type; RESTKV_Q4, d/2 bytes of codes, and in a second
+ * array (k_scale, v_scale) d/32 pairs {step, zero} of bfloat16.  Channel c of a 4-bit row is in byte c/2, the even one in
+ * the low half; it belongs to group (c mod (d/16)) / 2, and stands for zero + step * code.  restkv_append makes them so,
+ * in float32, each operation rounded to nearest:
+ *     zero = least of the group, rounded down to bfloat16;  step = (greatest - zero) / 15, rounded up to bfloat16, and at
+ *     least 2^-100 (0 if greatest = zero);  code = (x - zero) * (1 / step), rounded to the nearest integer (even).
+ * So no value is further off than half a step (and float32 rounding).  A group that holds a NaN or an infinity, or
+ * spans more than float32 does, comes back as NaN.
+ *
+ * Lengths.  `lens` says how many positions each sequence (or each KV head of it, after an eviction with
+ * budgets per head) holds INCLUDING the new tokens of the call: new token i of n goes to position len - n + i, and as a
+ * query it sees positions 0 .. len - n + i (all len with causal = 0).  The calls only read `lens`.
+ * New tokens are packed: those of sequence s are rows new_start[s] .. new_start[s+1]-1 of the token tensors
+ * (new_start NULL: max_new of each sequence).  Rows outside all sequences are left as they are.
+ *
+ * Values on the device cannot be refused.  A length beyond the room (max_len) or below 0, a new_start outside
+ * [0, n_tokens] or falling, counts as brought inside; a sequence takes part with its first max_new new tokens at most; a
+ * position without a page (its table entry outside [0, n_pages)) is neither written nor seen.  Table entries behind
+ * the last position in use are not read as pages.  Two positions of one call must not share a slot.
+ */
+#define RESTKV_Q4 4   /* restkv_cache.format: 4-bit codes with a step and a zero for every 32 channels */
+
+typedef struct restkv_cache {
+  int32_t n_seqs;        /* sequences, up to 16384 (0: nothing is done)                          */
+  int32_t n_q_heads;     /* Hq                                                                   */
+  int32_t n_kv_heads;    /* Hkv, divides Hq                                                      */
+  int32_t head_dim;      /* d: 64 or 128                                                         */
+  int32_t dtype;         /* tokens, queries, fetched rows: RESTKV_F32 or RESTKV_BF16             */
+  int32_t format;        /* pages: the same, or RESTKV_Q4                                        */
+  int32_t page_size;     /* positions of a page: a power of two, 16 .. 65536                     */
+  int32_t n_pages;       /* pages there are                                                      */
+  int32_t max_pages;     /* table entries of a sequence; max_pages * page_size <= 2^30           */
+  int32_t max_len;       /* no length is above this (0: max_pages * page_size); a tight one spares launches */
+  int32_t max_new;       /* most new tokens of one sequence in a call                            */
+  int32_t n_tokens;      /* rows of the packed token tensors                                     */
+  int32_t causal;        /* 1: a query sees positions up to its own; 0: all                      */
+  int32_t rotary_dim;    /* channels that are rotated: 0 (none) or a multiple of 16 up to d      */
+  int32_t rotary_pairs;  /* 0: channel c turns with c + rotary_dim/2; 1: channel 2c with 2c + 1  */
+  int32_t n_positions;   /* rows of the tables of cosines and sines                              */
+  int32_t out_dtype;     /* attention output: dtype, or RESTKV_F32                               */
+  float   scale;         /* logit scale; 0 selects 1/sqrt(d)                                     */
+  int64_t page_stride, head_stride, token_stride;   /* rows; token_stride 0: [page][Hkv][page_size];
+                            with tables per head head_stride may be 0.  token_stride <= 2^16     */
+  int64_t table_stride_s, table_stride_h;   /* int32 entries; 0, 0: max_pages, 0 (heads share)   */
+  int64_t lens_stride_s, lens_stride_h;     /* int32 entries; 0, 0: 1, 0 (heads share)           */
+  int64_t q_stride_t, q_stride_h;           /* elements; 0: Hq*d, 0: d                           */
+  int64_t kv_stride_t, kv_stride_h;         /* elements; 0: Hkv*d, 0: d                          */
+  int64_t out_stride_t, out_stride_h;       /* elements; 0: Hq*d, 0: d                           */
+  int64_t lse_stride_t, lse_stride_h;       /* floats;   0: Hq, 0: 1                             */
+} restkv_cache;
+
+/*
+ * New tokens into the pages, keys rotated by their position on the way, and new queries rotated beside them.
+ *   k, v    [n_tokens, Hkv, d] (strides kv_stride_*);  q  [n_tokens, Hq, d] (q_stride_*) or NULL;
+ *   q_out   with q's strides; may be q itself
+ *   k_pages, v_pages (and k_scale, v_scale with RESTKV_Q4): 16-byte aligned
+ *   positions [n_tokens] int32: where each token stands in its text (an evicted cache is shorter than the text);
+ *           NULL: its cache position (not with lens per head).  A token whose position lies outside [0, n_positions)
+ *           is left out: nothing of it is written
+ *   cos, sin [n_positions, rotary_dim/2] float32;  with rotary_dim = 0 all three may be NULL
+ * y[a] = x[a] cos - x[b] sin, y[b] = x[b] cos + x[a] sin for the channels a, b that turn together, in float32 with
+ * each product and each sum rounded, then rounded once to the type of the pages (4-bit: the codes are made from float32).
+ */
+int restkv_append(const restkv_cache* c, const void* k, const void* v, void* k_pages, void* v_pages, void* k_scale,
+                  void* v_scale, const int32_t* table, const int32_t* lens, const int32_t* new_start,
+                  const int32_t* positions, const float* cos, const float* sin, const void* q, void* q_out,
+                  restkv_stream_t stream);
+
+/*
+ * Attention of the new tokens' queries over the pages, which hold their keys and values already (restkv_append):
+ *   out  [n_tokens, Hq, d] out_dtype (out_stride_*):  softmax(scale q K^T) V over the positions a query sees
+ *   lse  [n_tokens, Hq] float32 (lse_stride_*), may be NULL: natural logarithm of the softmax denominator
+ * A query that sees nothing, or only keys of logit -inf, gets 0 and -inf.  What a query does not see has no influence,
+ * whatever it holds (infinities and NaN included); what it sees and is not finite gives an output that is not finite
+ * (with bf16 and 4-bit pages an infinity may come out as NaN).  With out_dtype RESTKV_F32, out_stride_h = W*d, out_stride_t = d,
+ * lse_stride_h = W and lse_stride_t = 1 one sequence's W queries give what restkv_score_from_attention takes.
+ * Logits, statistics and sums are float32 (bf16 products are exact in it); softmax weights enter the products with
+ * values to 2^-17, with float32 output to 2^-24.  Results do not depend on timing: no atomics.
+ * Workspace: restkv_attend_workspace_bytes(c), as for the other calls; not needed (0 bytes) where that returns 0.
+ */
+size_t restkv_attend_workspace_bytes(const restkv_cache* c);
+int restkv_attend(const restkv_cache* c, const void* q, const void* k_pages, const void* v_pages, const void* k_scale,
+                  const void* v_scale, const int32_t* table, const int32_t* lens, const int32_t* new_start, void* out,
+                  float* lse, void* workspace, size_t workspace_bytes, restkv_stream_t stream);
+
+/*
+ * Rows of the pages as dense tensors, 4-bit rows as the values they stand for (the paged sibling of restkv_compact):
+ *   k_out, v_out [n_seqs, Hkv, n_rows, d] dtype, contiguous, 16-byte aligned
+ *   idx  [n_seqs, Hkv, n_rows] int32 positions, or NULL: positions first .. first + n_rows - 1
+ * A position outside [0, len) or without a page gives a row of zeros.
+ */
+int restkv_fetch(const restkv_cache* c, const void* k_pages, const void* v_pages, const void* k_scale, const void* v_scale,
+                 const int32_t* table, const int32_t* lens, const int32_t* idx, int32_t first, int32_t n_rows, void* k_out,
+                 void* v_out, restkv_stream_t stream);
+
+/*
  * Profiling aid (not part of the method): every kernel launch of a selected stage
  * is bracketed by two HIP events on the caller's stream.  stage_mask: bit s selects
  * stage s (see restkv_stage_name), -1 selects all, 0 turns timing off.  A bracket

@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from dataclasses import dataclass
+from dataclasses import dataclass, field
 from typing import Optional
 
 import torch
@@ -20,6 +20,7 @@ LIB_PATH = os.environ.get("RESTKV_LIB") or os.path.join(_PKG, "librestkv.so")
 
 RESTKV_F32 = 0
 RESTKV_BF16 = 1
+RESTKV_Q4 = 4
 # ablation variants (restkv_params.variant, see include/restkv.h)
 RESTKV_IND_ATTENTION = 1
 RESTKV_IND_VALUE_NORM = 2
@@ -39,6 +40,16 @@ class RestkvParams(ctypes.Structure):
         ("q_stride_h", ctypes.c_int64), ("q_stride_t", ctypes.c_int64),
         ("kv_stride_h", ctypes.c_int64), ("kv_stride_t", ctypes.c_int64), ("ld_score", ctypes.c_int64),
     ]
+
+
+class RestkvCache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "n_seqs", "n_q_heads", "n_kv_heads", "head_dim", "dtype", "format", "page_size", "n_pages", "max_pages", "max_len",
+        "max_new", "n_tokens", "causal", "rotary_dim", "rotary_pairs", "n_positions", "out_dtype")] + [
+        ("scale", ctypes.c_float)] + [(n, ctypes.c_int64) for n in (
+            "page_stride", "head_stride", "token_stride", "table_stride_s", "table_stride_h", "lens_stride_s", "lens_stride_h",
+            "q_stride_t", "q_stride_h", "kv_stride_t", "kv_stride_h", "out_stride_t", "out_stride_h", "lse_stride_t",
+            "lse_stride_h")]
 
 
 class RestkvError(RuntimeError):
@@ -78,6 +89,15 @@ def lib() -> ctypes.CDLL:
         L.restkv_compact.argtypes = [P, vp, vp, vp, vp, vp, vp]
         L.restkv_evict.argtypes = [P] + [vp] * 13 + [sz, vp]
         L.restkv_evict.restype = ctypes.c_int
+        C, i32 = ctypes.POINTER(RestkvCache), ctypes.c_int32
+        L.restkv_append.argtypes = [C] + [vp] * 15
+        L.restkv_append.restype = ctypes.c_int
+        L.restkv_attend_workspace_bytes.argtypes = [C]
+        L.restkv_attend_workspace_bytes.restype = sz
+        L.restkv_attend.argtypes = [C] + [vp] * 11 + [sz, vp]
+        L.restkv_attend.restype = ctypes.c_int
+        L.restkv_fetch.argtypes = [C] + [vp] * 7 + [i32, i32, vp, vp, vp]
+        L.restkv_fetch.restype = ctypes.c_int
         L.restkv_strerror.restype = ctypes.c_char_p
         L.restkv_strerror.argtypes = [ctypes.c_int]
         L.restkv_timing_read.argtypes = [vp, vp, ctypes.c_int]
@@ -302,3 +322,213 @@ def evict_layer(p: RestkvParams, q, k, v, gram, buf: LayerBuffers, stream=None, 
     _chk(lib().restkv_evict(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(gram), _ptr(buf.score), _ptr(buf.ema),
                             _ptr(buf.final), _ptr(buf.aws_info), _ptr(buf.aws_d), _ptr(buf.idx), _ptr(buf.k_out),
                             _ptr(buf.v_out), wp, wn, _stream(stream)), "restkv_evict")
+
+
+# ---- paged cache ------------------------------------------------------------------------------
+# Unlike the calls above these check their tensors: what a description says of them is what the kernels go by.
+
+_TYPES = {torch.float32: RESTKV_F32, torch.bfloat16: RESTKV_BF16, "f32": RESTKV_F32, "bf16": RESTKV_BF16, "q4": RESTKV_Q4}
+_TORCH = {RESTKV_F32: torch.float32, RESTKV_BF16: torch.bfloat16, RESTKV_Q4: torch.uint8}
+
+
+def make_cache(*, n_seqs, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages, dtype, format=None, max_new=1,
+               n_tokens=None, max_len=0, causal=True, scale=0.0, rotary_dim=0, interleaved=False, n_positions=0, out_dtype=None,
+               token_major=False, head_lens=False, head_tables=False, out_head_major=False, page_strides=None) -> RestkvCache:
+    """Description of a paged cache and of the calls on it (see restkv_cache in include/restkv.h).
+
+    n_tokens: rows of the packed token tensors (default n_seqs * max_new).  token_major: pages [n_pages, page_size, Hkv, ..]
+    in place of [n_pages, Hkv, page_size, ..].  head_lens: lens [n_seqs, Hkv] in place of [n_seqs].  head_tables: table
+    [n_seqs, Hkv, max_pages] in place of [n_seqs, max_pages], and pages of one head.  page_strides: (page, head, position)
+    in rows, of arrays that are not contiguous.  Strides of token tensors are taken from the tensors of each call."""
+    dt = int(_TYPES.get(dtype, dtype))
+    fmt = dt if format is None else int(_TYPES.get(format, format))
+    heads = 1 if head_tables else n_kv_heads
+    c = RestkvCache(n_seqs, n_q_heads, n_kv_heads, head_dim, dt, fmt, page_size, n_pages, max_pages, max_len, max_new,
+                    n_seqs * max_new if n_tokens is None else n_tokens, int(bool(causal)), rotary_dim, int(bool(interleaved)),
+                    n_positions, dt if out_dtype is None else int(_TYPES.get(out_dtype, out_dtype)), float(scale))
+    c.page_stride, c.head_stride, c.token_stride = page_strides or (
+        page_size * heads, 0 if head_tables else 1 if token_major else page_size, heads if token_major else 1)
+    c.table_stride_s, c.table_stride_h = (n_kv_heads * max_pages, max_pages) if head_tables else (max_pages, 0)
+    c.lens_stride_s, c.lens_stride_h = (n_kv_heads, 1) if head_lens else (1, 0)
+    c.q_stride_t, c.q_stride_h, c.kv_stride_t, c.kv_stride_h = n_q_heads * head_dim, head_dim, n_kv_heads * head_dim, head_dim
+    c.out_stride_t, c.out_stride_h, c.lse_stride_t, c.lse_stride_h = n_q_heads * head_dim, head_dim, n_q_heads, 1
+    if out_head_major:
+        n = max(c.n_tokens, 1)
+        c.out_stride_t, c.out_stride_h, c.lse_stride_t, c.lse_stride_h = head_dim, n * head_dim, 1, n
+    return c
+
+
+@dataclass(frozen=True)
+class CachePages:
+    """The arrays of a paged cache: k, v [n_pages, Hkv, page_size, d] ([n_pages, page_size, Hkv, d] token-major) of the
+    cache's type, or for 4 bits uint8 [..., d/2] with k_scale, v_scale bfloat16 [..., d/32, 2] ({step, zero})."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+    rows: tuple = field(init=False, repr=False)      # shape and strides in rows of all arrays, checked once
+
+    def __post_init__(self):
+        q4 = self.k.dtype == torch.uint8
+        arrays = [self.k, self.v]
+        if q4:
+            arrays += [self.k_scale, self.v_scale]
+        elif self.k_scale is not None or self.v_scale is not None:
+            raise RestkvError(-1, "CachePages: scales go with codes (uint8)")
+        seen = set()
+        for n, x in enumerate(arrays):
+            if x is None:
+                raise RestkvError(-1, "CachePages: codes come with k_scale and v_scale")
+            tail = x.shape[3:]
+            size = tail.numel()
+            if x.dim() != (5 if n > 1 else 4) or x.stride()[3:] != ((2, 1) if n > 1 else (1,)) or \
+                    any(st % size for st in x.stride()[:3]):
+                raise RestkvError(-1, "CachePages: rows that are contiguous, a whole number of rows apart")
+            if x.dtype != (torch.bfloat16 if n > 1 else self.k.dtype) or x.device != self.k.device or \
+                    (n > 1 and (tail[0] * 16 != self.k.shape[3] or tail[1] != 2)) or (n == 1 and tail != self.k.shape[3:]):
+                raise RestkvError(-1, "CachePages: arrays of one cache on one device")
+            seen.add((tuple(x.shape[:3]), tuple(st // size for st in x.stride()[:3])))
+        if len(seen) != 1:
+            raise RestkvError(-1, "CachePages: all arrays of one layout")
+        object.__setattr__(self, "rows", seen.pop() + (self.k.dtype, self.k.shape[3] * (2 if q4 else 1), self.k.get_device()))
+
+
+def alloc_cache_pages(c: RestkvCache, device="cuda") -> CachePages:
+    """Pages of the described cache (contiguous), zeroed."""
+    heads = 1 if c.head_stride == 0 else c.n_kv_heads
+    token_major = heads > 1 and c.token_stride >= heads
+    shape = (c.n_pages, c.page_size, heads) if token_major else (c.n_pages, heads, c.page_size)
+    d = c.head_dim
+    if c.format != RESTKV_Q4:
+        return CachePages(*(torch.zeros(shape + (d,), dtype=_TORCH[c.format], device=device) for _ in range(2)))
+    return CachePages(*(torch.zeros(shape + (d // 2,), dtype=torch.uint8, device=device) for _ in range(2)),
+                      *(torch.zeros(shape + (d // 32, 2), dtype=torch.bfloat16, device=device) for _ in range(2)))
+
+
+def restkv_attend_workspace_bytes(c: RestkvCache) -> int:
+    return int(lib().restkv_attend_workspace_bytes(ctypes.byref(c)))
+
+
+def alloc_attend_workspace(c: RestkvCache, device="cuda") -> Optional[torch.Tensor]:
+    """Scratch of restkv_attend, or None where it needs none."""
+    n = restkv_attend_workspace_bytes(c)
+    return torch.empty(n + 256, dtype=torch.uint8, device=device) if n else None
+
+
+def _check_pages(what: str, c: RestkvCache, pages: CachePages, table, lens, new_start=None) -> int:
+    """The GPU that the cache is on."""
+    shape, strides, dtype, d, dev = pages.rows
+    heads = 1 if c.table_stride_h else c.n_kv_heads
+    page, head, pos = c.page_stride, c.head_stride, c.token_stride
+    # (a stride along one entry says nothing)
+    as_told = [(shape[0] >= c.n_pages and a == heads and b == c.page_size and (strides[0] == page or c.n_pages == 1) and
+                (sa == head or a == 1) and sb == pos)
+               for a, b, sa, sb in ((shape[1], shape[2], strides[1], strides[2]), (shape[2], shape[1], strides[2], strides[1]))]
+    if not any(as_told) or d != c.head_dim or dtype != _TORCH.get(c.format):
+        raise RestkvError(-1, f"{what}: pages {shape} with strides {strides} in rows of {d} {dtype} are not the described ones")
+    if dev < 0:
+        raise RestkvError(-1, f"{what}: the pages are not on a GPU")
+    n = c.n_seqs
+    _check_flat(what, dev, torch.int32, "table", table, n * c.table_stride_s)
+    _check_flat(what, dev, torch.int32, "lens", lens, n * c.lens_stride_s)
+    if new_start is not None:
+        _check_flat(what, dev, torch.int32, "new_start", new_start, n + 1)
+    return dev
+
+
+def _check_flat(what, dev, dtype, name, t, n):
+    if t is None or t.dtype != dtype or t.get_device() != dev or t.numel() < n or not t.is_contiguous():
+        raise RestkvError(-1, f"{what}: {name} has to be contiguous {dtype}, {n} values on GPU {dev}")
+
+
+def _check_rows(what, dev, dtype, name, t, shape):
+    """Strides of a tensor [tokens, heads, d] or [tokens, heads]."""
+    if t.dtype != dtype or t.get_device() != dev or t.shape != shape or (len(shape) == 3 and t.stride(2) != 1):
+        raise RestkvError(-1, f"{what}: {name} has to be {dtype} {tuple(shape)} on GPU {dev}, contiguous along the last")
+    st, least = t.stride(), shape[2] if len(shape) == 3 else 1
+    # (a stride along one entry, or none, says nothing; the library asks for one that a contiguous tensor could have)
+    along, across = st[0] if shape[0] > 1 else shape[1] * least, st[1] if shape[1] > 1 else least
+    if along < least or across < least:
+        raise RestkvError(-1, f"{what}: rows of {name} overlap")
+    return along, across
+
+
+def _as_strided(c: RestkvCache, kind: str, strides) -> RestkvCache:
+    """The description with these strides of a token tensor: itself where it has them."""
+    t, h = kind + "_stride_t", kind + "_stride_h"
+    if (getattr(c, t), getattr(c, h)) == strides:
+        return c
+    c = RestkvCache.from_buffer_copy(c)
+    setattr(c, t, strides[0])
+    setattr(c, h, strides[1])
+    return c
+
+
+def _on_gpu(dev: int, stream, what: str, f, *args):
+    """The call on GPU `dev`, on the given stream or that GPU's current one."""
+    s = ctypes.c_void_p((torch.cuda.current_stream(dev) if stream is None else stream).cuda_stream)
+    if dev == torch.cuda.current_device():
+        _chk(f(*args, s), what)
+    else:
+        with torch.cuda.device(dev):
+            _chk(f(*args, s), what)
+
+
+def restkv_append(c: RestkvCache, k, v, pages: CachePages, table, lens, *, new_start=None, positions=None, cos=None, sin=None,
+                  q=None, q_out=None, stream=None):
+    """New keys (rotated by their positions) and values [n_tokens, Hkv, d] into the pages, and new queries [n_tokens, Hq, d]
+    rotated beside them; lens counts the new tokens already."""
+    what = "restkv_append"
+    dev, dt = _check_pages(what, c, pages, table, lens, new_start), _TORCH.get(c.dtype)
+    shape, told = (c.n_tokens, c.n_kv_heads, c.head_dim), c
+    strides = _check_rows(what, dev, dt, "k", k, shape)
+    if _check_rows(what, dev, dt, "v", v, shape) != strides:
+        raise RestkvError(-1, f"{what}: k and v have to have the same strides")
+    c = _as_strided(c, "kv", strides)
+    if q is not None and q_out is not None:
+        shape = (told.n_tokens, told.n_q_heads, told.head_dim)
+        strides = _check_rows(what, dev, dt, "q", q, shape)
+        if q_out is not q and _check_rows(what, dev, dt, "q_out", q_out, shape) != strides:
+            raise RestkvError(-1, f"{what}: q and q_out have to have the same strides")
+        c = _as_strided(c, "q", strides)
+    if c.rotary_dim:
+        n = c.n_positions * (c.rotary_dim // 2)
+        _check_flat(what, dev, torch.float32, "cos", cos, n)
+        _check_flat(what, dev, torch.float32, "sin", sin, n)
+    if positions is not None:
+        _check_flat(what, dev, torch.int32, "positions", positions, c.n_tokens)
+    _on_gpu(dev, stream, what, lib().restkv_append, ctypes.byref(c), _ptr(k), _ptr(v), _ptr(pages.k), _ptr(pages.v),
+            _ptr(pages.k_scale), _ptr(pages.v_scale), _ptr(table), _ptr(lens), _ptr(new_start), _ptr(positions), _ptr(cos),
+            _ptr(sin), _ptr(q), _ptr(q_out))
+
+
+def restkv_attend(c: RestkvCache, q, pages: CachePages, table, lens, out, lse=None, workspace=None, *, new_start=None,
+                  stream=None):
+    """Attention of the newest tokens' queries q [n_tokens, Hq, d] over the pages: out [n_tokens, Hq, d], lse [n_tokens, Hq]."""
+    what = "restkv_attend"
+    dev = _check_pages(what, c, pages, table, lens, new_start)
+    shape, told = (c.n_tokens, c.n_q_heads, c.head_dim), c
+    c = _as_strided(c, "q", _check_rows(what, dev, _TORCH.get(told.dtype), "q", q, shape))
+    c = _as_strided(c, "out", _check_rows(what, dev, _TORCH.get(told.out_dtype), "out", out, shape))
+    if lse is not None:
+        c = _as_strided(c, "lse", _check_rows(what, dev, torch.float32, "lse", lse, shape[:2]))
+    if workspace is not None and (workspace.get_device() != dev or workspace.dtype != torch.uint8):
+        raise RestkvError(-1, f"{what}: the workspace has to be uint8 on GPU {dev}")
+    wp, wn = _ws(workspace)
+    _on_gpu(dev, stream, what, lib().restkv_attend, ctypes.byref(c), _ptr(q), _ptr(pages.k), _ptr(pages.v), _ptr(pages.k_scale),
+            _ptr(pages.v_scale), _ptr(table), _ptr(lens), _ptr(new_start), _ptr(out), _ptr(lse), wp, wn)
+
+
+def restkv_fetch(c: RestkvCache, pages: CachePages, table, lens, k_out, v_out, *, idx=None, first=0, stream=None):
+    """Rows of the pages as dense k_out, v_out [n_seqs, Hkv, n, d]: positions idx [n_seqs, Hkv, n], or first .. first + n - 1."""
+    what = "restkv_fetch"
+    dev = _check_pages(what, c, pages, table, lens)
+    n, dt = k_out.shape[2] if k_out.dim() == 4 else -1, _TORCH.get(c.dtype)
+    if n < 0 or k_out.shape != (c.n_seqs, c.n_kv_heads, n, c.head_dim) or v_out.shape != k_out.shape:
+        raise RestkvError(-1, f"{what}: k_out and v_out have to be [n_seqs, Hkv, n, d]")
+    _check_flat(what, dev, dt, "k_out", k_out, 0)
+    _check_flat(what, dev, dt, "v_out", v_out, 0)
+    if idx is not None:
+        _check_flat(what, dev, torch.int32, "idx", idx, c.n_seqs * c.n_kv_heads * n)
+    _on_gpu(dev, stream, what, lib().restkv_fetch, ctypes.byref(c), _ptr(pages.k), _ptr(pages.v), _ptr(pages.k_scale),
+            _ptr(pages.v_scale), _ptr(table), _ptr(lens), _ptr(idx), int(first), n, _ptr(k_out), _ptr(v_out))

@@ -1,0 +1,132 @@
+// Attention over pages: how the work is cut, and the join of the chunks of a sequence.
+#include <algorithm>
+
+#include "attend.hpp"
+
+namespace restkv {
+
+namespace {
+
+// Sums of an entry's chunks joined into its output: a workgroup a row (new token, query head), 256 threads as 1024 / d
+// groups that take every so manyeth chunk, four channels a thread.
+template <int D>
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
+  constexpr int TPR = D / 4, NGR = 256 / TPR;
+  __shared__ float4 sm_x[NGR][TPR];
+  __shared__ float sm_ml[2][NGR];
+  const Pages& pg = a.pg;
+  const int64_t b = wide_block(), per = (int64_t)pg.max_new * pg.Hq;
+  if (b >= per * pg.n_seqs) return;
+  const int s = (int)(b / per), i = (int)(b % per) / pg.Hq, head = (int)(b % per) % pg.Hq, h = head / pg.G;
+  const NewRows nr = new_rows(pg, s);
+  if (i >= nr.n) return;
+  const int2 pl = a.plan[a.per_head ? s * pg.Hkv + h : s];
+  if (pl.y < 2) return;
+  const int hy = a.per_head ? 0 : h, row = i * pg.G + head - h * pg.G, rows = pg.G * pg.max_new;
+  const int g = threadIdx.x / TPR, c = threadIdx.x % TPR;
+  float M = -INFINITY, L = 0.f;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k = g; k < pl.y; k += NGR) {
+    const int64_t at = (int64_t)((pl.x + k) * a.Hy + hy) * rows + row;
+    const float m = a.part_m[at], l = a.part_l[at];
+    const float4 y = *(const float4*)&a.part_o[at * D + c * 4];
+    const float n = fmaxf(M, m);
+    // (a chunk of which the row sees nothing has a reference of -inf and sums of 0)
+    const float fo = M == n ? 1.f : __builtin_amdgcn_exp2f(M - n), fn = m == n ? 1.f : __builtin_amdgcn_exp2f(m - n);
+    M = n;
+    L = L * fo + l * fn;
+    x.x = x.x * fo + y.x * fn; x.y = x.y * fo + y.y * fn; x.z = x.z * fo + y.z * fn; x.w = x.w * fo + y.w * fn;
+  }
+  sm_x[g][c] = x;
+  if (c == 0) { sm_ml[0][g] = M; sm_ml[1][g] = L; }
+  __syncthreads();
+  if (g) return;
+  float N = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < NGR; ++k) N = fmaxf(N, sm_ml[0][k]);
+  L = 0.f;
+  x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int k = 0; k < NGR; ++k) {
+    const float m = sm_ml[0][k], f = m == N ? 1.f : __builtin_amdgcn_exp2f(m - N);
+    const float4 y = sm_x[k][c];
+    L = __builtin_fmaf(f, sm_ml[1][k], L);
+    x.x = __builtin_fmaf(f, y.x, x.x); x.y = __builtin_fmaf(f, y.y, x.y); x.z = __builtin_fmaf(f, y.z, x.z); x.w = __builtin_fmaf(f, y.w, x.w);
+  }
+  store_out(a, nr.first + i, head, c * 4, x, N, L);
+}
+
+// Blocks of 16 rows of a wavefront: as many as the rows fill, up to what its registers hold.
+int rows_of(const Pages& pg) {
+  return (int64_t)pg.G * pg.max_new <= 16 ? 1 : 2;
+}
+
+struct AttendPlan { int R, c_min, target; int64_t row_blocks, entries, Hy, chunks, slots; };
+AttendPlan attend_plan(const Pages& pg) {
+  AttendPlan p;
+  p.R = rows_of(pg);
+  const int64_t rows = (int64_t)pg.G * pg.max_new;
+  const bool per_head = pg.lens_sh != 0;
+  p.row_blocks = (rows + 16 * p.R - 1) / (16 * p.R);
+  p.entries = per_head ? (int64_t)pg.n_seqs * pg.Hkv : pg.n_seqs;
+  p.Hy = per_head ? 1 : pg.Hkv;
+  p.c_min = pg.fmt == RESTKV_Q4 ? 4 : 2;          // (a tile for each wavefront)
+  p.target = n_cu() * (p.R == 1 ? 4 : 2);
+  const int64_t tiles = (pg.max_len + ATT_TILE - 1) / ATT_TILE, each = p.Hy * p.row_blocks;
+  // no entry has two chunks: chunks hold the sum of all tiles, or the longest entry fits the smallest chunk
+  const bool single = each >= p.target || tiles <= p.c_min;
+  const int64_t more = std::min<int64_t>(p.target / each + 1, p.entries * ((tiles + p.c_min - 1) / p.c_min));
+  p.chunks = p.entries + (single ? 0 : more);
+  p.slots = single ? 0 : std::min<int64_t>(2 * more, p.entries * ((tiles + p.c_min - 1) / p.c_min));
+  return p;
+}
+
+struct AttendWs { size_t plan, m, l, o, bytes; };
+AttendWs attend_ws(const Pages& pg, const AttendPlan& p) {
+  AttendWs w = {};
+  if (!p.slots) return w;
+  size_t off = 0;
+  auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes); return o; };
+  const size_t rows = (size_t)p.slots * p.Hy * pg.G * pg.max_new;
+  w.plan = take((size_t)p.entries * 8);
+  w.m = take(rows * 4);
+  w.l = take(rows * 4);
+  w.o = take(rows * pg.d * 4);
+  w.bytes = off;
+  return w;
+}
+
+}  // namespace
+
+size_t attend_ws_bytes(const Pages& pg) { return attend_ws(pg, attend_plan(pg)).bytes; }
+
+int launch_attend(const Pages& pg, const void* q, const void* k_pages, const void* v_pages, const void* k_scale,
+                  const void* v_scale, void* out, float* lse, char* ws, hipStream_t st) {
+  const AttendPlan p = attend_plan(pg);
+  const AttendWs lay = attend_ws(pg, p);
+  if (p.chunks * p.Hy > (int64_t)1 << 30) return RESTKV_EUNSUPPORTED;
+  AttendArgs a = {};
+  a.pg = pg;
+  a.q = q; a.k = (const char*)k_pages; a.v = (const char*)v_pages;
+  a.ks = (const uint32_t*)k_scale; a.vs = (const uint32_t*)v_scale;
+  a.out = out; a.lse = lse;
+  if (p.slots) {
+    a.plan = (int2*)(ws + lay.plan);
+    a.part_m = (float*)(ws + lay.m); a.part_l = (float*)(ws + lay.l); a.part_o = (float*)(ws + lay.o);
+  }
+  a.entries = (int)p.entries; a.per_head = pg.lens_sh != 0; a.Hy = (int)p.Hy;
+  a.row_blocks = (int)p.row_blocks; a.units = (int)(p.chunks * p.Hy);
+  a.c_min = p.c_min; a.target = p.target;
+  const int qel = pg.dtype == RESTKV_F32 ? 4 : 8;
+  a.vec_q = !((uintptr_t)q & 15u) && !((pg.q_st | pg.q_sh) & (qel - 1));
+  const int oal = pg.out_dtype == RESTKV_F32 ? 15 : 7;
+  a.vec_out = !((uintptr_t)out & oal) && !((pg.o_st | pg.o_sh) & 3);
+  const int rc = pg.fmt == RESTKV_F32 ? run_attend_f32(a, p.R, st) : pg.fmt == RESTKV_BF16 ? run_attend_bf16(a, p.R, st) : run_attend_q4(a, p.R, st);
+  if (rc || !p.slots) return rc;
+  const dim3 grid = wide_grid((int64_t)pg.n_seqs * pg.max_new * pg.Hq);
+  if (pg.d == 128) hipLaunchKernelGGL(k_attend_join<128>, grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(k_attend_join<64>, grid, dim3(256), 0, st, a);
+  return hip_status();
+}
+
+}  // namespace restkv

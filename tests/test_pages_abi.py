@@ -1,0 +1,144 @@
+"""Host side of the paged cache: descriptions and arguments that are refused before anything is enqueued (no GPU needed)."""
+import ctypes
+import os
+
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def rk():
+    import paper_2605_08840_amd as r
+    if not os.path.exists(r.LIB_PATH):
+        import __graft_entry__
+        __graft_entry__.build()
+    return r
+
+
+def good(rk, **kw):
+    base = dict(n_seqs=3, n_q_heads=4, n_kv_heads=2, head_dim=64, page_size=32, n_pages=20, max_pages=6, dtype="bf16")
+    base.update(kw)
+    c = rk.make_cache(**{k: v for k, v in base.items() if not k.startswith("_")})
+    for k, v in base.items():
+        if k.startswith("_"):
+            setattr(c, k[1:], v)
+    return c
+
+
+ONE = ctypes.c_void_p(256)            # never dereferenced on the host
+
+
+def append(rk, c, **over):
+    a = dict(k=ONE, v=ONE, kp=ONE, vp=ONE, ks=ONE, vs=ONE, table=ONE, lens=ONE, new_start=None, positions=None, cos=None, sin=None,
+             q=None, q_out=None)
+    a.update(over)
+    return rk.lib().restkv_append(ctypes.byref(c), *a.values(), None)
+
+
+def attend(rk, c, ws=ONE, ws_n=1 << 40, **over):
+    a = dict(q=ONE, kp=ONE, vp=ONE, ks=ONE, vs=ONE, table=ONE, lens=ONE, new_start=None, out=ONE, lse=None)
+    a.update(over)
+    return rk.lib().restkv_attend(ctypes.byref(c), *a.values(), ws, ws_n, None)
+
+
+def fetch(rk, c, first=0, n=8, **over):
+    a = dict(kp=ONE, vp=ONE, ks=ONE, vs=ONE, table=ONE, lens=ONE, idx=None)
+    a.update({k: v for k, v in over.items() if k in a})
+    return rk.lib().restkv_fetch(ctypes.byref(c), *a.values(), first, n, over.get("k_out", ONE), over.get("v_out", ONE), None)
+
+
+def test_description_layout_matches_header(rk):
+    assert ctypes.sizeof(rk.RestkvCache) == 18 * 4 + 15 * 8
+
+
+BAD = [
+    (dict(n_seqs=-1), -1), (dict(n_q_heads=3), -1), (dict(n_q_heads=0), -1), (dict(n_kv_heads=0), -1), (dict(n_pages=0), -1),
+    (dict(max_pages=0), -1), (dict(max_new=0), -1), (dict(n_tokens=-1), -1), (dict(max_len=-1), -1),
+    (dict(max_len=6 * 32 + 1), -1),            # more than the table names
+    (dict(scale=-1.0), -1), (dict(scale=float("inf")), -1), (dict(scale=float("nan")), -1),
+    (dict(rotary_dim=80), -1), (dict(rotary_dim=-16), -1), (dict(rotary_dim=24), -2),
+    (dict(head_dim=96), -2), (dict(dtype=7), -2), (dict(format="f32"), -2), (dict(dtype="f32", format="bf16"), -2),
+    (dict(dtype="f32", out_dtype="bf16"), -2),
+    (dict(page_size=8), -2), (dict(page_size=48), -2), (dict(page_size=1 << 17), -2), (dict(max_pages=1 << 26), -2),
+    (dict(n_seqs=16385), -2), (dict(max_new=1 << 29), -2),
+    (dict(page_strides=(64, 32, -1)), -1), (dict(page_strides=(0, 32, 1)), -1), (dict(page_strides=(64, -1, 1)), -1),
+    (dict(page_strides=(1 << 20, 1, 65537)), -2),
+    (dict(_token_stride=0), -1),               # the default layout with strides beside it
+    (dict(_q_stride_t=63), -1), (dict(_kv_stride_h=-64), -1), (dict(_out_stride_h=8), -1), (dict(_lse_stride_t=-1), -1),
+    (dict(_table_stride_s=-1), -1), (dict(_lens_stride_h=-1), -1),
+]
+
+
+@pytest.mark.parametrize("over,code", BAD, ids=lambda x: str(x))
+def test_descriptions_that_are_refused(rk, over, code):
+    c = good(rk, **over)
+    assert append(rk, c) == code
+    assert attend(rk, c) == code
+    assert fetch(rk, c) == code
+    assert rk.restkv_attend_workspace_bytes(c) == 0
+
+
+def test_arguments_that_are_refused(rk):
+    c, q4, turn = good(rk), good(rk, format="q4"), good(rk, rotary_dim=64, n_positions=10)
+    odd = ctypes.c_void_p(264)
+    for name in ("k", "v", "kp", "vp", "table", "lens"):
+        assert append(rk, c, **{name: None}) == -1, name
+    for name in ("q", "kp", "vp", "table", "lens", "out"):
+        assert attend(rk, c, **{name: None}) == -1, name
+    for name in ("kp", "vp", "table", "lens", "k_out", "v_out"):
+        assert fetch(rk, c, **{name: None}) == -1, name
+    for call in (append, attend, fetch):
+        assert call(rk, q4, ks=None) == -1 and call(rk, q4, vs=None) == -1
+        assert call(rk, c, kp=odd) == -1 and call(rk, q4, vs=odd) == -1
+    assert append(rk, c, q=ONE) == -1 and append(rk, c, q_out=ONE) == -1
+    assert append(rk, turn) == -1 and append(rk, turn, cos=ONE) == -1 and append(rk, good(rk, rotary_dim=64), cos=ONE, sin=ONE) == -1
+    # cache positions are no positions where every head has its own
+    assert append(rk, good(rk, rotary_dim=64, n_positions=10, head_lens=True), cos=ONE, sin=ONE) == -1
+    # without new_start every sequence has max_new tokens
+    short = good(rk, n_tokens=5, max_new=2)
+    assert append(rk, short) == -1 and attend(rk, short) == -1
+    assert fetch(rk, c, k_out=odd) == -1 and fetch(rk, c, first=-1) == -1 and fetch(rk, c, n=-1) == -1
+    assert fetch(rk, c, n=(1 << 30) + 1) == -2
+    # workspace: missing, too small, misaligned
+    need = rk.restkv_attend_workspace_bytes(good(rk, max_pages=600, n_pages=900))
+    long = good(rk, max_pages=600, n_pages=900)
+    assert need > 0
+    assert attend(rk, long, ws=None) == -3 and attend(rk, long, ws_n=need - 1) == -3 and attend(rk, long, ws=odd, ws_n=need) == -3
+
+
+def test_nothing_to_do_is_no_error(rk):
+    for c in (good(rk, n_seqs=0), good(rk, n_tokens=0, n_seqs=0)):
+        assert append(rk, c) == 0 and attend(rk, c, ws=None, ws_n=0) == 0 and fetch(rk, c) == 0
+    assert append(rk, good(rk, n_tokens=0), new_start=ONE) == 0 and attend(rk, good(rk, n_tokens=0), new_start=ONE) == 0
+    assert fetch(rk, good(rk), n=0) == 0
+
+
+def test_short_caches_need_no_workspace(rk):
+    assert rk.restkv_attend_workspace_bytes(good(rk, page_size=64, max_pages=100, n_pages=400, max_len=128)) == 0
+    assert rk.alloc_attend_workspace(good(rk, max_len=100), device="cpu") is None
+    # bounded however large the batch of row blocks is
+    big = good(rk, n_seqs=48, n_q_heads=64, n_kv_heads=8, head_dim=128, max_pages=4096, n_pages=1 << 17, max_new=64)
+    assert 0 < rk.restkv_attend_workspace_bytes(big) < 1 << 28
+
+
+def test_binding_refuses_tensors_that_are_not_what_they_are_said_to_be(rk):
+    c = good(rk)
+    pages = rk.alloc_cache_pages(c, device="cpu")
+    assert pages.k.shape == (20, 2, 32, 64) and rk.alloc_cache_pages(good(rk, token_major=True), device="cpu").k.shape == (20, 32, 2, 64)
+    assert rk.alloc_cache_pages(good(rk, head_tables=True), device="cpu").k.shape == (20, 1, 32, 64)
+    q4 = rk.alloc_cache_pages(good(rk, format="q4"), device="cpu")
+    assert q4.k.shape == (20, 2, 32, 32) and q4.k_scale.shape == (20, 2, 32, 2, 2)
+    x = torch.zeros(3, 2, 64, dtype=torch.bfloat16)
+    table, lens = torch.zeros(3, 6, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    with pytest.raises(rk.RestkvError, match="not on a GPU"):
+        rk.restkv_append(c, x, x, pages, table, lens)
+    for other in (dict(n_kv_heads=1), dict(page_size=64), dict(n_pages=21), dict(head_dim=128), dict(format="q4"),
+                  dict(dtype="f32"), dict(token_major=True), dict(head_tables=True), dict(page_strides=(128, 32, 1))):
+        with pytest.raises(rk.RestkvError, match="are not the described ones"):
+            rk.restkv_append(good(rk, **other), x, x, pages, table, lens)
+    k, s = q4.k, q4.k_scale
+    for bad in ((k, k), (k, k, s, None), (k, k[..., :16], s, s), (k, k, s[..., :1], s[..., :1]), (k, k.transpose(1, 2), s, s),
+                (k[0], k[0], s, s), (k, k, s.float(), s.float()), (pages.k, pages.v, s, s), (pages.k, pages.v.float()),
+                (pages.k[..., ::2], pages.v[..., ::2]), (k, k, s.transpose(3, 4), s)):
+        with pytest.raises(rk.RestkvError):
+            rk.CachePages(*bad)
