@@ -145,14 +145,63 @@ __device__ __forceinline__ void store_out(const AttendArgs& a, int64_t t, int64_
 
 enum { FMT_F32, FMT_BF16, FMT_Q4 };
 
+// Wave-uniform reads of what the kernel does not write, through the scalar cache.
+__device__ __forceinline__ int uniform_load(const int32_t* p) {
+  return *(const __attribute__((address_space(4))) int32_t*)(uintptr_t)p;
+}
+
+// N words at a uniform address (held in scalar registers, so that the load adds the lane's 32-bit offset by itself).
+template <int N>
+__device__ __forceinline__ void load_words(const char* base, uint32_t off, uint32_t* x) {
+  uint64_t u = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)base >> 32)) << 32 |
+               (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(uint64_t)base);
+  asm("" : "+s"(u));
+  typedef uint32_t words __attribute__((ext_vector_type(N)));
+  typedef const __attribute__((address_space(1))) char* global;
+  const words w = *(const __attribute__((address_space(1))) words*)((global)u + off);
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = w[i];
+}
+
+__device__ __forceinline__ uint32_t load_half(const char* base, uint32_t off) {
+  uint64_t u = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)base >> 32)) << 32 |
+               (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(uint64_t)base);
+  asm("" : "+s"(u));
+  typedef const __attribute__((address_space(1))) char* global;
+  return *(const __attribute__((address_space(1))) uint16_t*)((global)u + off);
+}
+
+// A copy in a vector register, so that what it is made of stays in scalar ones.
+__device__ __forceinline__ uint32_t vector(uint32_t x) {
+  uint32_t y;
+  asm("v_mov_b32 %0, %1" : "=v"(y) : "s"(__builtin_amdgcn_readfirstlane(x)));
+  return y;
+}
+// Rare code works on copies that the compiler knows nothing of, so that none of it moves into the common path.
+template <int N, int M>
+__device__ __forceinline__ void keep_here(uint32_t (&x)[N][M]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int k = 0; k < M; ++k) asm volatile("" : "+v"(x[i][k]));
+}
+
+// Nibble i of each half word as the bfloat16 16 + code: the code goes to the upper four of its seven mantissa bits.
+__device__ __forceinline__ uint32_t sixteen_plus(uint32_t x, int i, uint32_t mask, uint32_t base) {
+  return ((i == 0 ? x << 3 : x >> (4 * i - 3)) & mask) | base;
+}
+
 // FMT: pages; T: queries; NP: bf16 parts of a softmax weight (products with float32 pages take the weight itself); R: blocks
-// of 16 rows of a wavefront.
+// of 16 rows of a wavefront.  Of a tile the keys are loaded anew (for the next one) as soon as the logits are there, the
+// values as soon as they are in the sums: a load has the other half's arithmetic, and other wavefronts', to come back,
+// and costs no second set of registers.
 template <int FMT, typename T, int D, int NP, int R>
-__global__ __launch_bounds__(256) void k_attend(AttendArgs a) {
+__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(2)))
+void k_attend(AttendArgs a) {
   constexpr int UN = D / 16, NG = D / 32;
   constexpr int QP = FMT == FMT_Q4 ? planes_of<T> : 1;
   constexpr int TK = FMT == FMT_F32 ? 16 : FMT == FMT_BF16 ? 32 : 64, NB = TK / 16;
-  constexpr int64_t ROWB = FMT == FMT_F32 ? D * 4 : FMT == FMT_BF16 ? D * 2 : D / 2;
+  constexpr int ROWB = FMT == FMT_F32 ? D * 4 : FMT == FMT_BF16 ? D * 2 : D / 2;
   constexpr int LDO = D + 4;
   extern __shared__ __align__(16) float sm[];
   const Pages& pg = a.pg;
@@ -187,7 +236,7 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a) {
   const int last_row = min(row0 + 16 * R, rows) - 1;
   const int k_end = __builtin_amdgcn_readfirstlane(min(ch.tile1 * ATT_TILE, limit(last_row)));
   const int lim_lo = __builtin_amdgcn_readfirstlane(limit(row0));
-  const int k_begin = __builtin_amdgcn_readfirstlane(ch.tile0 * ATT_TILE);
+  const int k_begin = __builtin_amdgcn_readfirstlane(ch.tile0 * ATT_TILE) + wv * TK;
   const float sc = pg.scale * 1.44269504088896341f;
 
   int lim[R];
@@ -195,7 +244,7 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a) {
   constexpr int QC = FMT == FMT_F32 ? D / 16 : D / 32;
   float4 qf[FMT == FMT_F32 ? R : 1][FMT == FMT_F32 ? QC : 1];
   Op<QP> qo[FMT == FMT_F32 ? 1 : R][FMT == FMT_F32 ? 1 : QC];
-  float qsum[FMT == FMT_Q4 ? R : 1][NG];
+  uint4 qz[FMT == FMT_Q4 ? R : 1];
 #pragma unroll
   for (int cb = 0; cb < R; ++cb) {
     const int row = min(row0 + cb * 16 + n, rows - 1);
@@ -217,8 +266,10 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a) {
         qo[cb][c] = split8<1>(x);
       }
     } else {
-      float x[4 * UN];               // units 4j .. 4j+3
+      float x[4 * UN], z[8];         // units 4j .. 4j+3
       load_row<T, 4 * UN>(p + j * 4 * UN, a.vec_q, x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z[i] = 0.f;
 #pragma unroll
       for (int f = 0; f < NG; ++f) {
         float y[8], t = 0.f;
@@ -228,8 +279,16 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a) {
           t += y[i];
         }
         qo[cb][f] = split8<QP>(y);
-        qsum[cb][f] = quad_sum(t);
+        t = quad_sum(t);
+        if (j == f) z[0] = t;        // lane j: the sum of the group j that its eight places of the zeros' product stand for
       }
+      // (zero, zero, zero, step, step, step, 0, 0) of a key times the sum's three parts h, m, l and -16 of them
+      const Op<3> zp = split8<3>(z);
+      const uint32_t zh = zp.p[0].x & 0xFFFFu, zm = zp.p[1].x & 0xFFFFu, zl = zp.p[2].x & 0xFFFFu;
+      auto times = [](uint32_t b) {  // -16 of a bfloat16
+        return __float_as_uint(-16.f * __uint_as_float(b << 16)) >> 16;
+      };
+      qz[cb] = make_uint4(zh | zm << 16, zl | times(zh) << 16, times(zm) | times(zl) << 16, 0u);
     }
   }
 
@@ -245,121 +304,150 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a) {
 #pragma unroll
       for (int f = 0; f < NG; ++f) corr[cb][f] = 0.f;
   }
-  float* scales = sm + wv * (2 * 64 * NG * 2);       // [K | V][64 keys][group]{step, zero - 16 step} of this wavefront's tile
+  // of this wavefront's tile: {step, zero} of the keys as they are [64][NG], their steps [NG][64], the values' steps and
+  // zeros - 16 steps [NG][64] each (a read takes four keys of a group)
+  uint32_t* s_kz = (uint32_t*)sm + wv * (4 * 64 * NG);
+  float* s_ks = (float*)s_kz + 64 * NG;
+  float* s_vs = s_ks + 64 * NG;
+  float* s_vz = s_vs + 64 * NG;
+  uint32_t* s_rare = (uint32_t*)sm + wv * (TK / 4 * (ROWB / 64) * 64);     // a tile's values (float32 and bfloat16 pages)
 
-  for (int k0 = k_begin + wv * TK; k0 < k_end; k0 += 4 * TK) {
-    // the 16-key blocks of the tile: each lies in one page
-    int64_t base[NB];
-    int there[NB];
-    bool whole = k0 + TK <= min(k_end, lim_lo);
+  // ---- tiles: where the 16-key blocks are (each lies in one page)
+  const int32_t* table = pg.table + s * pg.table_ss + h * pg.table_sh;
+  const int64_t tokb = pg.tok_s * ROWB;
+  const char* const kh = a.k + h * pg.head_s * ROWB;
+  const char* const vh = a.v + h * pg.head_s * ROWB;
+  struct Where { uint32_t row[NB]; int ok; };    // first rows, and a bit for each block that has a page
+  auto find = [&](int k0) {
+    Where w;
+    w.ok = 0;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const int t = k0 + 16 * b;
-      const int page = t < k_end ? page_of(pg, s, h, t) : -1;
-      there[b] = page >= 0 ? min(k_end - t, 16) : 0;
-      base[b] = page >= 0 ? row_of(pg, page, h, t) : 0;
-      whole = whole && page >= 0;
+      const int page = t < k_end ? uniform_load(table + (t >> pg.lg_ps)) : -1;
+      const bool ok = (uint32_t)page < (uint32_t)pg.n_pages;
+      w.row[b] = ok ? (uint32_t)page * (uint32_t)pg.page_s + (t & ((1 << pg.lg_ps) - 1)) * (uint32_t)pg.tok_s : 0u;
+      w.ok |= ok ? 1 << b : 0;
     }
-    const int tok = (int)pg.tok_s;
-
-    f32x4 p[NB][R];
+    return w;
+  };
+  // lane offsets of a block: key n, part j of its row; value row 4 j + r, unit n
+  const uint32_t k_off = (uint32_t)(n * tokb) + j * (FMT == FMT_Q4 ? UN * 2 : 16);
+  const uint32_t v_off = (uint32_t)(4 * j * tokb) + n * (ROWB / 16);
+  constexpr int KW = FMT == FMT_Q4 ? UN / 2 : 4 * QC;       // words of a lane per block
+  uint32_t kr[NB][KW];
+  constexpr int VW = FMT == FMT_F32 ? UN : FMT == FMT_BF16 ? UN / 2 : 1;
+  uint32_t vw[NB * 4][VW];
+  uint32_t sk[NG], sv[NG];
+  auto load_keys = [&](const Where& w) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const char* p = kh + (uint64_t)w.row[b] * ROWB;
+      if constexpr (FMT == FMT_Q4) load_words<UN / 2>(p, k_off, kr[b]);
+      else
+#pragma unroll
+        for (int c = 0; c < QC; ++c) load_words<4>(p, k_off + c * 64, &kr[b][4 * c]);
+    }
+  };
+  auto load_values = [&](const Where& w) {
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int cb = 0; cb < R; ++cb) p[b][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-    // values, loaded ahead of their use
-    uint32_t vw[FMT == FMT_F32 ? 1 : NB * 4][FMT == FMT_BF16 ? UN / 2 : 1];
-    float vf[FMT == FMT_F32 ? 4 : 1][UN];
-    if constexpr (FMT == FMT_F32) {
-      float4 kr[QC];
-      const char* kp = a.k + base[0] * ROWB + (int64_t)(min(n, max(there[0] - 1, 0)) * tok) * ROWB + j * 16;
-#pragma unroll
-      for (int c = 0; c < QC; ++c) kr[c] = *(const float4*)(kp + c * 64);
-#pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const char* vp = a.v + base[0] * ROWB + (int64_t)(min(4 * j + r, max(there[0] - 1, 0)) * tok) * ROWB + n * (UN * 4);
-#pragma unroll
-        for (int i = 0; i < UN; i += 4) *(float4*)&vf[r][i] = *(const float4*)(vp + i * 4);
+        const char* p = vh + ((uint64_t)w.row[b] * ROWB + r * tokb);
+        uint32_t (&x)[VW] = vw[b * 4 + r];
+        if constexpr (FMT == FMT_Q4 && UN == 4) {
+          x[0] = load_half(p, v_off);
+        } else {
+          load_words<VW < 4 ? VW : 4>(p, v_off, x);
+          if constexpr (VW == 8) load_words<4>(p, v_off + 16, &x[4]);
+        }
       }
+  };
+  auto scales_of = [&](const Where& w, const uint32_t* from, uint32_t (&x)[NG]) {       // lane = key of the tile
+    uint32_t row0 = vector(w.row[0]);
+#pragma unroll
+    for (int b = 1; b < NB; ++b) row0 = j == b ? vector(w.row[b]) : row0;
+    const uint64_t row = (row0 + (uint64_t)(h * pg.head_s + n * pg.tok_s)) * NG;
+    if constexpr (NG == 4) *(uint4*)x = *(const uint4*)(from + row);
+    else *(uint2*)x = *(const uint2*)(from + row);
+  };
+  auto load_scales = [&](const Where& w) {
+    scales_of(w, a.ks, sk);
+    scales_of(w, a.vs, sv);
+  };
+
+  Where at = find(k_begin);
+  if (k_begin < k_end) {
+    load_keys(at);
+    if constexpr (FMT == FMT_Q4) load_scales(at);
+    load_values(at);
+  }
+  uint32_t nib_mask = 0x00780078u, nib_base = 0x41804180u;
+  if constexpr (FMT == FMT_Q4) asm("" : "+s"(nib_mask), "+v"(nib_base));      // (one of two constants may be scalar)
+
+  for (int k0 = k_begin; k0 < k_end; k0 += 4 * TK) {
+    const Where next = find(k0 + 4 * TK);
+    const bool more = k0 + 4 * TK < k_end;
+    f32x4 p[NB][R];
+    const bool masked = k0 + TK > min(k_end, lim_lo) || at.ok != (1 << NB) - 1;
+    auto there = [&](int b) { return at.ok >> b & 1 ? min(k_end - (k0 + 16 * b), 16) : 0; };
+    auto seen = [&](int b, int r, int cb) { return 4 * j + r < there(b) && k0 + 16 * b + 4 * j + r < lim[cb]; };
+    bool odd_scales = false;
+
+    // ---- logits
+    if constexpr (FMT == FMT_F32) {
+#pragma unroll
+      for (int cb = 0; cb < R; ++cb) p[0][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < QC; ++c)
 #pragma unroll
         for (int cb = 0; cb < R; ++cb) {
-          p[0][cb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[c].x, qf[cb][c].x, p[0][cb], 0, 0, 0);
-          p[0][cb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[c].y, qf[cb][c].y, p[0][cb], 0, 0, 0);
-          p[0][cb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[c].z, qf[cb][c].z, p[0][cb], 0, 0, 0);
-          p[0][cb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[c].w, qf[cb][c].w, p[0][cb], 0, 0, 0);
+          const float y[4] = {qf[cb][c].x, qf[cb][c].y, qf[cb][c].z, qf[cb][c].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            p[0][cb] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[0][4 * c + i]), y[i], p[0][cb], 0, 0, 0);
         }
     } else if constexpr (FMT == FMT_BF16) {
-      uint4 kr[NB][QC];
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const char* kp = a.k + base[b] * ROWB + (int64_t)(n * tok) * ROWB + j * 16;
-#pragma unroll
-        for (int c = 0; c < QC; ++c) kr[b][c] = *(const uint4*)(kp + c * 64);
-      }
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const char* vp = a.v + base[b] * ROWB + (int64_t)((4 * j + r) * tok) * ROWB + n * (UN * 2);
-          if constexpr (UN == 8) *(uint4*)vw[b * 4 + r] = *(const uint4*)vp;
-          else *(uint2*)vw[b * 4 + r] = *(const uint2*)vp;
-        }
+        for (int cb = 0; cb < R; ++cb) p[b][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < QC; ++c)
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int cb = 0; cb < R; ++cb) p[b][cb] = mfma(kr[b][c], qo[cb][c].p[0], p[b][cb]);
+          for (int cb = 0; cb < R; ++cb) p[b][cb] = mfma(*(const uint4*)&kr[b][4 * c], qo[cb][c].p[0], p[b][cb]);
     } else {
-      uint32_t kr[NB][UN / 2];       // units 4j .. 4j+3 of key n of each block
+      __builtin_amdgcn_wave_barrier();
+      if constexpr (NG == 4) *(uint4*)&s_kz[lane * NG] = *(const uint4*)sk;
+      else *(uint2*)&s_kz[lane * NG] = *(const uint2*)sk;
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const char* kp = a.k + base[b] * ROWB + (int64_t)(n * tok) * ROWB + j * (UN * 2);
-        if constexpr (UN == 8) *(uint4*)kr[b] = *(const uint4*)kp;
-        else *(uint2*)kr[b] = *(const uint2*)kp;
-      }
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const char* vp = a.v + base[b] * ROWB + (int64_t)((4 * j + r) * tok) * ROWB + n * (UN / 2);
-          vw[b * 4 + r][0] = UN == 8 ? *(const uint32_t*)vp : *(const uint16_t*)vp;
-        }
-      // steps and zeros: lane = key of the tile
-      {
-        int64_t row = base[0];
-#pragma unroll
-        for (int b = 1; b < NB; ++b) row = j == b ? base[b] : row;
-        row = (row + (int64_t)(n * tok)) * NG;
-        uint32_t w[2][NG];
-        if constexpr (NG == 4) {
-          *(uint4*)w[0] = *(const uint4*)(a.ks + row);
-          *(uint4*)w[1] = *(const uint4*)(a.vs + row);
-        } else {
-          *(uint2*)w[0] = *(const uint2*)(a.ks + row);
-          *(uint2*)w[1] = *(const uint2*)(a.vs + row);
-        }
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          float y[2 * NG];
-#pragma unroll
-          for (int f = 0; f < NG; ++f) {
-            y[2 * f] = __uint_as_float(w[m][f] << 16);
-            y[2 * f + 1] = __builtin_fmaf(-16.f, y[2 * f], __uint_as_float(w[m][f] & 0xFFFF0000u));
+      for (int f = 0; f < NG; ++f) {
+        if (masked) {
+          const float x = __uint_as_float(sv[f] << 16), y = __uint_as_float(sv[f] & 0xFFFF0000u);
+          if (!(x - x == 0.f && y - y == 0.f)) {
+            sv[f] = 0u;
+            odd_scales = true;
           }
-#pragma unroll
-          for (int f = 0; f < NG; f += 2)
-            *(float4*)&scales[(m * 64 + lane) * (2 * NG) + 2 * f] = make_float4(y[2 * f], y[2 * f + 1], y[2 * f + 2], y[2 * f + 3]);
         }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        const float st = __uint_as_float(sv[f] << 16);
+        s_ks[f * 64 + lane] = __uint_as_float(sk[f] << 16);
+        s_vs[f * 64 + lane] = st;
+        s_vz[f * 64 + lane] = __builtin_fmaf(-16.f, st, __uint_as_float(sv[f] & 0xFFFF0000u));
       }
+      odd_scales = __ballot(odd_scales);
+      if (more) load_scales(next);
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
+        // sum over the groups of zero * (sum of q) - 16 step * (sum of q), as one product: lane j the group j
+        uint32_t zw = s_kz[(16 * b + n) * NG + (NG == 4 ? j : (j & 1))];
+        if (NG == 2 && j > 1) zw = 0u;
+        const uint4 za = make_uint4(__builtin_amdgcn_perm(zw, zw, 0x07060706u), __builtin_amdgcn_perm(zw, zw, 0x05040706u),
+                                    __builtin_amdgcn_perm(zw, zw, 0x05040504u), 0u);
         uint4 op[NG];                 // 16 + code as bf16, group by group
 #pragma unroll
         for (int f = 0; f < NG; ++f) {
@@ -372,42 +460,41 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a) {
             lo = kr[b][0];
             hi = kr[b][1];
           }
-          const int e0 = (2 * f) & 3;  // nibble of a half word; to bits 3 .. 6
-          auto put = [](uint32_t x, int i) {
-            return ((i == 0 ? x << 3 : x >> (4 * i - 3)) & 0x00780078u) | 0x41804180u;
-          };
-          op[f] = make_uint4(put(lo, e0), put(hi, e0), put(lo, e0 + 1), put(hi, e0 + 1));
+          const int e0 = (2 * f) & 3;
+          op[f] = make_uint4(sixteen_plus(lo, e0, nib_mask, nib_base), sixteen_plus(hi, e0, nib_mask, nib_base),
+                             sixteen_plus(lo, e0 + 1, nib_mask, nib_base), sixteen_plus(hi, e0 + 1, nib_mask, nib_base));
         }
-        float y[4][2 * NG];
+        f32x4 st[NG];                 // steps of keys 4 j .. 4 j + 3
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int f = 0; f < NG; ++f) st[f] = *(const f32x4*)&s_ks[f * 64 + 16 * b + 4 * j];
 #pragma unroll
-          for (int f = 0; f < 2 * NG; f += 4) *(float4*)&y[r][f] = *(const float4*)&scales[(16 * b + 4 * j + r) * (2 * NG) + f];
-#pragma unroll
-        for (int cb = 0; cb < R; ++cb)
+        for (int cb = 0; cb < R; ++cb) {
+          p[b][cb] = mfma(za, qz[cb], f32x4{0.f, 0.f, 0.f, 0.f});
+          f32x4 t[NG];
 #pragma unroll
           for (int f = 0; f < NG; ++f) {
-            f32x4 t = {0.f, 0.f, 0.f, 0.f};
+            t[f] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int pl = 0; pl < QP; ++pl) t = mfma(op[f], qo[cb][f].p[pl], t);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const float z = __builtin_fmaf(y[r][2 * f + 1], qsum[cb][f], p[b][cb][r]);
-              p[b][cb][r] = __builtin_fmaf(y[r][2 * f], t[r], z);
-            }
+            for (int pl = 0; pl < QP; ++pl) t[f] = mfma(op[f], qo[cb][f].p[pl], t[f]);
           }
+#pragma unroll
+          for (int f = 0; f < NG; ++f)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) p[b][cb][r] = __builtin_fmaf(st[f][r], t[f][r], p[b][cb][r]);
+        }
+        __builtin_amdgcn_sched_barrier(0);        // (operands of one block at a time: registers)
       }
     }
+    if (more) load_keys(next);
 
     // ---- softmax: lane = row, key 16 b + 4 j + r in register r of block b
-    if (!whole) {
+    if (masked) {
 #pragma unroll
       for (int cb = 0; cb < R; ++cb)
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (4 * j + r >= there[b] || k0 + 16 * b + 4 * j + r >= lim[cb]) p[b][cb][r] = -INFINITY;
+          for (int r = 0; r < 4; ++r) p[b][cb][r] = seen(b, r, cb) ? p[b][cb][r] : -INFINITY;
     }
     bool far = false;
     float top[R];
@@ -450,45 +537,52 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a) {
 
     // ---- O^T += V^T P^T
     if constexpr (FMT == FMT_F32) {
-      bool bad = false;
-      if (!whole) {
+      auto val = [&](int r, int i) { return __uint_as_float(vw[r][i]); };
+      if (masked) {
+        keep_here(vw);
+        bool bad = false;
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
           for (int i = 0; i < UN; ++i) {
-            if (4 * j + r >= there[0]) vf[r][i] = 0.f;
-            bad = bad || !(vf[r][i] - vf[r][i] == 0.f);
+            if (4 * j + r >= there(0)) vw[r][i] = 0u;
+            bad = bad || !(val(r, i) - val(r, i) == 0.f);
           }
-      }
-      if (__builtin_expect(__ballot(bad) != 0, 0)) {
-        // values that are not finite, in a tile where some rows do not see every key (0 times them would be NaN): they come
-        // first and key by key, a row that does not see the key keeps its sums, and zeros take their places below
-        for (int kk = 0; kk < 16; ++kk) {
+        if (__ballot(bad)) {
+          // values that are not finite, in a tile where some rows do not see every key (0 times them would be NaN): they come
+          // first and key by key, from LDS, a row that does not see the key keeps its sums, and zeros take their places below
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (r == (kk & 3)) {
 #pragma unroll
-              for (int i = 0; i < UN; ++i) {
-                const float x = j == kk >> 2 && !(vf[r][i] - vf[r][i] == 0.f) ? vf[r][i] : 0.f;
+            for (int i = 0; i < UN; ++i) {
+              s_rare[(r * UN + i) * 64 + lane] = val(r, i) - val(r, i) == 0.f ? 0u : vw[r][i];
+              if (!(val(r, i) - val(r, i) == 0.f)) vw[r][i] = 0u;
+            }
+#pragma unroll 1
+          for (int kk = 0; kk < 16; ++kk) {
+            const int r = kk & 3;
+            const bool see = kk < there(0);
+            float w[R];
 #pragma unroll
-                for (int cb = 0; cb < R; ++cb) {
-                  const f32x4 t = __builtin_amdgcn_mfma_f32_16x16x4f32(x, p[0][cb][r], o[i][cb], 0, 0, 0);
-                  o[i][cb] = kk < there[0] && k0 + kk < lim[cb] ? t : o[i][cb];
-                }
+            for (int cb = 0; cb < R; ++cb) w[cb] = r == 0 ? p[0][cb][0] : r == 1 ? p[0][cb][1] : r == 2 ? p[0][cb][2] : p[0][cb][3];
+#pragma unroll
+            for (int i = 0; i < UN; ++i) {
+              const float x = j == kk >> 2 ? __uint_as_float(s_rare[(r * UN + i) * 64 + lane]) : 0.f;
+#pragma unroll
+              for (int cb = 0; cb < R; ++cb) {
+                const f32x4 t = __builtin_amdgcn_mfma_f32_16x16x4f32(x, w[cb], o[i][cb], 0, 0, 0);
+                o[i][cb] = see && k0 + kk < lim[cb] ? t : o[i][cb];
               }
             }
+          }
         }
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int i = 0; i < UN; ++i) vf[r][i] = vf[r][i] - vf[r][i] == 0.f ? vf[r][i] : 0.f;
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int i = 0; i < UN; ++i)
 #pragma unroll
-          for (int cb = 0; cb < R; ++cb) o[i][cb] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[r][i], p[0][cb][r], o[i][cb], 0, 0, 0);
+          for (int cb = 0; cb < R; ++cb) o[i][cb] = __builtin_amdgcn_mfma_f32_16x16x4f32(val(r, i), p[0][cb][r], o[i][cb], 0, 0, 0);
     } else if constexpr (FMT == FMT_BF16) {
       // eight keys of a lane: registers r of both blocks
       Op<NP> po[R];
@@ -502,41 +596,44 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a) {
         return make_uint4(__builtin_amdgcn_perm(w[1][i / 2], w[0][i / 2], sel), __builtin_amdgcn_perm(w[3][i / 2], w[2][i / 2], sel),
                           __builtin_amdgcn_perm(w[5][i / 2], w[4][i / 2], sel), __builtin_amdgcn_perm(w[7][i / 2], w[6][i / 2], sel));
       };
-      bool bad = false;
-      if (!whole) {
+      if (masked) {
+        keep_here(vw);
+        bool bad = false;
 #pragma unroll
         for (int x = 0; x < 8; ++x)
 #pragma unroll
           for (int i = 0; i < UN / 2; ++i) {
-            if (4 * j + (x & 3) >= there[x >> 2]) vw[x][i] = 0u;
+            if (4 * j + (x & 3) >= there(x >> 2)) vw[x][i] = 0u;
             bad = bad || (vw[x][i] & 0x7F80u) == 0x7F80u || (vw[x][i] & 0x7F800000u) == 0x7F800000u;
           }
-      }
-      if (__builtin_expect(__ballot(bad) != 0, 0)) {       // as above
-        auto odd = [](uint32_t w) {   // the halves that are not finite
-          return ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
-        };
-        for (int kk = 0; kk < 32; ++kk) {
-          const int at = kk >> 4 << 2 | (kk & 3), have = kk >> 4 ? there[1] : there[0];
-          const bool mine = j == (kk >> 2 & 3);
-          uint32_t w1[8][UN / 2];
+        if (__ballot(bad)) {       // as above
 #pragma unroll
           for (int x = 0; x < 8; ++x)
 #pragma unroll
-            for (int i = 0; i < UN / 2; ++i) w1[x][i] = mine && x == at ? vw[x][i] & odd(vw[x][i]) : 0u;
-#pragma unroll
-          for (int i = 0; i < UN; ++i)
-#pragma unroll
-            for (int cb = 0; cb < R; ++cb) {
-              // (the first part of a weight alone: parts of unlike sign would make a NaN of an infinity)
-              const f32x4 t = mfma(operand(w1, i), po[cb].p[0], o[i][cb]);
-              o[i][cb] = (kk & 15) < have && k0 + kk < lim[cb] ? t : o[i][cb];
+            for (int i = 0; i < UN / 2; ++i) {
+              const uint32_t w = vw[x][i];      // the halves that are not finite
+              const uint32_t odd = ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+              s_rare[(x * (UN / 2) + i) * 64 + lane] = w & odd;
+              vw[x][i] = w & ~odd;
             }
+#pragma unroll 1
+          for (int kk = 0; kk < 32; ++kk) {
+            const int x = kk >> 4 << 2 | (kk & 3);
+            const bool see = (kk & 15) < (kk >> 4 ? there(1) : there(0));
+#pragma unroll
+            for (int i = 0; i < UN; ++i) {
+              uint32_t w = j == (kk >> 2 & 3) ? s_rare[(x * (UN / 2) + i / 2) * 64 + lane] : 0u;
+              w = (i & 1 ? w >> 16 : w & 0xFFFFu) << (16 * (x & 1));
+              const uint4 one = make_uint4(x >> 1 == 0 ? w : 0u, x >> 1 == 1 ? w : 0u, x >> 1 == 2 ? w : 0u, x >> 1 == 3 ? w : 0u);
+#pragma unroll
+              for (int cb = 0; cb < R; ++cb) {
+                // (the first part of a weight alone: parts of unlike sign would make a NaN of an infinity)
+                const f32x4 t = mfma(one, po[cb].p[0], o[i][cb]);
+                o[i][cb] = see && k0 + kk < lim[cb] ? t : o[i][cb];
+              }
+            }
+          }
         }
-#pragma unroll
-        for (int x = 0; x < 8; ++x)
-#pragma unroll
-          for (int i = 0; i < UN / 2; ++i) vw[x][i] &= ~odd(vw[x][i]);
       }
 #pragma unroll
       for (int i = 0; i < UN; ++i) {
@@ -547,14 +644,32 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a) {
           for (int pl = NP - 1; pl >= 0; --pl) o[i][cb] = mfma(x, po[cb].p[pl], o[i][cb]);
       }
     } else {
+      if (masked && odd_scales) {
+        // steps or zeros that are not finite, in a tile where some rows do not see every key (0 times them would be NaN): zeros
+        // stand in their places, and here the rows that see the key get what it adds to their groups
+        uint32_t raw[NG];
+        scales_of(at, a.vs, raw);
+#pragma unroll 1
+        for (int kk = 0; kk < 64; ++kk) {
+          const int b = kk >> 4, r = kk & 3;
+#pragma unroll
+          for (int f = 0; f < NG; ++f) {
+            const uint32_t w = __builtin_amdgcn_readlane(raw[f], kk);
+            const float step = __uint_as_float(w << 16), zero = __uint_as_float(w & 0xFFFF0000u);
+            if (step - step == 0.f && zero - zero == 0.f) continue;
+            const float z = step - step == 0.f ? zero : __builtin_nanf("");
+#pragma unroll
+            for (int cb = 0; cb < R; ++cb) {
+              float x = 0.f;
+#pragma unroll
+              for (int i = 0; i < NB * 4; ++i) x = i == b * 4 + r ? p[i >> 2][cb][i & 3] : x;
+              if (j == (kk >> 2 & 3) && (kk & 15) < there(b) && k0 + kk < lim[cb]) corr[cb][f] = __builtin_fmaf(x, z, corr[cb][f]);
+            }
+          }
+        }
+      }
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
-        float y[8][2 * NG];           // {step, zero - 16 step} of the lane's eight keys
-#pragma unroll
-        for (int x = 0; x < 8; ++x)
-#pragma unroll
-          for (int f = 0; f < 2 * NG; f += 4)
-            *(float4*)&y[x][f] = *(const float4*)&scales[(64 + 32 * hf + (x >> 2) * 16 + 4 * j + (x & 3)) * (2 * NG) + f];
         // codes of keys (2 i, 2 i + 1), a half word of a unit each
         uint32_t pr[4][UN / 4];
 #pragma unroll
@@ -564,6 +679,12 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a) {
         }
 #pragma unroll
         for (int f = 0; f < NG; ++f) {
+          f32x4 st[2], z[2];
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            st[b] = *(const f32x4*)&s_vs[f * 64 + 32 * hf + 16 * b + 4 * j];
+            z[b] = *(const f32x4*)&s_vz[f * 64 + 32 * hf + 16 * b + 4 * j];
+          }
           Op<NP> po[R];
 #pragma unroll
           for (int cb = 0; cb < R; ++cb) {
@@ -571,34 +692,34 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               const float w = p[2 * hf + (i >> 2)][cb][i & 3];
-              float st = y[i][2 * f], z = y[i][2 * f + 1];
-              // (a key that is not seen: its scale may hold anything, and 0 times it need not be 0)
-              const int at = (i >> 2) * 16 + 4 * j + (i & 3);
-              if (!whole && (4 * j + (i & 3) >= there[2 * hf + (i >> 2)] || k0 + 32 * hf + at >= lim[cb])) { st = 0.f; z = 0.f; }
-              x[i] = w * st;
-              corr[cb][f] = __builtin_fmaf(w, z, corr[cb][f]);
+              x[i] = w * st[i >> 2][i & 3];
+              corr[cb][f] = __builtin_fmaf(w, z[i >> 2][i & 3], corr[cb][f]);
             }
             po[cb] = split8<NP>(x);
           }
 #pragma unroll
           for (int i = 2 * f; i < 2 * f + 2; ++i) {
-            const int nib = i & 3;
-            auto put = [&](uint32_t x) {
-              return ((nib == 0 ? x << 3 : x >> (4 * nib - 3)) & 0x00780078u) | 0x41804180u;
-            };
-            const uint4 x = make_uint4(put(pr[0][i / 4]), put(pr[1][i / 4]), put(pr[2][i / 4]), put(pr[3][i / 4]));
+            const uint4 x = make_uint4(sixteen_plus(pr[0][i / 4], i & 3, nib_mask, nib_base), sixteen_plus(pr[1][i / 4], i & 3, nib_mask, nib_base),
+                                       sixteen_plus(pr[2][i / 4], i & 3, nib_mask, nib_base), sixteen_plus(pr[3][i / 4], i & 3, nib_mask, nib_base));
 #pragma unroll
             for (int cb = 0; cb < R; ++cb)
 #pragma unroll
               for (int pl = NP - 1; pl >= 0; --pl) o[i][cb] = mfma(x, po[cb].p[pl], o[i][cb]);
           }
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
     }
+    if (more) load_values(next);
+    at = next;
   }
 
   // ---- the four wavefronts' sums joined in LDS
   __syncthreads();                    // (the scales of the last tile lie in the same place)
+  // (what the end takes of the arguments is read here, not held in scalar registers through the loop)
+  auto* again = (const __attribute__((address_space(4))) AttendArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(again));
+  const AttendArgs& z = *(const AttendArgs*)again;
   float* sm_m = sm;                   // [4][16 R]
   float* sm_l = sm + 4 * 16 * R;
   float* sm_o = sm + 8 * 16 * R;      // [4][16 R][LDO]
@@ -647,22 +768,22 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a) {
     }
     const int row = row0 + r;
     if (ch.count > 1) {
-      const int64_t at = (int64_t)((ch.slot0 + ch.index) * a.Hy + hy) * ((int64_t)pg.G * pg.max_new) + row;
-      *(float4*)&a.part_o[at * D + c] = x;
+      const int64_t at = (int64_t)((ch.slot0 + ch.index) * z.Hy + hy) * ((int64_t)z.pg.G * z.pg.max_new) + row;
+      *(float4*)&z.part_o[at * D + c] = x;
       if (c == 0) {
-        a.part_m[at] = M;
-        a.part_l[at] = L;
+        z.part_m[at] = M;
+        z.part_l[at] = L;
       }
     } else {
-      const int tok = row / pg.G, head = h * pg.G + row - tok * pg.G;
-      store_out(a, nr.first + tok, head, c, x, M, L);
+      const int tok = row / z.pg.G, head = h * z.pg.G + row - tok * z.pg.G;
+      store_out(z, nr.first + tok, head, c, x, M, L);
     }
   }
 }
 
 template <int FMT, typename T, int D, int NP, int R>
 int run_attend(const AttendArgs& a, hipStream_t st) {
-  constexpr size_t join = (8 * 16 * R + (size_t)4 * 16 * R * (D + 4)) * 4, scales = FMT == FMT_Q4 ? 4 * 2 * 64 * (D / 32) * 2 * 4 : 0;
+  constexpr size_t join = (8 * 16 * R + (size_t)4 * 16 * R * (D + 4)) * 4, scales = FMT == FMT_Q4 ? 4 * 4 * 64 * (D / 32) * 4 : 0;
   constexpr size_t lds = join > scales ? join : scales;
   const int64_t blocks = a.row_blocks == 1 ? a.units : (int64_t)(a.units + 7) / 8 * 8 * a.row_blocks;
   auto kern = k_attend<FMT, T, D, NP, R>;
