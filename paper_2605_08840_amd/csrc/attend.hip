@@ -13,7 +13,7 @@ template <int D>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
   constexpr int TPR = D / 4, NGR = 256 / TPR;
   __shared__ float4 sm_x[NGR][TPR];
-  __shared__ float sm_ml[2][NGR];
+  __shared__ float sm_l[NGR], sm_m[4];
   const Pages& pg = a.pg;
   const int64_t b = wide_block(), per = (int64_t)pg.max_new * pg.Hq;
   if (b >= per * pg.n_seqs) return;
@@ -24,36 +24,38 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
   if (pl.y < 2) return;
   const int hy = a.per_head ? 0 : h, row = i * pg.G + head - h * pg.G, rows = pg.G * pg.max_new;
   const int g = threadIdx.x / TPR, c = threadIdx.x % TPR;
+  auto slot = [&](int k) { return (int64_t)((pl.x + k) * a.Hy + hy) * rows + row; };
+  // references and sums first, a chunk each thread: the factors of the sums then need no second look
   float M = -INFINITY, L = 0.f;
+  for (int k = threadIdx.x; k < pl.y; k += 256) M = fmaxf(M, a.part_m[slot(k)]);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) M = fmaxf(M, __shfl_xor(M, d));
+  if ((threadIdx.x & 63) == 0) sm_m[threadIdx.x >> 6] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(sm_m[0], sm_m[1]), fmaxf(sm_m[2], sm_m[3]));
+  // (a chunk of which the row sees nothing has a reference of -inf and sums of 0)
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
   for (int k = g; k < pl.y; k += NGR) {
-    const int64_t at = (int64_t)((pl.x + k) * a.Hy + hy) * rows + row;
-    const float m = a.part_m[at], l = a.part_l[at];
-    const float4 y = *(const float4*)&a.part_o[at * D + c * 4];
-    const float n = fmaxf(M, m);
-    // (a chunk of which the row sees nothing has a reference of -inf and sums of 0)
-    const float fo = M == n ? 1.f : __builtin_amdgcn_exp2f(M - n), fn = m == n ? 1.f : __builtin_amdgcn_exp2f(m - n);
-    M = n;
-    L = L * fo + l * fn;
-    x.x = x.x * fo + y.x * fn; x.y = x.y * fo + y.y * fn; x.z = x.z * fo + y.z * fn; x.w = x.w * fo + y.w * fn;
+    const float m = a.part_m[slot(k)], l = a.part_l[slot(k)];
+    const float4 y = *(const float4*)&a.part_o[slot(k) * D + c * 4];
+    const float f = m == M ? 1.f : __builtin_amdgcn_exp2f(m - M);
+    L = __builtin_fmaf(f, l, L);
+    x.x = __builtin_fmaf(f, y.x, x.x); x.y = __builtin_fmaf(f, y.y, x.y); x.z = __builtin_fmaf(f, y.z, x.z); x.w = __builtin_fmaf(f, y.w, x.w);
   }
   sm_x[g][c] = x;
-  if (c == 0) { sm_ml[0][g] = M; sm_ml[1][g] = L; }
+  if (c == 0) sm_l[g] = L;
   __syncthreads();
   if (g) return;
-  float N = -INFINITY;
-#pragma unroll
-  for (int k = 0; k < NGR; ++k) N = fmaxf(N, sm_ml[0][k]);
   L = 0.f;
   x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
   for (int k = 0; k < NGR; ++k) {
-    const float m = sm_ml[0][k], f = m == N ? 1.f : __builtin_amdgcn_exp2f(m - N);
     const float4 y = sm_x[k][c];
-    L = __builtin_fmaf(f, sm_ml[1][k], L);
-    x.x = __builtin_fmaf(f, y.x, x.x); x.y = __builtin_fmaf(f, y.y, x.y); x.z = __builtin_fmaf(f, y.z, x.z); x.w = __builtin_fmaf(f, y.w, x.w);
+    L += sm_l[k];
+    x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
   }
-  store_out(a, nr.first + i, head, c * 4, x, N, L);
+  store_out(a, nr.first + i, head, c * 4, x, M, L);
 }
 
 // Blocks of 16 rows of a wavefront: as many as the rows fill, up to what its registers hold.
@@ -71,7 +73,7 @@ AttendPlan attend_plan(const Pages& pg) {
   p.entries = per_head ? (int64_t)pg.n_seqs * pg.Hkv : pg.n_seqs;
   p.Hy = per_head ? 1 : pg.Hkv;
   p.c_min = pg.fmt == RESTKV_Q4 ? 4 : 2;          // (a tile for each wavefront)
-  p.target = n_cu() * (p.R == 1 ? 4 : 2);
+  p.target = n_cu() * 2;
   const int64_t tiles = (pg.max_len + ATT_TILE - 1) / ATT_TILE, each = p.Hy * p.row_blocks;
   // no entry has two chunks: chunks hold the sum of all tiles, or the longest entry fits the smallest chunk
   const bool single = each >= p.target || tiles <= p.c_min;
@@ -116,7 +118,7 @@ int launch_attend(const Pages& pg, const void* q, const void* k_pages, const voi
   }
   a.entries = (int)p.entries; a.per_head = pg.lens_sh != 0; a.Hy = (int)p.Hy;
   a.row_blocks = (int)p.row_blocks; a.units = (int)(p.chunks * p.Hy);
-  a.c_min = p.c_min; a.target = p.target;
+  a.c_min = p.c_min; a.share = (float)((double)(p.Hy * p.row_blocks) / p.target * (1 + 0x1p-23));
   const int qel = pg.dtype == RESTKV_F32 ? 4 : 8;
   a.vec_q = !((uintptr_t)q & 15u) && !((pg.q_st | pg.q_sh) & (qel - 1));
   const int oal = pg.out_dtype == RESTKV_F32 ? 15 : 7;

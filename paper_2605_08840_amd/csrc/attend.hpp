@@ -23,50 +23,73 @@ struct AttendArgs {
   int2* plan;                       // [entries] {first slot, chunks} of an entry (chunks < 2: the output is there already)
   float* part_m; float* part_l; float* part_o;   // [slots * Hy, rows] and [.., d]: chunks of entries that have several
   int entries, per_head, Hy;        // an entry is a sequence, or with lengths per head a (sequence, head); Hy heads share it
-  int row_blocks, units, c_min, target, vec_q, vec_out;
+  int row_blocks, units, c_min, vec_q, vec_out;
+  float share;                      // Hy * row_blocks / workgroups wanted
 };
 
 constexpr int ATT_TILE = 64;        // chunks are whole tiles of 64 keys
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
+// Sum over the lanes up to this one.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);   // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);   // row_shr:2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);   // row_shr:4
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);   // row_shr:8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);   // lane 15 of rows 0, 2 to the rows behind them
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);   // lane 31 to the upper half
+  return x;
+}
+
 // What a workgroup takes.  Chunks are of equal size C over all entries: enough for `target` workgroups in all, so that a
-// long sequence among short ones is cut as finely as the whole asks for, and short batches not at all.
-struct Chunk { int e, tile0, tile1, index, count, slot0; };
+// long sequence among short ones is cut as finely as the whole asks for, and short batches not at all.  Every wavefront
+// works this out for itself from the lengths, 64 entries at a time.
+struct Chunk { int e, tile0, tile1, index, count, slot0, told, first, n; };
 __device__ __forceinline__ bool find_chunk(const AttendArgs& a, int x, Chunk& o) {
   const Pages& pg = a.pg;
   const int lane = threadIdx.x & 63;
-  auto tiles_of = [&](int e) {
-    if (e >= a.entries) return 0;
-    const int s = a.per_head ? e / pg.Hkv : e, h = a.per_head ? e - s * pg.Hkv : 0;
-    const int n = pg.new_start ? pg.new_start[s + 1] > pg.new_start[s] : 1;
-    return n ? (cache_len(pg, s, h) + ATT_TILE - 1) / ATT_TILE : 0;
+  int told = 0, first = 0, n = 0, tiles = 0;     // of entry base + lane
+  auto read = [&](int base) {
+    const int e = base + lane;
+    told = first = n = tiles = 0;
+    if (e < a.entries) {
+      const int s = a.per_head ? e / pg.Hkv : e, h = a.per_head ? e - s * pg.Hkv : 0;
+      told = told_len(pg, s, h);
+      const NewRows nr = new_rows(pg, s);
+      first = nr.first;
+      n = nr.n;
+      if (n) tiles = (min(told, pg.max_len) + ATT_TILE - 1) / ATT_TILE;
+    }
   };
-  int64_t total = 0;
-  for (int base = 0; base < a.entries; base += 64) total += wave_sum((uint32_t)tiles_of(base + lane));
-  const int64_t want = (total * (a.Hy * a.row_blocks) + a.target - 1) / a.target;
-  const int C = (int)(want < a.c_min ? a.c_min : want > (1 << 25) ? (1 << 25) : want);
+  read(0);
+  int64_t total = wave_sum((uint32_t)tiles);
+  for (int base = 64; base < a.entries; base += 64) {
+    read(base);
+    total += wave_sum((uint32_t)tiles);
+  }
+  // tiles of a chunk: total / (chunks per head and row block), rounded up (share is, too, and so is the product)
+  const float want = (float)total * a.share * (1.f + 0x1p-20f) + 1.f;
+  const int C = want < (float)a.c_min ? a.c_min : want > 0x1p25f ? 1 << 25 : (int)want;
   int run = 0, slots = 0;
   for (int base = 0; base < a.entries; base += 64) {
-    const int e = base + lane, tiles = tiles_of(e);
-    const int cnt = e < a.entries ? max(1, (tiles + C - 1) / C) : 0;
-    int inc = cnt, sl = cnt > 1 ? cnt : 0;
-    const int own = sl;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int p = __shfl_up(inc, d), q = __shfl_up(sl, d);
-      if (lane >= d) { inc += p; sl += q; }
-    }
+    if (a.entries > 64) read(base);
+    const int cnt = base + lane < a.entries ? max(1, (tiles + C - 1) / C) : 0, own = cnt > 1 ? cnt : 0;
+    const int inc = wave_scan(cnt), sl = wave_scan(own);
     const unsigned long long hit = __ballot(run + inc > x);
     if (hit) {
       const int l = __builtin_ctzll(hit);
+      auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
       o.e = base + l;
-      o.count = __builtin_amdgcn_readlane(cnt, l);
-      o.index = x - run - __builtin_amdgcn_readlane(inc, l) + o.count;
-      o.slot0 = slots + __builtin_amdgcn_readlane(sl - own, l);
-      const int t = __builtin_amdgcn_readlane(tiles, l), each = (t + o.count - 1) / o.count;
+      o.count = of(cnt);
+      o.index = x - run - of(inc) + o.count;
+      o.slot0 = slots + of(sl - own);
+      const int t = of(tiles), each = o.count == 1 ? t : (t + o.count - 1) / o.count;
       o.tile0 = min(o.index * each, t);
       o.tile1 = min(o.tile0 + each, t);
+      o.told = of(told);
+      o.first = of(first);
+      o.n = of(n);
       return true;
     }
     run += __builtin_amdgcn_readlane(inc, 63);
@@ -151,22 +174,21 @@ __device__ __forceinline__ int uniform_load(const int32_t* p) {
 }
 
 // N words at a uniform address (held in scalar registers, so that the load adds the lane's 32-bit offset by itself).
+template <int N> struct WordsOf { typedef uint32_t type __attribute__((ext_vector_type(N))); };
+template <> struct WordsOf<1> { typedef uint32_t type; };
+template <int N> using Words = typename WordsOf<N>::type;
 template <int N>
-__device__ __forceinline__ void load_words(const char* base, uint32_t off, uint32_t* x) {
+__device__ __forceinline__ Words<N> load_words(const char* base, uint32_t off) {
   uint64_t u = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)base >> 32)) << 32 |
                (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(uint64_t)base);
-  asm("" : "+s"(u));
-  typedef uint32_t words __attribute__((ext_vector_type(N)));
+  asm("" : "+s"(u), "+v"(off));      // (the offset's extension stays beside the load)
   typedef const __attribute__((address_space(1))) char* global;
-  const words w = *(const __attribute__((address_space(1))) words*)((global)u + off);
-#pragma unroll
-  for (int i = 0; i < N; ++i) x[i] = w[i];
+  return *(const __attribute__((address_space(1))) Words<N>*)((global)u + off);
 }
-
 __device__ __forceinline__ uint32_t load_half(const char* base, uint32_t off) {
   uint64_t u = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)base >> 32)) << 32 |
                (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(uint64_t)base);
-  asm("" : "+s"(u));
+  asm("" : "+s"(u), "+v"(off));
   typedef const __attribute__((address_space(1))) char* global;
   return *(const __attribute__((address_space(1))) uint16_t*)((global)u + off);
 }
@@ -178,12 +200,16 @@ __device__ __forceinline__ uint32_t vector(uint32_t x) {
   return y;
 }
 // Rare code works on copies that the compiler knows nothing of, so that none of it moves into the common path.
-template <int N, int M>
-__device__ __forceinline__ void keep_here(uint32_t (&x)[N][M]) {
+template <typename V, int N>
+__device__ __forceinline__ void keep_here(V (&x)[N]) {
 #pragma unroll
-  for (int i = 0; i < N; ++i)
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
+}
+// Registers without a value from here on (where a load is left out, so that the old values need not be kept for it).
+template <typename V, int N>
+__device__ __forceinline__ void forget(V (&x)[N]) {
 #pragma unroll
-    for (int k = 0; k < M; ++k) asm volatile("" : "+v"(x[i][k]));
+  for (int i = 0; i < N; ++i) asm("" : "=v"(x[i]));
 }
 
 // Nibble i of each half word as the bfloat16 16 + code: the code goes to the upper four of its seven mantissa bits.
@@ -202,7 +228,7 @@ void k_attend(AttendArgs a) {
   constexpr int QP = FMT == FMT_Q4 ? planes_of<T> : 1;
   constexpr int TK = FMT == FMT_F32 ? 16 : FMT == FMT_BF16 ? 32 : 64, NB = TK / 16;
   constexpr int ROWB = FMT == FMT_F32 ? D * 4 : FMT == FMT_BF16 ? D * 2 : D / 2;
-  constexpr int LDO = D + 4;
+  constexpr int LDO = D + 4, QC = FMT == FMT_F32 ? D / 16 : D / 32;
   extern __shared__ __align__(16) float sm[];
   const Pages& pg = a.pg;
   const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
@@ -224,12 +250,12 @@ void k_attend(AttendArgs a) {
   if (!find_chunk(a, unit / a.Hy, ch)) return;
   const int e = __builtin_amdgcn_readfirstlane(ch.e);
   const int s = a.per_head ? e / pg.Hkv : e, h = a.per_head ? e - s * pg.Hkv : hy;
-  const NewRows nr = new_rows(pg, s);
+  const NewRows nr = {ch.first, ch.n};
   const int rows = pg.G * nr.n, row0 = rb * 16 * R;
   if (row0 >= rows) return;
   if (a.plan && ch.index == 0 && hy == 0 && rb == 0 && threadIdx.x == 0) a.plan[e] = make_int2(ch.slot0, ch.count);
 
-  const int told = told_len(pg, s, h), len = min(told, pg.max_len);
+  const int told = ch.told, len = min(told, pg.max_len);
   auto limit = [&](int row) {       // positions that a row sees
     return pg.causal ? min(max(told - nr.n + row / pg.G + 1, 0), len) : len;
   };
@@ -239,9 +265,92 @@ void k_attend(AttendArgs a) {
   const int k_begin = __builtin_amdgcn_readfirstlane(ch.tile0 * ATT_TILE) + wv * TK;
   const float sc = pg.scale * 1.44269504088896341f;
 
+  f32x4 o[UN][R];
+  float ref[R], l[R], corr[FMT == FMT_Q4 ? R : 1][NG];
+#pragma unroll
+  for (int cb = 0; cb < R; ++cb) {
+#pragma unroll
+    for (int i = 0; i < UN; ++i) o[i][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    ref[cb] = -INFINITY;
+    l[cb] = 0.f;
+    if constexpr (FMT == FMT_Q4)
+#pragma unroll
+      for (int f = 0; f < NG; ++f) corr[cb][f] = 0.f;
+  }
+  // of this wavefront's tile: {step, zero} of the keys as they are [64][NG], their steps [NG][64], the values' steps and
+  // zeros - 16 steps [NG][64] each (a read takes four keys of a group)
+  uint32_t* s_kz = (uint32_t*)sm + wv * (4 * 64 * NG);
+  float* s_ks = (float*)s_kz + 64 * NG;
+  float* s_vs = s_ks + 64 * NG;
+  float* s_vz = s_vs + 64 * NG;
+  float* s_rare = sm + wv * (UN * 4 * R * 64);       // the sums, for a moment (float32 and bfloat16 pages)
+
+  // ---- tiles: where the 16-key blocks are (each lies in one page)
+  const int32_t* table = pg.table + s * pg.table_ss + h * pg.table_sh;
+  const int64_t tokb = pg.tok_s * ROWB;
+  const char* const kh = a.k + h * pg.head_s * ROWB;
+  const char* const vh = a.v + h * pg.head_s * ROWB;
+  struct Where { uint32_t row[NB]; int ok; };    // first rows, and a bit for each block that has a page
+  auto find = [&](int k0) {
+    Where w;
+    w.ok = 0;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int t = k0 + 16 * b;
+      const int page = uniform_load(table + (min(t, k_end - 1) >> pg.lg_ps));
+      const bool ok = (uint32_t)page < (uint32_t)pg.n_pages && t < k_end;
+      w.row[b] = ok ? (uint32_t)page * (uint32_t)pg.page_s + (t & ((1 << pg.lg_ps) - 1)) * (uint32_t)pg.tok_s : 0u;
+      w.ok |= ok ? 1 << b : 0;
+    }
+    return w;
+  };
+  // lane offsets of a block: key n, part j of its row; value row 4 j + r, unit n
+  const uint32_t k_off = (uint32_t)(n * tokb) + j * (FMT == FMT_Q4 ? UN * 2 : 16);
+  const uint32_t v_off = (uint32_t)(4 * j * tokb) + n * (ROWB / 16);
+  constexpr int KV = FMT == FMT_Q4 ? UN / 2 : 4, KN = FMT == FMT_Q4 ? 1 : QC;      // words of a load, loads of a lane per block
+  constexpr int VV = FMT == FMT_F32 ? 4 : FMT == FMT_BF16 ? UN / 2 : 1, VN = FMT == FMT_F32 ? UN / 4 : 1;
+  Words<KV> kr[NB * KN];
+  Words<VV> vr[NB * 4 * VN];
+  Words<NG> sk[1], sv[1];
+  auto load_keys = [&](const Where& w) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int c = 0; c < KN; ++c) kr[b * KN + c] = load_words<KV>(kh + (uint64_t)w.row[b] * ROWB, k_off + c * 64);
+  };
+  auto load_values = [&](const Where& w) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < VN; ++c) {
+          const char* p = vh + ((uint64_t)w.row[b] * ROWB + r * tokb);
+          if constexpr (FMT == FMT_Q4 && UN == 4) vr[b * 4 + r] = load_half(p, v_off);
+          else vr[(b * 4 + r) * VN + c] = load_words<VV>(p, v_off + c * 16);
+        }
+  };
+  auto scales_of = [&](const Where& w, const uint32_t* from) {       // lane = key of the tile
+    uint32_t row0 = vector(w.row[0]);
+#pragma unroll
+    for (int b = 1; b < NB; ++b) row0 = j == b ? vector(w.row[b]) : row0;
+    const uint64_t row = (row0 + (uint64_t)(h * pg.head_s + n * pg.tok_s)) * NG;
+    return *(const Words<NG>*)(from + row);
+  };
+  auto load_scales = [&](const Where& w) {
+    sk[0] = scales_of(w, a.ks);
+    sv[0] = scales_of(w, a.vs);
+  };
+
+  Where at;
+  if (k_begin < k_end) {
+    at = find(k_begin);
+    load_keys(at);
+    if constexpr (FMT == FMT_Q4) load_scales(at);
+    load_values(at);
+  }
   int lim[R];
   // queries, as operands
-  constexpr int QC = FMT == FMT_F32 ? D / 16 : D / 32;
   float4 qf[FMT == FMT_F32 ? R : 1][FMT == FMT_F32 ? QC : 1];
   Op<QP> qo[FMT == FMT_F32 ? 1 : R][FMT == FMT_F32 ? 1 : QC];
   uint4 qz[FMT == FMT_Q4 ? R : 1];
@@ -292,97 +401,6 @@ void k_attend(AttendArgs a) {
     }
   }
 
-  f32x4 o[UN][R];
-  float ref[R], l[R], corr[FMT == FMT_Q4 ? R : 1][NG];
-#pragma unroll
-  for (int cb = 0; cb < R; ++cb) {
-#pragma unroll
-    for (int i = 0; i < UN; ++i) o[i][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
-    ref[cb] = -INFINITY;
-    l[cb] = 0.f;
-    if constexpr (FMT == FMT_Q4)
-#pragma unroll
-      for (int f = 0; f < NG; ++f) corr[cb][f] = 0.f;
-  }
-  // of this wavefront's tile: {step, zero} of the keys as they are [64][NG], their steps [NG][64], the values' steps and
-  // zeros - 16 steps [NG][64] each (a read takes four keys of a group)
-  uint32_t* s_kz = (uint32_t*)sm + wv * (4 * 64 * NG);
-  float* s_ks = (float*)s_kz + 64 * NG;
-  float* s_vs = s_ks + 64 * NG;
-  float* s_vz = s_vs + 64 * NG;
-  uint32_t* s_rare = (uint32_t*)sm + wv * (TK / 4 * (ROWB / 64) * 64);     // a tile's values (float32 and bfloat16 pages)
-
-  // ---- tiles: where the 16-key blocks are (each lies in one page)
-  const int32_t* table = pg.table + s * pg.table_ss + h * pg.table_sh;
-  const int64_t tokb = pg.tok_s * ROWB;
-  const char* const kh = a.k + h * pg.head_s * ROWB;
-  const char* const vh = a.v + h * pg.head_s * ROWB;
-  struct Where { uint32_t row[NB]; int ok; };    // first rows, and a bit for each block that has a page
-  auto find = [&](int k0) {
-    Where w;
-    w.ok = 0;
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int t = k0 + 16 * b;
-      const int page = t < k_end ? uniform_load(table + (t >> pg.lg_ps)) : -1;
-      const bool ok = (uint32_t)page < (uint32_t)pg.n_pages;
-      w.row[b] = ok ? (uint32_t)page * (uint32_t)pg.page_s + (t & ((1 << pg.lg_ps) - 1)) * (uint32_t)pg.tok_s : 0u;
-      w.ok |= ok ? 1 << b : 0;
-    }
-    return w;
-  };
-  // lane offsets of a block: key n, part j of its row; value row 4 j + r, unit n
-  const uint32_t k_off = (uint32_t)(n * tokb) + j * (FMT == FMT_Q4 ? UN * 2 : 16);
-  const uint32_t v_off = (uint32_t)(4 * j * tokb) + n * (ROWB / 16);
-  constexpr int KW = FMT == FMT_Q4 ? UN / 2 : 4 * QC;       // words of a lane per block
-  uint32_t kr[NB][KW];
-  constexpr int VW = FMT == FMT_F32 ? UN : FMT == FMT_BF16 ? UN / 2 : 1;
-  uint32_t vw[NB * 4][VW];
-  uint32_t sk[NG], sv[NG];
-  auto load_keys = [&](const Where& w) {
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const char* p = kh + (uint64_t)w.row[b] * ROWB;
-      if constexpr (FMT == FMT_Q4) load_words<UN / 2>(p, k_off, kr[b]);
-      else
-#pragma unroll
-        for (int c = 0; c < QC; ++c) load_words<4>(p, k_off + c * 64, &kr[b][4 * c]);
-    }
-  };
-  auto load_values = [&](const Where& w) {
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const char* p = vh + ((uint64_t)w.row[b] * ROWB + r * tokb);
-        uint32_t (&x)[VW] = vw[b * 4 + r];
-        if constexpr (FMT == FMT_Q4 && UN == 4) {
-          x[0] = load_half(p, v_off);
-        } else {
-          load_words<VW < 4 ? VW : 4>(p, v_off, x);
-          if constexpr (VW == 8) load_words<4>(p, v_off + 16, &x[4]);
-        }
-      }
-  };
-  auto scales_of = [&](const Where& w, const uint32_t* from, uint32_t (&x)[NG]) {       // lane = key of the tile
-    uint32_t row0 = vector(w.row[0]);
-#pragma unroll
-    for (int b = 1; b < NB; ++b) row0 = j == b ? vector(w.row[b]) : row0;
-    const uint64_t row = (row0 + (uint64_t)(h * pg.head_s + n * pg.tok_s)) * NG;
-    if constexpr (NG == 4) *(uint4*)x = *(const uint4*)(from + row);
-    else *(uint2*)x = *(const uint2*)(from + row);
-  };
-  auto load_scales = [&](const Where& w) {
-    scales_of(w, a.ks, sk);
-    scales_of(w, a.vs, sv);
-  };
-
-  Where at = find(k_begin);
-  if (k_begin < k_end) {
-    load_keys(at);
-    if constexpr (FMT == FMT_Q4) load_scales(at);
-    load_values(at);
-  }
   uint32_t nib_mask = 0x00780078u, nib_base = 0x41804180u;
   if constexpr (FMT == FMT_Q4) asm("" : "+s"(nib_mask), "+v"(nib_base));      // (one of two constants may be scalar)
 
@@ -406,7 +424,7 @@ void k_attend(AttendArgs a) {
           const float y[4] = {qf[cb][c].x, qf[cb][c].y, qf[cb][c].z, qf[cb][c].w};
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            p[0][cb] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[0][4 * c + i]), y[i], p[0][cb], 0, 0, 0);
+            p[0][cb] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[c][i]), y[i], p[0][cb], 0, 0, 0);
         }
     } else if constexpr (FMT == FMT_BF16) {
 #pragma unroll
@@ -418,27 +436,30 @@ void k_attend(AttendArgs a) {
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int cb = 0; cb < R; ++cb) p[b][cb] = mfma(*(const uint4*)&kr[b][4 * c], qo[cb][c].p[0], p[b][cb]);
+          for (int cb = 0; cb < R; ++cb) p[b][cb] = mfma(__builtin_bit_cast(uint4, kr[b * KN + c]), qo[cb][c].p[0], p[b][cb]);
     } else {
       __builtin_amdgcn_wave_barrier();
-      if constexpr (NG == 4) *(uint4*)&s_kz[lane * NG] = *(const uint4*)sk;
-      else *(uint2*)&s_kz[lane * NG] = *(const uint2*)sk;
+      *(Words<NG>*)&s_kz[lane * NG] = sk[0];
 #pragma unroll
       for (int f = 0; f < NG; ++f) {
         if (masked) {
-          const float x = __uint_as_float(sv[f] << 16), y = __uint_as_float(sv[f] & 0xFFFF0000u);
+          const float x = __uint_as_float(sv[0][f] << 16), y = __uint_as_float(sv[0][f] & 0xFFFF0000u);
           if (!(x - x == 0.f && y - y == 0.f)) {
-            sv[f] = 0u;
+            sv[0][f] = 0u;
             odd_scales = true;
           }
         }
-        const float st = __uint_as_float(sv[f] << 16);
-        s_ks[f * 64 + lane] = __uint_as_float(sk[f] << 16);
+        const float st = __uint_as_float(sv[0][f] << 16);
+        s_ks[f * 64 + lane] = __uint_as_float(sk[0][f] << 16);
         s_vs[f * 64 + lane] = st;
-        s_vz[f * 64 + lane] = __builtin_fmaf(-16.f, st, __uint_as_float(sv[f] & 0xFFFF0000u));
+        s_vz[f * 64 + lane] = __builtin_fmaf(-16.f, st, __uint_as_float(sv[0][f] & 0xFFFF0000u));
       }
       odd_scales = __ballot(odd_scales);
       if (more) load_scales(next);
+      else {
+        forget(sk);
+        forget(sv);
+      }
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -482,10 +503,14 @@ void k_attend(AttendArgs a) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) p[b][cb][r] = __builtin_fmaf(st[f][r], t[f][r], p[b][cb][r]);
         }
-        __builtin_amdgcn_sched_barrier(0);        // (operands of one block at a time: registers)
+        // (one block at a time, finished here: else its sums are put off past the next loads, with all they are made of in registers)
+#pragma unroll
+        for (int cb = 0; cb < R; ++cb) asm volatile("" : "+v"(p[b][cb]));
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     if (more) load_keys(next);
+    else forget(kr);
 
     // ---- softmax: lane = row, key 16 b + 4 j + r in register r of block b
     if (masked) {
@@ -509,7 +534,7 @@ void k_attend(AttendArgs a) {
       far = far || top[cb] > ref[cb] + 8.f;
     }
     // the reference follows the largest logit when it is 2^8 behind: rarely
-    if (__ballot(far)) {
+    if (__builtin_expect(__ballot(far) != 0, 0)) {
 #pragma unroll
       for (int cb = 0; cb < R; ++cb) {
         const float m = fmaxf(ref[cb], top[cb]);
@@ -535,46 +560,74 @@ void k_attend(AttendArgs a) {
         }
     }
 
+    // Values that are not finite, in a tile where some rows do not see every key (0 times them would be NaN): each is added to
+    // the sums of the rows that see its key, with the sums in LDS (rare, so kept out of the registers); zeros then take their
+    // places in the products.
+    auto odd_values = [&]() {
+#pragma unroll
+      for (int cb = 0; cb < R; ++cb)
+#pragma unroll
+        for (int i = 0; i < UN; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s_rare[((cb * UN + i) * 4 + r) * 64 + lane] = o[i][cb][r];
+#pragma unroll 1
+      for (int kk = 0; kk < TK; ++kk) {
+        const int b = kk >> 4;
+        uint32_t row = at.row[0];
+        int have = there(0);
+#pragma unroll
+        for (int x = 1; x < NB; ++x)
+          if (b == x) { row = at.row[x]; have = there(x); }
+        if ((kk & 15) >= have) continue;
+        float w[R];
+#pragma unroll
+        for (int cb = 0; cb < R; ++cb) {
+          w[cb] = p[0][cb][0];
+#pragma unroll
+          for (int x = 1; x < NB * 4; ++x) w[cb] = x == b * 4 + (kk & 3) ? p[x >> 2][cb][x & 3] : w[cb];
+          w[cb] = __shfl(w[cb], n + 16 * (kk >> 2 & 3));      // the lane that holds the key's weight
+        }
+        const char* vp = vh + (uint64_t)row * ROWB + (kk & 15) * tokb;
+#pragma unroll 1
+        for (int i = 0; i < UN; ++i) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int ch = (4 * j + r) * UN + i;
+            const float v = FMT == FMT_F32 ? ((const float*)vp)[ch] : __uint_as_float((uint32_t)((const uint16_t*)vp)[ch] << 16);
+#pragma unroll
+            for (int cb = 0; cb < R; ++cb)
+              if (!(v - v == 0.f) && k0 + kk < lim[cb]) s_rare[((cb * UN + i) * 4 + r) * 64 + lane] += w[cb] * v;
+          }
+        }
+      }
+#pragma unroll
+      for (int cb = 0; cb < R; ++cb)
+#pragma unroll
+        for (int i = 0; i < UN; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[i][cb][r] = s_rare[((cb * UN + i) * 4 + r) * 64 + lane];
+    };
+
     // ---- O^T += V^T P^T
     if constexpr (FMT == FMT_F32) {
-      auto val = [&](int r, int i) { return __uint_as_float(vw[r][i]); };
-      if (masked) {
-        keep_here(vw);
+      auto val = [&](int r, int i) { return __uint_as_float(vr[r * VN + i / 4][i & 3]); };
+      if (__builtin_expect(masked, 0)) {
+        keep_here(vr);
         bool bad = false;
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
           for (int i = 0; i < UN; ++i) {
-            if (4 * j + r >= there(0)) vw[r][i] = 0u;
+            if (4 * j + r >= there(0)) vr[r * VN + i / 4][i & 3] = 0u;
             bad = bad || !(val(r, i) - val(r, i) == 0.f);
           }
-        if (__ballot(bad)) {
-          // values that are not finite, in a tile where some rows do not see every key (0 times them would be NaN): they come
-          // first and key by key, from LDS, a row that does not see the key keeps its sums, and zeros take their places below
+        if (__builtin_expect(__ballot(bad) != 0, 0)) {
+          odd_values();
 #pragma unroll
           for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int i = 0; i < UN; ++i) {
-              s_rare[(r * UN + i) * 64 + lane] = val(r, i) - val(r, i) == 0.f ? 0u : vw[r][i];
-              if (!(val(r, i) - val(r, i) == 0.f)) vw[r][i] = 0u;
-            }
-#pragma unroll 1
-          for (int kk = 0; kk < 16; ++kk) {
-            const int r = kk & 3;
-            const bool see = kk < there(0);
-            float w[R];
-#pragma unroll
-            for (int cb = 0; cb < R; ++cb) w[cb] = r == 0 ? p[0][cb][0] : r == 1 ? p[0][cb][1] : r == 2 ? p[0][cb][2] : p[0][cb][3];
-#pragma unroll
-            for (int i = 0; i < UN; ++i) {
-              const float x = j == kk >> 2 ? __uint_as_float(s_rare[(r * UN + i) * 64 + lane]) : 0.f;
-#pragma unroll
-              for (int cb = 0; cb < R; ++cb) {
-                const f32x4 t = __builtin_amdgcn_mfma_f32_16x16x4f32(x, w[cb], o[i][cb], 0, 0, 0);
-                o[i][cb] = see && k0 + kk < lim[cb] ? t : o[i][cb];
-              }
-            }
-          }
+            for (int i = 0; i < UN; ++i)
+              if (!(val(r, i) - val(r, i) == 0.f)) vr[r * VN + i / 4][i & 3] = 0u;
         }
       }
 #pragma unroll
@@ -591,64 +644,45 @@ void k_attend(AttendArgs a) {
         const float x[8] = {p[0][cb][0], p[0][cb][1], p[0][cb][2], p[0][cb][3], p[1][cb][0], p[1][cb][1], p[1][cb][2], p[1][cb][3]};
         po[cb] = split8<NP>(x);
       }
-      auto operand = [](const uint32_t (&w)[8][UN / 2], int i) {      // place i of every unit, keys 0 .. 7
+      auto operand = [&](int i) {      // place i of every unit, keys 0 .. 7
         const uint32_t sel = i & 1 ? 0x07060302u : 0x05040100u;
-        return make_uint4(__builtin_amdgcn_perm(w[1][i / 2], w[0][i / 2], sel), __builtin_amdgcn_perm(w[3][i / 2], w[2][i / 2], sel),
-                          __builtin_amdgcn_perm(w[5][i / 2], w[4][i / 2], sel), __builtin_amdgcn_perm(w[7][i / 2], w[6][i / 2], sel));
+        return make_uint4(__builtin_amdgcn_perm(vr[1][i / 2], vr[0][i / 2], sel), __builtin_amdgcn_perm(vr[3][i / 2], vr[2][i / 2], sel),
+                          __builtin_amdgcn_perm(vr[5][i / 2], vr[4][i / 2], sel), __builtin_amdgcn_perm(vr[7][i / 2], vr[6][i / 2], sel));
       };
-      if (masked) {
-        keep_here(vw);
+      if (__builtin_expect(masked, 0)) {
+        keep_here(vr);
         bool bad = false;
 #pragma unroll
         for (int x = 0; x < 8; ++x)
 #pragma unroll
           for (int i = 0; i < UN / 2; ++i) {
-            if (4 * j + (x & 3) >= there(x >> 2)) vw[x][i] = 0u;
-            bad = bad || (vw[x][i] & 0x7F80u) == 0x7F80u || (vw[x][i] & 0x7F800000u) == 0x7F800000u;
+            if (4 * j + (x & 3) >= there(x >> 2)) vr[x][i] = 0u;
+            bad = bad || (vr[x][i] & 0x7F80u) == 0x7F80u || (vr[x][i] & 0x7F800000u) == 0x7F800000u;
           }
-        if (__ballot(bad)) {       // as above
+        if (__builtin_expect(__ballot(bad) != 0, 0)) {
+          odd_values();
 #pragma unroll
           for (int x = 0; x < 8; ++x)
 #pragma unroll
             for (int i = 0; i < UN / 2; ++i) {
-              const uint32_t w = vw[x][i];      // the halves that are not finite
-              const uint32_t odd = ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
-              s_rare[(x * (UN / 2) + i) * 64 + lane] = w & odd;
-              vw[x][i] = w & ~odd;
+              const uint32_t w = vr[x][i];
+              vr[x][i] = w & ~(((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u));
             }
-#pragma unroll 1
-          for (int kk = 0; kk < 32; ++kk) {
-            const int x = kk >> 4 << 2 | (kk & 3);
-            const bool see = (kk & 15) < (kk >> 4 ? there(1) : there(0));
-#pragma unroll
-            for (int i = 0; i < UN; ++i) {
-              uint32_t w = j == (kk >> 2 & 3) ? s_rare[(x * (UN / 2) + i / 2) * 64 + lane] : 0u;
-              w = (i & 1 ? w >> 16 : w & 0xFFFFu) << (16 * (x & 1));
-              const uint4 one = make_uint4(x >> 1 == 0 ? w : 0u, x >> 1 == 1 ? w : 0u, x >> 1 == 2 ? w : 0u, x >> 1 == 3 ? w : 0u);
-#pragma unroll
-              for (int cb = 0; cb < R; ++cb) {
-                // (the first part of a weight alone: parts of unlike sign would make a NaN of an infinity)
-                const f32x4 t = mfma(one, po[cb].p[0], o[i][cb]);
-                o[i][cb] = see && k0 + kk < lim[cb] ? t : o[i][cb];
-              }
-            }
-          }
         }
       }
 #pragma unroll
       for (int i = 0; i < UN; ++i) {
-        const uint4 x = operand(vw, i);
+        const uint4 x = operand(i);
 #pragma unroll
         for (int cb = 0; cb < R; ++cb)
 #pragma unroll
           for (int pl = NP - 1; pl >= 0; --pl) o[i][cb] = mfma(x, po[cb].p[pl], o[i][cb]);
       }
     } else {
-      if (masked && odd_scales) {
+      if (__builtin_expect(masked && odd_scales, 0)) {
         // steps or zeros that are not finite, in a tile where some rows do not see every key (0 times them would be NaN): zeros
         // stand in their places, and here the rows that see the key get what it adds to their groups
-        uint32_t raw[NG];
-        scales_of(at, a.vs, raw);
+        const Words<NG> raw = scales_of(at, a.vs);
 #pragma unroll 1
         for (int kk = 0; kk < 64; ++kk) {
           const int b = kk >> 4, r = kk & 3;
@@ -674,8 +708,8 @@ void k_attend(AttendArgs a) {
         uint32_t pr[4][UN / 4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          pr[i][0] = __builtin_amdgcn_perm(vw[8 * hf + 2 * i + 1][0], vw[8 * hf + 2 * i][0], 0x05040100u);
-          if constexpr (UN == 8) pr[i][1] = __builtin_amdgcn_perm(vw[8 * hf + 2 * i + 1][0], vw[8 * hf + 2 * i][0], 0x07060302u);
+          pr[i][0] = __builtin_amdgcn_perm(vr[8 * hf + 2 * i + 1], vr[8 * hf + 2 * i], 0x05040100u);
+          if constexpr (UN == 8) pr[i][1] = __builtin_amdgcn_perm(vr[8 * hf + 2 * i + 1], vr[8 * hf + 2 * i], 0x07060302u);
         }
 #pragma unroll
         for (int f = 0; f < NG; ++f) {
@@ -706,11 +740,14 @@ void k_attend(AttendArgs a) {
 #pragma unroll
               for (int pl = NP - 1; pl >= 0; --pl) o[i][cb] = mfma(x, po[cb].p[pl], o[i][cb]);
           }
+#pragma unroll
+          for (int cb = 0; cb < R; ++cb) asm volatile("" : "+v"(o[2 * f][cb]), "+v"(o[2 * f + 1][cb]), "+v"(corr[cb][f]));      // (as above)
           __builtin_amdgcn_sched_barrier(0);
         }
       }
     }
     if (more) load_values(next);
+    else forget(vr);
     at = next;
   }
 
