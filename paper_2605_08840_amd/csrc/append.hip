@@ -59,113 +59,213 @@ __device__ __forceinline__ void store_unit(T* p, const float (&x)[UN]) {
   }
 }
 
-// Rotation of the unit at channel c0: each product and each sum rounded to 32 bits (no contraction), so that the codes of
-// a 4-bit cache follow from the definition bit by bit.
-template <typename T, int UN, bool VEC>
-__device__ __forceinline__ void rotate_unit(const Pages& pg, const T* row, int c0, const float* cos, const float* sin, int pos,
-                                            float (&x)[UN]) {
-#pragma clang fp contract(off)
-  if (c0 >= pg.rot) return;
+__device__ __forceinline__ float other_half(float x) {       // the value eight lanes on, of sixteen
+  return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0x128, 0xF, 0xF, true));
+}
+
+// Angles of the unit at channel c0: UN cosines and sines (UN / 2 where neighbours turn together).
+template <int UN>
+struct Turn { float c[UN], s[UN]; };
+template <int UN>
+__device__ __forceinline__ Turn<UN> angles(const Pages& pg, int c0, const float* cos, const float* sin, int pos) {
+  Turn<UN> t;
   const int half = pg.rot >> 1;
   if (pg.rot_pairs) {
     const int64_t at = (int64_t)pos * half + c0 / 2;
 #pragma unroll
+    for (int i = 0; i < UN / 2; ++i) { t.c[i] = cos[at + i]; t.s[i] = sin[at + i]; }
+  } else {
+    const int64_t at = (int64_t)pos * half + (c0 >= half ? c0 - half : c0);
+#pragma unroll
+    for (int i = 0; i < UN; ++i) { t.c[i] = cos[at + i]; t.s[i] = sin[at + i]; }
+  }
+  return t;
+}
+
+// Rotation of the unit at channel c0: each product and each sum rounded to 32 bits (no contraction), so that the codes of
+// a 4-bit cache follow from the definition bit by bit.  other: the channels it turns with (where not its own).
+template <int UN>
+__device__ __forceinline__ void rotate_unit(const Pages& pg, int c0, const Turn<UN>& t, const float (&other)[UN], float (&x)[UN]) {
+#pragma clang fp contract(off)
+  if (pg.rot_pairs) {
+#pragma unroll
     for (int i = 0; i < UN / 2; ++i) {
-      const float c = cos[at + i], s = sin[at + i], a = x[2 * i], b = x[2 * i + 1];
-      x[2 * i] = a * c - b * s;
-      x[2 * i + 1] = b * c + a * s;
+      const float a = x[2 * i], b = x[2 * i + 1];
+      x[2 * i] = a * t.c[i] - b * t.s[i];
+      x[2 * i + 1] = b * t.c[i] + a * t.s[i];
     }
   } else {
-    const bool second = c0 >= half;
-    const int f0 = second ? c0 - half : c0;
-    float other[UN];
-    load_unit<T, UN, VEC>(row + (second ? f0 : c0 + half), other);
-    const float* cp = cos + (int64_t)pos * half + f0;
-    const float* sp = sin + (int64_t)pos * half + f0;
+    const bool second = c0 >= pg.rot >> 1;
 #pragma unroll
     for (int i = 0; i < UN; ++i) {
-      const float p = x[i] * cp[i], r = other[i] * sp[i];
-      x[i] = second ? p + r : p - r;
+      const float p = x[i] * t.c[i], r = other[i] * t.s[i];
+      x[i] = p + (second ? r : -r);
     }
   }
 }
 
-// One wavefront per four rows of a token (rows: KV heads' keys, their values, query heads), sixteen lanes a row, a lane the
-// d/16 channels of a unit: accesses run along rows, and a group's extremes are a reduction over sixteen lanes.
-template <typename T, int D, bool Q4, bool VEC>
+// Codes of the unit, a group's extremes over the sixteen lanes of the row, and the row's {step, zero} of every group.
+// Lane u works out the scale of group u mod NG for all.
+template <int UN>
+__device__ __forceinline__ uint32_t unit_codes(const float (&x)[UN], int u, uint32_t (&scale)[UN / 2]) {
+#pragma clang fp contract(off)
+  constexpr int NG = UN / 2;
+  float low = 0.f, high = 0.f;
+  bool nan = false;
+#pragma unroll
+  for (int f = 0; f < NG; ++f) {
+    const float a = x[2 * f], b = x[2 * f + 1];
+    const float lo = row16_min(fminf(a, b)), hi = row16_max(fmaxf(a, b));
+    nan = nan || !(a == a && b == b);
+    if (f == (u & (NG - 1))) { low = lo; high = hi; }
+  }
+  bool fine = true;                  // (infinities are seen by the extremes)
+  if (__ballot(nan)) {
+#pragma unroll
+    for (int f = 0; f < NG; ++f) {
+      const float off = row16_max(x[2 * f] == x[2 * f] && x[2 * f + 1] == x[2 * f + 1] ? 0.f : 1.f);
+      if (f == (u & (NG - 1))) fine = off == 0.f;
+    }
+  }
+  float step, zero, inverse;
+  group_scale(low, high, fine, step, zero, inverse);
+  const uint32_t packed = __float_as_uint(step) >> 16 | (__float_as_uint(zero) & 0xFFFF0000u);
+  auto codes = [&](auto rare) {
+    uint32_t code = 0u;
+#pragma unroll
+    for (int f = NG - 1; f >= 0; --f) {
+      // lane f of every NG: quad_perm
+      auto of = [&](uint32_t v) -> uint32_t {
+        if constexpr (NG == 4) return f == 0 ? __builtin_amdgcn_mov_dpp(v, 0x00, 0xF, 0xF, true) : f == 1 ? __builtin_amdgcn_mov_dpp(v, 0x55, 0xF, 0xF, true)
+                                    : f == 2 ? __builtin_amdgcn_mov_dpp(v, 0xAA, 0xF, 0xF, true) : __builtin_amdgcn_mov_dpp(v, 0xFF, 0xF, 0xF, true);
+        else return f == 0 ? __builtin_amdgcn_mov_dpp(v, 0xA0, 0xF, 0xF, true) : __builtin_amdgcn_mov_dpp(v, 0xF5, 0xF, 0xF, true);
+      };
+      scale[f] = of(packed);
+      const float z = __uint_as_float(scale[f] & 0xFFFF0000u), inv = __uint_as_float(of(__float_as_uint(inverse)));
+#pragma unroll
+      for (int i = 1; i >= 0; --i) {
+        // 0 <= (x - zero) / step <= 15 (1 + 2^-21), since zero and step are rounded outwards: adding 2^23 rounds it to the
+        // nearest whole number, even at a tie, which then is in the low bits
+        float t = (x[2 * f + i] - z) * inv;
+        if (rare && !(z == z)) t = 0.f;
+        code = (code << 4) + __float_as_uint(t + 8388608.f);
+      }
+    }
+    return code - 0xFB000000u;       // 0x4B000000 (1 + 16 + 256 + ...), mod 2^32
+  };
+  return __ballot(!(zero == zero)) ? codes(std::true_type{}) : codes(std::false_type{});      // (groups without a scale)
+}
+
+// A wavefront takes U times four rows of a token (rows: KV heads' keys, their values, query heads), sixteen lanes a row, a lane
+// the d/16 channels of a unit: accesses run along rows, and a group's extremes are a reduction over sixteen lanes.  U = 4 has
+// four rows a lane in flight and reads the angles once for them; few tokens take U = 1, for more wavefronts.
+template <typename T, int D, bool Q4, bool VEC, int U>
 __global__ __launch_bounds__(256) void k_append(Pages pg, const T* k, const T* v, char* k_pages, char* v_pages,
                                                 uint32_t* k_scale, uint32_t* v_scale, const int32_t* __restrict__ positions,
                                                 const float* __restrict__ cos, const float* __restrict__ sin, const T* q, T* q_out,
-                                                int chunks, int n_rows) {
+                                                int parts, int n_rows) {
   constexpr int UN = D / 16, NG = D / 32;
   const int lane = threadIdx.x & 63;
   const int64_t w = wide_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int t = (int)(w / chunks), r = (int)(w % chunks) * 4 + (lane >> 4);
-  if (w >= (int64_t)pg.n_tokens * chunks) return;
+  if (w >= (int64_t)pg.n_tokens * parts) return;
+  const int t = (int)(w / parts), part = (int)(w % parts);
   // the sequence of token t: the last one that starts at or before it
-  int s;
+  int s = 0;
+  NewRows nr = {0, pg.max_new};
   if (pg.new_start) {
-    int lo = 0;
-    for (int base = 0; base < pg.n_seqs; base += 64) {
+    for (int base = 0; base < pg.n_seqs && pg.n_seqs > 1; base += 64) {
       const int e = base + lane;
       const unsigned long long before = __ballot(e < pg.n_seqs && pg.new_start[e] <= t);
-      if (before) lo = base + 63 - __builtin_clzll(before);
+      if (before) s = base + 63 - __builtin_clzll(before);
       if (before != ~0ull) break;
     }
-    s = lo;
+    const int a = min(max(uniform_load(pg.new_start + s), 0), pg.n_tokens);
+    const int b = min(max(uniform_load(pg.new_start + s + 1), a), pg.n_tokens);
+    nr = {a, min(b - a, pg.max_new)};
   } else {
     s = t / pg.max_new;
+    nr.first = s * pg.max_new;
   }
   if (s >= pg.n_seqs) return;
-  const NewRows nr = new_rows(pg, s);
   const int i = t - nr.first;
-  if (i < 0 || i >= nr.n || r >= n_rows) return;
-  const bool is_q = r >= 2 * pg.Hkv, is_v = !is_q && r >= pg.Hkv;
-  const int h = is_q ? r - 2 * pg.Hkv : is_v ? r - pg.Hkv : r;
+  if (i < 0 || i >= nr.n) return;
   const int u = lane & 15, c0 = u * UN;
-  const T* row = is_q ? q + t * pg.q_st + h * pg.q_sh : (is_v ? v : k) + t * pg.kv_st + h * pg.kv_sh;
-  float x[UN];
-  load_unit<T, UN, VEC>(row + c0, x);
-  const int at = told_len(pg, s, is_q ? 0 : h) - nr.n + i;
-  if (pg.rot) {
-    const int pos = positions ? positions[t] : at;
-    if (pos < 0 || pos >= pg.n_pos) return;        // (all rows of the token alike)
-    if (!is_v) rotate_unit<T, UN, VEC>(pg, row, c0, cos, sin, pos, x);
-  }
-  if (is_q) {
-    store_unit<T, UN, VEC>(q_out + t * pg.q_st + h * pg.q_sh + c0, x);
-    return;
-  }
-  if (at < 0 || at >= pg.max_len) return;
-  const int page = page_of(pg, s, h, at);
-  if (page < 0) return;
-  const int64_t slot = row_of(pg, page, h, at);
-  char* dst = is_v ? v_pages : k_pages;
-  if constexpr (!Q4) {
-    store_unit<T, UN, true>((T*)dst + slot * D + c0, x);
-  } else {
-    uint32_t code = 0u, scale[NG];
+  const bool turns = c0 < pg.rot;
+  const int32_t* lens = pg.lens + s * pg.lens_ss;
+  const int32_t* table = pg.table + s * pg.table_ss;
+  // all that is read, asked for before any of it is used: rows (the last one again behind the last), angles, and where the
+  // rows go
+  int r[U];
+  float x[U][UN], other[U][UN];
+  // (what does not turn with its own neighbour has its partner eight lanes on if the whole row turns, else in memory)
+  const bool far = pg.rot && !pg.rot_pairs && pg.rot != D;
 #pragma unroll
-    for (int f = 0; f < NG; ++f) {
-#pragma clang fp contract(off)
-      const float a = x[2 * f], b = x[2 * f + 1];
-      // (a NaN or an infinity leaves a difference that is not zero)
-      const float off = row16_max(a - a == 0.f && b - b == 0.f ? 0.f : 1.f);
-      float step, zero, inverse;
-      group_scale(row16_min(fminf(a, b)), row16_max(fmaxf(a, b)), off == 0.f, step, zero, inverse);
-      const float ca = __builtin_rintf((a - zero) * inverse), cb = __builtin_rintf((b - zero) * inverse);
-      const uint32_t ia = step > 0.f ? (uint32_t)fminf(fmaxf(ca, 0.f), 15.f) : 0u;
-      const uint32_t ib = step > 0.f ? (uint32_t)fminf(fmaxf(cb, 0.f), 15.f) : 0u;
-      code |= (ia | ib << 4) << (8 * f);
-      scale[f] = __float_as_uint(step) >> 16 | (__float_as_uint(zero) & 0xFFFF0000u);
+  for (int c = 0; c < U; ++c) {
+    r[c] = (part * U + c) * 4 + (lane >> 4);
+    const int rc = min(r[c], n_rows - 1);
+    const T* row = rc >= 2 * pg.Hkv ? q + t * pg.q_st + (rc - 2 * pg.Hkv) * pg.q_sh
+                                    : (rc >= pg.Hkv ? v - pg.Hkv * pg.kv_sh : k) + t * pg.kv_st + rc * pg.kv_sh;
+    load_unit<T, UN, VEC>(row + c0, x[c]);
+    if (far && turns) load_unit<T, UN, VEC>(row + (c0 >= pg.rot >> 1 ? c0 - (pg.rot >> 1) : c0 + (pg.rot >> 1)), other[c]);
+  }
+  Turn<UN> turn;
+  if (pg.rot) {
+    const int pos = positions ? uniform_load(positions + t) : max(uniform_load(lens), 0) - nr.n + i;
+    if (pos < 0 || pos >= pg.n_pos) return;        // (the whole token)
+    if (turns) turn = angles<UN>(pg, c0, cos, sin, pos);
+  }
+  int64_t slot[U];                                 // -1: nowhere
+  if (!pg.lens_sh && !pg.table_sh) {
+    const int at = max(uniform_load(lens), 0) - nr.n + i;
+    const bool in = at >= 0 && at < pg.max_len;
+    const int page = in ? uniform_load(table + (at >> pg.lg_ps)) : -1;
+#pragma unroll
+    for (int c = 0; c < U; ++c) {
+      const int h = r[c] >= pg.Hkv ? r[c] - pg.Hkv : r[c];
+      slot[c] = page >= 0 && page < pg.n_pages ? row_of(pg, page, h, at) : -1;
     }
-    uint32_t* sc = (is_v ? v_scale : k_scale) + slot * NG;
-    if constexpr (UN == 8) {
-      *(uint32_t*)(dst + slot * (D / 2) + u * 4) = code;
-      if (u == 0) *(uint4*)sc = make_uint4(scale[0], scale[1], scale[2], scale[3]);
+  } else {
+    int at[U];
+#pragma unroll
+    for (int c = 0; c < U; ++c) {
+      const int h = min(r[c] >= pg.Hkv ? r[c] - pg.Hkv : r[c], pg.Hkv - 1);
+      at[c] = max(lens[h * pg.lens_sh], 0) - nr.n + i;
+    }
+#pragma unroll
+    for (int c = 0; c < U; ++c) {
+      const int h = min(r[c] >= pg.Hkv ? r[c] - pg.Hkv : r[c], pg.Hkv - 1);
+      const int page = at[c] >= 0 && at[c] < pg.max_len ? page_of(pg, s, h, at[c]) : -1;
+      slot[c] = page >= 0 ? row_of(pg, page, h, at[c]) : -1;
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < U; ++c) {
+    const bool is_q = r[c] >= 2 * pg.Hkv, is_v = !is_q && r[c] >= pg.Hkv;
+    if (pg.rot && !is_v) {
+      if (!far && !pg.rot_pairs)
+#pragma unroll
+        for (int m = 0; m < UN; ++m) other[c][m] = other_half(x[c][m]);
+      if (turns) rotate_unit<UN>(pg, c0, turn, other[c], x[c]);
+    }
+    if (is_q) {
+      if (r[c] < n_rows) store_unit<T, UN, VEC>(q_out + t * pg.q_st + (r[c] - 2 * pg.Hkv) * pg.q_sh + c0, x[c]);
+      continue;
+    }
+    if (slot[c] < 0) continue;
+    char* dst = is_v ? v_pages : k_pages;
+    if constexpr (!Q4) {
+      store_unit<T, UN, true>((T*)dst + slot[c] * D + c0, x[c]);
     } else {
-      *(uint16_t*)(dst + slot * (D / 2) + u * 2) = (uint16_t)code;
-      if (u == 0) *(uint2*)sc = make_uint2(scale[0], scale[1]);
+      uint32_t scale[NG];
+      const uint32_t code = unit_codes<UN>(x[c], u, scale);
+      uint32_t* sc = (is_v ? v_scale : k_scale) + slot[c] * NG;
+      if constexpr (UN == 8) {
+        *(uint32_t*)(dst + slot[c] * (D / 2) + u * 4) = code;
+        if (u == 0) *(uint4*)sc = make_uint4(scale[0], scale[1], scale[2], scale[3]);
+      } else {
+        *(uint16_t*)(dst + slot[c] * (D / 2) + u * 2) = (uint16_t)code;
+        if (u == 0) *(uint2*)sc = make_uint2(scale[0], scale[1]);
+      }
     }
   }
 }
@@ -174,16 +274,19 @@ template <typename T, int D, bool Q4>
 int run_append(const Pages& pg, const void* k, const void* v, void* k_pages, void* v_pages, void* k_scale, void* v_scale,
                const int32_t* positions, const float* cos, const float* sin, const void* q, void* q_out, hipStream_t st) {
   const int n_rows = 2 * pg.Hkv + (q ? pg.Hq : 0), chunks = (n_rows + 3) / 4;
-  const int64_t blocks = ((int64_t)pg.n_tokens * chunks + 3) / 4;
   const int unit = D / 16 * (int)sizeof(T), mask = (unit < 16 ? unit : 16) - 1, el = (mask + 1) / (int)sizeof(T) - 1;
   const bool vec = !(((uintptr_t)k | (uintptr_t)v | (uintptr_t)q | (uintptr_t)q_out) & mask) &&
                    !((pg.kv_st | pg.kv_sh | (q ? pg.q_st | pg.q_sh : 0)) & el);
-  auto go = [&](auto kern) {
-    hipLaunchKernelGGL(kern, wide_grid(blocks), dim3(256), 0, st, pg, (const T*)k, (const T*)v, (char*)k_pages, (char*)v_pages,
-                       (uint32_t*)k_scale, (uint32_t*)v_scale, positions, cos, sin, (const T*)q, (T*)q_out, chunks, n_rows);
+  // four groups of rows a wavefront where that still leaves every SIMD eight wavefronts
+  const bool few = (int64_t)pg.n_tokens * ((chunks + 3) / 4) < (int64_t)n_cu() * 32;
+  auto go = [&](auto kern, int U) {
+    const int parts = (chunks + U - 1) / U;
+    hipLaunchKernelGGL(kern, wide_grid(((int64_t)pg.n_tokens * parts + 3) / 4), dim3(256), 0, st, pg, (const T*)k, (const T*)v, (char*)k_pages,
+                       (char*)v_pages, (uint32_t*)k_scale, (uint32_t*)v_scale, positions, cos, sin, (const T*)q, (T*)q_out, parts, n_rows);
   };
-  if (vec) go(k_append<T, D, Q4, true>);
-  else go(k_append<T, D, Q4, false>);
+  if (!vec) go(k_append<T, D, Q4, false, 1>, 1);
+  else if (few) go(k_append<T, D, Q4, true, 1>, 1);
+  else go(k_append<T, D, Q4, true, 4>, 4);
   return hip_status();
 }
 

@@ -168,11 +168,6 @@ __device__ __forceinline__ void store_out(const AttendArgs& a, int64_t t, int64_
 
 enum { FMT_F32, FMT_BF16, FMT_Q4 };
 
-// Wave-uniform reads of what the kernel does not write, through the scalar cache.
-__device__ __forceinline__ int uniform_load(const int32_t* p) {
-  return *(const __attribute__((address_space(4))) int32_t*)(uintptr_t)p;
-}
-
 // N words at a uniform address (held in scalar registers, so that the load adds the lane's 32-bit offset by itself).
 template <int N> struct WordsOf { typedef uint32_t type __attribute__((ext_vector_type(N))); };
 template <> struct WordsOf<1> { typedef uint32_t type; };

@@ -5,62 +5,77 @@ namespace restkv {
 
 namespace {
 
-// Sixteen lanes a row, a lane the d/16 channels of a unit; sixteen rows of a head, of keys or of values, a workgroup.
-template <typename T, int D, bool Q4>
+// Sixteen lanes a row, a lane the d/16 channels of a unit; a workgroup 16 U rows of a head, of keys or of values, a lane with U
+// of them in flight.
+template <typename T, int D, bool Q4, int U>
 __global__ __launch_bounds__(256) void k_fetch(Pages pg, const char* k_pages, const char* v_pages, const uint32_t* k_scale,
                                                const uint32_t* v_scale, const int32_t* __restrict__ idx, int first, int n_rows,
                                                T* k_out, T* v_out) {
   constexpr int UN = D / 16, NG = D / 32;
+  constexpr int B = Q4 ? UN / 2 : UN * (int)sizeof(T);            // bytes of a unit in its page: 2, 4, 8, 16 or 32
+  constexpr int N = B < 4 ? 1 : B / 4;
   const int u = threadIdx.x & 15;
   const int64_t b = wide_block();
-  const int blocks = (n_rows + 15) / 16;
+  const int blocks = (n_rows + 16 * U - 1) / (16 * U);
   const bool is_v = b & 1;
   const int64_t e = (b >> 1) / blocks;
-  const int j = (int)((b >> 1) % blocks) * 16 + (threadIdx.x >> 4);
-  if (e >= (int64_t)pg.n_seqs * pg.Hkv || j >= n_rows) return;
-  const int s = (int)(e / pg.Hkv), h = (int)(e % pg.Hkv);
-  const int64_t o = e * n_rows + j;
-  const int t = idx ? idx[o] : first + j;
-  int page = -1;
-  if (t >= 0 && t < cache_len(pg, s, h)) page = page_of(pg, s, h, t);
-  const int64_t slot = page >= 0 ? row_of(pg, page, h, t) : 0;
+  const int j0 = (int)((b >> 1) % blocks) * (16 * U) + (threadIdx.x >> 4);
+  if (e >= (int64_t)pg.n_seqs * pg.Hkv) return;
+  const int s = (int)(e / pg.Hkv), h = (int)(e % pg.Hkv), len = cache_len(pg, s, h);
   const char* src = is_v ? v_pages : k_pages;
-  T* dst = (is_v ? v_out : k_out) + o * D + u * UN;
-  if constexpr (!Q4) {
-    constexpr int B = UN * sizeof(T);            // bytes of a unit: 8, 16 or 32
-    const char* p = src + slot * (D * (int64_t)sizeof(T)) + u * B;
-    if constexpr (B == 8) {
-      *(uint2*)dst = page >= 0 ? *(const uint2*)p : make_uint2(0, 0);
-    } else {
+  const uint32_t* scales = is_v ? v_scale : k_scale;
+  T* dst = (is_v ? v_out : k_out) + e * n_rows * D + u * UN;
+  int64_t slot[U];
 #pragma unroll
-      for (int i = 0; i < B / 16; ++i) ((uint4*)dst)[i] = page >= 0 ? ((const uint4*)p)[i] : make_uint4(0, 0, 0, 0);
+  for (int c = 0; c < U; ++c) {
+    const int j = min(j0 + 16 * c, n_rows - 1), t = idx ? idx[e * n_rows + j] : first + j;
+    int page = -1;
+    if (t >= 0 && t < len) page = page_of(pg, s, h, t);
+    slot[c] = page >= 0 ? row_of(pg, page, h, t) : -1;
+  }
+  uint32_t w[U][N], sc[U][Q4 ? NG : 1];
+#pragma unroll
+  for (int c = 0; c < U; ++c) {
+    const char* p = src + max(slot[c], (int64_t)0) * (B * 16) + u * B;
+    if constexpr (B == 2) w[c][0] = *(const uint16_t*)p;
+    else if constexpr (B == 4) w[c][0] = *(const uint32_t*)p;
+    else if constexpr (B == 8) *(uint2*)w[c] = *(const uint2*)p;
+    else
+#pragma unroll
+      for (int i = 0; i < N; i += 4) *(uint4*)&w[c][i] = *(const uint4*)(p + 4 * i);
+    if constexpr (Q4) {
+      const uint32_t* q = scales + max(slot[c], (int64_t)0) * NG;
+      if constexpr (NG == 4) *(uint4*)sc[c] = *(const uint4*)q;
+      else *(uint2*)sc[c] = *(const uint2*)q;
     }
-  } else {
-    float x[UN];
-    if (page >= 0) {
-      const uint32_t* sc = (is_v ? v_scale : k_scale) + slot * NG;
-      const uint32_t code = UN == 8 ? *(const uint32_t*)(src + slot * (D / 2) + u * 4)
-                                    : *(const uint16_t*)(src + slot * (D / 2) + u * 2);
+  }
 #pragma unroll
-      for (int i = 0; i < UN; ++i) {
-        const uint32_t w = sc[i / 2];
-        x[i] = __uint_as_float(w & 0xFFFF0000u) + __uint_as_float(w << 16) * (float)(code >> (4 * i) & 15u);
+  for (int c = 0; c < U; ++c) {
+    const int j = j0 + 16 * c;
+    if (j >= n_rows) break;
+    constexpr int M = UN * (int)sizeof(T) / 4;
+    uint32_t y[M];
+    if constexpr (Q4) {
+      float x[UN];
+#pragma unroll
+      for (int i = 0; i < UN; ++i)
+        x[i] = __uint_as_float(sc[c][i / 2] & 0xFFFF0000u) + __uint_as_float(sc[c][i / 2] << 16) * (float)(w[c][0] >> (4 * i) & 15u);
+#pragma unroll
+      for (int i = 0; i < M; ++i) {
+        if constexpr (sizeof(T) == 4) y[i] = __float_as_uint(x[i]);
+        else y[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x[2 * i], x[2 * i + 1]}, bf16x2));
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < UN; ++i) x[i] = 0.f;
+      for (int i = 0; i < M; ++i) y[i] = w[c][i];
     }
-    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-      for (int i = 0; i < UN; i += 4) *(float4*)((float*)dst + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
-    } else {
-      uint32_t w[UN / 2];
+    for (int i = 0; i < M; ++i) y[i] = slot[c] < 0 ? 0u : y[i];
+    T* o = dst + (int64_t)j * D;
+    if constexpr (M == 2) *(uint2*)o = *(const uint2*)y;
+    else
 #pragma unroll
-      for (int i = 0; i < UN / 2; ++i)
-        w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x[2 * i], x[2 * i + 1]}, bf16x2));
-      if constexpr (UN == 8) *(uint4*)dst = make_uint4(w[0], w[1], w[2], w[3]);
-      else *(uint2*)dst = make_uint2(w[0], w[1]);
-    }
+      for (int i = 0; i < M; i += 4) *(uint4*)((uint32_t*)o + i) = *(const uint4*)&y[i];
   }
 }
 
@@ -68,8 +83,9 @@ __global__ __launch_bounds__(256) void k_fetch(Pages pg, const char* k_pages, co
 
 int launch_fetch(const Pages& pg, const void* k_pages, const void* v_pages, const void* k_scale, const void* v_scale,
                  const int32_t* idx, int first, int n_rows, void* k_out, void* v_out, hipStream_t st) {
+  constexpr int U = 4;
   auto go = [&](auto kern, auto* out) {
-    hipLaunchKernelGGL(kern, wide_grid((int64_t)((n_rows + 15) / 16) * pg.n_seqs * pg.Hkv * 2), dim3(256), 0, st, pg, (const char*)k_pages,
+    hipLaunchKernelGGL(kern, wide_grid((int64_t)((n_rows + 16 * U - 1) / (16 * U)) * pg.n_seqs * pg.Hkv * 2), dim3(256), 0, st, pg, (const char*)k_pages,
                        (const char*)v_pages, (const uint32_t*)k_scale, (const uint32_t*)v_scale, idx, first, n_rows,
                        (decltype(out))k_out, (decltype(out))v_out);
     return hip_status();
@@ -77,12 +93,12 @@ int launch_fetch(const Pages& pg, const void* k_pages, const void* v_pages, cons
   const bool q4 = pg.fmt == RESTKV_Q4;
   if (pg.dtype == RESTKV_F32) {
     float* t = nullptr;
-    if (pg.d == 128) return q4 ? go(k_fetch<float, 128, true>, t) : go(k_fetch<float, 128, false>, t);
-    return q4 ? go(k_fetch<float, 64, true>, t) : go(k_fetch<float, 64, false>, t);
+    if (pg.d == 128) return q4 ? go(k_fetch<float, 128, true, U>, t) : go(k_fetch<float, 128, false, U>, t);
+    return q4 ? go(k_fetch<float, 64, true, U>, t) : go(k_fetch<float, 64, false, U>, t);
   }
   bf16_t* t = nullptr;
-  if (pg.d == 128) return q4 ? go(k_fetch<bf16_t, 128, true>, t) : go(k_fetch<bf16_t, 128, false>, t);
-  return q4 ? go(k_fetch<bf16_t, 64, true>, t) : go(k_fetch<bf16_t, 64, false>, t);
+  if (pg.d == 128) return q4 ? go(k_fetch<bf16_t, 128, true, U>, t) : go(k_fetch<bf16_t, 128, false, U>, t);
+  return q4 ? go(k_fetch<bf16_t, 64, true, U>, t) : go(k_fetch<bf16_t, 64, false, U>, t);
 }
 
 }  // namespace restkv

@@ -29,6 +29,11 @@ size_t attend_ws_bytes(const Pages& pg);
 int launch_attend(const Pages& pg, const void* q, const void* k_pages, const void* v_pages, const void* k_scale,
                   const void* v_scale, void* out, float* lse, char* ws, hipStream_t st);
 
+// Wave-uniform reads of what the kernel does not write, through the scalar cache.
+__device__ __forceinline__ int uniform_load(const int32_t* p) {
+  return *(const __attribute__((address_space(4))) int32_t*)(uintptr_t)p;
+}
+
 // New tokens of sequence s: rows [first, first + n) of the packed tensors.
 struct NewRows { int first, n; };
 __device__ __forceinline__ NewRows new_rows(const Pages& pg, int s) {
@@ -65,9 +70,9 @@ __device__ __forceinline__ float bf16_below(float x) {       // largest bfloat16
   return __uint_as_float((u >> 31) && u != cut ? cut + 0x10000u : cut);
 }
 
-// Sixteen lanes of a wavefront's row: min / max over them, in every lane.
+// Sixteen lanes of a wavefront's row: min / max over them, in every lane (of a NaN nothing is said).
 __device__ __forceinline__ float row16_min(float x) {
-#define RK_STEP(ctrl) x = fminf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), ctrl, 0xF, 0xF, false)))
+#define RK_STEP(ctrl) x = fminf(x, __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), ctrl, 0xF, 0xF, true)))
   RK_STEP(0x121); RK_STEP(0x122); RK_STEP(0x124); RK_STEP(0x128);
 #undef RK_STEP
   return x;
