@@ -51,6 +51,10 @@ class RestkvCache(ctypes.Structure):
             "q_stride_t", "q_stride_h", "kv_stride_t", "kv_stride_h", "out_stride_t", "out_stride_h", "lse_stride_t",
             "lse_stride_h")]
 
+    def __setattr__(self, name, value):
+        self.__dict__.pop("told", None)      # what the binding has worked out from the fields
+        super().__setattr__(name, value)
+
 
 class RestkvError(RuntimeError):
     def __init__(self, code: int, what: str):
@@ -415,9 +419,35 @@ def alloc_attend_workspace(c: RestkvCache, device="cuda") -> Optional[torch.Tens
     return torch.empty(n + 256, dtype=torch.uint8, device=device) if n else None
 
 
-def _check_pages(what: str, c: RestkvCache, pages: CachePages, table, lens, new_start=None) -> int:
+class _Told:
+    """What a description says of the tensors of a call, worked out once (a field that is set makes it new)."""
+
+    def __init__(self, c: RestkvCache):
+        self.ref = ctypes.byref(c)
+        self.dtype, self.out_dtype = _TORCH.get(c.dtype), _TORCH.get(c.out_dtype)
+        self.kv, self.q, self.lse = ((c.n_tokens, c.n_kv_heads, c.head_dim), (c.n_tokens, c.n_q_heads, c.head_dim),
+                                     (c.n_tokens, c.n_q_heads))
+        self.kv_stride, self.q_stride, self.out_stride, self.lse_stride = (
+            (c.kv_stride_t, c.kv_stride_h, 1), (c.q_stride_t, c.q_stride_h, 1), (c.out_stride_t, c.out_stride_h, 1),
+            (c.lse_stride_t, c.lse_stride_h))
+        self.n_table, self.n_lens, self.n_new = c.n_seqs * c.table_stride_s, c.n_seqs * c.lens_stride_s, c.n_seqs + 1
+        self.n_tokens, self.n_turns = c.n_tokens, c.n_positions * (c.rotary_dim // 2)
+        self.pages = None                    # the last layout of pages that was found to be the described one
+
+
+def _told(c: RestkvCache) -> _Told:
+    t = c.__dict__.get("told")
+    if t is None:
+        t = c.__dict__["told"] = _Told(c)
+    return t
+
+
+def _check_pages(what: str, c: RestkvCache, told: _Told, pages: CachePages) -> int:
     """The GPU that the cache is on."""
-    shape, strides, dtype, d, dev = pages.rows
+    rows = pages.rows
+    if rows == told.pages:
+        return rows[4]
+    shape, strides, dtype, d, dev = rows
     heads = 1 if c.table_stride_h else c.n_kv_heads
     page, head, pos = c.page_stride, c.head_stride, c.token_stride
     # (a stride along one entry says nothing)
@@ -428,107 +458,117 @@ def _check_pages(what: str, c: RestkvCache, pages: CachePages, table, lens, new_
         raise RestkvError(-1, f"{what}: pages {shape} with strides {strides} in rows of {d} {dtype} are not the described ones")
     if dev < 0:
         raise RestkvError(-1, f"{what}: the pages are not on a GPU")
-    n = c.n_seqs
-    _check_flat(what, dev, torch.int32, "table", table, n * c.table_stride_s)
-    _check_flat(what, dev, torch.int32, "lens", lens, n * c.lens_stride_s)
-    if new_start is not None:
-        _check_flat(what, dev, torch.int32, "new_start", new_start, n + 1)
+    told.pages = rows
     return dev
 
 
 def _check_flat(what, dev, dtype, name, t, n):
-    if t is None or t.dtype != dtype or t.get_device() != dev or t.numel() < n or not t.is_contiguous():
+    """Address of a contiguous tensor of n values at least."""
+    if t is None or t.dtype is not dtype or t.get_device() != dev or t.numel() < n or not t.is_contiguous():
         raise RestkvError(-1, f"{what}: {name} has to be contiguous {dtype}, {n} values on GPU {dev}")
+    return t.data_ptr()
 
 
-def _check_rows(what, dev, dtype, name, t, shape):
-    """Strides of a tensor [tokens, heads, d] or [tokens, heads]."""
-    if t.dtype != dtype or t.get_device() != dev or t.shape != shape or (len(shape) == 3 and t.stride(2) != 1):
-        raise RestkvError(-1, f"{what}: {name} has to be {dtype} {tuple(shape)} on GPU {dev}, contiguous along the last")
-    st, least = t.stride(), shape[2] if len(shape) == 3 else 1
+def _check_rows(what, dev, dtype, name, t, shape, strides):
+    """Strides of a tensor [tokens, heads, d] or [tokens, heads], those given where it has them."""
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape:
+        raise RestkvError(-1, f"{what}: {name} has to be {dtype} {tuple(shape)} on GPU {dev}")
+    st = t.stride()
+    if st == strides:
+        return strides
+    least = shape[2] if len(shape) == 3 else 1
+    if len(shape) == 3 and st[2] != 1:
+        raise RestkvError(-1, f"{what}: {name} has to be contiguous along its last dimension")
     # (a stride along one entry, or none, says nothing; the library asks for one that a contiguous tensor could have)
     along, across = st[0] if shape[0] > 1 else shape[1] * least, st[1] if shape[1] > 1 else least
     if along < least or across < least:
         raise RestkvError(-1, f"{what}: rows of {name} overlap")
-    return along, across
+    return (along, across) + strides[2:]
 
 
-def _as_strided(c: RestkvCache, kind: str, strides) -> RestkvCache:
-    """The description with these strides of a token tensor: itself where it has them."""
-    t, h = kind + "_stride_t", kind + "_stride_h"
-    if (getattr(c, t), getattr(c, h)) == strides:
-        return c
+def _as_strided(c: RestkvCache, **strides) -> ctypes.c_void_p:
+    """A copy of the description with these strides of token tensors."""
     c = RestkvCache.from_buffer_copy(c)
-    setattr(c, t, strides[0])
-    setattr(c, h, strides[1])
-    return c
+    for kind, st in strides.items():
+        setattr(c, kind + "_stride_t", st[0])
+        setattr(c, kind + "_stride_h", st[1])
+    return ctypes.byref(c)
 
 
 def _on_gpu(dev: int, stream, what: str, f, *args):
     """The call on GPU `dev`, on the given stream or that GPU's current one."""
-    s = ctypes.c_void_p((torch.cuda.current_stream(dev) if stream is None else stream).cuda_stream)
+    s = (torch.cuda.current_stream(dev) if stream is None else stream).cuda_stream
     if dev == torch.cuda.current_device():
-        _chk(f(*args, s), what)
+        rc = f(*args, s)
     else:
         with torch.cuda.device(dev):
-            _chk(f(*args, s), what)
+            rc = f(*args, s)
+    if rc:
+        raise RestkvError(rc, what)
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
 
 
 def restkv_append(c: RestkvCache, k, v, pages: CachePages, table, lens, *, new_start=None, positions=None, cos=None, sin=None,
                   q=None, q_out=None, stream=None):
     """New keys (rotated by their positions) and values [n_tokens, Hkv, d] into the pages, and new queries [n_tokens, Hq, d]
     rotated beside them; lens counts the new tokens already."""
-    what = "restkv_append"
-    dev, dt = _check_pages(what, c, pages, table, lens, new_start), _TORCH.get(c.dtype)
-    shape, told = (c.n_tokens, c.n_kv_heads, c.head_dim), c
-    strides = _check_rows(what, dev, dt, "k", k, shape)
-    if _check_rows(what, dev, dt, "v", v, shape) != strides:
+    what, told, i32 = "restkv_append", _told(c), torch.int32
+    dev, dt, ref = _check_pages(what, c, told, pages), told.dtype, told.ref
+    tb, ln = _check_flat(what, dev, i32, "table", table, told.n_table), _check_flat(what, dev, i32, "lens", lens, told.n_lens)
+    ns = None if new_start is None else _check_flat(what, dev, i32, "new_start", new_start, told.n_new)
+    kv = _check_rows(what, dev, dt, "k", k, told.kv, told.kv_stride)
+    if _check_rows(what, dev, dt, "v", v, told.kv, kv) != kv:
         raise RestkvError(-1, f"{what}: k and v have to have the same strides")
-    c = _as_strided(c, "kv", strides)
+    qs = told.q_stride
     if q is not None and q_out is not None:
-        shape = (told.n_tokens, told.n_q_heads, told.head_dim)
-        strides = _check_rows(what, dev, dt, "q", q, shape)
-        if q_out is not q and _check_rows(what, dev, dt, "q_out", q_out, shape) != strides:
+        qs = _check_rows(what, dev, dt, "q", q, told.q, qs)
+        if q_out is not q and _check_rows(what, dev, dt, "q_out", q_out, told.q, qs) != qs:
             raise RestkvError(-1, f"{what}: q and q_out have to have the same strides")
-        c = _as_strided(c, "q", strides)
-    if c.rotary_dim:
-        n = c.n_positions * (c.rotary_dim // 2)
-        _check_flat(what, dev, torch.float32, "cos", cos, n)
-        _check_flat(what, dev, torch.float32, "sin", sin, n)
-    if positions is not None:
-        _check_flat(what, dev, torch.int32, "positions", positions, c.n_tokens)
-    _on_gpu(dev, stream, what, lib().restkv_append, ctypes.byref(c), _ptr(k), _ptr(v), _ptr(pages.k), _ptr(pages.v),
-            _ptr(pages.k_scale), _ptr(pages.v_scale), _ptr(table), _ptr(lens), _ptr(new_start), _ptr(positions), _ptr(cos),
-            _ptr(sin), _ptr(q), _ptr(q_out))
+    cs = sn = None
+    if told.n_turns:
+        cs = _check_flat(what, dev, torch.float32, "cos", cos, told.n_turns)
+        sn = _check_flat(what, dev, torch.float32, "sin", sin, told.n_turns)
+    ps = None if positions is None else _check_flat(what, dev, i32, "positions", positions, told.n_tokens)
+    if kv is not told.kv_stride or qs is not told.q_stride:
+        ref = _as_strided(c, kv=kv, q=qs)
+    _on_gpu(dev, stream, what, lib().restkv_append, ref, k.data_ptr(), v.data_ptr(), pages.k.data_ptr(), pages.v.data_ptr(),
+            _addr(pages.k_scale), _addr(pages.v_scale), tb, ln, ns, ps, cs, sn, _addr(q), _addr(q_out))
 
 
 def restkv_attend(c: RestkvCache, q, pages: CachePages, table, lens, out, lse=None, workspace=None, *, new_start=None,
                   stream=None):
     """Attention of the newest tokens' queries q [n_tokens, Hq, d] over the pages: out [n_tokens, Hq, d], lse [n_tokens, Hq]."""
-    what = "restkv_attend"
-    dev = _check_pages(what, c, pages, table, lens, new_start)
-    shape, told = (c.n_tokens, c.n_q_heads, c.head_dim), c
-    c = _as_strided(c, "q", _check_rows(what, dev, _TORCH.get(told.dtype), "q", q, shape))
-    c = _as_strided(c, "out", _check_rows(what, dev, _TORCH.get(told.out_dtype), "out", out, shape))
-    if lse is not None:
-        c = _as_strided(c, "lse", _check_rows(what, dev, torch.float32, "lse", lse, shape[:2]))
-    if workspace is not None and (workspace.get_device() != dev or workspace.dtype != torch.uint8):
-        raise RestkvError(-1, f"{what}: the workspace has to be uint8 on GPU {dev}")
-    wp, wn = _ws(workspace)
-    _on_gpu(dev, stream, what, lib().restkv_attend, ctypes.byref(c), _ptr(q), _ptr(pages.k), _ptr(pages.v), _ptr(pages.k_scale),
-            _ptr(pages.v_scale), _ptr(table), _ptr(lens), _ptr(new_start), _ptr(out), _ptr(lse), wp, wn)
+    what, told, i32 = "restkv_attend", _told(c), torch.int32
+    dev, ref = _check_pages(what, c, told, pages), told.ref
+    tb, ln = _check_flat(what, dev, i32, "table", table, told.n_table), _check_flat(what, dev, i32, "lens", lens, told.n_lens)
+    ns = None if new_start is None else _check_flat(what, dev, i32, "new_start", new_start, told.n_new)
+    qs = _check_rows(what, dev, told.dtype, "q", q, told.q, told.q_stride)
+    outs = _check_rows(what, dev, told.out_dtype, "out", out, told.q, told.out_stride)
+    ls = told.lse_stride if lse is None else _check_rows(what, dev, torch.float32, "lse", lse, told.lse, told.lse_stride)
+    if qs is not told.q_stride or outs is not told.out_stride or ls is not told.lse_stride:
+        ref = _as_strided(c, q=qs, out=outs, lse=ls)
+    wp, wn = None, 0
+    if workspace is not None:
+        if workspace.get_device() != dev or workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
+            raise RestkvError(-1, f"{what}: the workspace has to be contiguous uint8 on GPU {dev}")
+        at = workspace.data_ptr()
+        wp, wn = at + -at % 256, max(workspace.numel() - -at % 256, 0)
+    _on_gpu(dev, stream, what, lib().restkv_attend, ref, q.data_ptr(), pages.k.data_ptr(), pages.v.data_ptr(), _addr(pages.k_scale),
+            _addr(pages.v_scale), tb, ln, ns, out.data_ptr(), _addr(lse), wp, wn)
 
 
 def restkv_fetch(c: RestkvCache, pages: CachePages, table, lens, k_out, v_out, *, idx=None, first=0, stream=None):
     """Rows of the pages as dense k_out, v_out [n_seqs, Hkv, n, d]: positions idx [n_seqs, Hkv, n], or first .. first + n - 1."""
-    what = "restkv_fetch"
-    dev = _check_pages(what, c, pages, table, lens)
-    n, dt = k_out.shape[2] if k_out.dim() == 4 else -1, _TORCH.get(c.dtype)
-    if n < 0 or k_out.shape != (c.n_seqs, c.n_kv_heads, n, c.head_dim) or v_out.shape != k_out.shape:
+    what, told, i32 = "restkv_fetch", _told(c), torch.int32
+    dev = _check_pages(what, c, told, pages)
+    tb, ln = _check_flat(what, dev, i32, "table", table, told.n_table), _check_flat(what, dev, i32, "lens", lens, told.n_lens)
+    shape = k_out.shape
+    if len(shape) != 4 or shape != (c.n_seqs, c.n_kv_heads, shape[2], c.head_dim) or v_out.shape != shape:
         raise RestkvError(-1, f"{what}: k_out and v_out have to be [n_seqs, Hkv, n, d]")
-    _check_flat(what, dev, dt, "k_out", k_out, 0)
-    _check_flat(what, dev, dt, "v_out", v_out, 0)
-    if idx is not None:
-        _check_flat(what, dev, torch.int32, "idx", idx, c.n_seqs * c.n_kv_heads * n)
-    _on_gpu(dev, stream, what, lib().restkv_fetch, ctypes.byref(c), _ptr(pages.k), _ptr(pages.v), _ptr(pages.k_scale),
-            _ptr(pages.v_scale), _ptr(table), _ptr(lens), _ptr(idx), int(first), n, _ptr(k_out), _ptr(v_out))
+    kp, vp = _check_flat(what, dev, told.dtype, "k_out", k_out, 0), _check_flat(what, dev, told.dtype, "v_out", v_out, 0)
+    ix = None if idx is None else _check_flat(what, dev, i32, "idx", idx, c.n_seqs * c.n_kv_heads * shape[2])
+    _on_gpu(dev, stream, what, lib().restkv_fetch, told.ref, pages.k.data_ptr(), pages.v.data_ptr(), _addr(pages.k_scale),
+            _addr(pages.v_scale), tb, ln, ix, int(first), shape[2], kp, vp)

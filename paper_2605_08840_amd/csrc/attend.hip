@@ -58,18 +58,17 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
   store_out(a, nr.first + i, head, c * 4, x, M, L);
 }
 
-// Blocks of 16 rows of a wavefront: as many as the rows fill, up to what its registers hold.
-int rows_of(const Pages& pg) {
-  return (int64_t)pg.G * pg.max_new <= 16 ? 1 : 2;
-}
-
-struct AttendPlan { int R, c_min, target; int64_t row_blocks, entries, Hy, chunks, slots; };
+struct AttendPlan { int R, many, c_min, target; int64_t row_blocks, entries, Hy, chunks, slots; };
 AttendPlan attend_plan(const Pages& pg) {
   AttendPlan p;
-  p.R = rows_of(pg);
+  // Up to 32 rows the four wavefronts of a workgroup share the rows and divide the keys; more rows of bfloat16 pages are
+  // divided among them, with the keys in LDS.
   const int64_t rows = (int64_t)pg.G * pg.max_new;
+  p.many = pg.fmt == RESTKV_BF16 && rows > 32;
+  p.R = rows <= (p.many ? 64 : 16) ? 1 : 2;
   const bool per_head = pg.lens_sh != 0;
-  p.row_blocks = (rows + 16 * p.R - 1) / (16 * p.R);
+  const int block = (p.many ? 64 : 16) * p.R;
+  p.row_blocks = (rows + block - 1) / block;
   p.entries = per_head ? (int64_t)pg.n_seqs * pg.Hkv : pg.n_seqs;
   p.Hy = per_head ? 1 : pg.Hkv;
   p.c_min = pg.fmt == RESTKV_Q4 ? 4 : 2;          // (a tile for each wavefront)
@@ -123,7 +122,7 @@ int launch_attend(const Pages& pg, const void* q, const void* k_pages, const voi
   a.vec_q = !((uintptr_t)q & 15u) && !((pg.q_st | pg.q_sh) & (qel - 1));
   const int oal = pg.out_dtype == RESTKV_F32 ? 15 : 7;
   a.vec_out = !((uintptr_t)out & oal) && !((pg.o_st | pg.o_sh) & 3);
-  const int rc = pg.fmt == RESTKV_F32 ? run_attend_f32(a, p.R, st) : pg.fmt == RESTKV_BF16 ? run_attend_bf16(a, p.R, st) : run_attend_q4(a, p.R, st);
+  const int rc = p.many ? run_attend_rows(a, p.R, st) : pg.fmt == RESTKV_F32 ? run_attend_f32(a, p.R, st) : pg.fmt == RESTKV_BF16 ? run_attend_bf16(a, p.R, st) : run_attend_q4(a, p.R, st);
   if (rc || !p.slots) return rc;
   const dim3 grid = wide_grid((int64_t)pg.n_seqs * pg.max_new * pg.Hq);
   if (pg.d == 128) hipLaunchKernelGGL(k_attend_join<128>, grid, dim3(256), 0, st, a);
