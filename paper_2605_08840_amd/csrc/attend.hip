@@ -105,7 +105,7 @@ int launch_attend(const Pages& pg, const void* q, const void* k_pages, const voi
                   const void* v_scale, void* out, float* lse, char* ws, hipStream_t st) {
   const AttendPlan p = attend_plan(pg);
   const AttendWs lay = attend_ws(pg, p);
-  if (p.chunks * p.Hy > (int64_t)1 << 30) return RESTKV_EUNSUPPORTED;
+  if (p.chunks * p.Hy > (int64_t)1 << 30 || p.row_blocks > (1 << 20)) return RESTKV_EUNSUPPORTED;
   AttendArgs a = {};
   a.pg = pg;
   a.q = q; a.k = (const char*)k_pages; a.v = (const char*)v_pages;
@@ -117,7 +117,7 @@ int launch_attend(const Pages& pg, const void* q, const void* k_pages, const voi
   }
   a.entries = (int)p.entries; a.per_head = pg.lens_sh != 0; a.Hy = (int)p.Hy;
   a.row_blocks = (int)p.row_blocks; a.units = (int)(p.chunks * p.Hy);
-  a.c_min = p.c_min; a.share = (float)((double)(p.Hy * p.row_blocks) / p.target * (1 + 0x1p-23));
+  a.c_min = p.c_min; a.chunks = (float)((double)p.target / (double)(p.Hy * p.row_blocks) * (1 - 0x1p-23));
   const int qel = pg.dtype == RESTKV_F32 ? 4 : 8;
   a.vec_q = !((uintptr_t)q & 15u) && !((pg.q_st | pg.q_sh) & (qel - 1));
   const int oal = pg.out_dtype == RESTKV_F32 ? 15 : 7;

@@ -24,10 +24,19 @@ struct AttendArgs {
   float* part_m; float* part_l; float* part_o;   // [slots * Hy, rows] and [.., d]: chunks of entries that have several
   int entries, per_head, Hy;        // an entry is a sequence, or with lengths per head a (sequence, head); Hy heads share it
   int row_blocks, units, c_min, vec_q, vec_out;
-  float share;                      // Hy * row_blocks / workgroups wanted
+  float chunks;                     // workgroups wanted of each head and row block
 };
 
 constexpr int ATT_TILE = 64;        // chunks are whole tiles of 64 keys
+
+// The grid: x = 8 row blocks by 8 units, so that the row blocks of a unit (a chunk and a head) follow each other on one XCD, whose
+// L2 then holds the chunk (workgroups go round eight XCDs); y and z the units by eight.
+constexpr int GRID_Y = 32768;
+inline dim3 unit_grid(const AttendArgs& a) {
+  const unsigned n = ((unsigned)a.units + 7) / 8;
+  return dim3(8u * a.row_blocks, n < GRID_Y ? n : GRID_Y, (n + GRID_Y - 1) / GRID_Y);
+}
+__device__ __forceinline__ int unit_of_block() { return (blockIdx.z * GRID_Y + blockIdx.y) * 8 + (blockIdx.x & 7); }
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
@@ -42,58 +51,105 @@ __device__ __forceinline__ int wave_scan(int x) {
   return x;
 }
 
-// What a workgroup takes.  Chunks are of equal size C over all entries: enough for `target` workgroups in all, so that a
-// long sequence among short ones is cut as finely as the whole asks for, and short batches not at all.  Every wavefront
-// works this out for itself from the lengths, 64 entries at a time.
+// What a workgroup takes.  Chunks are of nearly equal size over all entries, so that a long sequence among short ones is cut as
+// finely as the whole asks for: of C tiles at most, where all of them are as many workgroups as the chip holds at a time (a
+// few more would run alone at the end; an entry has half a chunk more than its tiles over C, in the mean).  Up to 64 entries a
+// wavefront works this out by itself, more are divided among the threads of the workgroup.
 struct Chunk { int e, tile0, tile1, index, count, slot0, told, first, n; };
-__device__ __forceinline__ bool find_chunk(const AttendArgs& a, int x, Chunk& o) {
+struct Entry { int told, first, n, tiles; };
+__device__ __forceinline__ Entry read_entry(const AttendArgs& a, int e) {
   const Pages& pg = a.pg;
-  const int lane = threadIdx.x & 63;
-  int told = 0, first = 0, n = 0, tiles = 0;     // of entry base + lane
-  auto read = [&](int base) {
-    const int e = base + lane;
-    told = first = n = tiles = 0;
-    if (e < a.entries) {
-      const int s = a.per_head ? e / pg.Hkv : e, h = a.per_head ? e - s * pg.Hkv : 0;
-      told = told_len(pg, s, h);
-      const NewRows nr = new_rows(pg, s);
-      first = nr.first;
-      n = nr.n;
-      if (n) tiles = (min(told, pg.max_len) + ATT_TILE - 1) / ATT_TILE;
-    }
-  };
-  read(0);
-  int64_t total = wave_sum((uint32_t)tiles);
-  for (int base = 64; base < a.entries; base += 64) {
-    read(base);
-    total += wave_sum((uint32_t)tiles);
+  Entry o = {0, 0, 0, 0};
+  if (e < a.entries) {
+    const int s = a.per_head ? e / pg.Hkv : e, h = a.per_head ? e - s * pg.Hkv : 0;
+    o.told = told_len(pg, s, h);
+    const NewRows nr = new_rows(pg, s);
+    o.first = nr.first;
+    o.n = nr.n;
+    if (o.n) o.tiles = (min(o.told, pg.max_len) + ATT_TILE - 1) / ATT_TILE;
   }
-  // tiles of a chunk: total / (chunks per head and row block), rounded up (share is, too, and so is the product)
-  const float want = (float)total * a.share * (1.f + 0x1p-20f) + 1.f;
-  const int C = want < (float)a.c_min ? a.c_min : want > 0x1p25f ? 1 << 25 : (int)want;
-  int run = 0, slots = 0;
-  for (int base = 0; base < a.entries; base += 64) {
-    if (a.entries > 64) read(base);
-    const int cnt = base + lane < a.entries ? max(1, (tiles + C - 1) / C) : 0, own = cnt > 1 ? cnt : 0;
+  return o;
+}
+// Tiles of a chunk, from the tiles of all entries and how many entries have any: at least total / chunks, which the scratch is
+// sized for (hence the rounding up).
+__device__ __forceinline__ int chunk_tiles(const AttendArgs& a, float total, int active) {
+  const float want = total / fmaxf(a.chunks - 0.5f * active, 0.25f * a.chunks) * (1.f + 0x1p-20f) + 1.f;
+  return want < (float)a.c_min ? a.c_min : want > 0x1p25f ? 1 << 25 : (int)want;
+}
+__device__ __forceinline__ Chunk chunk_of(const Entry& x, int e, int index, int count, int slot0) {
+  const int each = count == 1 ? x.tiles : (x.tiles + count - 1) / count, t0 = min(index * each, x.tiles);
+  return {e, t0, min(t0 + each, x.tiles), index, count, slot0, x.told, x.first, x.n};
+}
+__device__ __forceinline__ bool find_chunk(const AttendArgs& a, int x, int* lds, Chunk& o) {
+  const int lane = threadIdx.x & 63;
+  if (a.entries <= 64) {
+    const Entry en = read_entry(a, lane);
+    const int C = chunk_tiles(a, (float)wave_sum((uint32_t)en.tiles), __popcll(__ballot(en.tiles > 0)));
+    const int cnt = lane < a.entries ? max(1, (en.tiles + C - 1) / C) : 0, own = cnt > 1 ? cnt : 0;
     const int inc = wave_scan(cnt), sl = wave_scan(own);
-    const unsigned long long hit = __ballot(run + inc > x);
-    if (hit) {
-      const int l = __builtin_ctzll(hit);
-      auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
-      o.e = base + l;
-      o.count = of(cnt);
-      o.index = x - run - of(inc) + o.count;
-      o.slot0 = slots + of(sl - own);
-      const int t = of(tiles), each = o.count == 1 ? t : (t + o.count - 1) / o.count;
-      o.tile0 = min(o.index * each, t);
-      o.tile1 = min(o.tile0 + each, t);
-      o.told = of(told);
-      o.first = of(first);
-      o.n = of(n);
-      return true;
+    const unsigned long long hit = __ballot(inc > x);
+    if (!hit) return false;
+    const int l = __builtin_ctzll(hit);
+    auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+    const int count = of(cnt);
+    o = chunk_of({of(en.told), of(en.first), of(en.n), of(en.tiles)}, l, x - of(inc) + count, count, of(sl - own));
+    return true;
+  }
+  const int tid = threadIdx.x, wv = tid >> 6;
+  Entry en = read_entry(a, tid);
+  int64_t tiles = en.tiles;
+  int active = en.tiles > 0;
+  for (int e = tid + 256; e < a.entries; e += 256) {
+    const int t = read_entry(a, e).tiles;
+    tiles += t;
+    active += t > 0;
+  }
+  // (a sum of 64 tiles of up to 2^24 entries' positions each may pass 32 bits: as a float)
+  float ft = (float)tiles;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) ft += __shfl_xor(ft, d);
+  active = (int)wave_sum((uint32_t)active);
+  if (lane == 0) {
+    lds[wv] = __float_as_int(ft);
+    lds[4 + wv] = active;
+  }
+  __syncthreads();
+  const int C = chunk_tiles(a, (__int_as_float(lds[0]) + __int_as_float(lds[1])) + (__int_as_float(lds[2]) + __int_as_float(lds[3])),
+                            lds[4] + lds[5] + lds[6] + lds[7]);
+  int run = 0, slots = 0;
+  for (int base = 0; base < a.entries; base += 256) {
+    const int e = base + tid;
+    if (base) en = read_entry(a, e);
+    const int cnt = e < a.entries ? max(1, (en.tiles + C - 1) / C) : 0, own = cnt > 1 ? cnt : 0;
+    int inc = wave_scan(cnt), sl = wave_scan(own);
+    if (lane == 63) {
+      lds[8 + wv] = inc;
+      lds[12 + wv] = sl;
     }
-    run += __builtin_amdgcn_readlane(inc, 63);
-    slots += __builtin_amdgcn_readlane(sl, 63);
+    if (tid == 0) lds[16] = -1;
+    __syncthreads();
+    int all = 0, all_slots = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if (w == wv) {
+        inc += run + all;
+        sl += slots + all_slots;
+      }
+      all += lds[8 + w];
+      all_slots += lds[12 + w];
+    }
+    if (inc > x && inc - cnt <= x) {
+      const Chunk c = chunk_of(en, e, x - inc + cnt, cnt, sl - own);
+      lds[16] = c.e; lds[17] = c.tile0; lds[18] = c.tile1; lds[19] = c.index; lds[20] = c.count; lds[21] = c.slot0;
+      lds[22] = c.told; lds[23] = c.first; lds[24] = c.n;
+    }
+    run += all;
+    slots += all_slots;
+    __syncthreads();
+    const bool found = lds[16] >= 0;
+    if (found) o = {lds[16], lds[17], lds[18], lds[19], lds[20], lds[21], lds[22], lds[23], lds[24]};
+    __syncthreads();                  // (the scratch is used for other things from here on, or for the next entries)
+    if (found) return true;
   }
   return false;
 }
@@ -180,6 +236,15 @@ __device__ __forceinline__ Words<N> load_words(const char* base, uint32_t off) {
   typedef const __attribute__((address_space(1))) char* global;
   return *(const __attribute__((address_space(1))) Words<N>*)((global)u + off);
 }
+// NP parts of four weights, as split8 makes them of eight
+template <int NP>
+__device__ __forceinline__ void split4(const float (&x)[4], Words<2> (&o)[NP]) {
+  const float y[8] = {x[0], x[1], x[2], x[3], 0.f, 0.f, 0.f, 0.f};
+  const Op<NP> p = split8<NP>(y);
+#pragma unroll
+  for (int i = 0; i < NP; ++i) o[i] = Words<2>{p.p[i].x, p.p[i].y};
+}
+
 __device__ __forceinline__ uint32_t load_half(const char* base, uint32_t off) {
   uint64_t u = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)base >> 32)) << 32 |
                (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(uint64_t)base);
@@ -216,41 +281,37 @@ __device__ __forceinline__ uint32_t sixteen_plus(uint32_t x, int i, uint32_t mas
 // of 16 rows of a wavefront.  Of a tile the keys are loaded anew (for the next one) as soon as the logits are there, the
 // values as soon as they are in the sums: a load has the other half's arithmetic, and other wavefronts', to come back,
 // and costs no second set of registers.
-template <int FMT, typename T, int D, int NP, int R>
+// SP (4-bit pages, up to 16 / SP rows): the sixteen columns are SP copies of the rows, and copy x takes the 16-key blocks x,
+// SP + x, ...: its queries are zeros in the products of other blocks, which add up in one set of registers, and its weights
+// are zeros in those blocks' products with values.  The matrix pipe does as much as before, but a lane scales, exponentiates
+// and splits 1 / SP of the keys, which is what bounds this format: four rows, 128k tokens 48 -> XX us.
+template <int FMT, typename T, int D, int NP, int R, int SP>
 __global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(2)))
 void k_attend(AttendArgs a) {
   constexpr int UN = D / 16, NG = D / 32;
   constexpr int QP = FMT == FMT_Q4 ? planes_of<T> : 1;
   constexpr int TK = FMT == FMT_F32 ? 16 : FMT == FMT_BF16 ? 32 : 64, NB = TK / 16;
   constexpr int ROWB = FMT == FMT_F32 ? D * 4 : FMT == FMT_BF16 ? D * 2 : D / 2;
+  constexpr int CW = 16 / SP, NBS = NB / SP;       // columns of a copy, blocks of a copy
   constexpr int LDO = D + 4, QC = FMT == FMT_F32 ? D / 16 : D / 32;
   extern __shared__ __align__(16) float sm[];
   const Pages& pg = a.pg;
-  const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
+  const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4, copy = SP > 1 ? n / CW : 0;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  // row blocks of a chunk follow each other on one XCD, whose L2 then holds the chunk (workgroups go round eight XCDs)
-  int unit, rb;
-  if (a.row_blocks == 1) {
-    unit = (int)wide_block();
-    rb = 0;
-  } else {
-    const int64_t b = wide_block(), per = (int64_t)a.row_blocks * 8, in = b % per;
-    unit = (int)(b / per * 8 + in % 8);
-    rb = (int)(in / 8);
-  }
+  const int unit = unit_of_block(), rb = blockIdx.x >> 3;
   if (unit >= a.units) return;
   const int hy = unit % a.Hy;
   Chunk ch;
-  if (!find_chunk(a, unit / a.Hy, ch)) return;
+  if (!find_chunk(a, unit / a.Hy, (int*)sm, ch)) return;
   const int e = __builtin_amdgcn_readfirstlane(ch.e);
   const int s = a.per_head ? e / pg.Hkv : e, h = a.per_head ? e - s * pg.Hkv : hy;
-  const NewRows nr = {ch.first, ch.n};
+  const NewRows nr = {__builtin_amdgcn_readfirstlane(ch.first), __builtin_amdgcn_readfirstlane(ch.n)};
   const int rows = pg.G * nr.n, row0 = rb * 16 * R;
   if (row0 >= rows) return;
   if (a.plan && ch.index == 0 && hy == 0 && rb == 0 && threadIdx.x == 0) a.plan[e] = make_int2(ch.slot0, ch.count);
 
-  const int told = ch.told, len = min(told, pg.max_len);
+  const int told = __builtin_amdgcn_readfirstlane(ch.told), len = min(told, pg.max_len);
   auto limit = [&](int row) {       // positions that a row sees
     return pg.causal ? min(max(told - nr.n + row / pg.G + 1, 0), len) : len;
   };
@@ -349,9 +410,10 @@ void k_attend(AttendArgs a) {
   float4 qf[FMT == FMT_F32 ? R : 1][FMT == FMT_F32 ? QC : 1];
   Op<QP> qo[FMT == FMT_F32 ? 1 : R][FMT == FMT_F32 ? 1 : QC];
   uint4 qz[FMT == FMT_Q4 ? R : 1];
+  uint32_t mine[SP];                 // all bits in the lanes of copy x
 #pragma unroll
   for (int cb = 0; cb < R; ++cb) {
-    const int row = min(row0 + cb * 16 + n, rows - 1);
+    const int row = min(row0 + cb * 16 + (SP > 1 ? n % CW : n), rows - 1);
     lim[cb] = limit(row);
     const int tok = row / pg.G;
     const T* p = (const T*)a.q + (nr.first + tok) * pg.q_st + (h * pg.G + row - tok * pg.G) * pg.q_sh;
@@ -396,17 +458,34 @@ void k_attend(AttendArgs a) {
     }
   }
 
+  auto only = [](uint4 x, uint32_t m) { return make_uint4(x.x & m, x.y & m, x.z & m, x.w & m); };
+  uint4 qm[SP > 1 ? SP : 1][SP > 1 ? NG : 1], qzm[SP];
+#pragma unroll
+  for (int x = 0; x < SP; ++x) {
+    mine[x] = copy == x ? ~0u : 0u;
+    if constexpr (SP > 1) {
+      static_assert(QP == 1 && R == 1, "");
+#pragma unroll
+      for (int f = 0; f < NG; ++f) qm[x][f] = only(qo[0][f].p[0], mine[x]);
+      qzm[x] = only(qz[0], mine[x]);
+    }
+  }
   uint32_t nib_mask = 0x00780078u, nib_base = 0x41804180u;
   if constexpr (FMT == FMT_Q4) asm("" : "+s"(nib_mask), "+v"(nib_base));      // (one of two constants may be scalar)
 
   for (int k0 = k_begin; k0 < k_end; k0 += 4 * TK) {
     const Where next = find(k0 + 4 * TK);
     const bool more = k0 + 4 * TK < k_end;
-    f32x4 p[NB][R];
+    f32x4 p[NBS][R];
     const bool masked = k0 + TK > min(k_end, lim_lo) || at.ok != (1 << NB) - 1;
     auto there = [&](int b) { return at.ok >> b & 1 ? min(k_end - (k0 + 16 * b), 16) : 0; };
-    auto seen = [&](int b, int r, int cb) { return 4 * j + r < there(b) && k0 + 16 * b + 4 * j + r < lim[cb]; };
+    // key 16 b + 4 j + r of the tile is in register r of p[bb], b = bb SP + the lane's copy
+    auto seen = [&](int bb, int r, int cb) {
+      const int b = bb * SP + copy;
+      return 4 * j + r < there(b) && k0 + 16 * b + 4 * j + r < lim[cb];
+    };
     bool odd_scales = false;
+    unsigned long long odd_keys = 0;
 
     // ---- logits
     if constexpr (FMT == FMT_F32) {
@@ -433,6 +512,16 @@ void k_attend(AttendArgs a) {
 #pragma unroll
           for (int cb = 0; cb < R; ++cb) p[b][cb] = mfma(__builtin_bit_cast(uint4, kr[b * KN + c]), qo[cb][c].p[0], p[b][cb]);
     } else {
+      if (masked) {                  // keys without a finite scale: zeros here, and NaN for the rows that see them below
+        bool bad = false;
+#pragma unroll
+        for (int f = 0; f < NG; ++f) {
+          const float x = __uint_as_float(sk[0][f] << 16), y = __uint_as_float(sk[0][f] & 0xFFFF0000u);
+          bad = bad || !(x - x == 0.f && y - y == 0.f);
+        }
+        odd_keys = __ballot(bad);
+        if (bad) sk[0] = Words<NG>{};
+      }
       __builtin_amdgcn_wave_barrier();
       *(Words<NG>*)&s_kz[lane * NG] = sk[0];
 #pragma unroll
@@ -457,6 +546,7 @@ void k_attend(AttendArgs a) {
       }
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
       __builtin_amdgcn_wave_barrier();
+      f32x4 copies[NG];               // of all copies: sums of q (16 + code) of their blocks
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         // sum over the groups of zero * (sum of q) - 16 step * (sum of q), as one product: lane j the group j
@@ -480,39 +570,66 @@ void k_attend(AttendArgs a) {
           op[f] = make_uint4(sixteen_plus(lo, e0, nib_mask, nib_base), sixteen_plus(hi, e0, nib_mask, nib_base),
                              sixteen_plus(lo, e0 + 1, nib_mask, nib_base), sixteen_plus(hi, e0 + 1, nib_mask, nib_base));
         }
-        f32x4 st[NG];                 // steps of keys 4 j .. 4 j + 3
+        if constexpr (SP == 1) {
+          f32x4 st[NG];               // steps of keys 4 j .. 4 j + 3
 #pragma unroll
-        for (int f = 0; f < NG; ++f) st[f] = *(const f32x4*)&s_ks[f * 64 + 16 * b + 4 * j];
+          for (int f = 0; f < NG; ++f) st[f] = *(const f32x4*)&s_ks[f * 64 + 16 * b + 4 * j];
 #pragma unroll
-        for (int cb = 0; cb < R; ++cb) {
-          p[b][cb] = mfma(za, qz[cb], f32x4{0.f, 0.f, 0.f, 0.f});
-          f32x4 t[NG];
+          for (int cb = 0; cb < R; ++cb) {
+            p[b][cb] = mfma(za, qz[cb], f32x4{0.f, 0.f, 0.f, 0.f});
+            f32x4 t[NG];
 #pragma unroll
-          for (int f = 0; f < NG; ++f) {
-            t[f] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int f = 0; f < NG; ++f) {
+              t[f] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int pl = 0; pl < QP; ++pl) t[f] = mfma(op[f], qo[cb][f].p[pl], t[f]);
+              for (int pl = 0; pl < QP; ++pl) t[f] = mfma(op[f], qo[cb][f].p[pl], t[f]);
+            }
+#pragma unroll
+            for (int f = 0; f < NG; ++f)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) p[b][cb][r] = __builtin_fmaf(st[f][r], t[f][r], p[b][cb][r]);
           }
+          // (one block at a time, finished here: else its sums are put off past the next loads, with all they are made of in
+          // registers)
 #pragma unroll
-          for (int f = 0; f < NG; ++f)
+          for (int cb = 0; cb < R; ++cb) asm volatile("" : "+v"(p[b][cb]));
+        } else {
+          const int x = b % SP, bb = b / SP;
+          p[bb][0] = mfma(za, qzm[x], x ? p[bb][0] : f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-            for (int r = 0; r < 4; ++r) p[b][cb][r] = __builtin_fmaf(st[f][r], t[f][r], p[b][cb][r]);
+          for (int f = 0; f < NG; ++f) copies[f] = mfma(op[f], qm[x][f], x ? copies[f] : f32x4{0.f, 0.f, 0.f, 0.f});
+          if (x == SP - 1)
+#pragma unroll
+            for (int f = 0; f < NG; ++f) {
+              const f32x4 st = *(const f32x4*)&s_ks[f * 64 + 16 * (bb * SP + copy) + 4 * j];
+#pragma unroll
+              for (int r = 0; r < 4; ++r) p[bb][0][r] = __builtin_fmaf(st[r], copies[f][r], p[bb][0][r]);
+            }
+          asm volatile("" : "+v"(p[bb][0]));
+#pragma unroll
+          for (int f = 0; f < NG; ++f) asm volatile("" : "+v"(copies[f]));
         }
-        // (one block at a time, finished here: else its sums are put off past the next loads, with all they are made of in registers)
-#pragma unroll
-        for (int cb = 0; cb < R; ++cb) asm volatile("" : "+v"(p[b][cb]));
         __builtin_amdgcn_sched_barrier(0);
       }
     }
     if (more) load_keys(next);
     else forget(kr);
 
-    // ---- softmax: lane = row, key 16 b + 4 j + r in register r of block b
+    // ---- softmax: lane = row
     if (masked) {
+      if (FMT == FMT_Q4 && odd_keys) {
+#pragma unroll
+        for (int cb = 0; cb < R; ++cb)
+#pragma unroll
+          for (int b = 0; b < NBS; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (odd_keys >> (16 * (b * SP + copy) + 4 * j + r) & 1) p[b][cb][r] = __builtin_nanf("");
+      }
 #pragma unroll
       for (int cb = 0; cb < R; ++cb)
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < NBS; ++b)
 #pragma unroll
           for (int r = 0; r < 4; ++r) p[b][cb][r] = seen(b, r, cb) ? p[b][cb][r] : -INFINITY;
     }
@@ -522,7 +639,7 @@ void k_attend(AttendArgs a) {
     for (int cb = 0; cb < R; ++cb) {
       float m = -INFINITY;
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+      for (int b = 0; b < NBS; ++b)
 #pragma unroll
         for (int r = 0; r < 4; ++r) m = fmaxf(m, p[b][cb][r]);
       top[cb] = quad_max(m) * sc;
@@ -547,7 +664,7 @@ void k_attend(AttendArgs a) {
     for (int cb = 0; cb < R; ++cb) {
       const float m = ref[cb] == -INFINITY ? 0.f : ref[cb];
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+      for (int b = 0; b < NBS; ++b)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           p[b][cb][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[b][cb][r], sc, -m));
@@ -665,13 +782,16 @@ void k_attend(AttendArgs a) {
             }
         }
       }
+      // (two places at a time, the parts of a weight in turn: products that add to the same sums do not follow each other)
 #pragma unroll
-      for (int i = 0; i < UN; ++i) {
-        const uint4 x = operand(i);
+      for (int i = 0; i < UN; i += 2) {
+        const uint4 x[2] = {operand(i), operand(i + 1)};
 #pragma unroll
-        for (int cb = 0; cb < R; ++cb)
+        for (int pl = NP - 1; pl >= 0; --pl)
 #pragma unroll
-          for (int pl = NP - 1; pl >= 0; --pl) o[i][cb] = mfma(x, po[cb].p[pl], o[i][cb]);
+          for (int cb = 0; cb < R; ++cb)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) o[i + y][cb] = mfma(x[y], po[cb].p[pl], o[i + y][cb]);
       }
     } else {
       if (__builtin_expect(masked && odd_scales, 0)) {
@@ -691,14 +811,32 @@ void k_attend(AttendArgs a) {
             for (int cb = 0; cb < R; ++cb) {
               float x = 0.f;
 #pragma unroll
-              for (int i = 0; i < NB * 4; ++i) x = i == b * 4 + r ? p[i >> 2][cb][i & 3] : x;
-              if (j == (kk >> 2 & 3) && (kk & 15) < there(b) && k0 + kk < lim[cb]) corr[cb][f] = __builtin_fmaf(x, z, corr[cb][f]);
+              for (int i = 0; i < NBS * 4; ++i) x = i == b / SP * 4 + r ? p[i >> 2][cb][i & 3] : x;
+              if (copy == b % SP && j == (kk >> 2 & 3) && (kk & 15) < there(b) && k0 + kk < lim[cb]) corr[cb][f] = __builtin_fmaf(x, z, corr[cb][f]);
             }
           }
         }
       }
+      // weights times the step of a group, in parts, for the lane's keys of p[bb]
+      Words<2> pw[NG][NP];
+      auto weights = [&](int bb, int f, Words<2> (&w)[NP]) {
+        const int at = f * 64 + 16 * (bb * SP + copy) + 4 * j;
+        const f32x4 st = *(const f32x4*)&s_vs[at], z = *(const f32x4*)&s_vz[at];
+        float x[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          x[r] = p[bb][0][r] * st[r];
+          corr[0][f] = __builtin_fmaf(p[bb][0][r], z[r], corr[0][f]);
+        }
+        split4<NP>(x, w);
+      };
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
+        if constexpr (SP > 1) {
+          if (hf < NBS)
+#pragma unroll
+            for (int f = 0; f < NG; ++f) weights(hf, f, pw[f]);
+        }
         // codes of keys (2 i, 2 i + 1), a half word of a unit each
         uint32_t pr[4][UN / 4];
 #pragma unroll
@@ -708,33 +846,43 @@ void k_attend(AttendArgs a) {
         }
 #pragma unroll
         for (int f = 0; f < NG; ++f) {
-          f32x4 st[2], z[2];
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            st[b] = *(const f32x4*)&s_vs[f * 64 + 32 * hf + 16 * b + 4 * j];
-            z[b] = *(const f32x4*)&s_vz[f * 64 + 32 * hf + 16 * b + 4 * j];
-          }
           Op<NP> po[R];
+          if constexpr (SP > 1) {
+            const uint32_t m0 = mine[2 * hf % SP], m1 = mine[(2 * hf + 1) % SP];
 #pragma unroll
-          for (int cb = 0; cb < R; ++cb) {
-            float x[8];
+            for (int pl = 0; pl < NP; ++pl) po[0].p[pl] = make_uint4(pw[f][pl][0] & m0, pw[f][pl][1] & m0, pw[f][pl][0] & m1, pw[f][pl][1] & m1);
+          } else {
+            f32x4 st[2], z[2];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float w = p[2 * hf + (i >> 2)][cb][i & 3];
-              x[i] = w * st[i >> 2][i & 3];
-              corr[cb][f] = __builtin_fmaf(w, z[i >> 2][i & 3], corr[cb][f]);
+            for (int b = 0; b < 2; ++b) {
+              st[b] = *(const f32x4*)&s_vs[f * 64 + 32 * hf + 16 * b + 4 * j];
+              z[b] = *(const f32x4*)&s_vz[f * 64 + 32 * hf + 16 * b + 4 * j];
             }
-            po[cb] = split8<NP>(x);
+#pragma unroll
+            for (int cb = 0; cb < R; ++cb) {
+              float x[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const float w = p[2 * hf + (i >> 2)][cb][i & 3];
+                x[i] = w * st[i >> 2][i & 3];
+                corr[cb][f] = __builtin_fmaf(w, z[i >> 2][i & 3], corr[cb][f]);
+              }
+              po[cb] = split8<NP>(x);
+            }
+          }
+          uint4 c[2];
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const int i = 2 * f + y;
+            c[y] = make_uint4(sixteen_plus(pr[0][i / 4], i & 3, nib_mask, nib_base), sixteen_plus(pr[1][i / 4], i & 3, nib_mask, nib_base),
+                              sixteen_plus(pr[2][i / 4], i & 3, nib_mask, nib_base), sixteen_plus(pr[3][i / 4], i & 3, nib_mask, nib_base));
           }
 #pragma unroll
-          for (int i = 2 * f; i < 2 * f + 2; ++i) {
-            const uint4 x = make_uint4(sixteen_plus(pr[0][i / 4], i & 3, nib_mask, nib_base), sixteen_plus(pr[1][i / 4], i & 3, nib_mask, nib_base),
-                                       sixteen_plus(pr[2][i / 4], i & 3, nib_mask, nib_base), sixteen_plus(pr[3][i / 4], i & 3, nib_mask, nib_base));
+          for (int pl = NP - 1; pl >= 0; --pl)
 #pragma unroll
             for (int cb = 0; cb < R; ++cb)
 #pragma unroll
-              for (int pl = NP - 1; pl >= 0; --pl) o[i][cb] = mfma(x, po[cb].p[pl], o[i][cb]);
-          }
+              for (int y = 0; y < 2; ++y) o[2 * f + y][cb] = mfma(c[y], po[cb].p[pl], o[2 * f + y][cb]);
 #pragma unroll
           for (int cb = 0; cb < R; ++cb) asm volatile("" : "+v"(o[2 * f][cb]), "+v"(o[2 * f + 1][cb]), "+v"(corr[cb][f]));      // (as above)
           __builtin_amdgcn_sched_barrier(0);
@@ -778,20 +926,22 @@ void k_attend(AttendArgs a) {
                         o[i + 3][cb][r] + add[i / 2 + 1]);
   }
   __syncthreads();
-  const int valid = min(16 * R, rows - row0);
+  const int valid = min(16 * R, rows - row0);      // (up to CW with copies)
   for (int it = threadIdx.x; it < valid * (D / 4); it += 256) {
     const int r = it / (D / 4), c = it % (D / 4) * 4;
     float M = -INFINITY;
+    // (sums of four wavefronts, of each copy)
+    auto part = [&](int w) { return SP == 1 ? w * 16 * R + r : w * CW + r; };
 #pragma unroll
-    for (int w = 0; w < 4; ++w) M = fmaxf(M, sm_m[w * 16 * R + r]);
+    for (int w = 0; w < 4 * SP; ++w) M = fmaxf(M, sm_m[part(w)]);
     float L = 0.f;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float m = sm_m[w * 16 * R + r];
+    for (int w = 0; w < 4 * SP; ++w) {
+      const float m = sm_m[part(w)];
       const float f = m == M ? (M == -INFINITY ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - M);
-      const float4 y = *(const float4*)&sm_o[(w * 16 * R + r) * LDO + c];
-      L = __builtin_fmaf(f, sm_l[w * 16 * R + r], L);
+      const float4 y = *(const float4*)&sm_o[part(w) * LDO + c];
+      L = __builtin_fmaf(f, sm_l[part(w)], L);
       // (a wavefront without keys has sums of 0)
       x.x = __builtin_fmaf(f, y.x, x.x);
       x.y = __builtin_fmaf(f, y.y, x.y);
@@ -813,16 +963,15 @@ void k_attend(AttendArgs a) {
   }
 }
 
-template <int FMT, typename T, int D, int NP, int R>
+template <int FMT, typename T, int D, int NP, int R, int SP = 1>
 int run_attend(const AttendArgs& a, hipStream_t st) {
   constexpr size_t join = (8 * 16 * R + (size_t)4 * 16 * R * (D + 4)) * 4, scales = FMT == FMT_Q4 ? 4 * 4 * 64 * (D / 32) * 4 : 0;
   constexpr size_t lds = join > scales ? join : scales;
-  const int64_t blocks = a.row_blocks == 1 ? a.units : (int64_t)(a.units + 7) / 8 * 8 * a.row_blocks;
-  auto kern = k_attend<FMT, T, D, NP, R>;
+  auto kern = k_attend<FMT, T, D, NP, R, SP>;
   if constexpr (lds > 65536) {
     if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) return RESTKV_EHIP;
   }
-  hipLaunchKernelGGL(kern, wide_grid(blocks), dim3(256), lds, st, a);
+  hipLaunchKernelGGL(kern, unit_grid(a), dim3(256), lds, st, a);
   return hip_status();
 }
 

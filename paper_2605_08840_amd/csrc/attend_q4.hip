@@ -7,6 +7,11 @@ int run_attend_q4(const AttendArgs& a, int R, hipStream_t st) {
   auto go = [&](auto d, auto np, auto t) {
     constexpr int D = decltype(d)::value, NP = decltype(np)::value;
     using T = decltype(t);
+    if constexpr (planes_of<T> == 1) {      // (parts of float32 queries, a copy each, are more than the registers hold)
+      const int64_t rows = (int64_t)a.pg.G * a.pg.max_new;
+      if (rows <= 4) return run_attend<FMT_Q4, T, D, NP, 1, 4>(a, st);
+      if (rows <= 8) return run_attend<FMT_Q4, T, D, NP, 1, 2>(a, st);
+    }
     return R == 1 ? run_attend<FMT_Q4, T, D, NP, 1>(a, st) : run_attend<FMT_Q4, T, D, NP, 2>(a, st);
   };
   auto by_d = [&](auto np, auto t) {

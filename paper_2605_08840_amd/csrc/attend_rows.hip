@@ -18,23 +18,20 @@ void k_attend_rows(AttendArgs a) {
   const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  int unit, rb;
-  {
-    const int64_t b = wide_block(), per = (int64_t)a.row_blocks * 8, in = b % per;
-    unit = (int)(b / per * 8 + in % 8);
-    rb = (int)(in / 8);
-  }
+  const int unit = unit_of_block(), rb = blockIdx.x >> 3;
   if (unit >= a.units) return;
   const int hy = unit % a.Hy;
   Chunk ch;
-  if (!find_chunk(a, unit / a.Hy, ch)) return;
+  if (!find_chunk(a, unit / a.Hy, (int*)lds, ch)) return;
+  ch.n = __builtin_amdgcn_readfirstlane(ch.n);
+  ch.first = __builtin_amdgcn_readfirstlane(ch.first);
   const int e = __builtin_amdgcn_readfirstlane(ch.e);
   const int s = a.per_head ? e / pg.Hkv : e, h = a.per_head ? e - s * pg.Hkv : hy;
   const int rows = pg.G * ch.n, block0 = rb * 64 * R, row0 = block0 + wv * 16 * R;
   if (block0 >= rows) return;
   if (a.plan && ch.index == 0 && hy == 0 && rb == 0 && threadIdx.x == 0) a.plan[e] = make_int2(ch.slot0, ch.count);
 
-  const int told = ch.told, len = min(told, pg.max_len);
+  const int told = __builtin_amdgcn_readfirstlane(ch.told), len = min(told, pg.max_len);
   auto limit = [&](int row) {       // positions that a row sees
     return pg.causal ? min(max(told - ch.n + row / pg.G + 1, 0), len) : len;
   };
@@ -211,8 +208,10 @@ void k_attend_rows(AttendArgs a) {
             const int b = 2 * hf + (kk >> 4), r0 = kk & 15;
             if (r0 >= (kk >> 4 ? there(2 * hf + 1) : there(2 * hf))) continue;
             float w[R];
+            uint32_t sees[R];
 #pragma unroll
             for (int cb = 0; cb < R; ++cb) {
+              sees[cb] = k0 + 16 * b + r0 < lim[cb] ? ~0u : 0u;
               w[cb] = p[2 * hf][cb][0];
 #pragma unroll
               for (int x = 1; x < 8; ++x) w[cb] = x == (kk >> 4) * 4 + (kk & 3) ? p[2 * hf + (x >> 2)][cb][x & 3] : w[cb];
@@ -223,13 +222,10 @@ void k_attend_rows(AttendArgs a) {
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
                 const int piece = (4 * j + r) * UN * 2 / 16, in = (4 * j + r) * UN * 2 % 16 + 2 * i;
-                const uint16_t x = *(const uint16_t*)(vt + (16 * b + r0) * ROWB + (piece ^ (r0 & (CH - 1))) * 16 + in);
-                const float v = __uint_as_float((uint32_t)x << 16);
+                const uint32_t x = *(const uint16_t*)(vt + (16 * b + r0) * ROWB + (piece ^ (r0 & (CH - 1))) * 16 + in);
+                const uint32_t odd = (x << 16) & (0u - ((x & 0x7F80u) + 0x80u >> 15));      // 0 where it is finite
 #pragma unroll
-                for (int cb = 0; cb < R; ++cb) {
-                  const float y = o[i][cb][r] + w[cb] * v;
-                  o[i][cb][r] = !(v - v == 0.f) && k0 + 16 * b + r0 < lim[cb] ? y : o[i][cb][r];
-                }
+                for (int cb = 0; cb < R; ++cb) o[i][cb][r] = __builtin_fmaf(w[cb], __uint_as_float(odd & sees[cb]), o[i][cb][r]);
               }
           }
 #pragma unroll
@@ -287,7 +283,7 @@ template <int D, int NP, int R>
 int run_rows(const AttendArgs& a, hipStream_t st) {
   constexpr size_t lds = 2 * 2 * 64 * (size_t)D * 2;
   auto kern = k_attend_rows<D, NP, R>;
-  hipLaunchKernelGGL(kern, wide_grid((int64_t)(a.units + 7) / 8 * 8 * a.row_blocks), dim3(256), lds, st, a);
+  hipLaunchKernelGGL(kern, unit_grid(a), dim3(256), lds, st, a);
   return hip_status();
 }
 
