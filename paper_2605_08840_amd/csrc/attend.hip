@@ -8,53 +8,54 @@ namespace restkv {
 namespace {
 
 // Sums of an entry's chunks joined into its output: a workgroup a row (new token, query head), 256 threads as 1024 / d
-// groups that take every so manyeth chunk, four channels a thread.
+// groups that take every so manyeth chunk, four channels a thread.  A chain of two reads (where the chunks are, what they
+// hold) and a launch: chunks are read four at a time, references with the sums.
 template <int D>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
-  constexpr int TPR = D / 4, NGR = 256 / TPR;
+  constexpr int TPR = D / 4, NGR = 256 / TPR, AHEAD = 4;
   __shared__ float4 sm_x[NGR][TPR];
-  __shared__ float sm_l[NGR], sm_m[4];
+  __shared__ float sm_m[NGR], sm_l[NGR];
   const Pages& pg = a.pg;
-  const int64_t b = wide_block(), per = (int64_t)pg.max_new * pg.Hq;
-  if (b >= per * pg.n_seqs) return;
-  const int s = (int)(b / per), i = (int)(b % per) / pg.Hq, head = (int)(b % per) % pg.Hq, h = head / pg.G;
+  const int i = blockIdx.x / pg.Hq, head = blockIdx.x % pg.Hq, h = head / pg.G, s = blockIdx.y;
+  const int2 pl = a.plan[a.per_head ? s * pg.Hkv + h : s];       // (of a sequence without new tokens: whatever it is, not used)
   const NewRows nr = new_rows(pg, s);
-  if (i >= nr.n) return;
-  const int2 pl = a.plan[a.per_head ? s * pg.Hkv + h : s];
-  if (pl.y < 2) return;
+  if (i >= nr.n || pl.y < 2) return;
   const int hy = a.per_head ? 0 : h, row = i * pg.G + head - h * pg.G, rows = pg.G * pg.max_new;
   const int g = threadIdx.x / TPR, c = threadIdx.x % TPR;
-  auto slot = [&](int k) { return (int64_t)((pl.x + k) * a.Hy + hy) * rows + row; };
-  // references and sums first, a chunk each thread: the factors of the sums then need no second look
   float M = -INFINITY, L = 0.f;
-  for (int k = threadIdx.x; k < pl.y; k += 256) M = fmaxf(M, a.part_m[slot(k)]);
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) M = fmaxf(M, __shfl_xor(M, d));
-  if ((threadIdx.x & 63) == 0) sm_m[threadIdx.x >> 6] = M;
-  __syncthreads();
-  M = fmaxf(fmaxf(sm_m[0], sm_m[1]), fmaxf(sm_m[2], sm_m[3]));
-  // (a chunk of which the row sees nothing has a reference of -inf and sums of 0)
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int k = g; k < pl.y; k += NGR) {
-    const float m = a.part_m[slot(k)], l = a.part_l[slot(k)];
-    const float4 y = *(const float4*)&a.part_o[slot(k) * D + c * 4];
-    const float f = m == M ? 1.f : __builtin_amdgcn_exp2f(m - M);
-    L = __builtin_fmaf(f, l, L);
-    x.x = __builtin_fmaf(f, y.x, x.x); x.y = __builtin_fmaf(f, y.y, x.y); x.z = __builtin_fmaf(f, y.z, x.z); x.w = __builtin_fmaf(f, y.w, x.w);
+  auto take = [&](float m, float l, float4 y) {
+    // (a chunk of which the row sees nothing has a reference of -inf and sums of 0)
+    const float n = fmaxf(M, m);
+    const float fo = M == n ? 1.f : __builtin_amdgcn_exp2f(M - n), fn = m == n ? 1.f : __builtin_amdgcn_exp2f(m - n);
+    M = n;
+    L = L * fo + l * fn;
+    x.x = x.x * fo + y.x * fn; x.y = x.y * fo + y.y * fn; x.z = x.z * fo + y.z * fn; x.w = x.w * fo + y.w * fn;
+  };
+  for (int k = g; k < pl.y; k += NGR * AHEAD) {
+    float m[AHEAD], l[AHEAD];
+    float4 y[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int kk = min(k + u * NGR, pl.y - 1);
+      const int64_t at = (int64_t)((pl.x + kk) * a.Hy + hy) * rows + row;
+      m[u] = a.part_m[at];
+      l[u] = a.part_l[at];
+      y[u] = *(const float4*)&a.part_o[at * D + c * 4];
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (k + u * NGR < pl.y) take(m[u], l[u], y[u]);
   }
   sm_x[g][c] = x;
-  if (c == 0) sm_l[g] = L;
+  if (c == 0) {
+    sm_m[g] = M;
+    sm_l[g] = L;
+  }
   __syncthreads();
   if (g) return;
-  L = 0.f;
-  x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-  for (int k = 0; k < NGR; ++k) {
-    const float4 y = sm_x[k][c];
-    L += sm_l[k];
-    x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
-  }
+  for (int k = 1; k < NGR; ++k) take(sm_m[k], sm_l[k], sm_x[k][c]);
   store_out(a, nr.first + i, head, c * 4, x, M, L);
 }
 
@@ -105,7 +106,8 @@ int launch_attend(const Pages& pg, const void* q, const void* k_pages, const voi
                   const void* v_scale, void* out, float* lse, char* ws, hipStream_t st) {
   const AttendPlan p = attend_plan(pg);
   const AttendWs lay = attend_ws(pg, p);
-  if (p.chunks * p.Hy > (int64_t)1 << 30 || p.row_blocks > (1 << 20)) return RESTKV_EUNSUPPORTED;
+  if (p.chunks * p.Hy > (int64_t)1 << 30 || p.row_blocks > (1 << 20) || (p.slots && (int64_t)pg.max_new * pg.Hq >= (1 << 24)))
+    return RESTKV_EUNSUPPORTED;
   AttendArgs a = {};
   a.pg = pg;
   a.q = q; a.k = (const char*)k_pages; a.v = (const char*)v_pages;
@@ -124,7 +126,7 @@ int launch_attend(const Pages& pg, const void* q, const void* k_pages, const voi
   a.vec_out = !((uintptr_t)out & oal) && !((pg.o_st | pg.o_sh) & 3);
   const int rc = p.many ? run_attend_rows(a, p.R, st) : pg.fmt == RESTKV_F32 ? run_attend_f32(a, p.R, st) : pg.fmt == RESTKV_BF16 ? run_attend_bf16(a, p.R, st) : run_attend_q4(a, p.R, st);
   if (rc || !p.slots) return rc;
-  const dim3 grid = wide_grid((int64_t)pg.n_seqs * pg.max_new * pg.Hq);
+  const dim3 grid(pg.max_new * pg.Hq, pg.n_seqs);
   if (pg.d == 128) hipLaunchKernelGGL(k_attend_join<128>, grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL(k_attend_join<64>, grid, dim3(256), 0, st, a);
   return hip_status();

@@ -84,9 +84,15 @@ __device__ __forceinline__ bool find_chunk(const AttendArgs& a, int x, int* lds,
   const int lane = threadIdx.x & 63;
   if (a.entries <= 64) {
     const Entry en = read_entry(a, lane);
-    const int C = chunk_tiles(a, (float)wave_sum((uint32_t)en.tiles), __popcll(__ballot(en.tiles > 0)));
-    const int cnt = lane < a.entries ? max(1, (en.tiles + C - 1) / C) : 0, own = cnt > 1 ? cnt : 0;
-    const int inc = wave_scan(cnt), sl = wave_scan(own);
+    int C = chunk_tiles(a, (float)wave_sum((uint32_t)en.tiles), __popcll(__ballot(en.tiles > 0)));
+    int cnt = 0, inc = 0;
+    for (int i = 0; i < 8; ++i) {       // (until they are as many as wanted: a few too many cost a sixth of the time of 24 lengths)
+      cnt = lane < a.entries ? max(1, (en.tiles + C - 1) / C) : 0;
+      inc = wave_scan(cnt);
+      if (__builtin_amdgcn_readlane(inc, 63) <= a.chunks || a.entries >= a.chunks) break;
+      C += C / 16 + 1;
+    }
+    const int own = cnt > 1 ? cnt : 0, sl = wave_scan(own);
     const unsigned long long hit = __ballot(inc > x);
     if (!hit) return false;
     const int l = __builtin_ctzll(hit);

@@ -191,6 +191,35 @@ ATTENDS = [
 ]
 
 
+ATTENDS += [
+    # 1 to 16 rows: copies of the rows that divide the keys (4 bits), with and without a tile cut short
+    ([64, 129, 200], [1, 1, 1], dict(hq=3, hkv=3, d=128)),                    # 1 row
+    ([64, 127, 333], [1, 1, 1], dict(hq=10, hkv=2, d=128, ps=32)),            # 5 rows
+    ([70, 128, 385], [2, 1, 2], dict(hq=8, hkv=2, d=128)),                    # 8
+    ([70, 128, 385], [3, 1, 2], dict(hq=6, hkv=2, d=64)),                     # 9
+    ([100, 17], [2, 2], dict(hq=16, hkv=2, d=128, causal=False)),             # 16
+    # rows of a window: one and two blocks of a wavefront, several workgroups, some without rows
+    ([300, 65], [11, 3], dict(hq=6, hkv=2, d=128, ps=64)),                    # 33 rows
+    ([700, 90], [16, 16], dict(hq=8, hkv=2, d=128, ps=32, token_major=True)),  # 64
+    ([129, 400, 33], [33, 20, 33], dict(hq=4, hkv=2, d=128)),                 # 66
+    ([260, 1000], [70, 65], dict(hq=8, hkv=2, d=64, ps=64)),                  # 280
+    ([[30, 400], [500, 3]], [24, 2], dict(hq=12, hkv=2, d=128, head_lens=True)),
+    ([200, 190], [40, 40], dict(hq=2, hkv=2, d=128, causal=False)),
+]
+
+
+def test_attention_of_many_sequences_and_heads():
+    """More entries than a workgroup has threads, lengths of 0 to 2000 among them."""
+    for head_lens in (True, False):
+        n = 150 if head_lens else 300
+        g = torch.Generator().manual_seed(7)
+        lens = torch.randint(0, 9, (n, 2), generator=g)
+        lens[torch.randint(0, n, (6,), generator=g), 0] = torch.tensor([2000, 700, 130, 65, 64, 1])
+        lens = lens.tolist() if head_lens else lens[:, 0].tolist()
+        p = Plain(rk, lens=lens, new=[(s % 5 > 0) * 1 for s in range(n)], hq=2, hkv=2, head_lens=head_lens, out_dtype="f32")
+        check_attend(p, p.normal(p.tokens, 2, 64).bfloat16(), torch.float32)
+
+
 def run_attend(p, q, out_type, lse=True, **more):
     out = torch.full((p.tokens, p.hq, p.d), 5.0, dtype=out_type, device="cuda")
     l = torch.full((p.tokens, p.hq), 5.0, dtype=torch.float32, device="cuda") if lse else None
@@ -334,7 +363,7 @@ def test_long_cache_many_chunks(dtype, fmt):
     f = rk.make_cache(n_seqs=1, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, page_size=ps, n_pages=pages, max_pages=pages,
                       dtype="f32" if fmt else dtype, format=fmt)
     rk.restkv_fetch(f, pool, table, lens, ko, vo)
-    for new in (1, 5):
+    for new in (1, 2, 5, 20, 64):
         c = rk.make_cache(n_seqs=1, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, page_size=ps, n_pages=pages, max_pages=pages,
                           dtype=dtype, format=fmt, max_new=new, out_dtype="f32")
         q = torch.randn((new, hq, d), generator=g, device="cuda").to(vt)
@@ -483,6 +512,21 @@ def test_decode_step_replayed_from_a_hip_graph(fmt):
         assert torch.equal(sides[0][2], sides[1][2]) and torch.equal(sides[0][3], sides[1][3]) and torch.equal(sides[0][4], sides[1][4])
         assert torch.equal(sides[0][1].v.view(torch.uint8), sides[1][1].v.view(torch.uint8))
     assert sides[0][2].tolist() == [606, 9]
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each: the results of the calls one after the other."""
+    p = Plain(rk, lens=[1500, 700], new=[2, 1], d=128, hq=8, hkv=2)
+    q = p.normal(p.tokens, 8, 128).bfloat16().cuda()
+    streams, outs, ws = [torch.cuda.Stream() for _ in range(2)], [torch.empty_like(q) for _ in range(3)], [rk.alloc_attend_workspace(p.c) for _ in range(2)]
+    t = p.tensors
+    rk.restkv_attend(p.c, q, p.pages, t["table"], t["lens"], outs[2], None, ws[0], new_start=t["new_start"])
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            rk.restkv_attend(p.c, q, p.pages, t["table"], t["lens"], outs[i], None, ws[i], new_start=t["new_start"], stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[2])
 
 
 def test_calls_on_another_stream():
