@@ -110,25 +110,15 @@ template <int UN>
 __device__ __forceinline__ uint32_t unit_codes(const float (&x)[UN], int u, uint32_t (&scale)[UN / 2]) {
 #pragma clang fp contract(off)
   constexpr int NG = UN / 2;
-  float low = 0.f, high = 0.f;
-  bool nan = false;
+  int low = 0, high = 0;
 #pragma unroll
   for (int f = 0; f < NG; ++f) {
-    const float a = x[2 * f], b = x[2 * f + 1];
-    const float lo = row16_min(fminf(a, b)), hi = row16_max(fmaxf(a, b));
-    nan = nan || !(a == a && b == b);
+    const int a = order_of(x[2 * f]), b = order_of(x[2 * f + 1]);
+    const int lo = row16_min(min(a, b)), hi = row16_max(max(a, b));
     if (f == (u & (NG - 1))) { low = lo; high = hi; }
   }
-  bool fine = true;                  // (infinities are seen by the extremes)
-  if (__ballot(nan)) {
-#pragma unroll
-    for (int f = 0; f < NG; ++f) {
-      const float off = row16_max(x[2 * f] == x[2 * f] && x[2 * f + 1] == x[2 * f + 1] ? 0.f : 1.f);
-      if (f == (u & (NG - 1))) fine = off == 0.f;
-    }
-  }
   float step, zero, inverse;
-  group_scale(low, high, fine, step, zero, inverse);
+  group_scale(of_order(low), of_order(high), step, zero, inverse);
   const uint32_t packed = __float_as_uint(step) >> 16 | (__float_as_uint(zero) & 0xFFFF0000u);
   auto codes = [&](auto rare) {
     uint32_t code = 0u;
@@ -214,7 +204,8 @@ __global__ __launch_bounds__(256) void k_append(Pages pg, const T* k, const T* v
     if (pos < 0 || pos >= pg.n_pos) return;        // (the whole token)
     if (turns) turn = angles<UN>(pg, c0, cos, sin, pos);
   }
-  int64_t slot[U];                                 // -1: nowhere
+  uint32_t slot[U];                                // where there is room
+  bool room[U];
   if (!pg.lens_sh && !pg.table_sh) {
     const int at = max(uniform_load(lens), 0) - nr.n + i;
     const bool in = at >= 0 && at < pg.max_len;
@@ -222,7 +213,8 @@ __global__ __launch_bounds__(256) void k_append(Pages pg, const T* k, const T* v
 #pragma unroll
     for (int c = 0; c < U; ++c) {
       const int h = r[c] >= pg.Hkv ? r[c] - pg.Hkv : r[c];
-      slot[c] = page >= 0 && page < pg.n_pages ? row_of(pg, page, h, at) : -1;
+      room[c] = page >= 0 && page < pg.n_pages;
+      slot[c] = row_of(pg, page, h, at);
     }
   } else {
     int at[U];
@@ -235,7 +227,8 @@ __global__ __launch_bounds__(256) void k_append(Pages pg, const T* k, const T* v
     for (int c = 0; c < U; ++c) {
       const int h = min(r[c] >= pg.Hkv ? r[c] - pg.Hkv : r[c], pg.Hkv - 1);
       const int page = at[c] >= 0 && at[c] < pg.max_len ? page_of(pg, s, h, at[c]) : -1;
-      slot[c] = page >= 0 ? row_of(pg, page, h, at[c]) : -1;
+      room[c] = page >= 0;
+      slot[c] = row_of(pg, page, h, at[c]);
     }
   }
 #pragma unroll
@@ -251,19 +244,19 @@ __global__ __launch_bounds__(256) void k_append(Pages pg, const T* k, const T* v
       if (r[c] < n_rows) store_unit<T, UN, VEC>(q_out + t * pg.q_st + (r[c] - 2 * pg.Hkv) * pg.q_sh + c0, x[c]);
       continue;
     }
-    if (slot[c] < 0) continue;
+    if (!room[c]) continue;
     char* dst = is_v ? v_pages : k_pages;
     if constexpr (!Q4) {
-      store_unit<T, UN, true>((T*)dst + slot[c] * D + c0, x[c]);
+      store_unit<T, UN, true>((T*)dst + (int64_t)slot[c] * D + c0, x[c]);
     } else {
       uint32_t scale[NG];
       const uint32_t code = unit_codes<UN>(x[c], u, scale);
-      uint32_t* sc = (is_v ? v_scale : k_scale) + slot[c] * NG;
+      uint32_t* sc = (is_v ? v_scale : k_scale) + (int64_t)slot[c] * NG;
       if constexpr (UN == 8) {
-        *(uint32_t*)(dst + slot[c] * (D / 2) + u * 4) = code;
+        *(uint32_t*)(dst + (int64_t)slot[c] * (D / 2) + u * 4) = code;
         if (u == 0) *(uint4*)sc = make_uint4(scale[0], scale[1], scale[2], scale[3]);
       } else {
-        *(uint16_t*)(dst + slot[c] * (D / 2) + u * 2) = (uint16_t)code;
+        *(uint16_t*)(dst + (int64_t)slot[c] * (D / 2) + u * 2) = (uint16_t)code;
         if (u == 0) *(uint2*)sc = make_uint2(scale[0], scale[1]);
       }
     }

@@ -31,7 +31,7 @@ __global__ __launch_bounds__(256) void k_fetch(Pages pg, const char* k_pages, co
     const int j = min(j0 + 16 * c, n_rows - 1), t = idx ? idx[e * n_rows + j] : first + j;
     int page = -1;
     if (t >= 0 && t < len) page = page_of(pg, s, h, t);
-    slot[c] = page >= 0 ? row_of(pg, page, h, t) : -1;
+    slot[c] = page >= 0 ? (int64_t)row_of(pg, page, h, t) : -1;
   }
   uint32_t w[U][N], sc[U][Q4 ? NG : 1];
 #pragma unroll

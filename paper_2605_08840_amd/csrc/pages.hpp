@@ -56,8 +56,9 @@ __device__ __forceinline__ int page_of(const Pages& pg, int s, int h, int t) {
   const int p = pg.table[s * pg.table_ss + h * pg.table_sh + (t >> pg.lg_ps)];
   return p >= 0 && p < pg.n_pages ? p : -1;
 }
-__device__ __forceinline__ int64_t row_of(const Pages& pg, int page, int h, int t) {
-  return page * pg.page_s + h * pg.head_s + (t & ((1 << pg.lg_ps) - 1)) * pg.tok_s;
+// Row of that position (rows of an array are counted in 32 bits: resolve_cache).
+__device__ __forceinline__ uint32_t row_of(const Pages& pg, int page, int h, int t) {
+  return (uint32_t)page * (uint32_t)pg.page_s + (uint32_t)h * (uint32_t)pg.head_s + (t & ((1 << pg.lg_ps) - 1)) * (uint32_t)pg.tok_s;
 }
 
 // ---- 4-bit rows ---------------------------------------------------------------
@@ -70,24 +71,36 @@ __device__ __forceinline__ float bf16_below(float x) {       // largest bfloat16
   return __uint_as_float((u >> 31) && u != cut ? cut + 0x10000u : cut);
 }
 
-// Sixteen lanes of a wavefront's row: min / max over them, in every lane (of a NaN nothing is said).
-__device__ __forceinline__ float row16_min(float x) {
-#define RK_STEP(ctrl) x = fminf(x, __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), ctrl, 0xF, 0xF, true)))
+// Floats as integers of the same order, and back (a NaN lies beyond the infinities): least and greatest of integers take a
+// lane shift in the same instruction, those of floats do not.
+__device__ __forceinline__ int order_of(float x) {
+  const int b = __float_as_int(x);
+  return b ^ ((b >> 31) & 0x7FFFFFFF);
+}
+__device__ __forceinline__ float of_order(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7FFFFFFF)); }
+// Least and greatest over the sixteen lanes of a wavefront's row, in every lane.
+__device__ __forceinline__ int row16_min(int x) {
+#define RK_STEP(ctrl) x = min(x, (int)__builtin_amdgcn_mov_dpp(x, ctrl, 0xF, 0xF, true))
+  RK_STEP(0x121); RK_STEP(0x122); RK_STEP(0x124); RK_STEP(0x128);
+  return x;
+}
+__device__ __forceinline__ int row16_max(int x) {
+#undef RK_STEP
+#define RK_STEP(ctrl) x = max(x, (int)__builtin_amdgcn_mov_dpp(x, ctrl, 0xF, 0xF, true))
   RK_STEP(0x121); RK_STEP(0x122); RK_STEP(0x124); RK_STEP(0x128);
 #undef RK_STEP
   return x;
 }
-__device__ __forceinline__ float row16_max(float x) { return -row16_min(-x); }
 
-// Step and zero of a group from its extremes (fine: every value of it is finite); inverse: 1/step, or 0.
-__device__ __forceinline__ void group_scale(float low, float high, bool fine, float& step, float& zero, float& inverse) {
+// Step and zero of a group from its extremes; inverse: 1/step, or 0.
+__device__ __forceinline__ void group_scale(float low, float high, float& step, float& zero, float& inverse) {
 #pragma clang fp contract(off)
   zero = bf16_below(low);
   const float spread = high - zero;
   step = -bf16_below(-(spread / 15.0f));
   step = spread > 0.f ? fmaxf(step, 0x1p-100f) : 0.f;
-  fine = fine && __builtin_isfinite(step) && __builtin_isfinite(zero);
-  if (!fine) { step = 0.f; zero = __builtin_nanf(""); }
+  // (a group with a NaN or an infinity has it for an extreme)
+  if (!(__builtin_isfinite(spread) && __builtin_isfinite(step) && __builtin_isfinite(zero))) { step = 0.f; zero = __builtin_nanf(""); }
   inverse = step > 0.f ? 1.0f / step : 0.f;
 }
 

@@ -35,9 +35,9 @@ int resolve_cache(const restkv_cache* c, Pages* o) {
     o->tok_s = 1; o->head_s = c->page_size; o->page_s = (int64_t)c->page_size * o->Hkv;
   }
   if (o->page_s < 1 || o->head_s < 0 || o->tok_s < 1) return RESTKV_EINVAL;
-  // (the kernels count rows of an array in 32 bits)
-  if ((int64_t)(c->n_pages - 1) > ((int64_t)1 << 31) / o->page_s || (int64_t)c->page_size * o->tok_s > (int64_t)1 << 31) return RESTKV_EUNSUPPORTED;
-  if (o->tok_s > 65536 || o->page_s > (int64_t)1 << 40 || o->head_s > (int64_t)1 << 40) return RESTKV_EUNSUPPORTED;
+  if (o->tok_s > 65536 || o->page_s > (int64_t)1 << 31 || o->head_s > (int64_t)1 << 31) return RESTKV_EUNSUPPORTED;
+  // the kernels count rows of an array in 32 bits
+  if ((o->n_pages - 1) * o->page_s + (o->Hkv - 1) * o->head_s + (c->page_size - 1) * o->tok_s >= (int64_t)0xFFFFFFFF) return RESTKV_EUNSUPPORTED;
   o->table_ss = c->table_stride_s; o->table_sh = c->table_stride_h;
   if (!o->table_ss && !o->table_sh) o->table_ss = c->max_pages;
   o->lens_ss = c->lens_stride_s; o->lens_sh = c->lens_stride_h;
