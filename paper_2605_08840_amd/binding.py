@@ -430,7 +430,10 @@ class _Told:
         self.kv_stride, self.q_stride, self.out_stride, self.lse_stride = (
             (c.kv_stride_t, c.kv_stride_h, 1), (c.q_stride_t, c.q_stride_h, 1), (c.out_stride_t, c.out_stride_h, 1),
             (c.lse_stride_t, c.lse_stride_h))
-        self.n_table, self.n_lens, self.n_new = c.n_seqs * c.table_stride_s, c.n_seqs * c.lens_stride_s, c.n_seqs + 1
+        # entries from the first to the last that is read (strides 0, 0: the library's own)
+        span = lambda s, h, n, default: ((c.n_seqs - 1) * (s if s or h else default) + (c.n_kv_heads - 1) * h + n) * (c.n_seqs > 0)  # noqa: E731
+        self.n_table = span(c.table_stride_s, c.table_stride_h, c.max_pages, c.max_pages)
+        self.n_lens, self.n_new = span(c.lens_stride_s, c.lens_stride_h, 1, 1), c.n_seqs + 1
         self.n_tokens, self.n_turns = c.n_tokens, c.n_positions * (c.rotary_dim // 2)
         self.pages = None                    # the last layout of pages that was found to be the described one
 
@@ -448,8 +451,10 @@ def _check_pages(what: str, c: RestkvCache, told: _Told, pages: CachePages) -> i
     if rows == told.pages:
         return rows[4]
     shape, strides, dtype, d, dev = rows
-    heads = 1 if c.table_stride_h else c.n_kv_heads
     page, head, pos = c.page_stride, c.head_stride, c.token_stride
+    if not pos:
+        page, head, pos = c.page_size * c.n_kv_heads, c.page_size, 1
+    heads = 1 if c.table_stride_h and not head else c.n_kv_heads
     # (a stride along one entry says nothing)
     as_told = [(shape[0] >= c.n_pages and a == heads and b == c.page_size and (strides[0] == page or c.n_pages == 1) and
                 (sa == head or a == 1) and sb == pos)

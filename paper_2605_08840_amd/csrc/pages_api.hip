@@ -9,7 +9,7 @@ int resolve_cache(const restkv_cache* c, Pages* o) {
   if (!c || !o) return RESTKV_EINVAL;
   if (c->n_seqs < 0 || c->n_tokens < 0 || c->max_new < 1 || c->n_pages < 1 || c->max_pages < 1 || c->max_len < 0) return RESTKV_EINVAL;
   if (c->n_q_heads <= 0 || c->n_kv_heads <= 0 || c->n_q_heads % c->n_kv_heads) return RESTKV_EINVAL;
-  if (!(c->scale >= 0.f) || isinf(c->scale)) return RESTKV_EINVAL;
+  if (!(c->scale >= 0.f) || isinf(c->scale * 1.44269504f)) return RESTKV_EINVAL;       // (the kernels take powers of 2)
   if (c->head_dim != 64 && c->head_dim != 128) return RESTKV_EUNSUPPORTED;
   if (c->dtype != RESTKV_F32 && c->dtype != RESTKV_BF16) return RESTKV_EUNSUPPORTED;
   if (c->format != c->dtype && c->format != RESTKV_Q4) return RESTKV_EUNSUPPORTED;
@@ -81,13 +81,12 @@ int restkv_append(const restkv_cache* c, const void* k, const void* v, void* k_p
                   restkv_stream_t stream) {
   Pages pg;
   int rc = resolve_cache(c, &pg);
-  if (!rc) rc = take_arrays(&pg, k_pages, v_pages, k_scale, v_scale, table, lens);
   if (!rc) rc = take_new(&pg, new_start);
-  if (rc) return rc;
+  if (!rc && pg.n_seqs && pg.n_tokens) rc = take_arrays(&pg, k_pages, v_pages, k_scale, v_scale, table, lens);
+  if (rc || !pg.n_seqs || !pg.n_tokens) return rc;
   if (!k || !v || (q && !q_out) || (!q && q_out)) return RESTKV_EINVAL;
   if (pg.rot && (!cos || !sin || pg.n_pos < 1)) return RESTKV_EINVAL;
   if (pg.rot && !positions && pg.lens_sh) return RESTKV_EINVAL;
-  if (!pg.n_seqs || !pg.n_tokens) return RESTKV_OK;
   return launch_append(pg, k, v, k_pages, v_pages, k_scale, v_scale, positions, cos, sin, q, q_out, (hipStream_t)stream);
 }
 
@@ -102,11 +101,10 @@ int restkv_attend(const restkv_cache* c, const void* q, const void* k_pages, con
                   float* lse, void* workspace, size_t workspace_bytes, restkv_stream_t stream) {
   Pages pg;
   int rc = resolve_cache(c, &pg);
-  if (!rc) rc = take_arrays(&pg, k_pages, v_pages, k_scale, v_scale, table, lens);
   if (!rc) rc = take_new(&pg, new_start);
-  if (rc) return rc;
+  if (!rc && pg.n_seqs && pg.n_tokens) rc = take_arrays(&pg, k_pages, v_pages, k_scale, v_scale, table, lens);
+  if (rc || !pg.n_seqs || !pg.n_tokens) return rc;
   if (!q || !out) return RESTKV_EINVAL;
-  if (!pg.n_seqs || !pg.n_tokens) return RESTKV_OK;
   const size_t need = attend_ws_bytes(pg);
   if (need && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need)) return RESTKV_EWORKSPACE;
   return launch_attend(pg, q, k_pages, v_pages, k_scale, v_scale, out, lse, (char*)workspace, (hipStream_t)stream);
@@ -117,11 +115,13 @@ int restkv_fetch(const restkv_cache* c, const void* k_pages, const void* v_pages
                  void* v_out, restkv_stream_t stream) {
   Pages pg;
   int rc = resolve_cache(c, &pg);
-  if (!rc) rc = take_arrays(&pg, k_pages, v_pages, k_scale, v_scale, table, lens);
   if (rc) return rc;
-  if (!k_out || !v_out || (((uintptr_t)k_out | (uintptr_t)v_out) & 15u) || first < 0 || n_rows < 0) return RESTKV_EINVAL;
+  if (first < 0 || n_rows < 0) return RESTKV_EINVAL;
   if (n_rows > 1 << 30 || first > 1 << 30) return RESTKV_EUNSUPPORTED;
   if (!pg.n_seqs || !n_rows) return RESTKV_OK;
+  rc = take_arrays(&pg, k_pages, v_pages, k_scale, v_scale, table, lens);
+  if (rc) return rc;
+  if (!k_out || !v_out || (((uintptr_t)k_out | (uintptr_t)v_out) & 15u)) return RESTKV_EINVAL;
   return launch_fetch(pg, k_pages, v_pages, k_scale, v_scale, idx, first, n_rows, k_out, v_out, (hipStream_t)stream);
 }
 

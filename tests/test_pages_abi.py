@@ -142,3 +142,46 @@ def test_binding_refuses_tensors_that_are_not_what_they_are_said_to_be(rk):
                 (pages.k[..., ::2], pages.v[..., ::2]), (k, k, s.transpose(3, 4), s)):
         with pytest.raises(rk.RestkvError):
             rk.CachePages(*bad)
+
+
+def test_an_empty_call_needs_no_arrays(rk):
+    """No sequence, no token or no row: tensors without an element have no address."""
+    none = dict(kp=None, vp=None, ks=None, vs=None, table=None, lens=None)
+    for c in (good(rk, n_seqs=0), good(rk, n_seqs=0, n_tokens=0, format="q4"), good(rk, n_seqs=0, rotary_dim=64)):
+        assert append(rk, c, k=None, v=None, **none) == 0
+        assert attend(rk, c, ws=None, ws_n=0, q=None, out=None, **none) == 0
+        assert fetch(rk, c, k_out=None, v_out=None, **none) == 0
+    c = good(rk, n_tokens=0)
+    assert append(rk, c, k=None, v=None, new_start=ONE) == 0 and attend(rk, c, ws=None, ws_n=0, q=None, out=None, new_start=ONE) == 0
+    assert fetch(rk, good(rk), n=0, k_out=None, v_out=None) == 0
+    assert fetch(rk, good(rk, n_seqs=0), n=-1) == -1 and append(rk, good(rk, n_seqs=0, head_dim=96)) == -2
+
+
+def test_scales_whose_logits_pass_float32_are_refused(rk):
+    assert attend(rk, good(rk, scale=3e38)) == -1
+
+
+def test_binding_asks_for_all_entries_that_are_read(rk):
+    told = rk.binding._Told
+    assert told(good(rk)).n_table == 3 * 6 and told(good(rk)).n_lens == 3
+    assert told(good(rk, head_tables=True, head_lens=True)).n_table == 3 * 2 * 6
+    assert told(good(rk, head_tables=True, head_lens=True)).n_lens == 3 * 2
+    assert told(good(rk, _table_stride_s=0, _lens_stride_s=0)).n_table == 3 * 6                     # the library's defaults
+    assert told(good(rk, _table_stride_s=0, _lens_stride_s=0)).n_lens == 3
+    assert told(good(rk, _table_stride_s=1)).n_table == 2 + 6                                       # rows that overlap
+    assert told(good(rk, _table_stride_s=6, _table_stride_h=18)).n_table == 12 + 18 + 6              # heads outermost
+    assert told(good(rk, _lens_stride_s=1, _lens_stride_h=3)).n_lens == 2 + 3 + 1
+    assert told(good(rk, n_seqs=0)).n_table == 0 and told(good(rk, n_seqs=0)).n_lens == 0
+
+
+def test_binding_knows_pages_by_their_head_stride(rk):
+    x, table, lens = torch.zeros(3, 2, 64, dtype=torch.bfloat16), torch.zeros(3, 2, 6, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    one, both = (rk.alloc_cache_pages(good(rk, head_tables=h), device="cpu") for h in (True, False))
+    # tables per head over pages of one head that are said to be a head apart: rows behind the array
+    apart = good(rk, head_tables=True, page_strides=(64, 32, 1))
+    with pytest.raises(rk.RestkvError, match="are not the described ones"):
+        rk.restkv_append(apart, x, x, one, table, lens)
+    for c, pages in ((apart, both), (good(rk, head_tables=True), one),
+                     (good(rk, _page_stride=0, _head_stride=0, _token_stride=0), both)):
+        with pytest.raises(rk.RestkvError, match="not on a GPU"):
+            rk.restkv_append(c, x, x, pages, table, lens)
