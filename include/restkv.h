@@ -293,6 +293,10 @@ int restkv_evict(const restkv_params* p, const void* q, const void* k, const voi
  * [0, n_tokens] or falling, counts as brought inside; a sequence takes part with its first max_new new tokens at most; a
  * position without a page (its table entry outside [0, n_pages)) is neither written nor seen.  Table entries behind
  * the last position in use are not read as pages.  Two positions of one call must not share a slot.
+ *
+ * Limits beside those at the fields: an array of pages has fewer than 2^32 - 1 rows from its first to its last; values are of
+ * magnitude 2^80 at most (sums are not divided before the end, so larger ones may pass float32).  A call without
+ * a sequence, a token or a row does nothing and looks at no array.
  */
 #define RESTKV_Q4 4   /* restkv_cache.format: 4-bit codes with a step and a zero for every 32 channels */
 
@@ -314,7 +318,7 @@ typedef struct restkv_cache {
   int32_t rotary_pairs;  /* 0: channel c turns with c + rotary_dim/2; 1: channel 2c with 2c + 1  */
   int32_t n_positions;   /* rows of the tables of cosines and sines                              */
   int32_t out_dtype;     /* attention output: dtype, or RESTKV_F32                               */
-  float   scale;         /* logit scale; 0 selects 1/sqrt(d)                                     */
+  float   scale;         /* logit scale, below 2^127; 0 selects 1/sqrt(d)                        */
   int64_t page_stride, head_stride, token_stride;   /* rows; token_stride 0: [page][Hkv][page_size];
                             with tables per head head_stride may be 0.  token_stride <= 2^16     */
   int64_t table_stride_s, table_stride_h;   /* int32 entries; 0, 0: max_pages, 0 (heads share)   */
@@ -352,7 +356,8 @@ int restkv_append(const restkv_cache* c, const void* k, const void* v, void* k_p
  * lse_stride_h = W and lse_stride_t = 1 one sequence's W queries give what restkv_score_from_attention takes.
  * Logits, statistics and sums are float32 (bf16 products are exact in it); softmax weights enter the products with
  * values to 2^-17, with float32 output to 2^-24.  Results do not depend on timing: no atomics.
- * Workspace: restkv_attend_workspace_bytes(c), as for the other calls; not needed (0 bytes) where that returns 0.
+ * Workspace: restkv_attend_workspace_bytes(c), 256-byte aligned, whatever it holds; none where that returns 0.  Calls, or
+ * replays of captured ones, that run at the same time need one each.
  */
 size_t restkv_attend_workspace_bytes(const restkv_cache* c);
 int restkv_attend(const restkv_cache* c, const void* q, const void* k_pages, const void* v_pages, const void* k_scale,

@@ -291,14 +291,14 @@ const char* restkv_strerror(int code) {
   switch (code) {
     case RESTKV_OK: return "ok";
     case RESTKV_EINVAL: return "invalid argument (null pointer, inconsistent shape or budget outside (W, L])";
-    case RESTKV_EUNSUPPORTED: return "unsupported configuration (head_dim must be 64 or 128; dtype f32 or bf16)";
-    case RESTKV_EWORKSPACE: return "workspace missing, not 256-byte aligned or smaller than restkv_workspace_bytes() (restkv_select_static: the problem needs more than the library's static scratch)";
+    case RESTKV_EUNSUPPORTED: return "unsupported configuration (head_dim must be 64 or 128; dtype f32 or bf16; pages: a power of two of 16 .. 65536 positions, and the limits of restkv_cache)";
+    case RESTKV_EWORKSPACE: return "workspace missing, not 256-byte aligned or smaller than restkv_workspace_bytes() or restkv_attend_workspace_bytes() (restkv_select_static: the problem needs more than the library's static scratch)";
     case RESTKV_EHIP: return "HIP runtime error at kernel launch";
     default: return "unknown error code";
   }
 }
 
-int restkv_version(void) { return 100; }
+int restkv_version(void) { return 200; }
 
 int restkv_debug_force_fp32(int on) {
   g_force_fp32 = on != 0;

@@ -570,3 +570,62 @@ def test_binding_refuses_wrong_tensors_on_the_gpu():
     refused(rk.restkv_fetch, p.c, p.pages, t["table"], t["lens"], ko, ko[:, :, :4])
     refused(rk.restkv_fetch, p.c, p.pages, t["table"], t["lens"], ko.float(), ko.float())
     refused(rk.restkv_fetch, p.c, p.pages, t["table"], t["lens"], ko, ko.clone(), idx=t["lens"])
+
+
+@pytest.mark.parametrize("dtype,fmt,new", [("bf16", None, 5), ("bf16", None, 20), ("bf16", "q4", 1), ("bf16", "q4", 6), ("f32", None, 5)])
+def test_attention_of_more_rows_replayed_from_a_hip_graph(dtype, fmt, new):
+    """20, 80, 4 and 24 rows: the kernels of several row blocks and of many rows, captured, with lengths that change."""
+    lens = [[2000, 77], [40, 2047], [1, 900]]
+    p = Plain(rk, lens=[2048, 2048], new=[new, new], dtype=dtype, fmt=fmt, d=128, hq=8, hkv=2, ps=64)
+    t, q = p.tensors, p.normal(2 * new, 8, 128).to(p.type).cuda()
+    ws, told = rk.alloc_attend_workspace(p.c), torch.tensor([2048, 2048], dtype=torch.int32, device="cuda")
+    assert ws is not None
+    outs, lses = [torch.empty_like(q) for _ in range(2)], [torch.empty(q.shape[:2], device="cuda") for _ in range(2)]
+
+    def step(i):
+        rk.restkv_attend(p.c, q, p.pages, t["table"], told, outs[i], lses[i], ws, new_start=t["new_start"])
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(0)
+    for l in lens + lens:
+        told.copy_(torch.tensor(l, dtype=torch.int32))
+        q.mul_(0.9)
+        graph.replay()
+        torch.cuda.synchronize()
+        step(1)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], outs[1]) and torch.equal(lses[0], lses[1])
+
+
+@pytest.mark.parametrize("fmt", [None, "q4"])
+def test_pages_that_pass_four_gigabytes(fmt):
+    """Pages of 65536 positions, the last of an array of more than 2^32 bytes: the results of a small array."""
+    ps, d, hq, hkv, n, new = 65536, 64, 4, 1, 65700, 65600
+    row = d // 2 if fmt else 2 * d
+    many = (1 << 32) // (ps * row) + 3
+    assert many * ps * row > 1 << 32
+    g = torch.Generator(device="cuda").manual_seed(4)
+    k, v = (torch.randn((n, hkv, d), generator=g, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn((n, hq, d), generator=g, device="cuda").bfloat16()
+    start, lens = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, new, n], [new, n - new]))
+    got = []
+    for pages, table in ((4, [[2, 0], [3, 1]]), (many, [[many - 1, 1], [0, many - 2]])):
+        args = dict(n_seqs=2, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, page_size=ps, n_pages=pages, max_pages=2, dtype="bf16", format=fmt)
+        c = rk.make_cache(max_new=new, n_tokens=n, **args)
+        pool, tb = rk.alloc_cache_pages(c), torch.tensor(table, dtype=torch.int32, device="cuda")
+        rk.restkv_append(c, k, v, pool, tb, lens, new_start=start)
+        ko, vo = (torch.zeros((2, hkv, new, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        rk.restkv_fetch(c, pool, tb, lens, ko, vo)
+        if not fmt:
+            assert torch.equal(ko[0, 0], k[:new, 0]) and torch.equal(vo[1, 0, :n - new], v[new:, 0])
+        res = [ko, vo]
+        for m in (1, 12):
+            cd = rk.make_cache(max_new=m, **args)
+            out, lse = torch.empty((2 * m, hq, d), dtype=torch.bfloat16, device="cuda"), torch.empty((2 * m, hq), device="cuda")
+            rk.restkv_attend(cd, q[:2 * m], pool, tb, lens, out, lse, rk.alloc_attend_workspace(cd))
+            assert torch.isfinite(lse).all()
+            res += [out, lse]
+        got.append(res)
+        del pool
+    assert all(torch.equal(a, b) for a, b in zip(*got))
