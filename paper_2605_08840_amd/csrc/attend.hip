@@ -59,7 +59,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
   store_out(a, nr.first + i, head, c * 4, x, M, L);
 }
 
-struct AttendPlan { int R, many, c_min, target; int64_t row_blocks, entries, Hy, chunks, slots; };
+struct AttendPlan { int R, many, waves, c_min, target; int64_t row_blocks, entries, Hy, chunks, slots; };
 AttendPlan attend_plan(const Pages& pg) {
   AttendPlan p;
   // Up to 32 rows the four wavefronts of a workgroup share the rows and divide the keys; more rows of bfloat16 pages are
@@ -68,13 +68,21 @@ AttendPlan attend_plan(const Pages& pg) {
   p.many = pg.fmt == RESTKV_BF16 && rows > 32;
   p.R = rows <= (p.many ? 64 : 16) ? 1 : 2;
   const bool per_head = pg.lens_sh != 0;
-  const int block = (p.many ? 64 : 16) * p.R;
+  // eight wavefronts on one copy of a tile, where blocks of so many rows leave no more of them empty than those of four do
+  p.waves = p.many && p.R == 2 && (rows + 127) / 128 % 2 == 0 ? 8 : 4;
+  const int block = (p.many ? 16 * p.waves : 16) * p.R;
   p.row_blocks = (rows + block - 1) / block;
   p.entries = per_head ? (int64_t)pg.n_seqs * pg.Hkv : pg.n_seqs;
   p.Hy = per_head ? 1 : pg.Hkv;
   p.c_min = pg.fmt == RESTKV_Q4 ? 4 : 2;          // (a tile for each wavefront)
-  p.target = n_cu() * 2;
+  p.target = n_cu() * 8 / p.waves;
   const int64_t tiles = (pg.max_len + ATT_TILE - 1) / ATT_TILE, each = p.Hy * p.row_blocks;
+  // One chunk where a workgroup has read the longest cache before chunks would be joined.  One chunk / several, us, d 128, one
+  // sequence of 2 KV heads with 2 rows each and one of 8 with 64 rows: bf16 192 keys 6.6 / 8.4 and 10.8 / 11.5, 384 keys 8.3 / 8.5
+  // and 14.7 / 12.9, 512 keys 9.3 / 8.7; 4 bits 512 keys 9.2 / 10.0, 768 keys 11.4 / 9.9, 64 rows 384 keys 15.7 / 14.4;
+  // f32 192 keys 8.3 / 9.8, 256 keys 9.9 / 9.9, 64 rows 192 keys 14.7 / 14.3.
+  const int alone = p.R > 1 || p.many ? (pg.fmt == RESTKV_F32 ? 2 : 4) : pg.fmt == RESTKV_F32 ? 3 : pg.fmt == RESTKV_BF16 ? 6 : 8;
+  if (tiles <= alone) p.c_min = std::max(p.c_min, (int)tiles);
   // no entry has two chunks: chunks hold the sum of all tiles, or the longest entry fits the smallest chunk
   const bool single = each >= p.target || tiles <= p.c_min;
   const int64_t more = std::min<int64_t>(p.target / each + 1, p.entries * ((tiles + p.c_min - 1) / p.c_min));
@@ -124,7 +132,7 @@ int launch_attend(const Pages& pg, const void* q, const void* k_pages, const voi
   a.vec_q = !((uintptr_t)q & 15u) && !((pg.q_st | pg.q_sh) & (qel - 1));
   const int oal = pg.out_dtype == RESTKV_F32 ? 15 : 7;
   a.vec_out = !((uintptr_t)out & oal) && !((pg.o_st | pg.o_sh) & 3);
-  const int rc = p.many ? run_attend_rows(a, p.R, st) : pg.fmt == RESTKV_F32 ? run_attend_f32(a, p.R, st) : pg.fmt == RESTKV_BF16 ? run_attend_bf16(a, p.R, st) : run_attend_q4(a, p.R, st);
+  const int rc = p.many ? run_attend_rows(a, p.R, p.waves, st) : pg.fmt == RESTKV_F32 ? run_attend_f32(a, p.R, st) : pg.fmt == RESTKV_BF16 ? run_attend_bf16(a, p.R, st) : run_attend_q4(a, p.R, st);
   if (rc || !p.slots) return rc;
   const dim3 grid(pg.max_new * pg.Hq, pg.n_seqs);
   if (pg.d == 128) hipLaunchKernelGGL(k_attend_join<128>, grid, dim3(256), 0, st, a);

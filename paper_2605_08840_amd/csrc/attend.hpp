@@ -80,6 +80,7 @@ __device__ __forceinline__ Chunk chunk_of(const Entry& x, int e, int index, int 
   const int each = count == 1 ? x.tiles : (x.tiles + count - 1) / count, t0 = min(index * each, x.tiles);
   return {e, t0, min(t0 + each, x.tiles), index, count, slot0, x.told, x.first, x.n};
 }
+template <int NW = 4>
 __device__ __forceinline__ bool find_chunk(const AttendArgs& a, int x, int* lds, Chunk& o) {
   const int lane = threadIdx.x & 63;
   if (a.entries <= 64) {
@@ -105,7 +106,7 @@ __device__ __forceinline__ bool find_chunk(const AttendArgs& a, int x, int* lds,
   Entry en = read_entry(a, tid);
   int64_t tiles = en.tiles;
   int active = en.tiles > 0;
-  for (int e = tid + 256; e < a.entries; e += 256) {
+  for (int e = tid + 64 * NW; e < a.entries; e += 64 * NW) {
     const int t = read_entry(a, e).tiles;
     tiles += t;
     active += t > 0;
@@ -117,43 +118,50 @@ __device__ __forceinline__ bool find_chunk(const AttendArgs& a, int x, int* lds,
   active = (int)wave_sum((uint32_t)active);
   if (lane == 0) {
     lds[wv] = __float_as_int(ft);
-    lds[4 + wv] = active;
+    lds[NW + wv] = active;
   }
   __syncthreads();
-  const int C = chunk_tiles(a, (__int_as_float(lds[0]) + __int_as_float(lds[1])) + (__int_as_float(lds[2]) + __int_as_float(lds[3])),
-                            lds[4] + lds[5] + lds[6] + lds[7]);
+  float total = 0.f;
+  active = 0;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    total += __int_as_float(lds[w]);
+    active += lds[NW + w];
+  }
+  const int C = chunk_tiles(a, total, active);
+  int* const at = lds + 4 * NW;         // the chunk, once found
   int run = 0, slots = 0;
-  for (int base = 0; base < a.entries; base += 256) {
+  for (int base = 0; base < a.entries; base += 64 * NW) {
     const int e = base + tid;
     if (base) en = read_entry(a, e);
     const int cnt = e < a.entries ? max(1, (en.tiles + C - 1) / C) : 0, own = cnt > 1 ? cnt : 0;
     int inc = wave_scan(cnt), sl = wave_scan(own);
     if (lane == 63) {
-      lds[8 + wv] = inc;
-      lds[12 + wv] = sl;
+      lds[2 * NW + wv] = inc;
+      lds[3 * NW + wv] = sl;
     }
-    if (tid == 0) lds[16] = -1;
+    if (tid == 0) at[0] = -1;
     __syncthreads();
     int all = 0, all_slots = 0;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < NW; ++w) {
       if (w == wv) {
         inc += run + all;
         sl += slots + all_slots;
       }
-      all += lds[8 + w];
-      all_slots += lds[12 + w];
+      all += lds[2 * NW + w];
+      all_slots += lds[3 * NW + w];
     }
     if (inc > x && inc - cnt <= x) {
       const Chunk c = chunk_of(en, e, x - inc + cnt, cnt, sl - own);
-      lds[16] = c.e; lds[17] = c.tile0; lds[18] = c.tile1; lds[19] = c.index; lds[20] = c.count; lds[21] = c.slot0;
-      lds[22] = c.told; lds[23] = c.first; lds[24] = c.n;
+      at[0] = c.e; at[1] = c.tile0; at[2] = c.tile1; at[3] = c.index; at[4] = c.count; at[5] = c.slot0;
+      at[6] = c.told; at[7] = c.first; at[8] = c.n;
     }
     run += all;
     slots += all_slots;
     __syncthreads();
-    const bool found = lds[16] >= 0;
-    if (found) o = {lds[16], lds[17], lds[18], lds[19], lds[20], lds[21], lds[22], lds[23], lds[24]};
+    const bool found = at[0] >= 0;
+    if (found) o = {at[0], at[1], at[2], at[3], at[4], at[5], at[6], at[7], at[8]};
     __syncthreads();                  // (the scratch is used for other things from here on, or for the next entries)
     if (found) return true;
   }
@@ -241,6 +249,30 @@ __device__ __forceinline__ Words<N> load_words(const char* base, uint32_t off) {
   asm("" : "+s"(u), "+v"(off));      // (the offset's extension stays beside the load)
   typedef const __attribute__((address_space(1))) char* global;
   return *(const __attribute__((address_space(1))) Words<N>*)((global)u + off);
+}
+// A weight's three parts by cutting off the mantissa (8 bits each: exact), in two plain instructions a part: in a loop that the
+// vector pipe bounds those of split8, one each, are slower (a window of 64 positions over 32k keys 89.9 -> 87.3 us).  Two
+// parts are rounded, for the ninth bit.
+template <int NP>
+__device__ __forceinline__ Op<NP> weight_parts(const float (&x)[8]) {
+  if constexpr (NP != 3) return split8<NP>(x);
+  Op<NP> o;
+  uint32_t w[NP][4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float a = x[2 * e], b = x[2 * e + 1];
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      w[p][e] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+      if (p + 1 < NP) {
+        a -= __uint_as_float(__float_as_uint(a) & 0xFFFF0000u);
+        b -= __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
+      }
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < NP; ++p) o.p[p] = make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
+  return o;
 }
 // NP parts of four weights, as split8 makes them of eight
 template <int NP>
@@ -982,7 +1014,7 @@ int run_attend(const AttendArgs& a, hipStream_t st) {
 }
 
 // by format, and for many rows (attend_*.hip)
-int run_attend_rows(const AttendArgs& a, int R, hipStream_t st);
+int run_attend_rows(const AttendArgs& a, int R, int waves, hipStream_t st);
 int run_attend_f32(const AttendArgs& a, int R, hipStream_t st);
 int run_attend_bf16(const AttendArgs& a, int R, hipStream_t st);
 int run_attend_q4(const AttendArgs& a, int R, hipStream_t st);

@@ -6,11 +6,16 @@ namespace restkv {
 
 namespace {
 
-// Four wavefronts of 16 R rows each share the tiles; otherwise the products and the softmax are those of k_attend.  Two tiles
-// are in LDS: the next one is copied (each wavefront a 16-key block) while this one is used.  Rows lie unpadded, the 16-byte
+// NW wavefronts of 16 R rows each share the tiles; otherwise the products and the softmax are those of k_attend.  Two tiles
+// are in LDS: the next one is copied (each wavefront 64 / NW rows of it) while this one is used.  Rows lie unpadded, the 16-byte
 // pieces of a row in the order piece ^ row, so that the reads of one piece of sixteen rows spread over the banks.
-template <int D, int NP, int R>
-__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(2)))
+// 256 queries a KV head, 32k keys, d 128, float32 output (three parts of a weight: 69 GFLOP of products for 34), us a call with
+// the join of its chunks: four wavefronts 89.6, eight 87.2 (half the copies); two tiles a copy and a barrier 90.8.  Of that,
+// without the copies 8 would go, without the second and third part of the weights 20, without the exponentials 3: no
+// one pipe bounds it, matrix and vector instructions add up (a wavefront alone takes 4500 cycles a tile, 2048 of them products),
+// and 33 MB of chunk sums are written and read again.
+template <int D, int NP, int R, int NW>
+__global__ __attribute__((amdgpu_flat_work_group_size(64 * NW, 64 * NW), amdgpu_waves_per_eu(2)))
 void k_attend_rows(AttendArgs a) {
   constexpr int UN = D / 16, QC = D / 32, ROWB = D * 2, TK = 64, NB = 4, CH = ROWB / 16, TILE = TK * ROWB;
   extern __shared__ __align__(16) char lds[];        // [2][keys | values][TILE]
@@ -22,12 +27,12 @@ void k_attend_rows(AttendArgs a) {
   if (unit >= a.units) return;
   const int hy = unit % a.Hy;
   Chunk ch;
-  if (!find_chunk(a, unit / a.Hy, (int*)lds, ch)) return;
+  if (!find_chunk<NW>(a, unit / a.Hy, (int*)lds, ch)) return;
   ch.n = __builtin_amdgcn_readfirstlane(ch.n);
   ch.first = __builtin_amdgcn_readfirstlane(ch.first);
   const int e = __builtin_amdgcn_readfirstlane(ch.e);
   const int s = a.per_head ? e / pg.Hkv : e, h = a.per_head ? e - s * pg.Hkv : hy;
-  const int rows = pg.G * ch.n, block0 = rb * 64 * R, row0 = block0 + wv * 16 * R;
+  const int rows = pg.G * ch.n, block0 = rb * 16 * NW * R, row0 = block0 + wv * 16 * R;
   if (block0 >= rows) return;
   if (a.plan && ch.index == 0 && hy == 0 && rb == 0 && threadIdx.x == 0) a.plan[e] = make_int2(ch.slot0, ch.count);
 
@@ -37,7 +42,7 @@ void k_attend_rows(AttendArgs a) {
   };
   // of the workgroup, and of this wavefront (none, if it has no rows)
   const int k_begin = __builtin_amdgcn_readfirstlane(ch.tile0 * ATT_TILE);
-  const int k_end = __builtin_amdgcn_readfirstlane(min(ch.tile1 * ATT_TILE, limit(min(block0 + 64 * R, rows) - 1)));
+  const int k_end = __builtin_amdgcn_readfirstlane(min(ch.tile1 * ATT_TILE, limit(min(block0 + 16 * NW * R, rows) - 1)));
   const int own_end = __builtin_amdgcn_readfirstlane(row0 < rows ? min(k_end, limit(min(row0 + 16 * R, rows) - 1)) : 0);
   const int lim_lo = __builtin_amdgcn_readfirstlane(limit(min(row0, rows - 1)));
   const float sc = pg.scale * 1.44269504088896341f;
@@ -53,17 +58,20 @@ void k_attend_rows(AttendArgs a) {
     row = ok ? (uint32_t)page * (uint32_t)pg.page_s + (t & ((1 << pg.lg_ps) - 1)) * (uint32_t)pg.tok_s : 0u;
     return ok;
   };
-  constexpr int PER = 1024 / ROWB, PIECES = 16 / PER;      // rows of a copy, copies of a block
+  // rows of a copy, a wavefront's rows of a tile and its copies of them
+  constexpr int PER = 1024 / ROWB, OWN = TK / NW, PIECES = OWN / PER;
+  static_assert(PIECES >= 1 && 16 % OWN == 0, "");
+  const int own0 = wv * OWN, in_block = own0 & 15;
   uint32_t off[PIECES];
 #pragma unroll
   for (int x = 0; x < PIECES; ++x) {
-    const int r = x * PER + lane / CH;
+    const int r = in_block + x * PER + lane / CH;
     off[x] = r * tokb + ((lane % CH) ^ (r & (CH - 1))) * 16;
   }
-  auto copy = [&](int k0, int buf) {                  // this wavefront's block of the tile
+  auto copy = [&](int k0, int buf) {                  // this wavefront's rows of the tile
     uint32_t row;
-    first_row(k0 + 16 * wv, row);
-    char* to = lds + buf * 2 * TILE + wv * 16 * ROWB;
+    first_row(k0 + (own0 & ~15), row);
+    char* to = lds + buf * 2 * TILE + own0 * ROWB;
 #pragma unroll
     for (int x = 0; x < PIECES; ++x) dma_1k(kh + (uint64_t)row * ROWB, off[x], to + x * 1024);
 #pragma unroll
@@ -188,7 +196,7 @@ void k_attend_rows(AttendArgs a) {
       for (int cb = 0; cb < R; ++cb) {
         const f32x4 u = p[2 * hf][cb], w = p[2 * hf + 1][cb];
         const float x[8] = {u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
-        po[cb] = split8<NP>(x);
+        po[cb] = weight_parts<NP>(x);
       }
       if (__builtin_expect(masked, 0)) {
         keep_here(vr);
@@ -243,9 +251,9 @@ void k_attend_rows(AttendArgs a) {
         const uint4 x = make_uint4(__builtin_amdgcn_perm(vr[1][i / 2], vr[0][i / 2], sel), __builtin_amdgcn_perm(vr[3][i / 2], vr[2][i / 2], sel),
                                    __builtin_amdgcn_perm(vr[5][i / 2], vr[4][i / 2], sel), __builtin_amdgcn_perm(vr[7][i / 2], vr[6][i / 2], sel));
 #pragma unroll
-        for (int cb = 0; cb < R; ++cb)
+        for (int pl = NP - 1; pl >= 0; --pl)
 #pragma unroll
-          for (int pl = NP - 1; pl >= 0; --pl) o[i][cb] = mfma(x, po[cb].p[pl], o[i][cb]);
+          for (int cb = 0; cb < R; ++cb) o[i][cb] = mfma(x, po[cb].p[pl], o[i][cb]);
       }
     }
   }
@@ -279,20 +287,19 @@ void k_attend_rows(AttendArgs a) {
   }
 }
 
-template <int D, int NP, int R>
+template <int D, int NP, int R, int NW>
 int run_rows(const AttendArgs& a, hipStream_t st) {
   constexpr size_t lds = 2 * 2 * 64 * (size_t)D * 2;
-  auto kern = k_attend_rows<D, NP, R>;
-  hipLaunchKernelGGL(kern, unit_grid(a), dim3(256), lds, st, a);
+  hipLaunchKernelGGL((k_attend_rows<D, NP, R, NW>), unit_grid(a), dim3(64 * NW), lds, st, a);
   return hip_status();
 }
 
 }  // namespace
 
-int run_attend_rows(const AttendArgs& a, int R, hipStream_t st) {
+int run_attend_rows(const AttendArgs& a, int R, int waves, hipStream_t st) {
   auto go = [&](auto d, auto np) {
     constexpr int D = decltype(d)::value, NP = decltype(np)::value;
-    return R == 1 ? run_rows<D, NP, 1>(a, st) : run_rows<D, NP, 2>(a, st);
+    return R == 1 ? run_rows<D, NP, 1, 4>(a, st) : waves == 4 ? run_rows<D, NP, 2, 4>(a, st) : run_rows<D, NP, 2, 8>(a, st);
   };
   auto by_d = [&](auto np) {
     return a.pg.d == 128 ? go(std::integral_constant<int, 128>{}, np) : go(std::integral_constant<int, 64>{}, np);

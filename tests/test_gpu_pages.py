@@ -629,3 +629,16 @@ def test_pages_that_pass_four_gigabytes(fmt):
         got.append(res)
         del pool
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("out", [None, "f32"])
+@pytest.mark.parametrize("lens,new,more", [
+    ([300, 65, 40], [40, 3, 33], dict(hq=8, hkv=2, d=128)),                   # 160 rows: eight wavefronts, five of them with rows
+    ([700, 90], [100, 90], dict(hq=8, hkv=2, d=64, ps=32)),                   # 400 and 360
+    ([700, 31], [64, 64], dict(hq=8, hkv=2, d=128, causal=False)),            # 256, more of them than positions
+    ([[200, 400], [500, 3]], [40, 22], dict(hq=12, hkv=2, d=128, head_lens=True)),
+    ([60] * 70 + [900], [34, 0, 3] * 23 + [5, 34], dict(hq=4, hkv=1, d=64)),  # 136, of more sequences than lanes
+])
+def test_attention_of_many_rows(lens, new, more, out):
+    p = Plain(rk, lens=lens, new=new, dtype="bf16", out_dtype=out, seed=sum(new), **more)
+    check_attend(p, p.normal(p.tokens, p.hq, p.d).bfloat16(), torch.float32 if out else torch.bfloat16, causal=more.get("causal", True))
