@@ -502,7 +502,8 @@ def _as_strided(c: RestkvCache, **strides) -> ctypes.c_void_p:
 
 def _on_gpu(dev: int, stream, what: str, f, *args):
     """The call on GPU `dev`, on the given stream or that GPU's current one."""
-    s = (torch.cuda.current_stream(dev) if stream is None else stream).cuda_stream
+    # (torch's own lookup without the Stream object around it: 0.1 us of 1.1, of a call of 10)
+    s = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
     if dev == torch.cuda.current_device():
         rc = f(*args, s)
     else:
