@@ -33,12 +33,12 @@ __device__ __forceinline__ void load_unit(const T* p, float (&x)[UN]) {
   }
 }
 
-template <typename T, int UN, bool VEC>
+template <typename T, int UN, bool VEC, bool PAST>
 __device__ __forceinline__ void store_unit(T* p, const float (&x)[UN]) {
   if constexpr (sizeof(T) == 4) {
     if constexpr (VEC) {
 #pragma unroll
-      for (int i = 0; i < UN; i += 4) *(float4*)((float*)p + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+      for (int i = 0; i < UN; i += 4) put<PAST>((float*)p + i, f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]});
     } else {
 #pragma unroll
       for (int i = 0; i < UN; ++i) ((float*)p)[i] = x[i];
@@ -52,9 +52,9 @@ __device__ __forceinline__ void store_unit(T* p, const float (&x)[UN]) {
 #pragma unroll
       for (int i = 0; i < UN; ++i) p[i].x = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
     } else if constexpr (UN == 8) {
-      *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
+      put<PAST>(p, Words<4>{w[0], w[1], w[2], w[3]});
     } else {
-      *(uint2*)p = make_uint2(w[0], w[1]);
+      put<PAST>(p, Words<2>{w[0], w[1]});
     }
   }
 }
@@ -148,7 +148,8 @@ __device__ __forceinline__ uint32_t unit_codes(const float (&x)[UN], int u, uint
 
 // A wavefront takes U times four rows of a token (rows: KV heads' keys, their values, query heads), sixteen lanes a row, a lane
 // the d/16 channels of a unit: accesses run along rows, and a group's extremes are a reduction over sixteen lanes.  U = 4 has
-// four rows a lane in flight and reads the angles once for them; few tokens take U = 1, for more wavefronts.
+// four rows a lane in flight and reads the angles once for them; few tokens take U = 1, for more wavefronts.  Many tokens' queries
+// go past the caches, their pages do not (2 / (G + 2) of it, and who attends or fetches reads them next).
 template <typename T, int D, bool Q4, bool VEC, int U>
 __global__ __launch_bounds__(256) void k_append(Pages pg, const T* k, const T* v, char* k_pages, char* v_pages,
                                                 uint32_t* k_scale, uint32_t* v_scale, const int32_t* __restrict__ positions,
@@ -241,13 +242,13 @@ __global__ __launch_bounds__(256) void k_append(Pages pg, const T* k, const T* v
       if (turns) rotate_unit<UN>(pg, c0, turn, other[c], x[c]);
     }
     if (is_q) {
-      if (r[c] < n_rows) store_unit<T, UN, VEC>(q_out + t * pg.q_st + (r[c] - 2 * pg.Hkv) * pg.q_sh + c0, x[c]);
+      if (r[c] < n_rows) store_unit<T, UN, VEC, U != 1>(q_out + t * pg.q_st + (r[c] - 2 * pg.Hkv) * pg.q_sh + c0, x[c]);
       continue;
     }
     if (!room[c]) continue;
     char* dst = is_v ? v_pages : k_pages;
     if constexpr (!Q4) {
-      store_unit<T, UN, true>((T*)dst + (int64_t)slot[c] * D + c0, x[c]);
+      store_unit<T, UN, true, false>((T*)dst + (int64_t)slot[c] * D + c0, x[c]);
     } else {
       uint32_t scale[NG];
       const uint32_t code = unit_codes<UN>(x[c], u, scale);

@@ -38,8 +38,6 @@ inline dim3 unit_grid(const AttendArgs& a) {
 }
 __device__ __forceinline__ int unit_of_block() { return (blockIdx.z * GRID_Y + blockIdx.y) * 8 + (blockIdx.x & 7); }
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
 // Sum over the lanes up to this one.
 __device__ __forceinline__ int wave_scan(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);   // row_shr:1
@@ -239,16 +237,14 @@ __device__ __forceinline__ void store_out(const AttendArgs& a, int64_t t, int64_
 enum { FMT_F32, FMT_BF16, FMT_Q4 };
 
 // N words at a uniform address (held in scalar registers, so that the load adds the lane's 32-bit offset by itself).
-template <int N> struct WordsOf { typedef uint32_t type __attribute__((ext_vector_type(N))); };
-template <> struct WordsOf<1> { typedef uint32_t type; };
-template <int N> using Words = typename WordsOf<N>::type;
-template <int N>
+template <int N, bool PAST = false>
 __device__ __forceinline__ Words<N> load_words(const char* base, uint32_t off) {
   uint64_t u = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)base >> 32)) << 32 |
                (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(uint64_t)base);
   asm("" : "+s"(u), "+v"(off));      // (the offset's extension stays beside the load)
   typedef const __attribute__((address_space(1))) char* global;
-  return *(const __attribute__((address_space(1))) Words<N>*)((global)u + off);
+  if constexpr (PAST) return __builtin_nontemporal_load((const __attribute__((address_space(1))) Words<N>*)((global)u + off));
+  else return *(const __attribute__((address_space(1))) Words<N>*)((global)u + off);
 }
 // A weight's three parts by cutting off the mantissa (8 bits each: exact), in two plain instructions a part: in a loop that the
 // vector pipe bounds those of split8, one each, are slower (a window of 64 positions over 32k keys 89.9 -> 87.3 us).  Two
@@ -406,11 +402,14 @@ void k_attend(AttendArgs a) {
   Words<KV> kr[NB * KN];
   Words<VV> vr[NB * 4 * VN];
   Words<NG> sk[1], sv[1];
+  // (Whole lines go past the caches, and leave them to the loads that take a line in parts: values of bf16 pages, whose keys come
+  // half a line of sixteen rows at a time, 1 x 128k positions 99.6 -> 90.4 us a call, 32 sequences of 1k to 2k 38.9 -> 34.1;
+  // keys of 4-bit pages, 128k positions 43.5 -> 41.2.  All loads so: 89.6, 37.4 and 40.8, f32 pages 47.4 -> 58.0.)
   auto load_keys = [&](const Where& w) {
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int c = 0; c < KN; ++c) kr[b * KN + c] = load_words<KV>(kh + (uint64_t)w.row[b] * ROWB, k_off + c * 64);
+      for (int c = 0; c < KN; ++c) kr[b * KN + c] = load_words<KV, FMT == FMT_Q4>(kh + (uint64_t)w.row[b] * ROWB, k_off + c * 64);
   };
   auto load_values = [&](const Where& w) {
 #pragma unroll
@@ -421,7 +420,7 @@ void k_attend(AttendArgs a) {
         for (int c = 0; c < VN; ++c) {
           const char* p = vh + ((uint64_t)w.row[b] * ROWB + r * tokb);
           if constexpr (FMT == FMT_Q4 && UN == 4) vr[b * 4 + r] = load_half(p, v_off);
-          else vr[(b * 4 + r) * VN + c] = load_words<VV>(p, v_off + c * 16);
+          else vr[(b * 4 + r) * VN + c] = load_words<VV, FMT == FMT_BF16>(p, v_off + c * 16);
         }
   };
   auto scales_of = [&](const Where& w, const uint32_t* from) {       // lane = key of the tile
