@@ -5,7 +5,7 @@ namespace restkv {
 
 namespace {
 
-template <typename T, int UN, bool VEC>
+template <typename T, int UN, bool VEC, bool PAST>
 __device__ __forceinline__ void load_unit(const T* p, float (&x)[UN]) {
   if constexpr (!VEC) {
 #pragma unroll
@@ -13,17 +13,17 @@ __device__ __forceinline__ void load_unit(const T* p, float (&x)[UN]) {
   } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
     for (int i = 0; i < UN; i += 4) {
-      const float4 v = *(const float4*)(p + i);
-      x[i] = v.x; x[i + 1] = v.y; x[i + 2] = v.z; x[i + 3] = v.w;
+      const f32x4 v = get<PAST && UN == 4, f32x4>(p + i);
+      x[i] = v[0]; x[i + 1] = v[1]; x[i + 2] = v[2]; x[i + 3] = v[3];
     }
   } else {
     uint32_t w[UN / 2];
     if constexpr (UN == 8) {
-      const uint4 v = *(const uint4*)p;
-      w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+      const Words<4> v = get<PAST, Words<4>>(p);
+      w[0] = v[0]; w[1] = v[1]; w[2] = v[2]; w[3] = v[3];
     } else {
-      const uint2 v = *(const uint2*)p;
-      w[0] = v.x; w[1] = v.y;
+      const Words<2> v = get<PAST, Words<2>>(p);
+      w[0] = v[0]; w[1] = v[1];
     }
 #pragma unroll
     for (int i = 0; i < UN / 2; ++i) {
@@ -150,7 +150,7 @@ __device__ __forceinline__ uint32_t unit_codes(const float (&x)[UN], int u, uint
 // the d/16 channels of a unit: accesses run along rows, and a group's extremes are a reduction over sixteen lanes.  U = 4 has
 // four rows a lane in flight and reads the angles once for them; few tokens take U = 1, for more wavefronts.  Many tokens' queries
 // go past the caches, their pages do not (2 / (G + 2) of it, and who attends or fetches reads them next).
-template <typename T, int D, bool Q4, bool VEC, int U>
+template <typename T, int D, bool Q4, bool VEC, int U, bool PAST>
 __global__ __launch_bounds__(256) void k_append(Pages pg, const T* k, const T* v, char* k_pages, char* v_pages,
                                                 uint32_t* k_scale, uint32_t* v_scale, const int32_t* __restrict__ positions,
                                                 const float* __restrict__ cos, const float* __restrict__ sin, const T* q, T* q_out,
@@ -196,8 +196,8 @@ __global__ __launch_bounds__(256) void k_append(Pages pg, const T* k, const T* v
     const int rc = min(r[c], n_rows - 1);
     const T* row = rc >= 2 * pg.Hkv ? q + t * pg.q_st + (rc - 2 * pg.Hkv) * pg.q_sh
                                     : (rc >= pg.Hkv ? v - pg.Hkv * pg.kv_sh : k) + t * pg.kv_st + rc * pg.kv_sh;
-    load_unit<T, UN, VEC>(row + c0, x[c]);
-    if (far && turns) load_unit<T, UN, VEC>(row + (c0 >= pg.rot >> 1 ? c0 - (pg.rot >> 1) : c0 + (pg.rot >> 1)), other[c]);
+    load_unit<T, UN, VEC, PAST>(row + c0, x[c]);
+    if (far && turns) load_unit<T, UN, VEC, false>(row + (c0 >= pg.rot >> 1 ? c0 - (pg.rot >> 1) : c0 + (pg.rot >> 1)), other[c]);
   }
   Turn<UN> turn;
   if (pg.rot) {
@@ -278,9 +278,14 @@ int run_append(const Pages& pg, const void* k, const void* v, void* k_pages, voi
     hipLaunchKernelGGL(kern, wide_grid(((int64_t)pg.n_tokens * parts + 3) / 4), dim3(256), 0, st, pg, (const T*)k, (const T*)v, (char*)k_pages,
                        (char*)v_pages, (uint32_t*)k_scale, (uint32_t*)v_scale, positions, cos, sin, (const T*)q, (T*)q_out, parts, n_rows);
   };
-  if (!vec) go(k_append<T, D, Q4, false, 1>, 1);
-  else if (few) go(k_append<T, D, Q4, true, 1>, 1);
-  else go(k_append<T, D, Q4, true, 4>, 4);
+  // more than the last-level cache holds, each row once: read past the caches (32k tokens of 32 and 8 heads of 128 bf16 147 -> 127 us, but 100 MB that the last
+  // call has read too: 36 -> 40)
+  const bool once = !(pg.rot && !pg.rot_pairs && pg.rot != D);
+  const bool past = once && (int64_t)pg.n_tokens * n_rows * D * (int)sizeof(T) > (int64_t)256 << 20;
+  if (!vec) go(k_append<T, D, Q4, false, 1, false>, 1);
+  else if (few) go(k_append<T, D, Q4, true, 1, false>, 1);
+  else if (past) go(k_append<T, D, Q4, true, 4, true>, 4);
+  else go(k_append<T, D, Q4, true, 4, false>, 4);
   return hip_status();
 }
 
