@@ -10,7 +10,7 @@ namespace {
 // are in LDS: the next one is copied (each wavefront 64 / NW rows of it) while this one is used.  Rows lie unpadded, the 16-byte
 // pieces of a row in the order piece ^ row, so that the reads of one piece of sixteen rows spread over the banks.
 // 256 queries a KV head, 32k keys, d 128, float32 output (three parts of a weight: 69 GFLOP of products for 34), us a call with
-// the join of its chunks: four wavefronts 89.6, eight 87.2 (half the copies); two tiles a copy and a barrier 90.8.  Of that,
+// the join of its chunks, 83.4 now: four wavefronts 89.6, eight 87.2 (half the copies); two tiles a copy and a barrier 90.8.  Of that,
 // without the copies 8 would go, without the second and third part of the weights 20, without the exponentials 3: no
 // one pipe bounds it, matrix and vector instructions add up (a wavefront alone takes 4500 cycles a tile, 2048 of them products),
 // and 33 MB of chunk sums are written and read again.
@@ -258,32 +258,42 @@ void k_attend_rows(AttendArgs a) {
     }
   }
 
-  // ---- a lane has four units of its rows: d/4 channels in a row
+  // ---- a lane has four units of its rows, 16 bytes at a time: by way of LDS to whole rows (where the tiles were), which are
+  // stored 512 bytes at a time (256 queries a KV head over 32k keys 86.5 -> 83.4 us)
+  __syncthreads();
+  char* const own = lds + wv * (16 * D * 4);
+  static_assert(NW * 16 * D * 4 <= 4 * TILE, "");
+  constexpr int Q = D / 4;
 #pragma unroll
   for (int cb = 0; cb < R; ++cb) {
-    const int row = row0 + cb * 16 + n;
     const float L = quad_sum(l[cb]);
-    if (row >= rows) continue;
-    if (ch.count > 1) {
-      const int64_t at = (int64_t)((ch.slot0 + ch.index) * a.Hy + hy) * ((int64_t)pg.G * pg.max_new) + row;
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int i = 0; i < UN; i += 4)
-          *(float4*)&a.part_o[at * D + (4 * j + r) * UN + i] = make_float4(o[i][cb][r], o[i + 1][cb][r], o[i + 2][cb][r], o[i + 3][cb][r]);
-      if (j == 0) {
-        a.part_m[at] = ref[cb];
-        a.part_l[at] = L;
+      for (int i = 0; i < UN; i += 4)
+        *(f32x4*)(own + n * (D * 4) + (((4 * j + r) * (UN / 4) + i / 4) ^ n) * 16) = f32x4{o[i][cb][r], o[i + 1][cb][r], o[i + 2][cb][r], o[i + 3][cb][r]};
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int k = 0; k < 16 * Q / 64; ++k) {
+      const int r = k * (64 / Q) + lane / Q, q = lane % Q, row = row0 + cb * 16 + r;
+      const float4 x = *(const float4*)(own + r * (D * 4) + (q ^ r) * 16);
+      const float m = __shfl(ref[cb], r), total = __shfl(L, r);
+      if (row >= rows) continue;
+      if (ch.count > 1) {
+        const int64_t at = (int64_t)((ch.slot0 + ch.index) * a.Hy + hy) * ((int64_t)pg.G * pg.max_new) + row;
+        *(float4*)&a.part_o[at * D + q * 4] = x;
+        if (q == 0) {
+          a.part_m[at] = m;
+          a.part_l[at] = total;
+        }
+      } else {
+        const int tok = row / pg.G;
+        store_out(a, ch.first + tok, h * pg.G + row - tok * pg.G, q * 4, x, m, total);
       }
-    } else {
-      const int tok = row / pg.G, head = h * pg.G + row - tok * pg.G;
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int i = 0; i < UN; i += 4)
-          store_out(a, ch.first + tok, head, (4 * j + r) * UN + i, make_float4(o[i][cb][r], o[i + 1][cb][r], o[i + 2][cb][r], o[i + 3][cb][r]),
-                    ref[cb], L);
     }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
