@@ -114,7 +114,7 @@ int launch_attend(const Pages& pg, const void* q, const void* k_pages, const voi
                   const void* v_scale, void* out, float* lse, char* ws, hipStream_t st) {
   const AttendPlan p = attend_plan(pg);
   const AttendWs lay = attend_ws(pg, p);
-  if (p.chunks * p.Hy > (int64_t)1 << 30 || p.row_blocks > (1 << 20) || (p.slots && (int64_t)pg.max_new * pg.Hq >= (1 << 24)))
+  if (p.chunks * p.Hy > (int64_t)1 << 30 || p.row_blocks * p.waves > (1 << 22) || (p.slots && (int64_t)pg.max_new * pg.Hq >= (1 << 24)))
     return RESTKV_EUNSUPPORTED;
   AttendArgs a = {};
   a.pg = pg;

@@ -185,3 +185,8 @@ def test_binding_knows_pages_by_their_head_stride(rk):
                      (good(rk, _page_stride=0, _head_stride=0, _token_stride=0), both)):
         with pytest.raises(rk.RestkvError, match="not on a GPU"):
             rk.restkv_append(c, x, x, pages, table, lens)
+
+
+def test_queries_of_more_threads_than_a_launch_takes_are_refused(rk):
+    for n, fmt in ((1 << 28, None), (1 << 28, "q4"), (1 << 30, None)):
+        assert attend(rk, good(rk, n_seqs=1, n_q_heads=1, n_kv_heads=1, max_new=n, n_tokens=n, format=fmt)) == -2
