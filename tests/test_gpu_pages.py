@@ -662,3 +662,43 @@ def test_float32_output_is_as_near_as_plain_float32(dtype, fmt, n, d):
             off += float((got[s, h * 4:h * 4 + 4].double() - want).square().sum())
             plain += float((near.double() - want).square().sum())
     assert off <= 4 * plain, (off / plain) ** 0.5
+
+
+@pytest.mark.parametrize("dtype,fmt,d,rot,pairs", [
+    ("bf16", None, 128, 128, False), ("bf16", None, 128, 64, False), ("bf16", "q4", 128, 128, True), ("bf16", None, 64, 64, True),
+    ("f32", None, 64, 64, False), ("f32", "q4", 128, 128, False), ("f32", None, 128, 0, False), ("bf16", "q4", 64, 32, False)])
+def test_large_calls_are_many_small_ones(dtype, fmt, d, rot, pairs):
+    """70000 tokens, queries in place: the bits that calls of 4000 leave; fetched at once and in parts."""
+    n, step, hq, hkv, ps, cap = 70000, 4000, 8, 8, 64, 70016
+    g = torch.Generator(device="cuda").manual_seed(d + rot)
+    t = torch.float32 if dtype == "f32" else torch.bfloat16
+    k, v, q = (torch.randn((n, h, d), generator=g, device="cuda").to(t) for h in (hkv, hkv, hq))
+    table = torch.randperm(cap // ps, generator=g, device="cuda").int()[None]
+    ang = torch.randn((n, max(rot // 2, 1)), generator=g, device="cuda")
+    cos, sin = ang.cos(), ang.sin()
+    args = dict(n_seqs=1, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, page_size=ps, n_pages=cap // ps, max_pages=cap // ps, dtype=dtype,
+                format=fmt, rotary_dim=rot, interleaved=pairs, n_positions=n)
+    pools, qs = [], []
+    for size in (n, step):
+        pool, x = rk.alloc_cache_pages(rk.make_cache(**args)), q.clone()
+        for a in range(0, n, size):
+            b = min(a + size, n)
+            lens = torch.tensor([b], dtype=torch.int32, device="cuda")
+            rk.restkv_append(rk.make_cache(max_new=b - a, **args), k[a:b], v[a:b], pool, table, lens, cos=cos, sin=sin, q=x[a:b], q_out=x[a:b])
+        pools.append(pool)
+        qs.append(x)
+    assert torch.equal(qs[0], qs[1]) and (rot == 0) == torch.equal(qs[0], q)
+    bits = lambda x: x.view(torch.uint8 if x.dtype == torch.uint8 else torch.int16 if x.element_size() == 2 else torch.int32)  # noqa: E731
+    for name in ("k", "v") + (("k_scale", "v_scale") if fmt else ()):
+        assert torch.equal(*(bits(getattr(p, name)) for p in pools)), name
+    c, out = rk.make_cache(**args), []
+    for size in (n, 20000):
+        parts = []
+        for a in range(0, n, size):
+            ko, vo = (torch.empty((1, hkv, min(size, n - a), d), dtype=t, device="cuda") for _ in range(2))
+            rk.restkv_fetch(c, pools[0], table, lens, ko, vo, first=a)
+            parts.append((ko, vo))
+        out.append([torch.cat(x, 2) for x in zip(*parts)])
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
+    if not fmt:
+        assert torch.equal(out[0][1][0].transpose(0, 1), v)
