@@ -271,8 +271,9 @@ int run_append(const Pages& pg, const void* k, const void* v, void* k_pages, voi
   const int unit = D / 16 * (int)sizeof(T), mask = (unit < 16 ? unit : 16) - 1, el = (mask + 1) / (int)sizeof(T) - 1;
   const bool vec = !(((uintptr_t)k | (uintptr_t)v | (uintptr_t)q | (uintptr_t)q_out) & mask) &&
                    !((pg.kv_st | pg.kv_sh | (q ? pg.q_st | pg.q_sh : 0)) & el);
-  // four groups of rows a wavefront where that still leaves every SIMD eight wavefronts
-  const bool few = (int64_t)pg.n_tokens * ((chunks + 3) / 4) < (int64_t)n_cu() * 32;
+  // four groups of rows a wavefront where that leaves five wavefronts a unit (4 bits: sixteen).  One / four, us, tokens of 32 and 8
+  // heads of 128: bf16 64 tokens 3.1 / 4.2, 512 5.4 / 4.9, 2048 13.1 / 9.5; 4 bits 512 5.8 / 7.1, 2048 14.5 / 13.1
+  const bool few = (int64_t)pg.n_tokens * ((chunks + 3) / 4) < (int64_t)n_cu() * (Q4 ? 16 : 5);
   auto go = [&](auto kern, int U) {
     const int parts = (chunks + U - 1) / U;
     hipLaunchKernelGGL(kern, wide_grid(((int64_t)pg.n_tokens * parts + 3) / 4), dim3(256), 0, st, pg, (const T*)k, (const T*)v, (char*)k_pages,

@@ -62,10 +62,11 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
 struct AttendPlan { int R, many, waves, c_min, target; int64_t row_blocks, entries, Hy, chunks, slots; };
 AttendPlan attend_plan(const Pages& pg) {
   AttendPlan p;
-  // Up to 32 rows the four wavefronts of a workgroup share the rows and divide the keys; more rows of bfloat16 pages are
-  // divided among them, with the keys in LDS.
+  // Up to 16 rows (32, where pages are not bfloat16) the four wavefronts of a workgroup share the rows and divide the keys; more
+  // rows of bfloat16 pages are divided among them, with the keys in LDS.  The one / the other, us, 32k keys of 8 KV heads of 128:
+  // 24 rows 32.4 / 31.6, 32 rows 33.5 / 31.7, 64 rows 41.1 / 34.4, 128 rows 62 / 46.
   const int64_t rows = (int64_t)pg.G * pg.max_new;
-  p.many = pg.fmt == RESTKV_BF16 && rows > 32;
+  p.many = pg.fmt == RESTKV_BF16 && rows > 16;
   p.R = rows <= (p.many ? 64 : 16) ? 1 : 2;
   const bool per_head = pg.lens_sh != 0;
   // eight wavefronts on one copy of a tile, where blocks of so many rows leave no more of them empty than those of four do
@@ -132,7 +133,7 @@ int launch_attend(const Pages& pg, const void* q, const void* k_pages, const voi
   a.vec_q = !((uintptr_t)q & 15u) && !((pg.q_st | pg.q_sh) & (qel - 1));
   const int oal = pg.out_dtype == RESTKV_F32 ? 15 : 7;
   a.vec_out = !((uintptr_t)out & oal) && !((pg.o_st | pg.o_sh) & 3);
-  const int rc = p.many ? run_attend_rows(a, p.R, p.waves, st) : pg.fmt == RESTKV_F32 ? run_attend_f32(a, p.R, st) : pg.fmt == RESTKV_BF16 ? run_attend_bf16(a, p.R, st) : run_attend_q4(a, p.R, st);
+  const int rc = p.many ? run_attend_rows(a, p.R, p.waves, st) : pg.fmt == RESTKV_F32 ? run_attend_f32(a, p.R, st) : pg.fmt == RESTKV_BF16 ? run_attend_bf16(a, st) : run_attend_q4(a, p.R, st);
   if (rc || !p.slots) return rc;
   const dim3 grid(pg.max_new * pg.Hq, pg.n_seqs);
   if (pg.d == 128) hipLaunchKernelGGL(k_attend_join<128>, grid, dim3(256), 0, st, a);

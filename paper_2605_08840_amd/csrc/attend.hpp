@@ -1027,7 +1027,7 @@ int run_attend(const AttendArgs& a, hipStream_t st) {
 // by format, and for many rows (attend_*.hip)
 int run_attend_rows(const AttendArgs& a, int R, int waves, hipStream_t st);
 int run_attend_f32(const AttendArgs& a, int R, hipStream_t st);
-int run_attend_bf16(const AttendArgs& a, int R, hipStream_t st);
+int run_attend_bf16(const AttendArgs& a, hipStream_t st);
 int run_attend_q4(const AttendArgs& a, int R, hipStream_t st);
 
 }  // namespace restkv

@@ -1,12 +1,12 @@
-// Attention over bfloat16 pages.
+// Attention over bfloat16 pages, up to 16 rows.
 #include "attend.hpp"
 
 namespace restkv {
 
-int run_attend_bf16(const AttendArgs& a, int R, hipStream_t st) {
+int run_attend_bf16(const AttendArgs& a, hipStream_t st) {
   auto go = [&](auto d, auto np) {
     constexpr int D = decltype(d)::value, NP = decltype(np)::value;
-    return R == 1 ? run_attend<FMT_BF16, bf16_t, D, NP, 1>(a, st) : run_attend<FMT_BF16, bf16_t, D, NP, 2>(a, st);
+    return run_attend<FMT_BF16, bf16_t, D, NP, 1>(a, st);
   };
   auto by_d = [&](auto np) {
     return a.pg.d == 128 ? go(std::integral_constant<int, 128>{}, np) : go(std::integral_constant<int, 64>{}, np);

@@ -668,8 +668,8 @@ def test_float32_output_is_as_near_as_plain_float32(dtype, fmt, n, d):
     ("bf16", None, 128, 128, False), ("bf16", None, 128, 64, False), ("bf16", "q4", 128, 128, True), ("bf16", None, 64, 64, True),
     ("f32", None, 64, 64, False), ("f32", "q4", 128, 128, False), ("f32", None, 128, 0, False), ("bf16", "q4", 64, 32, False)])
 def test_large_calls_are_many_small_ones(dtype, fmt, d, rot, pairs):
-    """70000 tokens, queries in place: the bits that calls of 4000 leave; fetched at once and in parts."""
-    n, step, hq, hkv, ps, cap = 70000, 4000, 8, 8, 64, 70016
+    """70000 tokens, queries in place: the bits that calls of 600 leave; fetched at once and in parts."""
+    n, step, hq, hkv, ps, cap = 70000, 600, 8, 8, 64, 70016
     g = torch.Generator(device="cuda").manual_seed(d + rot)
     t = torch.float32 if dtype == "f32" else torch.bfloat16
     k, v, q = (torch.randn((n, h, d), generator=g, device="cuda").to(t) for h in (hkv, hkv, hq))
