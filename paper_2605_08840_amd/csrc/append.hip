@@ -150,6 +150,8 @@ __device__ __forceinline__ uint32_t unit_codes(const float (&x)[UN], int u, uint
 // the d/16 channels of a unit: accesses run along rows, and a group's extremes are a reduction over sixteen lanes.  U = 4 has
 // four rows a lane in flight and reads the angles once for them; few tokens take U = 1, for more wavefronts.  Many tokens' queries
 // go past the caches, their pages do not (2 / (G + 2) of it, and who attends or fetches reads them next).
+// Bound by memory: 16 x 8k tokens of 32 and 8 heads of 128 bf16, 822 MB in 143.7 us (5.7 TB/s); into 4 bits by vector instructions too,
+// ten a code: 8k tokens 183 MB in 36.7 us.  32 tokens of a decoding step 4.0 us, a chain of lengths, page and rows.
 template <typename T, int D, bool Q4, bool VEC, int U, bool PAST>
 __global__ __launch_bounds__(256) void k_append(Pages pg, const T* k, const T* v, char* k_pages, char* v_pages,
                                                 uint32_t* k_scale, uint32_t* v_scale, const int32_t* __restrict__ positions,

@@ -8,6 +8,8 @@
 // memory into operand registers without LDS: a key operand is 16 bytes of a row, a value operand takes the same channel
 // of eight keys, which a lane that has loaded a unit of d/16 channels of each of them holds already (one byte
 // permute for two values).
+// Bound by memory (128k bf16 positions of 8 KV heads of 128, 537 MB in 89 us, 6.0 TB/s), for 4 bits by vector instructions as much
+// (168 MB in 36.5 us, about 500 instructions a tile of 64 keys), for short caches by a chain of lengths, pages, keys.
 #pragma once
 
 #include "pages.hpp"
