@@ -575,19 +575,19 @@ void k_attend(AttendArgs a) {
       }
       __builtin_amdgcn_wave_barrier();
       *(Words<NG>*)&s_kz[lane * NG] = sk[0];
+      // Zeros stand for the values' scales of slots that nobody sees, and of keys that some rows see wherever what the
+      // weights are multiplied with (zero + BASE step; not finite for finite steps of 2^124 too) would make NaN of a weight of 0.
+      if (masked && n >= there(j)) sv[0] = Words<NG>{};
 #pragma unroll
       for (int f = 0; f < NG; ++f) {
-        if (masked) {
-          const float x = __uint_as_float(sv[0][f] << 16), y = __uint_as_float(sv[0][f] & 0xFFFF0000u);
-          if (!(x - x == 0.f && y - y == 0.f)) {
-            sv[0][f] = 0u;
-            odd_scales = true;
-          }
+        float st = __uint_as_float(sv[0][f] << 16), z = __builtin_fmaf(BASE, st, __uint_as_float(sv[0][f] & 0xFFFF0000u));
+        if (masked && !(z - z == 0.f)) {
+          st = z = 0.f;
+          odd_scales = true;
         }
-        const float st = __uint_as_float(sv[0][f] << 16);
         s_ks[f * 64 + lane] = __uint_as_float(sk[0][f] << 16);
         s_vs[f * 64 + lane] = st;
-        s_vz[f * 64 + lane] = __builtin_fmaf(BASE, st, __uint_as_float(sv[0][f] & 0xFFFF0000u));
+        s_vz[f * 64 + lane] = z;
       }
       odd_scales = __ballot(odd_scales);
       if (more) load_scales(next);
@@ -846,8 +846,8 @@ void k_attend(AttendArgs a) {
       }
     } else {
       if (__builtin_expect(masked && odd_scales, 0)) {
-        // steps or zeros that are not finite, in a tile where some rows do not see every key (0 times them would be NaN): zeros
-        // stand in their places, and here the rows that see the key get what it adds to their groups
+        // scales for which zeros stand, in a tile where some rows do not see every key: here the rows that see the key get
+        // what it adds to their groups
         const Words<NG> raw = scales_of(at, a.vs);
 #pragma unroll 1
         for (int kk = 0; kk < 64; ++kk) {
@@ -856,8 +856,9 @@ void k_attend(AttendArgs a) {
           for (int f = 0; f < NG; ++f) {
             const uint32_t w = __builtin_amdgcn_readlane(raw[f], kk);
             const float step = __uint_as_float(w << 16), zero = __uint_as_float(w & 0xFFFF0000u);
-            if (step - step == 0.f && zero - zero == 0.f) continue;
-            const float z = step - step == 0.f ? zero : __builtin_nanf("");
+            float z = __builtin_fmaf(BASE, step, zero);
+            if (z - z == 0.f) continue;
+            z = step - step == 0.f ? z : __builtin_nanf("");
 #pragma unroll
             for (int cb = 0; cb < R; ++cb) {
               float x = 0.f;

@@ -702,3 +702,54 @@ def test_large_calls_are_many_small_ones(dtype, fmt, d, rot, pairs):
     assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
     if not fmt:
         assert torch.equal(out[0][1][0].transpose(0, 1), v)
+
+
+# ---- what is not seen, finite but as large as its type holds ---------------------------------------
+
+def page_zero_unused(p):
+    """Page 0 (whose rows stand in for those of absent pages) free of every sequence: its place is taken by a spare page."""
+    held = set(p.table.flatten().tolist())
+    if 0 in held:
+        spare = min(set(range(p.c.n_pages)) - held)
+        for x in p.pool.values():
+            x[[0, spare]] = x[[spare, 0]]
+        p.table[p.table == 0] = spare
+
+
+@pytest.mark.parametrize("dtype,fmt,out", FORMATS)
+@pytest.mark.parametrize("junk", [3e38, -3e38])
+def test_finite_junk_in_slots_that_nobody_sees(dtype, fmt, out, junk):
+    """Slots behind the last position and rows of page 0 (4 bits: their steps and zeros) that hold the largest finite values."""
+    out_type = torch.float32 if "f32" in (dtype, out) else torch.bfloat16
+    for hq, new, d in ((1, 1, 64), (4, 1, 128), (8, 1, 64), (8, 2, 128), (8, 4, 64), (16, 5, 128)):
+        p = Plain(rk, lens=[70, 129, 5, 17 * 16 - 3], new=[new] * 4, dtype=dtype, fmt=fmt, d=d, hq=hq, hkv=1, out_dtype=out, junk=junk,
+                  seed=hq + new)
+        page_zero_unused(p)
+        p.table[1, 0, 2], p.table[3, 0, 0] = -1, p.c.n_pages      # positions 32 .. 47 and the first ones
+        p.tensors["table"] = p.table[:, 0].contiguous().cuda()
+        p.up()
+        check_attend(p, p.normal(p.tokens, hq, d).to(p.type), out_type)
+
+
+@pytest.mark.parametrize("dtype,fmt,out", FORMATS)
+@pytest.mark.parametrize("bad", [3e38, -3e38])
+def test_finite_extremes_that_later_queries_see(dtype, fmt, out, bad):
+    """Tokens of the same call as large as their type holds (4 bits: steps, zeros, both): queries before them go by the rest."""
+    out_type = torch.float32 if "f32" in (dtype, out) else torch.bfloat16
+    for d, hq, n, names, at in ((64, 2, 6, "v", 0), (128, 8, 40, "v", 0), (128, 8, 3, "vk", 0), (64, 4, 2, "v", None), (64, 8, 9, "kv", None)):
+        p = Plain(rk, lens=[100, 70], new=[n, n], dtype=dtype, fmt=fmt, d=d, hq=hq, hkv=2, out_dtype=out)
+        first = [100 - n // 2, 70 - 1]                     # the first such position of each sequence
+        q = p.normal(p.tokens, p.hq, d).to(p.type)
+        for s in range(2):
+            for h in range(2):
+                for t in range(first[s], p.lens[s][h]):
+                    for name in names:
+                        x = p.pool[name + "_scale"][p.where(s, h, t)] if p.q4 else p.pool[name][p.where(s, h, t)]
+                        if at is None:
+                            x[:] = bad
+                        else:
+                            x.view(-1)[at::2] = bad
+        p.up()
+        got, lse = run_attend(p, q, out_type)
+        rows = [p.start[s] + i for s in range(2) for i in range(n) if p.lens[s][0] - n + i + 1 <= first[s]]
+        ref.assert_attention(got, lse, ref.attention(p, q), out_type, rows)
