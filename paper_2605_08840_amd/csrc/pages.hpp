@@ -117,8 +117,12 @@ __device__ __forceinline__ void group_scale(float low, float high, float& step, 
   const float spread = high - zero;
   step = -bf16_below(-(spread / 15.0f));
   step = spread > 0.f ? fmaxf(step, 0x1p-100f) : 0.f;
-  // (a group with a NaN or an infinity has it for an extreme)
-  if (!(__builtin_isfinite(spread) && __builtin_isfinite(step) && __builtin_isfinite(zero))) { step = 0.f; zero = __builtin_nanf(""); }
+  // (a group with a NaN or an infinity has it for an extreme: these are looked at as they are, since the integers that round
+  // a NaN may wrap to a finite number)
+  if (!(__builtin_isfinite(low) && __builtin_isfinite(high) && __builtin_isfinite(spread) && __builtin_isfinite(step) && __builtin_isfinite(zero))) {
+    step = 0.f;
+    zero = __builtin_nanf("");
+  }
   inverse = step > 0.f ? 1.0f / step : 0.f;
 }
 

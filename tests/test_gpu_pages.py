@@ -753,3 +753,27 @@ def test_finite_extremes_that_later_queries_see(dtype, fmt, out, bad):
         got, lse = run_attend(p, q, out_type)
         rows = [p.start[s] + i for s in range(2) for i in range(n) if p.lens[s][0] - n + i + 1 <= first[s]]
         ref.assert_attention(got, lse, ref.attention(p, q), out_type, rows)
+
+
+def test_four_bits_of_every_kind_of_nan():
+    """Quiet and signalling NaN of both signs, at even and odd channels, among finite values: the group is NaN, its neighbours are not."""
+    patterns = [0xFFFFFFFF, 0xFFFF0001, 0x7FFFFFFF, 0x7F800001, 0xFF800001, 0xFFC00000, 0x7FC00000, 0xFFFF0000]
+    for d in (64, 128):
+        n = 2 * len(patterns)
+        p = Plain(rk, lens=[n], new=[n], dtype="f32", fmt="q4", d=d, hq=2, hkv=1)
+        sides = dict(k=p.normal(n, 1, d), v=p.normal(n, 1, d))
+        for x in sides.values():
+            for i in range(n):
+                bits = patterns[i // 2]
+                x.view(torch.int32)[i, 0, d // 2 + 2 + i % 2] = bits - (1 << 32) if bits >> 31 else bits
+        rk.restkv_append(p.c, sides["k"].cuda(), sides["v"].cuda(), p.pages, p.tensors["table"], p.tensors["lens"])
+        got, group = p.down(), torch.arange(d) % (d // 16) // 2
+        ko, vo = (torch.empty((1, 1, n, d), device="cuda") for _ in range(2))
+        rk.restkv_fetch(p.c, p.pages, p.tensors["table"], p.tensors["lens"], ko, vo)
+        for name, x, back in (("k", sides["k"], ko), ("v", sides["v"], vo)):
+            codes, scale = ref.to_q4(x[:, 0])
+            for t in range(n):
+                w, what = p.where(0, 0, t), (name, d, hex(patterns[t // 2]), t % 2)
+                assert torch.equal(got[name][w], codes[t]), what
+                assert torch.equal(torch.nan_to_num(got[name + "_scale"][w].float(), 777.0), torch.nan_to_num(scale[t].float(), 777.0)), what
+                assert torch.equal(torch.isnan(back[0, 0, t]).cpu(), group == group[d // 2 + 2]), what
