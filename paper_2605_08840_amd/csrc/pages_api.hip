@@ -64,7 +64,7 @@ static int take_arrays(Pages* pg, const void* k_pages, const void* v_pages, cons
   return RESTKV_OK;
 }
 static int take_new(Pages* pg, const int32_t* new_start) {
-  if (!new_start && (int64_t)pg->n_seqs * pg->max_new > pg->n_tokens) return RESTKV_EINVAL;
+  if (!new_start && pg->n_tokens && (int64_t)pg->n_seqs * pg->max_new > pg->n_tokens) return RESTKV_EINVAL;
   pg->new_start = new_start;
   return RESTKV_OK;
 }

@@ -190,3 +190,12 @@ def test_binding_knows_pages_by_their_head_stride(rk):
 def test_queries_of_more_threads_than_a_launch_takes_are_refused(rk):
     for n, fmt in ((1 << 28, None), (1 << 28, "q4"), (1 << 30, None)):
         assert attend(rk, good(rk, n_seqs=1, n_q_heads=1, n_kv_heads=1, max_new=n, n_tokens=n, format=fmt)) == -2
+
+
+def test_a_call_without_a_token_does_nothing_with_or_without_new_start(rk):
+    none = dict(kp=None, vp=None, ks=None, vs=None, table=None, lens=None)
+    for c in (good(rk, n_tokens=0), good(rk, n_tokens=0, format="q4", max_new=7), good(rk, n_tokens=0, rotary_dim=64)):
+        for start in (None, ONE):
+            assert append(rk, c, k=None, v=None, new_start=start, **none) == 0
+            assert attend(rk, c, ws=None, ws_n=0, q=None, out=None, new_start=start, **none) == 0
+    assert append(rk, good(rk, n_tokens=2)) == -1 and attend(rk, good(rk, n_tokens=2)) == -1
