@@ -8,6 +8,7 @@ There is no CPU fallback: a missing library raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from dataclasses import dataclass, field
 from typing import Optional
@@ -343,7 +344,10 @@ def make_cache(*, n_seqs, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, m
     n_tokens: rows of the packed token tensors (default n_seqs * max_new).  token_major: pages [n_pages, page_size, Hkv, ..]
     in place of [n_pages, Hkv, page_size, ..].  head_lens: lens [n_seqs, Hkv] in place of [n_seqs].  head_tables: table
     [n_seqs, Hkv, max_pages] in place of [n_seqs, max_pages], and pages of one head.  page_strides: (page, head, position)
-    in rows, of arrays that are not contiguous.  Strides of token tensors are taken from the tensors of each call."""
+    in rows, of arrays that are not contiguous.  Strides of token tensors are taken from the tensors of each call.
+
+    The calls refuse a table, lens, new_start, cos, sin [n_positions, rotary_dim / 2], positions [n_tokens] or idx of another shape
+    (table, lens, new_start, cos and sin may have more rows); where strides are set by hand it has to be as long as is read."""
     dt = int(_TYPES.get(dtype, dtype))
     fmt = dt if format is None else int(_TYPES.get(format, format))
     heads = 1 if head_tables else n_kv_heads
@@ -433,8 +437,15 @@ class _Told:
         # entries from the first to the last that is read (strides 0, 0: the library's own)
         span = lambda s, h, n, default: ((c.n_seqs - 1) * (s if s or h else default) + (c.n_kv_heads - 1) * h + n) * (c.n_seqs > 0)  # noqa: E731
         self.n_table = span(c.table_stride_s, c.table_stride_h, c.max_pages, c.max_pages)
-        self.n_lens, self.n_new = span(c.lens_stride_s, c.lens_stride_h, 1, 1), c.n_seqs + 1
-        self.n_tokens, self.n_turns = c.n_tokens, c.n_positions * (c.rotary_dim // 2)
+        self.n_lens = span(c.lens_stride_s, c.lens_stride_h, 1, 1)
+        self.n_turns = c.n_positions * (c.rotary_dim // 2)
+        # their shapes (None where strides set by hand say more than a shape does)
+        heads, width = c.n_kv_heads, c.max_pages
+        self.table = {(0, 0): (c.n_seqs, width), (width, 0): (c.n_seqs, width),
+                      (heads * width, width): (c.n_seqs, heads, width)}.get((c.table_stride_s, c.table_stride_h))
+        self.lens = {(0, 0): (c.n_seqs,), (1, 0): (c.n_seqs,), (heads, 1): (c.n_seqs, heads)}.get((c.lens_stride_s, c.lens_stride_h))
+        self.new, self.turns, self.tokens = (c.n_seqs + 1,), (c.n_positions, c.rotary_dim // 2), (c.n_tokens,)
+        self.grid = (c.n_seqs, c.max_new) if c.n_seqs * c.max_new == c.n_tokens else self.tokens
         self.pages = None                    # the last layout of pages that was found to be the described one
 
 
@@ -467,10 +478,22 @@ def _check_pages(what: str, c: RestkvCache, told: _Told, pages: CachePages) -> i
     return dev
 
 
-def _check_flat(what, dev, dtype, name, t, n):
-    """Address of a contiguous tensor of n values at least."""
-    if t is None or t.dtype is not dtype or t.get_device() != dev or t.numel() < n or not t.is_contiguous():
-        raise RestkvError(-1, f"{what}: {name} has to be contiguous {dtype}, {n} values on GPU {dev}")
+def _reads_as(got, shape, longer) -> bool:
+    """Whether a contiguous tensor of shape `got` holds the described values where the kernels look for them: the same but for
+    dimensions of one, its rows one after the other, or (longer) with rows behind the last that is read."""
+    n = math.prod(shape)
+    if not n or (len(got) == 1 and got[0] == n):
+        return True
+    if longer and len(got) == len(shape) and got[1:] == shape[1:] and got[0] >= shape[0]:
+        return True
+    return [x for x in got if x != 1] == [x for x in shape if x != 1]
+
+
+def _check_flat(what, dev, dtype, name, t, n, shape=None, longer=False):
+    """Address of a contiguous tensor of the given shape, without one of n values at least."""
+    if t is None or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or \
+            (t.numel() < n if shape is None else t.shape != shape and not _reads_as(t.shape, shape, longer)):
+        raise RestkvError(-1, f"{what}: {name} has to be contiguous {dtype}, {n if shape is None else shape} values on GPU {dev}")
     return t.data_ptr()
 
 
@@ -523,8 +546,9 @@ def restkv_append(c: RestkvCache, k, v, pages: CachePages, table, lens, *, new_s
     rotated beside them; lens counts the new tokens already."""
     what, told, i32 = "restkv_append", _told(c), torch.int32
     dev, dt, ref = _check_pages(what, c, told, pages), told.dtype, told.ref
-    tb, ln = _check_flat(what, dev, i32, "table", table, told.n_table), _check_flat(what, dev, i32, "lens", lens, told.n_lens)
-    ns = None if new_start is None else _check_flat(what, dev, i32, "new_start", new_start, told.n_new)
+    tb = _check_flat(what, dev, i32, "table", table, told.n_table, told.table, True)
+    ln = _check_flat(what, dev, i32, "lens", lens, told.n_lens, told.lens, True)
+    ns = None if new_start is None else _check_flat(what, dev, i32, "new_start", new_start, 0, told.new, True)
     kv = _check_rows(what, dev, dt, "k", k, told.kv, told.kv_stride)
     if _check_rows(what, dev, dt, "v", v, told.kv, kv) != kv:
         raise RestkvError(-1, f"{what}: k and v have to have the same strides")
@@ -535,9 +559,12 @@ def restkv_append(c: RestkvCache, k, v, pages: CachePages, table, lens, *, new_s
             raise RestkvError(-1, f"{what}: q and q_out have to have the same strides")
     cs = sn = None
     if told.n_turns:
-        cs = _check_flat(what, dev, torch.float32, "cos", cos, told.n_turns)
-        sn = _check_flat(what, dev, torch.float32, "sin", sin, told.n_turns)
-    ps = None if positions is None else _check_flat(what, dev, i32, "positions", positions, told.n_tokens)
+        cs = _check_flat(what, dev, torch.float32, "cos", cos, 0, told.turns, True)
+        sn = _check_flat(what, dev, torch.float32, "sin", sin, 0, told.turns, True)
+    ps = None
+    if positions is not None:        # (or a row for each sequence, where each has max_new tokens)
+        by_row = positions.dim() == 2 and ns is None and positions.shape == told.grid
+        ps = _check_flat(what, dev, i32, "positions", positions, 0, told.grid if by_row else told.tokens)
     if kv is not told.kv_stride or qs is not told.q_stride:
         ref = _as_strided(c, kv=kv, q=qs)
     _on_gpu(dev, stream, what, lib().restkv_append, ref, k.data_ptr(), v.data_ptr(), pages.k.data_ptr(), pages.v.data_ptr(),
@@ -549,8 +576,9 @@ def restkv_attend(c: RestkvCache, q, pages: CachePages, table, lens, out, lse=No
     """Attention of the newest tokens' queries q [n_tokens, Hq, d] over the pages: out [n_tokens, Hq, d], lse [n_tokens, Hq]."""
     what, told, i32 = "restkv_attend", _told(c), torch.int32
     dev, ref = _check_pages(what, c, told, pages), told.ref
-    tb, ln = _check_flat(what, dev, i32, "table", table, told.n_table), _check_flat(what, dev, i32, "lens", lens, told.n_lens)
-    ns = None if new_start is None else _check_flat(what, dev, i32, "new_start", new_start, told.n_new)
+    tb = _check_flat(what, dev, i32, "table", table, told.n_table, told.table, True)
+    ln = _check_flat(what, dev, i32, "lens", lens, told.n_lens, told.lens, True)
+    ns = None if new_start is None else _check_flat(what, dev, i32, "new_start", new_start, 0, told.new, True)
     qs = _check_rows(what, dev, told.dtype, "q", q, told.q, told.q_stride)
     outs = _check_rows(what, dev, told.out_dtype, "out", out, told.q, told.out_stride)
     ls = told.lse_stride if lse is None else _check_rows(what, dev, torch.float32, "lse", lse, told.lse, told.lse_stride)
@@ -570,11 +598,12 @@ def restkv_fetch(c: RestkvCache, pages: CachePages, table, lens, k_out, v_out, *
     """Rows of the pages as dense k_out, v_out [n_seqs, Hkv, n, d]: positions idx [n_seqs, Hkv, n], or first .. first + n - 1."""
     what, told, i32 = "restkv_fetch", _told(c), torch.int32
     dev = _check_pages(what, c, told, pages)
-    tb, ln = _check_flat(what, dev, i32, "table", table, told.n_table), _check_flat(what, dev, i32, "lens", lens, told.n_lens)
+    tb = _check_flat(what, dev, i32, "table", table, told.n_table, told.table, True)
+    ln = _check_flat(what, dev, i32, "lens", lens, told.n_lens, told.lens, True)
     shape = k_out.shape
     if len(shape) != 4 or shape != (c.n_seqs, c.n_kv_heads, shape[2], c.head_dim) or v_out.shape != shape:
         raise RestkvError(-1, f"{what}: k_out and v_out have to be [n_seqs, Hkv, n, d]")
     kp, vp = _check_flat(what, dev, told.dtype, "k_out", k_out, 0), _check_flat(what, dev, told.dtype, "v_out", v_out, 0)
-    ix = None if idx is None else _check_flat(what, dev, i32, "idx", idx, c.n_seqs * c.n_kv_heads * shape[2])
+    ix = None if idx is None else _check_flat(what, dev, i32, "idx", idx, 0, shape[:3])
     _on_gpu(dev, stream, what, lib().restkv_fetch, told.ref, pages.k.data_ptr(), pages.v.data_ptr(), _addr(pages.k_scale),
             _addr(pages.v_scale), tb, ln, ix, int(first), shape[2], kp, vp)

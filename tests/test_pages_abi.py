@@ -199,3 +199,77 @@ def test_a_call_without_a_token_does_nothing_with_or_without_new_start(rk):
             assert append(rk, c, k=None, v=None, new_start=start, **none) == 0
             assert attend(rk, c, ws=None, ws_n=0, q=None, out=None, new_start=start, **none) == 0
     assert append(rk, good(rk, n_tokens=2)) == -1 and attend(rk, good(rk, n_tokens=2)) == -1
+
+
+@pytest.fixture
+def checks_only(rk, monkeypatch):
+    """The binding's checks of CPU tensors, with nothing behind them."""
+    monkeypatch.setattr(rk.binding, "_check_pages", lambda *a: -1)
+    monkeypatch.setattr(rk.binding, "_on_gpu", lambda *a: None)
+    return rk
+
+
+def i32(*shape):
+    return torch.zeros(shape, dtype=torch.int32)
+
+
+def calls_of(rk, c):
+    """The three calls with tensors as described, of which a case exchanges some."""
+    pages = rk.CachePages(*(torch.zeros(20, 2, 32, 64, dtype=torch.bfloat16) for _ in range(2)))
+    n = c.n_tokens
+    q, kv = torch.zeros(n, 4, 64, dtype=torch.bfloat16), torch.zeros(n, 2, 64, dtype=torch.bfloat16)
+    rows = torch.zeros(c.n_seqs, 2, 5, 64, dtype=torch.bfloat16)
+
+    def go(**over):
+        t = dict(table=i32(c.n_seqs, 6), lens=i32(c.n_seqs), new_start=None, positions=None, cos=torch.zeros(40, 16), sin=torch.zeros(40, 16), idx=None)
+        t.update(over)
+        turns = {x: t[x] for x in ("positions", "cos", "sin")}
+        rk.restkv_append(c, kv, kv, pages, t["table"], t["lens"], new_start=t["new_start"], q=q, q_out=q, **turns)
+        if not {"positions", "cos", "sin", "idx"} & set(over):
+            rk.restkv_attend(c, q, pages, t["table"], t["lens"], q.clone(), new_start=t["new_start"])
+        if not {"positions", "cos", "sin", "new_start"} & set(over):
+            rk.restkv_fetch(c, pages, t["table"], t["lens"], rows, rows.clone(), idx=t["idx"])
+    return go
+
+
+def test_binding_takes_arrays_of_the_described_shape(checks_only):
+    rk = checks_only
+    c = good(rk, rotary_dim=32, n_positions=40, max_new=2)
+    go = calls_of(rk, c)
+    go()
+    # what is read of these is what is meant: more rows than are used, dimensions of one, one row after the other
+    for fine in (dict(table=i32(9, 6)), dict(table=i32(3, 1, 6)), dict(table=i32(18)), dict(lens=i32(7)), dict(lens=i32(3, 1)),
+                 dict(new_start=i32(4)), dict(new_start=i32(9)), dict(positions=i32(6)), dict(positions=i32(1, 6)), dict(positions=i32(3, 2)),
+                 dict(cos=torch.zeros(99, 16), sin=torch.zeros(40, 1, 16)), dict(idx=i32(3, 2, 5)), dict(idx=i32(30))):
+        go(**fine)
+    for wrong in (dict(table=i32(3, 8)), dict(table=i32(6, 6).t()), dict(table=i32(6, 3)), dict(table=i32(3, 2, 6)), dict(table=i32(19)),
+                  dict(lens=i32(3, 2)), dict(lens=i32(2, 3)), dict(new_start=i32(2, 2)), dict(positions=i32(7)), dict(positions=i32(2, 3)),
+                  dict(positions=i32(3, 2), new_start=i32(4)), dict(cos=torch.zeros(40, 32)), dict(sin=torch.zeros(40, 32)), dict(cos=torch.zeros(16, 40)),
+                  dict(idx=i32(3, 2, 6)), dict(idx=i32(2, 3, 5)), dict(idx=i32(4, 2, 5)), dict(idx=i32(31))):
+        with pytest.raises(rk.RestkvError, match="has to be"):
+            go(**wrong)
+
+
+def test_binding_takes_arrays_of_one_sequence_and_by_head(checks_only):
+    rk = checks_only
+    go = calls_of(rk, good(rk, n_seqs=1, rotary_dim=32, n_positions=40))
+    for fine in (dict(table=i32(6)), dict(table=i32(4, 6)), dict(lens=i32(1)), dict(lens=i32(1, 1)), dict(idx=i32(2, 5)), dict(positions=i32(1, 1))):
+        go(**fine)
+    for wrong in (dict(table=i32(1, 8)), dict(lens=i32(1, 2)), dict(idx=i32(2, 6)), dict(idx=i32(5, 2))):
+        with pytest.raises(rk.RestkvError, match="has to be"):
+            go(**wrong)
+    c = good(rk, rotary_dim=32, n_positions=40, head_lens=True, head_tables=True)
+    go = calls_of(rk, c)
+    go(table=i32(3, 2, 6), lens=i32(3, 2))
+    go(table=i32(5, 2, 6), lens=i32(4, 2))
+    for wrong in (dict(table=i32(3, 6)), dict(table=i32(2, 3, 6)), dict(table=i32(3, 2, 8)), dict(lens=i32(6, 3)), dict(lens=i32(2, 3))):
+        with pytest.raises(rk.RestkvError, match="has to be"):
+            go(**{**dict(table=i32(3, 2, 6), lens=i32(3, 2)), **wrong})
+    # strides set by hand: as many entries as are read
+    c = good(rk, rotary_dim=32, n_positions=40, _table_stride_s=8, _lens_stride_s=2)
+    go = calls_of(rk, c)
+    go(table=i32(3, 8), lens=i32(3, 2))
+    go(table=i32(22), lens=i32(5))
+    for wrong in (dict(table=i32(21)), dict(lens=i32(4))):
+        with pytest.raises(rk.RestkvError, match="has to be"):
+            go(**{**dict(table=i32(3, 8), lens=i32(3, 2)), **wrong})
