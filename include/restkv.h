@@ -296,8 +296,8 @@ int restkv_evict(const restkv_params* p, const void* q, const void* k, const voi
  *
  * Limits beside those at the fields: an array of pages has fewer than 2^32 - 1 rows from its first to its last; values are of
  * magnitude 2^80 at most (sums are not divided before the end, so larger ones may pass float32); restkv_attend may refuse
- * max_new * n_q_heads of 2^24 and more (RESTKV_EUNSUPPORTED).  A call without a sequence, a token or a row does nothing and
- * looks at no array.
+ * max_new * n_q_heads of 2^24 and more (RESTKV_EUNSUPPORTED).  Strides by which rows of out, lse or q_out overlap are refused.  A call
+ * without a sequence, a token or a row does nothing and looks at no array.
  */
 #define RESTKV_Q4 4   /* restkv_cache.format: 4-bit codes with a step and a zero for every 32 channels */
 

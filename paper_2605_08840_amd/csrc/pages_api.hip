@@ -63,6 +63,17 @@ static int take_arrays(Pages* pg, const void* k_pages, const void* v_pages, cons
   pg->lens = lens;
   return RESTKV_OK;
 }
+// Whether rows of n values, at i * st + h * sh for tokens i and heads h, share any (their strides are n or more).
+static bool rows_overlap(int64_t st, int64_t sh, int tokens, int heads, int n) {
+  typedef __int128 wide;
+  if (st >= (wide)(heads - 1) * sh + n || sh >= (wide)(tokens - 1) * st + n) return false;
+  for (int h = 1; h < heads; ++h) {
+    // the row h heads on lies between those of tokens i and i + 1
+    const wide i = (wide)h * sh / st, over = (wide)h * sh - i * st;
+    if ((i < tokens && over < n) || (i + 1 < tokens && st - over < n)) return true;
+  }
+  return false;
+}
 static int take_new(Pages* pg, const int32_t* new_start) {
   if (!new_start && pg->n_tokens && (int64_t)pg->n_seqs * pg->max_new > pg->n_tokens) return RESTKV_EINVAL;
   pg->new_start = new_start;
@@ -85,6 +96,7 @@ int restkv_append(const restkv_cache* c, const void* k, const void* v, void* k_p
   if (!rc && pg.n_seqs && pg.n_tokens) rc = take_arrays(&pg, k_pages, v_pages, k_scale, v_scale, table, lens);
   if (rc || !pg.n_seqs || !pg.n_tokens) return rc;
   if (!k || !v || (q && !q_out) || (!q && q_out)) return RESTKV_EINVAL;
+  if (q_out && rows_overlap(pg.q_st, pg.q_sh, pg.n_tokens, pg.Hq, pg.d)) return RESTKV_EINVAL;
   if (pg.rot && (!cos || !sin || pg.n_pos < 1)) return RESTKV_EINVAL;
   if (pg.rot && !positions && pg.lens_sh) return RESTKV_EINVAL;
   return launch_append(pg, k, v, k_pages, v_pages, k_scale, v_scale, positions, cos, sin, q, q_out, (hipStream_t)stream);
@@ -105,6 +117,8 @@ int restkv_attend(const restkv_cache* c, const void* q, const void* k_pages, con
   if (!rc && pg.n_seqs && pg.n_tokens) rc = take_arrays(&pg, k_pages, v_pages, k_scale, v_scale, table, lens);
   if (rc || !pg.n_seqs || !pg.n_tokens) return rc;
   if (!q || !out) return RESTKV_EINVAL;
+  if (rows_overlap(pg.o_st, pg.o_sh, pg.n_tokens, pg.Hq, pg.d)) return RESTKV_EINVAL;
+  if (lse && rows_overlap(pg.lse_st, pg.lse_sh, pg.n_tokens, pg.Hq, 1)) return RESTKV_EINVAL;
   const size_t need = attend_ws_bytes(pg);
   if (need && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need)) return RESTKV_EWORKSPACE;
   return launch_attend(pg, q, k_pages, v_pages, k_scale, v_scale, out, lse, (char*)workspace, (hipStream_t)stream);

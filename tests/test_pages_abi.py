@@ -273,3 +273,30 @@ def test_binding_takes_arrays_of_one_sequence_and_by_head(checks_only):
     for wrong in (dict(table=i32(21)), dict(lens=i32(4))):
         with pytest.raises(rk.RestkvError, match="has to be"):
             go(**{**dict(table=i32(3, 8), lens=i32(3, 2)), **wrong})
+
+
+def test_outputs_whose_rows_overlap_are_refused(rk):
+    """Rows of different tokens and heads at the same place: each would hold what was written last."""
+    def out(t, h, **kw):          # past the strides a call without its workspace is refused for that
+        c = good(rk, max_pages=600, n_pages=900, _out_stride_t=t, _out_stride_h=h, **kw)
+        return attend(rk, c, ws=None)
+
+    def lse(t, h):
+        return attend(rk, good(rk, max_pages=600, n_pages=900, _lse_stride_t=t, _lse_stride_h=h), ws=None, lse=ONE)
+
+    # 3 tokens, 4 heads: tokens outermost, heads outermost, gaps, rows that interleave
+    for t, h in ((256, 64), (300, 70), (64, 192), (70, 300), (128, 384), (512, 128), (64, 200), (448, 128)):
+        assert out(t, h) == -3, (t, h)
+    for t, h in ((128, 64), (192, 64), (64, 64), (64, 128), (255, 64), (64, 191), (100, 130), (65, 66), (384, 192)):
+        assert out(t, h) == -1, (t, h)
+    assert out(64, 100, n_q_heads=2) == -1 and out(64, 200, n_q_heads=2) == -3
+    for t, h in ((4, 1), (1, 3), (7, 2), (2, 7)):
+        assert lse(t, h) == -3, (t, h)
+    for t, h in ((3, 1), (1, 2), (1, 1), (2, 4)):
+        assert lse(t, h) == -1, (t, h)
+    # a single token or head; strides of a log-sum-exp that is not asked for
+    assert out(64, 64, n_seqs=1) == -3 and out(64, 64, n_q_heads=1, n_kv_heads=1) == -3
+    assert attend(rk, good(rk, max_pages=600, n_pages=900, _lse_stride_t=1), ws=None) == -3
+    # rotated queries; queries that are only read may overlap
+    assert append(rk, good(rk, _q_stride_t=128), q=ONE, q_out=ONE) == -1
+    assert attend(rk, good(rk, max_pages=600, n_pages=900, _q_stride_t=128), ws=None) == -3
