@@ -68,7 +68,14 @@ AttendPlan attend_plan(const Pages& pg) {
   // 24 rows 32.4 / 31.6, 32 rows 33.5 / 31.7, 64 rows 41.1 / 34.4, 128 rows 62 / 46.
   const int64_t rows = (int64_t)pg.G * pg.max_new;
   p.many = pg.fmt == RESTKV_BF16 && rows > 16;
-  p.R = rows <= (p.many ? 64 : 16) ? 1 : 2;
+  // Two blocks of 16 rows a wavefront where one leaves rows for a second workgroup, which would read the tiles again.  One / two, us,
+  // 32k keys of 8 KV heads of 128: bf16 64 rows 34.7 / 43.6, 96 rows 43.7 / 45.8, 256 rows 79.9 / 70.0 (16 caches of 2k keys,
+  // 96 rows 59.4 / 57.9, 256 rows 88.8 / 120.5); 4 bits 32 rows 31.6 / 33.8, 64 rows 49.7 / 43.6, with float32 output 43.7 / 41.2,
+  // 75.2 / 57.8 and 256 rows 290 / 188; f32 pages 32 rows 70.5 / 63.6, 64 rows 118 / 91, 256 rows 437 / 326.  But not for float32 queries over
+  // 4 bits of 128 channels: two blocks of their three parts are more than the registers hold (32 rows 45.8 / 75.6, 64 rows 79 / 108,
+  // 256 rows 304 / 322).
+  const bool wide_q = pg.fmt == RESTKV_Q4 && pg.dtype == RESTKV_F32 && pg.d == 128;
+  p.R = rows <= (p.many ? 64 : 16) || wide_q ? 1 : 2;
   const bool per_head = pg.lens_sh != 0;
   // eight wavefronts on one copy of a tile, where blocks of so many rows leave no more of them empty than those of four do
   p.waves = p.many && p.R == 2 && (rows + 127) / 128 % 2 == 0 ? 8 : 4;
@@ -85,7 +92,7 @@ AttendPlan attend_plan(const Pages& pg) {
   // sequence of 2 KV heads with 2 rows each and one of 8 with 64 rows: bf16 192 keys 6.6 / 8.4 and 10.8 / 11.5, 384 keys 8.3 / 8.5
   // and 14.7 / 12.9, 512 keys 9.3 / 8.7; 4 bits 512 keys 9.2 / 10.0, 768 keys 11.4 / 9.9, 64 rows 384 keys 15.7 / 14.4;
   // f32 192 keys 8.3 / 9.8, 256 keys 9.9 / 9.9, 64 rows 192 keys 14.7 / 14.3.
-  const int alone = p.R > 1 || p.many ? (pg.fmt == RESTKV_F32 ? 2 : 4) : pg.fmt == RESTKV_F32 ? 3 : pg.fmt == RESTKV_BF16 ? 6 : 8;
+  const int alone = rows > 16 ? (pg.fmt == RESTKV_F32 ? 2 : 4) : pg.fmt == RESTKV_F32 ? 3 : pg.fmt == RESTKV_BF16 ? 6 : 8;
   if (tiles <= alone) p.c_min = std::max(p.c_min, (int)tiles);
   // no entry has two chunks: chunks hold the sum of all tiles, or the longest entry fits the smallest chunk
   const bool single = each >= p.target || tiles <= p.c_min;

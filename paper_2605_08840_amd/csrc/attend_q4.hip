@@ -14,7 +14,9 @@ int run_attend_q4(const AttendArgs& a, int R, hipStream_t st) {
       if (rows <= 4) return run_attend<FMT_Q4, T, D, NP, 1, 4>(a, st);
       if (rows <= 8) return run_attend<FMT_Q4, T, D, NP, 1, 2>(a, st);
     }
-    return R == 1 ? run_attend<FMT_Q4, T, D, NP, 1>(a, st) : run_attend<FMT_Q4, T, D, NP, 2>(a, st);
+    if constexpr (planes_of<T> == 1 || D == 64)
+      if (R == 2) return run_attend<FMT_Q4, T, D, NP, 2>(a, st);
+    return run_attend<FMT_Q4, T, D, NP, 1>(a, st);
   };
   auto by_d = [&](auto np, auto t) {
     return a.pg.d == 128 ? go(std::integral_constant<int, 128>{}, np, t) : go(std::integral_constant<int, 64>{}, np, t);
