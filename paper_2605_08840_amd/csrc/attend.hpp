@@ -575,19 +575,25 @@ void k_attend(AttendArgs a) {
       }
       __builtin_amdgcn_wave_barrier();
       *(Words<NG>*)&s_kz[lane * NG] = sk[0];
-      // Zeros stand for the values' scales of slots that nobody sees, and of keys that some rows see wherever what the
-      // weights are multiplied with (zero + BASE step; not finite for finite steps of 2^124 too) would make NaN of a weight of 0.
-      if (masked && n >= there(j)) sv[0] = Words<NG>{};
+      if (masked) {
+        // Zeros stand for the values' scales of slots that nobody sees, and of keys that some rows see wherever what the
+        // weights are multiplied with (zero + BASE step; not finite for finite steps of 2^124 too) would make NaN of a weight of 0.
+        if (n >= there(j)) sv[0] = Words<NG>{};
+#pragma unroll
+        for (int f = 0; f < NG; ++f) {
+          const float z = __builtin_fmaf(BASE, __uint_as_float(sv[0][f] << 16), __uint_as_float(sv[0][f] & 0xFFFF0000u));
+          if (!(z - z == 0.f)) {
+            sv[0][f] = 0u;
+            odd_scales = true;
+          }
+        }
+      }
 #pragma unroll
       for (int f = 0; f < NG; ++f) {
-        float st = __uint_as_float(sv[0][f] << 16), z = __builtin_fmaf(BASE, st, __uint_as_float(sv[0][f] & 0xFFFF0000u));
-        if (masked && !(z - z == 0.f)) {
-          st = z = 0.f;
-          odd_scales = true;
-        }
+        const float st = __uint_as_float(sv[0][f] << 16);
         s_ks[f * 64 + lane] = __uint_as_float(sk[0][f] << 16);
         s_vs[f * 64 + lane] = st;
-        s_vz[f * 64 + lane] = z;
+        s_vz[f * 64 + lane] = __builtin_fmaf(BASE, st, __uint_as_float(sv[0][f] & 0xFFFF0000u));
       }
       odd_scales = __ballot(odd_scales);
       if (more) load_scales(next);
