@@ -289,10 +289,12 @@ int restkv_evict(const restkv_params* p, const void* q, const void* k, const voi
  * New tokens are packed: those of sequence s are rows new_start[s] .. new_start[s+1]-1 of the token tensors
  * (new_start NULL: max_new of each sequence).  Rows outside all sequences are left as they are.
  *
- * Values on the device cannot be refused.  A length beyond the room (max_len) or below 0, a new_start outside
- * [0, n_tokens] or falling, counts as brought inside; a sequence takes part with its first max_new new tokens at most; a
- * position without a page (its table entry outside [0, n_pages)) is neither written nor seen.  Table entries behind
- * the last position in use are not read as pages.  Two positions of one call must not share a slot.
+ * Values on the device cannot be refused.  A length below 0 counts as 0; of one beyond the room (max_len) the places of the new
+ * tokens follow, and what they see, but no position from max_len on is written or seen.  A new_start outside [0, n_tokens], or
+ * below the one before it, counts as brought inside (a row that two sequences then claim belongs to either); a sequence takes
+ * part with its first max_new new tokens at most, and its places follow from the number that does; a position without a page
+ * (its table entry outside [0, n_pages)) is neither written nor seen.  Table entries behind the last position in use are not
+ * read as pages.  Two positions of one call must not share a slot.
  *
  * Limits beside those at the fields: an array of pages has fewer than 2^32 - 1 rows from its first to its last; values are of
  * magnitude 2^80 at most (sums are not divided before the end, so larger ones may pass float32); restkv_attend may refuse
@@ -338,7 +340,7 @@ typedef struct restkv_cache {
  *   positions [n_tokens] int32: where each token stands in its text (an evicted cache is shorter than the text);
  *           NULL: its cache position (not with lens per head).  A token whose position lies outside [0, n_positions)
  *           is left out: nothing of it is written
- *   cos, sin [n_positions, rotary_dim/2] float32;  with rotary_dim = 0 all three may be NULL
+ *   cos, sin [n_positions, rotary_dim/2] float32;  with rotary_dim = 0 none of the three is looked at
  * y[a] = x[a] cos - x[b] sin, y[b] = x[b] cos + x[a] sin for the channels a, b that turn together, in float32 with
  * each product and each sum rounded, then rounded once to the type of the pages (4-bit: the codes are made from float32).
  */

@@ -150,8 +150,8 @@ __device__ __forceinline__ uint32_t unit_codes(const float (&x)[UN], int u, uint
 // the d/16 channels of a unit: accesses run along rows, and a group's extremes are a reduction over sixteen lanes.  U = 4 has
 // four rows a lane in flight and reads the angles once for them; few tokens take U = 1, for more wavefronts.  Many tokens' queries
 // go past the caches, their pages do not (2 / (G + 2) of it, and who attends or fetches reads them next).
-// Bound by memory: 16 x 8k tokens of 32 and 8 heads of 128 bf16, 822 MB in 143.7 us (5.7 TB/s); into 4 bits by vector instructions too,
-// ten a code: 8k tokens 183 MB in 36.7 us.  32 tokens of a decoding step 4.0 us, a chain of lengths, page and rows.
+// Bound by memory: 32k tokens of 32 and 8 heads of 128 bf16, 822 MB in 143.9 us (5.7 TB/s); into 4 bits by vector instructions too,
+// ten a code: 8k tokens 183 MB in 36.7 us.  32 tokens of a decoding step 3.6 us, a chain of lengths, page and rows.
 template <typename T, int D, bool Q4, bool VEC, int U, bool PAST>
 __global__ __launch_bounds__(256) void k_append(Pages pg, const T* k, const T* v, char* k_pages, char* v_pages,
                                                 uint32_t* k_scale, uint32_t* v_scale, const int32_t* __restrict__ positions,
@@ -281,8 +281,9 @@ int run_append(const Pages& pg, const void* k, const void* v, void* k_pages, voi
     hipLaunchKernelGGL(kern, wide_grid(((int64_t)pg.n_tokens * parts + 3) / 4), dim3(256), 0, st, pg, (const T*)k, (const T*)v, (char*)k_pages,
                        (char*)v_pages, (uint32_t*)k_scale, (uint32_t*)v_scale, positions, cos, sin, (const T*)q, (T*)q_out, parts, n_rows);
   };
-  // more than the last-level cache holds, each row once: read past the caches (32k tokens of 32 and 8 heads of 128 bf16 147 -> 127 us, but 100 MB that the last
-  // call has read too: 36 -> 40)
+  // More than the last-level cache holds, each row once: read past the caches.  With the caches / past them, us, tokens of 32 and 8 heads
+  // of 128 bf16, three inputs in turn: 24k tokens 110.6 / 104.9, 32k 145.9 / 145.3, 64k 286.9 / 289.1, 64k into 4 bits 274.7 / 267.5; what the
+  // last call has read too, 32k 146.9 / 129.8, 64k 286.7 / 269.7, but 100 MB 36 / 40.
   const bool once = !(pg.rot && !pg.rot_pairs && pg.rot != D);
   const bool past = once && (int64_t)pg.n_tokens * n_rows * D * (int)sizeof(T) > (int64_t)256 << 20;
   if (!vec) go(k_append<T, D, Q4, false, 1, false>, 1);

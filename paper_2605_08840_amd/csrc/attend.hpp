@@ -8,8 +8,10 @@
 // memory into operand registers without LDS: a key operand is 16 bytes of a row, a value operand takes the same channel
 // of eight keys, which a lane that has loaded a unit of d/16 channels of each of them holds already (one byte
 // permute for two values).
-// Bound by memory (128k bf16 positions of 8 KV heads of 128, 537 MB in 89 us, 6.0 TB/s), for 4 bits by vector instructions as much
-// (168 MB in 36.5 us, about 500 instructions a tile of 64 keys), for short caches by a chain of lengths, pages, keys.
+// Bound by memory for bf16 (128k positions of 8 KV heads of 128, 537 MB in 89 us, 6.0 TB/s).  4 bits: by no one pipe (the same positions,
+// 168 MB in 37.3 us: 4.5 TB/s, about 500 vector instructions a tile of 64 keys, which issue half of the time, matrix pipe 15 %) but by
+// what two wavefronts a SIMD do not overlap, and by the longest chunk, nine passes of the loop where the mean is eight.  Short caches: by
+// a chain of lengths, pages, keys.
 #pragma once
 
 #include "pages.hpp"
@@ -51,10 +53,13 @@ __device__ __forceinline__ int wave_scan(int x) {
   return x;
 }
 
-// What a workgroup takes.  Chunks are of nearly equal size over all entries, so that a long sequence among short ones is cut as
-// finely as the whole asks for: of C tiles at most, where all of them are as many workgroups as the chip holds at a time (a
-// few more would run alone at the end; an entry has half a chunk more than its tiles over C, in the mean).  Up to 64 entries a
-// wavefront works this out by itself, more are divided among the threads of the workgroup.
+// What a workgroup takes.  An entry is cut into as few chunks of at most C tiles as it needs, with one C for all entries, so that a long
+// sequence among short ones is cut as finely as the whole asks for, and C such that all chunks are fewer than the workgroups that the
+// chip holds at a time (a few more would run alone at the end).  C is on the large side: an entry counts as half a chunk more than its tiles
+// over C, in the mean, and one tile is added for the rounding.  So the longest chunk is above an even share, and takes the more
+// passes: one sequence of 2048 tiles for 64 workgroups makes 63 chunks of up to 33, 24 sequences of 1 to 250 tiles (24.2 a workgroup) 61 of
+// up to 35, 256 entries of 9 to 33 tiles 497 of up to 13 for 512 workgroups (9.3 each).  Up to 64 entries a wavefront works this out by
+// itself, more are divided among the threads of the workgroup.
 struct Chunk { int e, tile0, tile1, index, count, slot0, told, first, n; };
 struct Entry { int told, first, n, tiles; };
 __device__ __forceinline__ Entry read_entry(const AttendArgs& a, int e) {
@@ -87,7 +92,7 @@ __device__ __forceinline__ bool find_chunk(const AttendArgs& a, int x, int* lds,
     const Entry en = read_entry(a, lane);
     int C = chunk_tiles(a, (float)wave_sum((uint32_t)en.tiles), __popcll(__ballot(en.tiles > 0)));
     int cnt = 0, inc = 0;
-    for (int i = 0; i < 8; ++i) {       // (until they are as many as wanted: a few too many cost a sixth of the time of 24 lengths)
+    for (int i = 0; i < 8; ++i) {       // (until they are fewer than the resident workgroups: a few too many cost a sixth of the time of 24 lengths)
       cnt = lane < a.entries ? max(1, (en.tiles + C - 1) / C) : 0;
       inc = wave_scan(cnt);
       if (__builtin_amdgcn_readlane(inc, 63) <= a.chunks || a.entries >= a.chunks) break;
@@ -323,8 +328,12 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t x, int i, uint32_t mask, 
   return __builtin_amdgcn_perm(__float_as_uint(__uint_as_float(w & 0xFFFF0000u) - 24.f), __float_as_uint(__uint_as_float(w << 16) - 24.f), 0x07060302u);
 }
 
-// FMT: pages; T: queries; NP: bf16 parts of a softmax weight (products with float32 pages take the weight itself); R: blocks
-// of 16 rows of a wavefront.  Of a tile the keys are loaded anew (for the next one) as soon as the logits are there, the
+// FMT: pages; T: queries; R: blocks of 16 rows of a wavefront; NP: bf16 parts of a softmax weight (products with float32 pages take
+// the weight itself).  Three hold all its bits, for float32 output.  bf16 output has two, 2^-17 beside the 2^-8 of its own rounding: 0.2 % of
+// its values (4 bits, 16 + code in place of the code: 1.5 %) are not the nearest bf16 but its neighbour, where sums in float32 leave 0.03 to 0.2 %,
+// and the error against 64 bits is the same, 1.7e-3 of the norm.  Three parts there take up to 2 % more time with few rows of bf16 pages, 12 % with
+// many, 3 to 15 % with 4 bits (and leave 0.8 %), centred codes 28 to 45 % (0.2 %).
+// Of a tile the keys are loaded anew (for the next one) as soon as the logits are there, the
 // values as soon as they are in the sums: a load has the other half's arithmetic, and other wavefronts', to come back,
 // and costs no second set of registers.
 // SP (4-bit pages, up to 16 / SP rows): the sixteen columns are SP copies of the rows, and copy x takes the 16-key blocks x,

@@ -1,5 +1,6 @@
-// Attention over bfloat16 pages for many rows (the queries of an observation window, prompts): the matrix pipe is what bounds
-// it, so a tile of 64 keys and values is copied to LDS once for the 64 R rows of a workgroup.
+// Attention over bfloat16 pages for many rows (the queries of an observation window, prompts): products and softmax take longer
+// than memory, so a tile of 64 keys and values is copied to LDS once for the rows of a workgroup, 16 R for each of its four or
+// eight wavefronts: 64 to 256.
 #include "attend.hpp"
 
 namespace restkv {
@@ -11,9 +12,10 @@ namespace {
 // pieces of a row in the order piece ^ row, so that the reads of one piece of sixteen rows spread over the banks.
 // 256 queries a KV head, 32k keys, d 128, float32 output (three parts of a weight: 69 GFLOP of products for 34), us a call with
 // the join of its chunks, 83.4 now: four wavefronts 89.6, eight 87.2 (half the copies); two tiles a copy and a barrier 90.8.  Of that,
-// without the copies 8 would go, without the second and third part of the weights 20, without the exponentials 3: no
-// one pipe bounds it, matrix and vector instructions add up (a wavefront alone takes 4500 cycles a tile, 2048 of them products),
-// and 33 MB of chunk sums are written and read again.
+// without the copies 8 would go, without the second and third part of the weights 20, without the exponentials 3.  No pipe is full
+// (matrix 36 % busy, vector issue 41 %): the two wavefronts of a SIMD do the same at the same time, behind one barrier a tile, so that products
+// and softmax follow each other (a wavefront alone takes 4500 cycles a tile, 2048 of them products); 31 chunks of up to 17 tiles stand
+// for 32 of 16, and 33 MB of chunk sums are written and read again.
 template <int D, int NP, int R, int NW>
 __global__ __attribute__((amdgpu_flat_work_group_size(64 * NW, 64 * NW), amdgpu_waves_per_eu(2)))
 void k_attend_rows(AttendArgs a) {

@@ -62,7 +62,7 @@ __device__ __forceinline__ uint32_t row_of(const Pages& pg, int page, int h, int
 }
 
 // Words of a store or load; PAST: past the caches (nontemporal), for what is more than they hold, a whole line at a time.  What is
-// written so is on its way before the kernel's end flushes the L2s: append of 16 x 8k tokens, whose queries are two thirds of
+// written so is on its way before the kernel's end flushes the L2s: append of 32k tokens, whose queries are two thirds of
 // it, 157 -> 143 us, fetch of 4-bit rows (10 MB into 34) 10.8 -> 9.7, of 270 MB with loads as they were 106 -> 98.
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 template <int N> struct WordsOf { typedef uint32_t type __attribute__((ext_vector_type(N))); };
@@ -97,17 +97,19 @@ __device__ __forceinline__ int order_of(float x) {
 }
 __device__ __forceinline__ float of_order(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7FFFFFFF)); }
 // Least and greatest over the sixteen lanes of a wavefront's row, in every lane.
+template <int CTRL>
+__device__ __forceinline__ int row_ror(int x) { return __builtin_amdgcn_mov_dpp(x, CTRL, 0xF, 0xF, true); }
 __device__ __forceinline__ int row16_min(int x) {
-#define RK_STEP(ctrl) x = min(x, (int)__builtin_amdgcn_mov_dpp(x, ctrl, 0xF, 0xF, true))
-  RK_STEP(0x121); RK_STEP(0x122); RK_STEP(0x124); RK_STEP(0x128);
-  return x;
+  x = min(x, row_ror<0x121>(x));        // by 1, 2, 4 and 8 lanes
+  x = min(x, row_ror<0x122>(x));
+  x = min(x, row_ror<0x124>(x));
+  return min(x, row_ror<0x128>(x));
 }
 __device__ __forceinline__ int row16_max(int x) {
-#undef RK_STEP
-#define RK_STEP(ctrl) x = max(x, (int)__builtin_amdgcn_mov_dpp(x, ctrl, 0xF, 0xF, true))
-  RK_STEP(0x121); RK_STEP(0x122); RK_STEP(0x124); RK_STEP(0x128);
-#undef RK_STEP
-  return x;
+  x = max(x, row_ror<0x121>(x));
+  x = max(x, row_ror<0x122>(x));
+  x = max(x, row_ror<0x124>(x));
+  return max(x, row_ror<0x128>(x));
 }
 
 // Step and zero of a group from its extremes; inverse: 1/step, or 0.
