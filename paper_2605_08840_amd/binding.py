@@ -434,18 +434,21 @@ class _Told:
         self.kv_stride, self.q_stride, self.out_stride, self.lse_stride = (
             (c.kv_stride_t, c.kv_stride_h, 1), (c.q_stride_t, c.q_stride_h, 1), (c.out_stride_t, c.out_stride_h, 1),
             (c.lse_stride_t, c.lse_stride_h))
-        # entries from the first to the last that is read (strides 0, 0: the library's own)
+        # flat arrays, as _check_flat takes them; where strides set by hand say more than a shape does, by the entries from the first
+        # to the last that is read (strides 0, 0: the library's own)
         span = lambda s, h, n, default: ((c.n_seqs - 1) * (s if s or h else default) + (c.n_kv_heads - 1) * h + n) * (c.n_seqs > 0)  # noqa: E731
-        self.n_table = span(c.table_stride_s, c.table_stride_h, c.max_pages, c.max_pages)
+        n_seqs, heads, width, i32 = c.n_seqs, c.n_kv_heads, c.max_pages, torch.int32
+        self.n_table = span(c.table_stride_s, c.table_stride_h, width, width)
         self.n_lens = span(c.lens_stride_s, c.lens_stride_h, 1, 1)
-        self.n_turns = c.n_positions * (c.rotary_dim // 2)
-        # their shapes (None where strides set by hand say more than a shape does)
-        heads, width = c.n_kv_heads, c.max_pages
-        self.table = {(0, 0): (c.n_seqs, width), (width, 0): (c.n_seqs, width),
-                      (heads * width, width): (c.n_seqs, heads, width)}.get((c.table_stride_s, c.table_stride_h))
-        self.lens = {(0, 0): (c.n_seqs,), (1, 0): (c.n_seqs,), (heads, 1): (c.n_seqs, heads)}.get((c.lens_stride_s, c.lens_stride_h))
-        self.new, self.turns, self.tokens = (c.n_seqs + 1,), (c.n_positions, c.rotary_dim // 2), (c.n_tokens,)
-        self.grid = (c.n_seqs, c.max_new) if c.n_seqs * c.max_new == c.n_tokens else self.tokens
+        shape = {(0, 0): (n_seqs, width), (width, 0): (n_seqs, width), (heads * width, width): (n_seqs, heads, width)}
+        self.table = (shape.get((c.table_stride_s, c.table_stride_h)), i32, "table", self.n_table)
+        shape = {(0, 0): (n_seqs,), (1, 0): (n_seqs,), (heads, 1): (n_seqs, heads)}
+        self.lens = (shape.get((c.lens_stride_s, c.lens_stride_h)), i32, "lens", self.n_lens)
+        self.new = ((n_seqs + 1,), i32, "new_start", 0)
+        self.cos, self.sin = (((c.n_positions, c.rotary_dim // 2), torch.float32, name, 0) for name in ("cos", "sin"))
+        self.turns = c.n_positions * (c.rotary_dim // 2) != 0
+        self.positions = ((c.n_tokens,), i32, "positions", None)
+        self.grid = ((n_seqs, c.max_new), i32, "positions", None) if n_seqs * c.max_new == c.n_tokens else self.positions
         self.pages = None                    # the last layout of pages that was found to be the described one
 
 
@@ -478,22 +481,25 @@ def _check_pages(what: str, c: RestkvCache, told: _Told, pages: CachePages) -> i
     return dev
 
 
-def _reads_as(got, shape, longer) -> bool:
-    """Whether a contiguous tensor of shape `got` holds the described values where the kernels look for them: the same but for
-    dimensions of one, its rows one after the other, or (longer) with rows behind the last that is read."""
-    n = math.prod(shape)
-    if not n or (len(got) == 1 and got[0] == n):
+def _reads_as(t, shape, n) -> bool:
+    """Whether a contiguous tensor holds the described values where the kernels look for them: the same but for dimensions of
+    one, its rows one after the other, or (unless n is None) with rows behind the last that is read; without a shape n values."""
+    if shape is None:
+        return t.numel() >= n
+    got, total = t.shape, math.prod(shape)
+    if not total or (len(got) == 1 and got[0] == total):
         return True
-    if longer and len(got) == len(shape) and got[1:] == shape[1:] and got[0] >= shape[0]:
+    if n is not None and len(got) == len(shape) and got[1:] == shape[1:] and got[0] >= shape[0]:
         return True
     return [x for x in got if x != 1] == [x for x in shape if x != 1]
 
 
-def _check_flat(what, dev, dtype, name, t, n, shape=None, longer=False):
-    """Address of a contiguous tensor of the given shape, without one of n values at least."""
+def _check_flat(what, dev, t, told):
+    """Address of a contiguous tensor that is as told: (shape, type, name, n); see _reads_as."""
+    shape, dtype, name, n = told
     if t is None or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or \
-            (t.numel() < n if shape is None else t.shape != shape and not _reads_as(t.shape, shape, longer)):
-        raise RestkvError(-1, f"{what}: {name} has to be contiguous {dtype}, {n if shape is None else shape} values on GPU {dev}")
+            (t.shape != shape and not _reads_as(t, shape, n)):
+        raise RestkvError(-1, f"{what}: {name} has to be contiguous {dtype}, {shape or n} values on GPU {dev}")
     return t.data_ptr()
 
 
@@ -544,11 +550,10 @@ def restkv_append(c: RestkvCache, k, v, pages: CachePages, table, lens, *, new_s
                   q=None, q_out=None, stream=None):
     """New keys (rotated by their positions) and values [n_tokens, Hkv, d] into the pages, and new queries [n_tokens, Hq, d]
     rotated beside them; lens counts the new tokens already."""
-    what, told, i32 = "restkv_append", _told(c), torch.int32
+    what, told = "restkv_append", _told(c)
     dev, dt, ref = _check_pages(what, c, told, pages), told.dtype, told.ref
-    tb = _check_flat(what, dev, i32, "table", table, told.n_table, told.table, True)
-    ln = _check_flat(what, dev, i32, "lens", lens, told.n_lens, told.lens, True)
-    ns = None if new_start is None else _check_flat(what, dev, i32, "new_start", new_start, 0, told.new, True)
+    tb, ln = _check_flat(what, dev, table, told.table), _check_flat(what, dev, lens, told.lens)
+    ns = None if new_start is None else _check_flat(what, dev, new_start, told.new)
     kv = _check_rows(what, dev, dt, "k", k, told.kv, told.kv_stride)
     if _check_rows(what, dev, dt, "v", v, told.kv, kv) != kv:
         raise RestkvError(-1, f"{what}: k and v have to have the same strides")
@@ -558,13 +563,12 @@ def restkv_append(c: RestkvCache, k, v, pages: CachePages, table, lens, *, new_s
         if q_out is not q and _check_rows(what, dev, dt, "q_out", q_out, told.q, qs) != qs:
             raise RestkvError(-1, f"{what}: q and q_out have to have the same strides")
     cs = sn = None
-    if told.n_turns:
-        cs = _check_flat(what, dev, torch.float32, "cos", cos, 0, told.turns, True)
-        sn = _check_flat(what, dev, torch.float32, "sin", sin, 0, told.turns, True)
+    if told.turns:
+        cs, sn = _check_flat(what, dev, cos, told.cos), _check_flat(what, dev, sin, told.sin)
     ps = None
     if positions is not None:        # (or a row for each sequence, where each has max_new tokens)
-        by_row = positions.dim() == 2 and ns is None and positions.shape == told.grid
-        ps = _check_flat(what, dev, i32, "positions", positions, 0, told.grid if by_row else told.tokens)
+        by_row = ns is None and positions.shape == told.grid[0]
+        ps = _check_flat(what, dev, positions, told.grid if by_row else told.positions)
     if kv is not told.kv_stride or qs is not told.q_stride:
         ref = _as_strided(c, kv=kv, q=qs)
     _on_gpu(dev, stream, what, lib().restkv_append, ref, k.data_ptr(), v.data_ptr(), pages.k.data_ptr(), pages.v.data_ptr(),
@@ -574,11 +578,10 @@ def restkv_append(c: RestkvCache, k, v, pages: CachePages, table, lens, *, new_s
 def restkv_attend(c: RestkvCache, q, pages: CachePages, table, lens, out, lse=None, workspace=None, *, new_start=None,
                   stream=None):
     """Attention of the newest tokens' queries q [n_tokens, Hq, d] over the pages: out [n_tokens, Hq, d], lse [n_tokens, Hq]."""
-    what, told, i32 = "restkv_attend", _told(c), torch.int32
+    what, told = "restkv_attend", _told(c)
     dev, ref = _check_pages(what, c, told, pages), told.ref
-    tb = _check_flat(what, dev, i32, "table", table, told.n_table, told.table, True)
-    ln = _check_flat(what, dev, i32, "lens", lens, told.n_lens, told.lens, True)
-    ns = None if new_start is None else _check_flat(what, dev, i32, "new_start", new_start, 0, told.new, True)
+    tb, ln = _check_flat(what, dev, table, told.table), _check_flat(what, dev, lens, told.lens)
+    ns = None if new_start is None else _check_flat(what, dev, new_start, told.new)
     qs = _check_rows(what, dev, told.dtype, "q", q, told.q, told.q_stride)
     outs = _check_rows(what, dev, told.out_dtype, "out", out, told.q, told.out_stride)
     ls = told.lse_stride if lse is None else _check_rows(what, dev, torch.float32, "lse", lse, told.lse, told.lse_stride)
@@ -596,14 +599,13 @@ def restkv_attend(c: RestkvCache, q, pages: CachePages, table, lens, out, lse=No
 
 def restkv_fetch(c: RestkvCache, pages: CachePages, table, lens, k_out, v_out, *, idx=None, first=0, stream=None):
     """Rows of the pages as dense k_out, v_out [n_seqs, Hkv, n, d]: positions idx [n_seqs, Hkv, n], or first .. first + n - 1."""
-    what, told, i32 = "restkv_fetch", _told(c), torch.int32
+    what, told = "restkv_fetch", _told(c)
     dev = _check_pages(what, c, told, pages)
-    tb = _check_flat(what, dev, i32, "table", table, told.n_table, told.table, True)
-    ln = _check_flat(what, dev, i32, "lens", lens, told.n_lens, told.lens, True)
+    tb, ln = _check_flat(what, dev, table, told.table), _check_flat(what, dev, lens, told.lens)
     shape = k_out.shape
     if len(shape) != 4 or shape != (c.n_seqs, c.n_kv_heads, shape[2], c.head_dim) or v_out.shape != shape:
         raise RestkvError(-1, f"{what}: k_out and v_out have to be [n_seqs, Hkv, n, d]")
-    kp, vp = _check_flat(what, dev, told.dtype, "k_out", k_out, 0), _check_flat(what, dev, told.dtype, "v_out", v_out, 0)
-    ix = None if idx is None else _check_flat(what, dev, i32, "idx", idx, 0, shape[:3])
+    kp, vp = _check_flat(what, dev, k_out, (shape, told.dtype, "k_out", None)), _check_flat(what, dev, v_out, (shape, told.dtype, "v_out", None))
+    ix = None if idx is None else _check_flat(what, dev, idx, (shape[:3], torch.int32, "idx", None))
     _on_gpu(dev, stream, what, lib().restkv_fetch, told.ref, pages.k.data_ptr(), pages.v.data_ptr(), _addr(pages.k_scale),
             _addr(pages.v_scale), tb, ln, ix, int(first), shape[2], kp, vp)
