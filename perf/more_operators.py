@@ -235,6 +235,8 @@ def prepare(case, seed):
                                                           ("k_pages", "v_pages")))) for i in range(layers)]
         if c["op"] == "attend":
             st["workspace"] = rk.alloc_attend_beams_workspace(st["cache"], beams)
+        else:
+            st["layers"] = rk.CacheLayers(st["pages"])
     return st
 
 
@@ -246,7 +248,7 @@ def run(st):
             rk.restkv_beam_select(st["beams"], st["logits"], st["scores"], st["new_scores"], st["parents"], st["tokens"], st["workspace"],
                                   finished=st["finished"], new_finished=st["new_finished"])
         elif c["op"] == "reorder":
-            rk.restkv_beam_reorder(st["cache"], c["n_beams"], st["parents"], st["table"], st["lens"], st["pages"], st["table_out"])
+            rk.restkv_beam_reorder(st["cache"], c["n_beams"], st["parents"], st["table"], st["lens"], st["layers"], st["table_out"])
         else:
             rk.restkv_attend_beams(st["cache"], c["n_beams"], st["shared"], st["q"], st["pages"][0], st["table"], st["lens"], st["out"],
                                    st["lse"], st["workspace"], new_start=st["new_start"])
