@@ -378,6 +378,84 @@ int restkv_fetch(const restkv_cache* c, const void* k_pages, const void* v_pages
                  void* v_out, restkv_stream_t stream);
 
 /*
+ * ---- Beams -------------------------------------------------------------------
+ * Requests that are decoded in several branches over one paged cache: the beams of a beam search, or conversations behind
+ * one prompt.  A group of n_beams neighbouring sequences belongs to a request, and beam b of group g is sequence
+ * g * n_beams + b of the cache.  One step:
+ *
+ *     restkv_append -> restkv_attend_beams   (each layer)   -> logits -> restkv_beam_select -> restkv_beam_reorder
+ *
+ * Pages of a beam search.  A page that is full may stand in the tables of all beams of a group; a page that is still
+ * written to belongs to one beam.  Which page a beam writes to next is in its table from the start (n_beams pages for each
+ * column that the search may reach), so a step allocates nothing: restkv_beam_reorder deals the pages of the open columns
+ * anew.  After a prompt in beam 0's pages a reorder with parents 0, 0, .. makes the other beams.
+ */
+typedef struct restkv_beams {
+  int32_t n_groups;      /* requests, up to 16384 (0: nothing is done)                          */
+  int32_t n_beams;       /* beams of a request, 1 .. 64                                          */
+  int32_t n_vocab;       /* logits of a beam, 1 .. 2^24                                          */
+  int32_t n_out;         /* continuations taken of a request, 1 .. 64                            */
+  int32_t dtype;         /* logits: RESTKV_F32 or RESTKV_BF16                                    */
+  int32_t end_token;     /* ends a beam, and is what a beam that has ended goes on with          */
+  int64_t logit_stride;  /* elements from a beam's logits to the next beam's; 0: n_vocab         */
+} restkv_beams;
+
+/*
+ * The best continuations of each request's beams.  With logits x[b, v] and the score c[b] that beam b has so far,
+ *     score(b, v) = c[b] + (x[b, v] - m_b) - ln(sum over v' of exp(x[b, v'] - m_b)),   m_b the largest logit of b,
+ * and a beam that has ended has one continuation, (b, end_token) of score c[b].  The n_out largest are taken; of equal
+ * scores the lower beam's is the larger, then the one of the larger logit, then the lower token's.  Only finite scores are
+ * taken: a logit of -inf (a token that is masked out) is none, a beam with a score that is not finite has none, nor has one
+ * with a NaN or +inf among its logits.  Places that are left get -inf, -1, -1 and 1.
+ *   logits   [n_groups * n_beams, n_vocab] dtype (logit_stride), any alignment of that type
+ *   scores   [n_groups, n_beams] float32;  finished [n_groups, n_beams] int32 (nonzero: ended) or NULL
+ *   new_scores [n_groups, n_out] float32, parents (the beam, 0 .. n_beams-1), tokens [n_groups, n_out] int32 out, best first
+ *   new_finished [n_groups, n_out] int32 out, may be NULL: 1 where the token is end_token or the beam had ended
+ * new_scores may be scores, and new_finished may be finished, if n_out = n_beams.
+ * Exponentials and their sums over up to 2048 neighbouring logits are float32 (sums of these, logarithms and scores 64 bits);
+ * scores are ordered in 64 bits and rounded once.  Results do not depend on timing: no atomics.
+ * Workspace: restkv_beam_workspace_bytes(b), 256-byte aligned, whatever it holds; calls that run at the same time need one each.
+ */
+size_t restkv_beam_workspace_bytes(const restkv_beams* b);
+int restkv_beam_select(const restkv_beams* b, const void* logits, const float* scores, const int32_t* finished,
+                       float* new_scores, int32_t* parents, int32_t* tokens, int32_t* new_finished, void* workspace,
+                       size_t workspace_bytes, restkv_stream_t stream);
+
+/*
+ * Beam b of each group goes on from beam parents[b] of the group: its table names the parent's pages where they are full, and
+ * in the columns that are still written to it has pages of its own with the parent's rows in them.
+ *   parents [n_groups] rows of n_beams int32, parents_stride entries apart (0: n_beams); n_groups = n_seqs / n_beams.  An entry
+ *           outside [0, n_beams) counts as b itself
+ *   lens    positions that are there (strides as ever; without new tokens); those of a group's first beam count for all of it
+ *   table   the tables before, table_out after; table_out may be table itself, else they must not overlap.  Strides as ever
+ *   layers  HOST array of n_layers (0 .. 256): the pages of each layer, all as the description says.  Read before the call returns
+ * A column is full if every KV head that shares the table has filled its page, and open from there to the last page in use.  In
+ * an open column the pages of the parents go to one child each (the parent itself where it is its own child, else its first
+ * child), those of beams without a child to the other children, in order of the beams; into these the rows in use are
+ * copied.  Columns behind the open ones stay as they are.  So no page is lost or doubled, and a step needs none.
+ * In open columns the beams of a group must have pages that differ.  An entry outside [0, n_pages) is dealt like any, and no row
+ * of it is read or written.  Rows behind the lengths are left as they were.
+ */
+typedef struct restkv_layer_pages { void *k_pages, *v_pages, *k_scale, *v_scale; } restkv_layer_pages;
+int restkv_beam_reorder(const restkv_cache* c, int32_t n_beams, const int32_t* parents, int64_t parents_stride,
+                        const int32_t* lens, const int32_t* table, int32_t* table_out, const restkv_layer_pages* layers,
+                        int32_t n_layers, restkv_stream_t stream);
+
+/*
+ * restkv_attend for beams whose tables begin with the same pages: these are read once for all beams of a group.
+ *   shared [n_seqs / n_beams] int32: so many table entries in front are the same for all sequences of the group (of each KV
+ *          head, with tables per head).  Values below 0 count as 0; pages beyond what every beam of the group with new tokens
+ *          has seen before them are each beam's own.
+ * Everything else, the result too, as restkv_attend says (n_beams 1 .. 64); where the tables differ after all, the first beam's
+ * pages count for the others.  Workspace: restkv_attend_beams_workspace_bytes(c, n_beams).
+ */
+size_t restkv_attend_beams_workspace_bytes(const restkv_cache* c, int32_t n_beams);
+int restkv_attend_beams(const restkv_cache* c, int32_t n_beams, const int32_t* shared, const void* q, const void* k_pages,
+                        const void* v_pages, const void* k_scale, const void* v_scale, const int32_t* table, const int32_t* lens,
+                        const int32_t* new_start, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                        restkv_stream_t stream);
+
+/*
  * Profiling aid (not part of the method): every kernel launch of a selected stage
  * is bracketed by two HIP events on the caller's stream.  stage_mask: bit s selects
  * stage s (see restkv_stage_name), -1 selects all, 0 turns timing off.  A bracket

@@ -57,6 +57,15 @@ class RestkvCache(ctypes.Structure):
         super().__setattr__(name, value)
 
 
+class RestkvBeams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_groups", "n_beams", "n_vocab", "n_out", "dtype", "end_token")] + [
+        ("logit_stride", ctypes.c_int64)]
+
+
+class RestkvLayerPages(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_pages", "v_pages", "k_scale", "v_scale")]
+
+
 class RestkvError(RuntimeError):
     def __init__(self, code: int, what: str):
         self.code = code
@@ -103,6 +112,17 @@ def lib() -> ctypes.CDLL:
         L.restkv_attend.restype = ctypes.c_int
         L.restkv_fetch.argtypes = [C] + [vp] * 7 + [i32, i32, vp, vp, vp]
         L.restkv_fetch.restype = ctypes.c_int
+        b = ctypes.POINTER(RestkvBeams)
+        L.restkv_beam_workspace_bytes.argtypes = [b]
+        L.restkv_beam_workspace_bytes.restype = sz
+        L.restkv_beam_select.argtypes = [b] + [vp] * 8 + [sz, vp]
+        L.restkv_beam_select.restype = ctypes.c_int
+        L.restkv_beam_reorder.argtypes = [C, i32, vp, i64, vp, vp, vp, vp, i32, vp]
+        L.restkv_beam_reorder.restype = ctypes.c_int
+        L.restkv_attend_beams_workspace_bytes.argtypes = [C, i32]
+        L.restkv_attend_beams_workspace_bytes.restype = sz
+        L.restkv_attend_beams.argtypes = [C, i32] + [vp] * 12 + [sz, vp]
+        L.restkv_attend_beams.restype = ctypes.c_int
         L.restkv_strerror.restype = ctypes.c_char_p
         L.restkv_strerror.argtypes = [ctypes.c_int]
         L.restkv_timing_read.argtypes = [vp, vp, ctypes.c_int]
@@ -575,11 +595,19 @@ def restkv_append(c: RestkvCache, k, v, pages: CachePages, table, lens, *, new_s
             _addr(pages.k_scale), _addr(pages.v_scale), tb, ln, ns, ps, cs, sn, _addr(q), _addr(q_out))
 
 
-def restkv_attend(c: RestkvCache, q, pages: CachePages, table, lens, out, lse=None, workspace=None, *, new_start=None,
-                  stream=None):
-    """Attention of the newest tokens' queries q [n_tokens, Hq, d] over the pages: out [n_tokens, Hq, d], lse [n_tokens, Hq]."""
-    what, told = "restkv_attend", _told(c)
-    dev, ref = _check_pages(what, c, told, pages), told.ref
+def _take_workspace(what, dev, workspace):
+    """Address (aligned) and bytes of a workspace, or None and 0."""
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != dev or workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
+        raise RestkvError(-1, f"{what}: the workspace has to be contiguous uint8 on GPU {dev}")
+    at = workspace.data_ptr()
+    return at + -at % 256, max(workspace.numel() - -at % 256, 0)
+
+
+def _attend(what, f, front, c, told, dev, q, pages, table, lens, out, lse, workspace, new_start, stream):
+    """The call f(description, *front, q, ...)."""
+    ref = told.ref
     tb, ln = _check_flat(what, dev, table, told.table), _check_flat(what, dev, lens, told.lens)
     ns = None if new_start is None else _check_flat(what, dev, new_start, told.new)
     qs = _check_rows(what, dev, told.dtype, "q", q, told.q, told.q_stride)
@@ -587,14 +615,17 @@ def restkv_attend(c: RestkvCache, q, pages: CachePages, table, lens, out, lse=No
     ls = told.lse_stride if lse is None else _check_rows(what, dev, torch.float32, "lse", lse, told.lse, told.lse_stride)
     if qs is not told.q_stride or outs is not told.out_stride or ls is not told.lse_stride:
         ref = _as_strided(c, q=qs, out=outs, lse=ls)
-    wp, wn = None, 0
-    if workspace is not None:
-        if workspace.get_device() != dev or workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
-            raise RestkvError(-1, f"{what}: the workspace has to be contiguous uint8 on GPU {dev}")
-        at = workspace.data_ptr()
-        wp, wn = at + -at % 256, max(workspace.numel() - -at % 256, 0)
-    _on_gpu(dev, stream, what, lib().restkv_attend, ref, q.data_ptr(), pages.k.data_ptr(), pages.v.data_ptr(), _addr(pages.k_scale),
+    wp, wn = _take_workspace(what, dev, workspace)
+    _on_gpu(dev, stream, what, f, ref, *front, q.data_ptr(), pages.k.data_ptr(), pages.v.data_ptr(), _addr(pages.k_scale),
             _addr(pages.v_scale), tb, ln, ns, out.data_ptr(), _addr(lse), wp, wn)
+
+
+def restkv_attend(c: RestkvCache, q, pages: CachePages, table, lens, out, lse=None, workspace=None, *, new_start=None,
+                  stream=None):
+    """Attention of the newest tokens' queries q [n_tokens, Hq, d] over the pages: out [n_tokens, Hq, d], lse [n_tokens, Hq]."""
+    what, told = "restkv_attend", _told(c)
+    dev = _check_pages(what, c, told, pages)
+    _attend(what, lib().restkv_attend, (), c, told, dev, q, pages, table, lens, out, lse, workspace, new_start, stream)
 
 
 def restkv_fetch(c: RestkvCache, pages: CachePages, table, lens, k_out, v_out, *, idx=None, first=0, stream=None):
@@ -609,3 +640,95 @@ def restkv_fetch(c: RestkvCache, pages: CachePages, table, lens, k_out, v_out, *
     ix = None if idx is None else _check_flat(what, dev, idx, (shape[:3], torch.int32, "idx", None))
     _on_gpu(dev, stream, what, lib().restkv_fetch, told.ref, pages.k.data_ptr(), pages.v.data_ptr(), _addr(pages.k_scale),
             _addr(pages.v_scale), tb, ln, ix, int(first), shape[2], kp, vp)
+
+
+# ---- beams --------------------------------------------------------------------------------------
+
+
+def make_beams(*, n_groups, n_beams, n_vocab, dtype, n_out=None, end_token=-1, logit_stride=0) -> RestkvBeams:
+    """Description of a choice of continuations (see restkv_beams in include/restkv.h): n_out (default n_beams) of each request's
+    n_beams; end_token ends a beam (default: none does).  logit_stride: elements from one row of logits to the next, 0: n_vocab."""
+    return RestkvBeams(n_groups, n_beams, n_vocab, n_beams if n_out is None else n_out, int(_TYPES.get(dtype, dtype)), end_token,
+                       logit_stride)
+
+
+def restkv_beam_workspace_bytes(b: RestkvBeams) -> int:
+    return int(lib().restkv_beam_workspace_bytes(ctypes.byref(b)))
+
+
+def alloc_beam_workspace(b: RestkvBeams, device="cuda") -> torch.Tensor:
+    """Scratch of restkv_beam_select."""
+    return torch.empty(restkv_beam_workspace_bytes(b) + 256, dtype=torch.uint8, device=device)
+
+
+def restkv_beam_select(b: RestkvBeams, logits, scores, new_scores, parents, tokens, workspace, *, finished=None, new_finished=None,
+                       stream=None):
+    """The n_out best continuations of each request, best first: new_scores, parents (beams), tokens [n_groups, n_out] from logits
+    [n_groups * n_beams, n_vocab] (or [n_groups, n_beams, n_vocab]) and scores [n_groups, n_beams]; finished and new_finished
+    (int32, nonzero: ended) beside them.  new_scores may be scores and new_finished finished, where n_out = n_beams."""
+    what, dev = "restkv_beam_select", logits.get_device()
+    rows, stride = b.n_groups * b.n_beams, b.logit_stride or b.n_vocab
+    shape, strides = logits.shape, logits.stride()
+    if dev < 0 or logits.dtype is not _TORCH.get(b.dtype) or \
+            not (shape == (rows, b.n_vocab) or shape == (b.n_groups, b.n_beams, b.n_vocab)) or \
+            (strides[-1] != 1 and b.n_vocab > 1) or (strides[-2] != stride and shape[-2] > 1) or \
+            (len(shape) == 3 and strides[0] != b.n_beams * stride and b.n_groups > 1):
+        raise RestkvError(-1, f"{what}: logits have to be {_TORCH.get(b.dtype)} [{rows}, {b.n_vocab}], rows {stride} apart, on a GPU")
+    into, of = (b.n_groups, b.n_out), (b.n_groups, b.n_beams)
+    sc = _check_flat(what, dev, scores, (of, torch.float32, "scores", None))
+    ns = _check_flat(what, dev, new_scores, (into, torch.float32, "new_scores", None))
+    ps, tk = _check_flat(what, dev, parents, (into, torch.int32, "parents", None)), _check_flat(what, dev, tokens, (into, torch.int32, "tokens", None))
+    fn = None if finished is None else _check_flat(what, dev, finished, (of, torch.int32, "finished", None))
+    nf = None if new_finished is None else _check_flat(what, dev, new_finished, (into, torch.int32, "new_finished", None))
+    wp, wn = _take_workspace(what, dev, workspace)
+    _on_gpu(dev, stream, what, lib().restkv_beam_select, ctypes.byref(b), logits.data_ptr(), sc, fn, ns, ps, tk, nf, wp, wn)
+
+
+class CacheLayers:
+    """The pages of a model's layers, all of one layout on one GPU, as restkv_beam_reorder takes them (kept while in use)."""
+
+    def __init__(self, layers):
+        self.pages = tuple(layers)
+        if len({x.rows for x in self.pages}) > 1:
+            raise RestkvError(-1, "CacheLayers: pages of one layout on one GPU")
+        self.array = (RestkvLayerPages * len(self.pages))(*((x.k.data_ptr(), x.v.data_ptr(), _addr(x.k_scale), _addr(x.v_scale))
+                                                           for x in self.pages))
+
+
+def restkv_beam_reorder(c: RestkvCache, n_beams, parents, table, lens, layers, table_out=None, *, stream=None):
+    """Beam b of each group of n_beams sequences goes on from beam parents[group, b] (int32, rows may be a stride apart): table_out
+    (default: in place) names the pages, and in all layers (CacheLayers, or CachePages of each) the rows of pages that are not full
+    are copied."""
+    what, told = "restkv_beam_reorder", _told(c)
+    if not isinstance(layers, CacheLayers):
+        layers = CacheLayers(layers)
+    dev = _check_pages(what, c, told, layers.pages[0]) if layers.pages else table.get_device()
+    n_groups = c.n_seqs // n_beams if n_beams > 0 else 0
+    tb, ln = _check_flat(what, dev, table, told.table), _check_flat(what, dev, lens, told.lens)
+    to = tb if table_out is None else _check_flat(what, dev, table_out, told.table)
+    st = parents.stride()
+    if parents.dtype is not torch.int32 or parents.get_device() != dev or dev < 0 or parents.shape != (n_groups, n_beams) or \
+            (st[1] != 1 and n_beams > 1) or (n_groups > 1 and st[0] < n_beams):
+        raise RestkvError(-1, f"{what}: parents have to be int32 [{n_groups}, {n_beams}] on GPU {dev}, rows that do not overlap")
+    _on_gpu(dev, stream, what, lib().restkv_beam_reorder, told.ref, n_beams, parents.data_ptr(), st[0] if n_groups > 1 else 0, ln, tb, to,
+            layers.array, len(layers.pages))
+
+
+def restkv_attend_beams_workspace_bytes(c: RestkvCache, n_beams) -> int:
+    return int(lib().restkv_attend_beams_workspace_bytes(ctypes.byref(c), n_beams))
+
+
+def alloc_attend_beams_workspace(c: RestkvCache, n_beams, device="cuda") -> Optional[torch.Tensor]:
+    """Scratch of restkv_attend_beams, or None where it needs none."""
+    n = restkv_attend_beams_workspace_bytes(c, n_beams)
+    return torch.empty(n + 256, dtype=torch.uint8, device=device) if n else None
+
+
+def restkv_attend_beams(c: RestkvCache, n_beams, shared, q, pages: CachePages, table, lens, out, lse=None, workspace=None, *,
+                        new_start=None, stream=None):
+    """restkv_attend where the tables of each n_beams neighbouring sequences begin with the same shared[group] pages (int32), which
+    are read once for all of them."""
+    what, told = "restkv_attend_beams", _told(c)
+    dev = _check_pages(what, c, told, pages)
+    sh = _check_flat(what, dev, shared, ((c.n_seqs // max(n_beams, 1),), torch.int32, "shared", None))
+    _attend(what, lib().restkv_attend_beams, (n_beams, sh), c, told, dev, q, pages, table, lens, out, lse, workspace, new_start, stream)

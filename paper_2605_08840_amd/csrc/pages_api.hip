@@ -1,7 +1,7 @@
-// C ABI of the paged cache: argument validation and dispatch.
+// C ABI of the paged cache and of beams over it: argument validation and dispatch.
 #include <math.h>
 
-#include "pages.hpp"
+#include "beams.hpp"
 
 namespace restkv {
 
@@ -80,6 +80,34 @@ static int take_new(Pages* pg, const int32_t* new_start) {
   return RESTKV_OK;
 }
 
+// What an attention reads and writes beside the pages.
+static int take_output(const Pages& pg, const void* q, const void* out, const float* lse) {
+  if (!q || !out) return RESTKV_EINVAL;
+  if (rows_overlap(pg.o_st, pg.o_sh, pg.n_tokens, pg.Hq, pg.d)) return RESTKV_EINVAL;
+  if (lse && rows_overlap(pg.lse_st, pg.lse_sh, pg.n_tokens, pg.Hq, 1)) return RESTKV_EINVAL;
+  return RESTKV_OK;
+}
+static int take_workspace(size_t need, const void* ws, size_t bytes) {
+  return need && (!ws || ((uintptr_t)ws & 255u) || bytes < need) ? RESTKV_EWORKSPACE : RESTKV_OK;
+}
+
+int resolve_beams(const restkv_beams* b, Beams* o) {
+  if (!b || !o) return RESTKV_EINVAL;
+  if (b->n_groups < 0 || b->n_beams < 1 || b->n_vocab < 1 || b->n_out < 1) return RESTKV_EINVAL;
+  if (b->n_groups > 16384 || b->n_beams > 64 || b->n_vocab > 1 << 24 || b->n_out > 64) return RESTKV_EUNSUPPORTED;
+  if (b->dtype != RESTKV_F32 && b->dtype != RESTKV_BF16) return RESTKV_EUNSUPPORTED;
+  if (b->logit_stride && b->logit_stride < b->n_vocab) return RESTKV_EINVAL;
+  if (b->logit_stride > (int64_t)1 << 40) return RESTKV_EUNSUPPORTED;
+  *o = {b->n_groups, b->n_beams, b->n_vocab, b->n_out, b->dtype, b->end_token, b->logit_stride ? b->logit_stride : b->n_vocab};
+  return RESTKV_OK;
+}
+// Groups of sequences.
+static int take_beams(const Pages& pg, int n_beams) {
+  if (n_beams < 1) return RESTKV_EINVAL;
+  if (n_beams > 64) return RESTKV_EUNSUPPORTED;
+  return pg.n_seqs % n_beams ? RESTKV_EINVAL : RESTKV_OK;
+}
+
 }  // namespace restkv
 
 using namespace restkv;
@@ -116,12 +144,72 @@ int restkv_attend(const restkv_cache* c, const void* q, const void* k_pages, con
   if (!rc) rc = take_new(&pg, new_start);
   if (!rc && pg.n_seqs && pg.n_tokens) rc = take_arrays(&pg, k_pages, v_pages, k_scale, v_scale, table, lens);
   if (rc || !pg.n_seqs || !pg.n_tokens) return rc;
-  if (!q || !out) return RESTKV_EINVAL;
-  if (rows_overlap(pg.o_st, pg.o_sh, pg.n_tokens, pg.Hq, pg.d)) return RESTKV_EINVAL;
-  if (lse && rows_overlap(pg.lse_st, pg.lse_sh, pg.n_tokens, pg.Hq, 1)) return RESTKV_EINVAL;
-  const size_t need = attend_ws_bytes(pg);
-  if (need && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need)) return RESTKV_EWORKSPACE;
+  if ((rc = take_output(pg, q, out, lse))) return rc;
+  if ((rc = take_workspace(attend_ws_bytes(pg), workspace, workspace_bytes))) return rc;
   return launch_attend(pg, q, k_pages, v_pages, k_scale, v_scale, out, lse, (char*)workspace, (hipStream_t)stream);
+}
+
+size_t restkv_attend_beams_workspace_bytes(const restkv_cache* c, int32_t n_beams) {
+  Pages pg;
+  if (resolve_cache(c, &pg) != RESTKV_OK || take_beams(pg, n_beams) != RESTKV_OK || !pg.n_seqs) return 0;
+  return attend_beams_ws_bytes(pg, n_beams);
+}
+
+int restkv_attend_beams(const restkv_cache* c, int32_t n_beams, const int32_t* shared, const void* q, const void* k_pages,
+                        const void* v_pages, const void* k_scale, const void* v_scale, const int32_t* table, const int32_t* lens,
+                        const int32_t* new_start, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                        restkv_stream_t stream) {
+  Pages pg;
+  int rc = resolve_cache(c, &pg);
+  if (!rc) rc = take_beams(pg, n_beams);
+  if (!rc) rc = take_new(&pg, new_start);
+  if (!rc && pg.n_seqs && pg.n_tokens) rc = take_arrays(&pg, k_pages, v_pages, k_scale, v_scale, table, lens);
+  if (rc || !pg.n_seqs || !pg.n_tokens) return rc;
+  if (!shared) return RESTKV_EINVAL;
+  if ((rc = take_output(pg, q, out, lse))) return rc;
+  if ((rc = take_workspace(attend_beams_ws_bytes(pg, n_beams), workspace, workspace_bytes))) return rc;
+  return launch_attend_beams(pg, n_beams, shared, q, k_pages, v_pages, k_scale, v_scale, out, lse, (char*)workspace,
+                             (hipStream_t)stream);
+}
+
+size_t restkv_beam_workspace_bytes(const restkv_beams* b) {
+  Beams o;
+  return resolve_beams(b, &o) == RESTKV_OK ? beam_ws_bytes(o) : 0;
+}
+
+int restkv_beam_select(const restkv_beams* b, const void* logits, const float* scores, const int32_t* finished,
+                       float* new_scores, int32_t* parents, int32_t* tokens, int32_t* new_finished, void* workspace,
+                       size_t workspace_bytes, restkv_stream_t stream) {
+  Beams o;
+  int rc = resolve_beams(b, &o);
+  if (rc || !o.n_groups) return rc;
+  if (!logits || !scores || !new_scores || !parents || !tokens) return RESTKV_EINVAL;
+  if ((uintptr_t)logits & (o.dtype == RESTKV_F32 ? 3u : 1u)) return RESTKV_EINVAL;
+  if (o.n_out != o.n_beams && (new_scores == scores || (finished && new_finished == finished))) return RESTKV_EINVAL;
+  if ((rc = take_workspace(beam_ws_bytes(o), workspace, workspace_bytes))) return rc;
+  return launch_beam_select(o, logits, scores, finished, new_scores, parents, tokens, new_finished, (char*)workspace, (hipStream_t)stream);
+}
+
+int restkv_beam_reorder(const restkv_cache* c, int32_t n_beams, const int32_t* parents, int64_t parents_stride,
+                        const int32_t* lens, const int32_t* table, int32_t* table_out, const restkv_layer_pages* layers,
+                        int32_t n_layers, restkv_stream_t stream) {
+  Pages pg;
+  int rc = resolve_cache(c, &pg);
+  if (!rc) rc = take_beams(pg, n_beams);
+  if (rc) return rc;
+  if (n_layers < 0 || parents_stride < 0 || (parents_stride && parents_stride < n_beams)) return RESTKV_EINVAL;
+  if (n_layers > 256) return RESTKV_EUNSUPPORTED;
+  if (!pg.n_seqs) return RESTKV_OK;
+  if (!parents || !lens || !table || !table_out || (n_layers && !layers)) return RESTKV_EINVAL;
+  for (int i = 0; i < n_layers; ++i)
+    if ((rc = take_arrays(&pg, layers[i].k_pages, layers[i].v_pages, layers[i].k_scale, layers[i].v_scale, table, lens))) return rc;
+  pg.table = table;
+  pg.lens = lens;
+  // tables are written: each entry by one beam
+  const int heads = pg.table_sh ? pg.Hkv : 1;
+  if ((pg.n_seqs > 1 && pg.table_ss < pg.max_pages) || (heads > 1 && pg.table_sh < pg.max_pages)) return RESTKV_EINVAL;
+  if (pg.n_seqs > 1 && heads > 1 && rows_overlap(pg.table_ss, pg.table_sh, pg.n_seqs, heads, pg.max_pages)) return RESTKV_EINVAL;
+  return launch_beam_reorder(pg, n_beams, parents, parents_stride ? parents_stride : n_beams, table_out, layers, n_layers, (hipStream_t)stream);
 }
 
 int restkv_fetch(const restkv_cache* c, const void* k_pages, const void* v_pages, const void* k_scale, const void* v_scale,
