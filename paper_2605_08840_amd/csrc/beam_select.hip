@@ -65,6 +65,17 @@ template <int LOW>
 __device__ __forceinline__ unsigned long long keep_best(unsigned long long* list, int& n, int K) {
   const int lane = threadIdx.x & 63;
   if (n < K) return 0;
+  if (n <= 64) {                       // each entry's place by counting
+    const unsigned long long e = lane < n ? list[lane] : 0;
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += list[j] > e;
+    __builtin_amdgcn_wave_barrier();
+    if (lane < n && rank < K) list[rank] = e;
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    n = K;
+    return list[K - 1];
+  }
   uint32_t hi[SEL_OWN], lo[SEL_OWN];
 #pragma unroll
   for (int j = 0; j < SEL_OWN; ++j) {
@@ -208,8 +219,8 @@ __global__ __launch_bounds__(SEL_THREADS) void k_select_rows(SelectArgs a) {
     bool any;
     if (tile == first) {
       const uint32_t t[1] = {mt > -INFINITY ? float_key(mt + 0.f) : 0u};
-      const uint32_t key = kth<LOW>(t, K);
-      bar = (unsigned long long)key << 32;             // (below every logit that reaches it)
+      bar = (unsigned long long)kth<16>(t, K) << 32;   // (its upper bits: below every logit that reaches it)
+      limit = bar ? logit_of(bar) : -INFINITY;
       any = true;
     } else {
       any = mt > limit;
@@ -217,10 +228,10 @@ __global__ __launch_bounds__(SEL_THREADS) void k_select_rows(SelectArgs a) {
     if (__ballot(any)) {
 #pragma unroll
       for (int c = 0; c < SEL_VECS; ++c) {
-        const bool look = tile == first ? top[c] > -INFINITY && (uint32_t)(bar >> 32) <= float_key(top[c] + 0.f) : top[c] > limit;
-        if (!__ballot(look)) continue;
+        if (!__ballot(tile == first ? top[c] >= limit : top[c] > limit)) continue;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
+          if (!__ballot(x[c][i] >= limit)) continue;
           const unsigned long long key = key_of(x[c][i], (uint32_t)(place(tile, c) - skip + i));
           unsigned long long mask = __ballot(key > bar);
           if (!mask) continue;
@@ -238,10 +249,10 @@ __global__ __launch_bounds__(SEL_THREADS) void k_select_rows(SelectArgs a) {
     }
     limit = bar ? logit_of(bar) : -INFINITY;
   }
-  keep_best<LOW>(list, n, K);
+  if (n > 64) keep_best<LOW>(list, n, K);
   const float wm = wave_join(m, [](float p, float q) { return fmaxf(p, q); });
   // (a thread of which everything is masked out has a sum of 0; a NaN stays one)
-  sum *= m == wm ? 1.0 : exp((double)m - (double)wm);
+  sum *= m == wm ? 1.0 : (double)exp_of(m - wm);
   sum = wave_join(sum, [](double p, double q) { return p + q; });
   if (lane == 0) {
     s_max[wv] = wm;
@@ -249,27 +260,25 @@ __global__ __launch_bounds__(SEL_THREADS) void k_select_rows(SelectArgs a) {
     s_n[wv] = n;
   }
   __syncthreads();
-  if (wv) return;
-  // ---- the wavefronts' lists and sums joined by the first one
+  // ---- the wavefronts' sums joined, and the best of their lists (up to 64 entries each), an entry a thread
   const int64_t at = row * a.pieces + piece;
-  if (lane == 0) {
+  if (tid == 0) {
     float M = s_max[0];
     for (int w = 1; w < NW; ++w) M = fmaxf(M, s_max[w]);
     double S = 0.0;
-    for (int w = 0; w < NW; ++w) S += s_sum[w] * (s_max[w] == M ? 1.0 : exp((double)s_max[w] - (double)M));
+    for (int w = 0; w < NW; ++w) S += s_sum[w] * (s_max[w] == M ? 1.0 : (double)exp_of(s_max[w] - M));
     a.part_m[at] = M;
     a.part_s[at] = S;
   }
-  static_assert(NW * 64 <= SEL_LIST, "");
-  int all = s_n[0];
-  for (int w = 1; w < NW; ++w) {
-    if (lane < s_n[w]) list[all + lane] = s_list[w][lane];
-    all += s_n[w];
+  const unsigned long long e = lane < n ? list[lane] : 0;
+  int rank = 0, all = 0;
+  for (int w = 0; w < NW; ++w) {
+    const int nw = s_n[w];
+    for (int j = 0; j < nw; ++j) rank += s_list[w][j] > e;
+    all += nw;
   }
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  keep_best<LOW>(list, all, K);
-  if (lane < K) a.keys[at * K + lane] = lane < all ? list[lane] : 0;
+  if (lane < n && rank < K) a.keys[at * K + rank] = e;
+  for (int k = all + tid; k < K; k += SEL_THREADS) a.keys[at * K + k] = 0;
 }
 
 // A continuation: larger first.
@@ -279,53 +288,33 @@ __device__ __forceinline__ bool before(const Cont& x, const Cont& y) {
 }
 __device__ __forceinline__ Cont better(const Cont& x, const Cont& y) { return before(x, y) ? x : y; }
 
-// A workgroup a request.  Of the continuations that its rows' pieces have left, those that reach a bound go into a list in LDS, and an
-// entry's place in the answer is the number of entries before it.  The bound: the n_out-th largest of the threads' maxima, of the
-// wavefront that has the highest.  Where more reach it than the list holds (scores that are all equal) the answer is found one at a time.
-constexpr int JOIN_THREADS = 256, JOIN_LIST = 1024;
-__global__ __launch_bounds__(JOIN_THREADS) void k_select_join(SelectArgs a) {
-  constexpr int NW = JOIN_THREADS / 64;
+// A workgroup a request, a wavefront a row or a part of one.  Of the continuations that the rows' pieces have left, those that reach a
+// bound go into a list in LDS, and an entry's place in the answer is the number of entries before it.  The bound: of the wavefront that
+// has the highest, the n_out-th largest of its lanes' maxima.  Where more reach it than the list holds (scores that are all equal) the answer is
+// found one at a time.
+constexpr int JOIN_WAVES = 16, JOIN_LIST = 64 * JOIN_WAVES, JOIN_AHEAD = 4;
+__global__ __launch_bounds__(JOIN_LIST) void k_select_join(SelectArgs a) {
+  constexpr int NW = JOIN_WAVES;
   __shared__ double s_score[64], s_log[64];
   __shared__ float s_top[64];
   __shared__ int s_end[64], s_count;
   __shared__ uint32_t s_bar[NW];
-  __shared__ Cont s_best[2][NW], s_list[JOIN_LIST];
-  const int B = a.b.n_beams, K = a.b.n_out, C = a.pieces, tid = threadIdx.x, wv = tid >> 6, lane = tid & 63;
+  __shared__ __align__(16) uint32_t s_floor[JOIN_LIST];
+  __shared__ Cont s_list[JOIN_LIST];
+  const int B = a.b.n_beams, K = a.b.n_out, C = a.pieces, tid = threadIdx.x, lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t g = blockIdx.x;
-  if (tid == 0) s_count = 0;
-  for (int b = wv; b < B; b += NW) {
-    const int64_t row = g * B + b;
-    const bool end = a.finished && a.finished[row];
-    double S = 0.0;
-    float M = -INFINITY;
-    if (!end) {
-      for (int c = lane; c < C; c += 64) M = fmaxf(M, a.part_m[row * C + c]);
-      M = wave_join(M, [](float p, float q) { return fmaxf(p, q); });
-      for (int c = lane; c < C; c += 64) {
-        const float m = a.part_m[row * C + c];
-        S += a.part_s[row * C + c] * (m == M ? 1.0 : exp((double)m - (double)M));
-      }
-      S = wave_join(S, [](double p, double q) { return p + q; });
-    }
-    if (lane == 0) {
-      s_score[b] = a.scores[row];
-      s_log[b] = log(S);
-      s_top[b] = M;
-      s_end[b] = end;
-    }
-  }
-  __syncthreads();
-  const int N = B * C * K;
+  const unsigned long long* const keys = a.keys + g * B * C * K;
+  // rows of this wavefront: row0, row0 + NW, ..; of such a row every `parts`-th 64 keys
+  const int parts = max(1, NW / B), row0 = wv / parts, part = wv % parts, per = C * K;
   const Cont none = {-INFINITY, 1 << 30, 0};
   // (none where the score is not finite)
-  auto cont = [&](int i) {
-    const int b = i / (C * K);
-    Cont x = none;
-    if (s_end[b]) {
-      if (i == b * C * K) x = {s_score[b], b, (unsigned long long)(uint32_t)~a.b.end_token};
-    } else if (const unsigned long long key = a.keys[(g * B) * C * K + i]) {
-      x = {s_score[b] + (((double)logit_of(key) - (double)s_top[b]) - s_log[b]), b, key};
-    }
+  auto cont = [&](int b, unsigned long long key) {
+    const Cont x = {s_score[b] + (((double)logit_of(key) - (double)s_top[b]) - s_log[b]), b, key};
+    return key && x.score - x.score == 0.0 ? x : none;
+  };
+  auto ended = [&](int b) {
+    const Cont x = {s_score[b], b, (unsigned long long)(uint32_t)~a.b.end_token};
     return x.score - x.score == 0.0 ? x : none;
   };
   // a score as a float that is not above it, as a whole number
@@ -334,19 +323,69 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_select_join(SelectArgs a) {
     const uint32_t k = float_key(f);
     return s > -INFINITY ? ((double)f > s ? k - 1 : k) : 0u;
   };
+  if (tid == 0) s_count = 0;
   uint32_t top[1] = {0};
-  for (int i = tid; i < N; i += JOIN_THREADS) top[0] = max(top[0], floor_of(cont(i).score));
-  const uint32_t own = kth<0>(top, K);
+  for (int b = row0; b < B; b += NW / parts) {
+    const int64_t row = g * B + b;
+    const bool end = a.finished && a.finished[row];
+    unsigned long long key[JOIN_AHEAD];
+#pragma unroll
+    for (int u = 0; u < JOIN_AHEAD; ++u) {
+      const int i = (u * parts + part) * 64 + lane;
+      key[u] = !end && i < per ? keys[b * per + i] : 0;
+    }
+    double S = 0.0;
+    float M = -INFINITY;
+    const double score = a.scores[row];
+    if (!end) {
+      float m = lane < C ? a.part_m[row * C + lane] : -INFINITY;
+      double s = lane < C ? a.part_s[row * C + lane] : 0.0;
+      for (int c = lane + 64; c < C; c += 64) {
+        const float mc = a.part_m[row * C + c], mx = fmaxf(m, mc);
+        s = s * (m == mx ? 1.0 : (double)exp_of(m - mx)) + a.part_s[row * C + c] * (mc == mx ? 1.0 : (double)exp_of(mc - mx));
+        m = mx;
+      }
+      M = wave_join(m, [](float p, float q) { return fmaxf(p, q); });
+      S = wave_join(s * (m == M ? 1.0 : (double)exp_of(m - M)), [](double p, double q) { return p + q; });
+    }
+    if (lane == 0 && part == 0) {
+      s_end[b] = end;
+    }
+    if (lane == 0) {                   // (all parts write the same)
+      s_score[b] = score;
+      s_log[b] = log(S);
+      s_top[b] = M;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (end) {
+      if (lane == 0) top[0] = max(top[0], floor_of(ended(b).score));
+      continue;
+    }
+#pragma unroll
+    for (int u = 0; u < JOIN_AHEAD; ++u) top[0] = max(top[0], floor_of(cont(b, key[u]).score));
+    for (int i = (JOIN_AHEAD * parts + part) * 64 + lane; i < per; i += parts * 64) top[0] = max(top[0], floor_of(cont(b, keys[b * per + i]).score));
+  }
+  const uint32_t own = kth<12>(top, K);
   if (lane == 0) s_bar[wv] = own;
   __syncthreads();
-  uint32_t bar = s_bar[0];
-  for (int w = 1; w < NW; ++w) bar = max(bar, s_bar[w]);
-  for (int i = tid; i < N; i += JOIN_THREADS) {
-    const Cont x = cont(i);
-    if (x.score > -INFINITY && floor_of(x.score) >= bar) {
-      const int at = atomicAdd(&s_count, 1);           // (in any order)
-      if (at < JOIN_LIST) s_list[at] = x;
+  uint32_t bar = 1;
+  for (int w = 0; w < NW; ++w) bar = max(bar, s_bar[w]);
+  auto put_in = [&](const Cont& x) {
+    const uint32_t f = floor_of(x.score);
+    if (f < bar) return;
+    const int at = atomicAdd(&s_count, 1);             // (in any order)
+    if (at < JOIN_LIST) {
+      s_list[at] = x;
+      s_floor[at] = f;
     }
+  };
+  for (int b = row0; b < B; b += NW / parts) {
+    if (s_end[b]) {
+      if (part == 0 && lane == 0) put_in(ended(b));
+      continue;
+    }
+    for (int i = part * 64 + lane; i < per; i += parts * 64) put_in(cont(b, keys[b * per + i]));
   }
   __syncthreads();
   const int n = s_count;
@@ -359,29 +398,44 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_select_join(SelectArgs a) {
     if (a.new_finished) a.new_finished[g * K + k] = !there || token == a.b.end_token || s_end[x.beam];
   };
   if (n <= JOIN_LIST) {
-    for (int i = tid; i < n; i += JOIN_THREADS) {
-      const Cont x = s_list[i];
-      int rank = 0;
-      for (int j = 0; j < n; ++j) rank += before(s_list[j], x);
+    // (whole floats first: only scores that are equal as such are compared in 64 bits)
+    if (tid < n) {
+      const uint32_t f = s_floor[tid];
+      int rank = 0, equal = 0;
+      for (int j = 0; j < n; ++j) {
+        rank += s_floor[j] > f;
+        equal += s_floor[j] == f;
+      }
+      const Cont x = s_list[tid];
+      if (equal > 1)
+        for (int j = 0; j < n; ++j) rank += s_floor[j] == f && before(s_list[j], x);
       if (rank < K) give(rank, x);
     }
-    for (int k = n + tid; k < K; k += JOIN_THREADS) give(k, none);
+    for (int k = n + tid; k < K; k += JOIN_LIST) give(k, none);
     return;
   }
   Cont last = {INFINITY, -1, ~0ull};
+  Cont* const s_best = s_list;         // [2][NW]
   for (int k = 0; k < K; ++k) {
     Cont best = none;
-    for (int i = tid; i < N; i += JOIN_THREADS) {
-      const Cont x = cont(i);
-      if (before(last, x)) best = better(best, x);
+    for (int b = row0; b < B; b += NW / parts) {
+      if (s_end[b]) {
+        const Cont x = ended(b);
+        if (before(last, x)) best = better(best, x);
+        continue;
+      }
+      for (int i = part * 64 + lane; i < per; i += parts * 64) {
+        const Cont x = cont(b, keys[b * per + i]);
+        if (before(last, x)) best = better(best, x);
+      }
     }
     for (int d = 1; d < 64; d <<= 1) {
       const Cont o = {__shfl_xor(best.score, d), __shfl_xor(best.beam, d), __shfl_xor(best.key, d)};
       best = better(best, o);
     }
-    if (lane == 0) s_best[k & 1][wv] = best;
+    if (lane == 0) s_best[(k & 1) * NW + wv] = best;
     __syncthreads();
-    for (int w = 0; w < NW; ++w) best = better(best, s_best[k & 1][w]);
+    for (int w = 0; w < NW; ++w) best = better(best, s_best[(k & 1) * NW + w]);
     last = best;
     if (tid == 0) give(k, best);
   }
@@ -424,7 +478,7 @@ int launch_beam_select(const Beams& b, const void* logits, const float* scores, 
   const dim3 grid = wide_grid((int64_t)b.n_groups * b.n_beams * a.pieces);
   if (b.dtype == RESTKV_F32) hipLaunchKernelGGL(k_select_rows<float>, grid, dim3(SEL_THREADS), 0, st, a);
   else hipLaunchKernelGGL(k_select_rows<bf16_t>, grid, dim3(SEL_THREADS), 0, st, a);
-  hipLaunchKernelGGL(k_select_join, dim3(b.n_groups), dim3(JOIN_THREADS), 0, st, a);
+  hipLaunchKernelGGL(k_select_join, dim3(b.n_groups), dim3(JOIN_LIST), 0, st, a);
   return hip_status();
 }
 
