@@ -1,6 +1,8 @@
 // The best continuations of each request's beams: score(b, v) = c[b] + (x[b, v] - m_b) - ln sum exp(x[b, .] - m_b).
 // One pass over the logits: a workgroup takes a piece of a row and leaves its maximum, its sum of exponentials and its n_out best
 // logits; a second launch joins the pieces of a request's rows.  Bound by memory, every logit read once.
+#include <float.h>
+
 #include <algorithm>
 
 #include "beams.hpp"
@@ -17,7 +19,7 @@ struct SelectArgs {
   const void* logits;
   const float* scores; const int32_t* finished;
   float* new_scores; int32_t* parents; int32_t* tokens; int32_t* new_finished;
-  int pieces, tiles;                                            // pieces of a row, tiles of a piece
+  int pieces, blocks;                                           // pieces of a row, 16-byte blocks of a piece
   double* part_s; float* part_m; unsigned long long* keys;      // [row, piece], [row, piece], [row, piece, n_out]
 };
 
@@ -32,11 +34,60 @@ __device__ __forceinline__ float logit_of(unsigned long long key) {
 }
 __device__ __forceinline__ uint32_t token_of(unsigned long long key) { return ~(uint32_t)key; }
 
-template <typename V, typename F>
-__device__ __forceinline__ V wave_join(V x, F f) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) x = f(x, __shfl_xor(x, d));
+// x of the lane that a data-parallel move names, for 32 and 64 bits.
+template <int CTRL, typename V>
+__device__ __forceinline__ V moved(V x) {
+  if constexpr (sizeof(V) == 4) {
+    return __builtin_bit_cast(V, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true));
+  } else {
+    const int2 w = __builtin_bit_cast(int2, x);
+    return __builtin_bit_cast(V, make_int2(moved<CTRL>(w.x), moved<CTRL>(w.y)));
+  }
+}
+// f over 4, 16 or 64 neighbouring lanes, the answer in all of them.
+template <int LANES, typename V, typename F>
+__device__ __forceinline__ V lanes_join(V x, F f) {
+  x = f(x, moved<0xB1>(x));            // neighbours, and pairs of them
+  x = f(x, moved<0x4E>(x));
+  if constexpr (LANES >= 16) {
+    x = f(x, moved<0x124>(x));         // round by 4 and by 8 of sixteen
+    x = f(x, moved<0x128>(x));
+  }
+  if constexpr (LANES == 64) {
+    x = f(x, __shfl_xor(x, 16));
+    x = f(x, __shfl_xor(x, 32));
+  }
   return x;
+}
+struct Max { template <typename V> __device__ __forceinline__ V operator()(V p, V q) const { return p > q ? p : q; } };
+struct MaxF { __device__ __forceinline__ float operator()(float p, float q) const { return fmaxf(p, q); } };
+struct Sum { template <typename V> __device__ __forceinline__ V operator()(V p, V q) const { return p + q; } };
+
+// What the wavefront has written to LDS, to itself.
+__device__ __forceinline__ void settle() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// A number that at least K <= 64 of the workgroup's x reach (their lowest six bits apart): the K-th largest of the maxima of 64
+// groups of threads.  lds: 65 words, 16-byte aligned; every thread has to come here.
+template <int THREADS>
+__device__ __forceinline__ uint32_t block_bound(uint32_t x, int K, uint32_t* lds) {
+  constexpr int L = THREADS / 64, N = 16 / L;        // threads of a group; each compares its maximum with 4 N others
+  const int g = threadIdx.x / L, l = threadIdx.x % L;
+  const uint32_t y = (lanes_join<L>(x, Max()) & ~63u) | (63 - g);
+  if (l == 0) lds[g] = y;
+  __syncthreads();
+  int rank = 0;
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    const uint4 v = ((const uint4*)lds)[l * N + u];
+    rank += (v.x > y) + (v.y > y) + (v.z > y) + (v.w > y);
+  }
+  rank = lanes_join<L>(rank, Sum());
+  if (l == 0 && rank == K - 1) lds[64] = y;
+  __syncthreads();
+  return lds[64] & ~63u;
 }
 
 // ---- lists of a wavefront's best logits, in LDS
@@ -60,6 +111,24 @@ __device__ __forceinline__ uint32_t kth(const uint32_t (&x)[N], int K) {
   return t;
 }
 
+// How many of a list's n entries are above e; behind them are zeros up to a multiple of eight.
+__device__ __forceinline__ int above(const unsigned long long* list, int n, unsigned long long e) {
+  int rank = 0;
+#pragma unroll 1
+  for (int j = 0; j < n; j += 8) {
+    ulonglong2 y[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) y[u] = ((const ulonglong2*)(list + j))[u];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) rank += (y[u].x > e) + (y[u].y > e);
+  }
+  return rank;
+}
+__device__ __forceinline__ void zeros_behind(unsigned long long* list, int n) {
+  if ((threadIdx.x & 63) < 8) list[n + (threadIdx.x & 63)] = 0;
+  settle();
+}
+
 // The K best of a list of n entries, to its front; n becomes min(n, K), the answer the K-th best (0: there are fewer).
 template <int LOW>
 __device__ __forceinline__ unsigned long long keep_best(unsigned long long* list, int& n, int K) {
@@ -67,12 +136,11 @@ __device__ __forceinline__ unsigned long long keep_best(unsigned long long* list
   if (n < K) return 0;
   if (n <= 64) {                       // each entry's place by counting
     const unsigned long long e = lane < n ? list[lane] : 0;
-    int rank = 0;
-    for (int j = 0; j < n; ++j) rank += list[j] > e;
+    zeros_behind(list, n);
+    const int rank = above(list, n, e);
     __builtin_amdgcn_wave_barrier();
     if (lane < n && rank < K) list[rank] = e;
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+    settle();
     n = K;
     return list[K - 1];
   }
@@ -109,7 +177,7 @@ __device__ __forceinline__ unsigned long long keep_best(unsigned long long* list
     uint32_t least = 0xFFFFFFFFu;
 #pragma unroll
     for (int j = 0; j < SEL_OWN; ++j) least = at[j] ? min(least, at[j]) : least;
-    low = wave_join(least, [](uint32_t p, uint32_t q) { return min(p, q); });
+    low = ~lanes_join<64>(~least, Max());
   }
   int base = 0;
   uint32_t full = 0;                   // of an entry at t
@@ -123,8 +191,7 @@ __device__ __forceinline__ unsigned long long keep_best(unsigned long long* list
     const unsigned long long edge = __ballot(at[j] == low);
     if (edge) full = __builtin_amdgcn_readlane(hi[j], __builtin_ctzll(edge));
   }
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
+  settle();
   n = base;
   return (unsigned long long)full << 32 | low;
 }
@@ -152,17 +219,17 @@ __device__ __forceinline__ float exp_of(float d) {
   return __builtin_amdgcn_exp2f(__builtin_fmaf(d, 0x1.715476p+0f, d * 0x1.4ae0cp-26f));
 }
 
-// Maximum, sum and best logits of a piece of a row: a.tiles tiles of 1024 16-byte blocks.  Each wavefront keeps its best logits in a
-// list, into which goes whatever is above the n_out-th best so far: of the first tile, above the n_out-th largest of the
-// lanes' maxima (which as many logits reach).  A later block of a wavefront holds later tokens, so that a logit equal to the n_out-th best
-// is not wanted any more and one comparison of a block's maximum decides.
+// Maximum, sum and best logits of a piece of a row: a.blocks blocks of 16 bytes, 1024 (a tile) at a time.  Each wavefront keeps a list
+// of its logits that reach a bound: one that n_out of the threads' maxima so far reach, made anew after 1, 2, 4, .. tiles, or where
+// a list has been full its n_out-th best.  At the end the same bound leaves few entries of all lists, and the best of these go out.
 template <typename T>
 __global__ __launch_bounds__(SEL_THREADS) void k_select_rows(SelectArgs a) {
   constexpr int VEC = 16 / sizeof(T), NW = SEL_THREADS / 64, LOW = SEL_LOW<T>;
   __shared__ double s_sum[NW];
   __shared__ float s_max[NW];
-  __shared__ int s_n[NW];
-  __shared__ unsigned long long s_list[NW][SEL_LIST];
+  __shared__ int s_count;
+  __shared__ __align__(16) uint32_t s_bound[68];
+  __shared__ __align__(16) unsigned long long s_list[NW][SEL_LIST + 8], s_all[SEL_THREADS + 8];
   const int64_t id = wide_block();
   const int64_t row = id / a.pieces;
   const int piece = (int)(id % a.pieces), V = a.b.n_vocab, K = a.b.n_out, tid = threadIdx.x, lane = tid & 63;
@@ -173,21 +240,30 @@ __global__ __launch_bounds__(SEL_THREADS) void k_select_rows(SelectArgs a) {
   const int skip = (int)((uintptr_t)p / sizeof(T) % VEC);
   p -= skip;
   unsigned long long* const list = s_list[wv];
-  const int first = piece * a.tiles, last = min(first + a.tiles, (skip + V + SEL_TILE * VEC - 1) / (SEL_TILE * VEC));
-  auto place = [&](int tile, int c) { return ((tile * SEL_VECS + c) * SEL_THREADS + tid) * VEC; };
+  const int first = piece * a.blocks, end = min((piece + 1) * a.blocks, (skip + V + VEC - 1) / VEC);
+  // first element of a thread's block (outside the row: behind the piece)
+  auto place = [&](int base, int c) {
+    const int b = base + c * SEL_THREADS + tid;
+    return b < end ? b * VEC : skip + V;
+  };
   uint4 next[SEL_VECS];
 #pragma unroll
   for (int c = 0; c < SEL_VECS; ++c) next[c] = load_block(p, place(first, c), skip, V);
-  float m = -INFINITY, limit = 0.f;
+  if (tid == 0) s_count = 0;
+  s_all[tid] = 0;
+  if (tid < 8) s_all[SEL_THREADS + tid] = 0;
+  float m = -INFINITY, limit = -FLT_MAX;
   double sum = 0.0;
-  int n = 0;
-  unsigned long long bar = 0;          // the n_out-th best so far, 0: there are fewer
-  for (int tile = first; tile < last; ++tile) {
+  int n = 0, tiles = 0;
+  unsigned long long bar = 0;          // what goes into the list is above this, 0: anything
+  for (int base = first; base < end; base += SEL_TILE) {
     float x[SEL_VECS][VEC], top[SEL_VECS];
+    int at[SEL_VECS];
 #pragma unroll
     for (int c = 0; c < SEL_VECS; ++c) {
       const uint32_t u[4] = {next[c].x, next[c].y, next[c].z, next[c].w};
       top[c] = -INFINITY;
+      at[c] = place(base, c) - skip;
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
         if constexpr (sizeof(T) == 4) x[c][i] = __uint_as_float(u[i]);
@@ -195,9 +271,9 @@ __global__ __launch_bounds__(SEL_THREADS) void k_select_rows(SelectArgs a) {
         top[c] = fmaxf(top[c], x[c][i]);
       }
     }
-    if (tile + 1 < last)
+    if (base + SEL_TILE < end)
 #pragma unroll
-      for (int c = 0; c < SEL_VECS; ++c) next[c] = load_block(p, place(tile + 1, c), skip, V);
+      for (int c = 0; c < SEL_VECS; ++c) next[c] = load_block(p, place(base + SEL_TILE, c), skip, V);
     float mt = top[0];
 #pragma unroll
     for (int c = 1; c < SEL_VECS; ++c) mt = fmaxf(mt, top[c]);
@@ -210,245 +286,253 @@ __global__ __launch_bounds__(SEL_THREADS) void k_select_rows(SelectArgs a) {
 #pragma unroll
     for (int c = 0; c < SEL_VECS; ++c)
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        s += exp_of(x[c][i] - ref);
-      }
+      for (int i = 0; i < VEC; ++i) s += exp_of(x[c][i] - ref);
     sum += (double)s;
 
     // ---- into the list
-    bool any;
-    if (tile == first) {
-      const uint32_t t[1] = {mt > -INFINITY ? float_key(mt + 0.f) : 0u};
-      bar = (unsigned long long)kth<16>(t, K) << 32;   // (its upper bits: below every logit that reaches it)
-      limit = bar ? logit_of(bar) : -INFINITY;
-      any = true;
-    } else {
-      any = mt > limit;
+    if ((tiles & (tiles + 1)) == 0) {
+      const unsigned long long least = (unsigned long long)block_bound<SEL_THREADS>(m > -INFINITY ? float_key(m + 0.f) : 0u, K, s_bound) << 32;
+      bar = least > bar ? least : bar;
+      limit = bar ? logit_of(bar) : -FLT_MAX;
     }
-    if (__ballot(any)) {
+    ++tiles;
+    if (!__ballot(mt >= limit)) continue;
 #pragma unroll
-      for (int c = 0; c < SEL_VECS; ++c) {
-        if (!__ballot(tile == first ? top[c] >= limit : top[c] > limit)) continue;
+    for (int c = 0; c < SEL_VECS; ++c) {
+      if (!__ballot(top[c] >= limit)) continue;
+      uint32_t hits = 0;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          if (!__ballot(x[c][i] >= limit)) continue;
-          const unsigned long long key = key_of(x[c][i], (uint32_t)(place(tile, c) - skip + i));
-          unsigned long long mask = __ballot(key > bar);
-          if (!mask) continue;
-          if (n + __popcll(mask) > SEL_LIST) {
-            bar = keep_best<LOW>(list, n, K);
-            mask = __ballot(key > bar);
-          }
-          if (key > bar) list[n + __popcll(mask & ((1ull << lane) - 1))] = key;
-          n += __popcll(mask);
-          __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-          __builtin_amdgcn_wave_barrier();
+      for (int i = 0; i < VEC; ++i) hits |= x[c][i] >= limit ? 1u << i : 0u;
+      while (__ballot(hits)) {         // one of each lane's at a time
+        const int which = __builtin_ctz(hits | 1u << VEC);
+        float y = x[c][0];
+#pragma unroll
+        for (int i = 1; i < VEC; ++i) y = which == i ? x[c][i] : y;
+        const unsigned long long key = hits ? key_of(y, (uint32_t)(at[c] + which)) : 0;
+        hits &= hits - 1;
+        unsigned long long mask = __ballot(key > bar);
+        if (n + __popcll(mask) > SEL_LIST) {
+          bar = keep_best<LOW>(list, n, K);            // (the list is full: n_out and more)
+          limit = logit_of(bar);
+          mask = __ballot(key > bar);
         }
+        if (key > bar) list[n + __popcll(mask & ((1ull << lane) - 1))] = key;
+        n += __popcll(mask);
+        settle();
       }
-      if (tile + 1 < last && (tile == first || n >= K + 64)) bar = keep_best<LOW>(list, n, K);
     }
-    limit = bar ? logit_of(bar) : -INFINITY;
   }
   if (n > 64) keep_best<LOW>(list, n, K);
-  const float wm = wave_join(m, [](float p, float q) { return fmaxf(p, q); });
+  const float wm = lanes_join<64>(m, MaxF());
   // (a thread of which everything is masked out has a sum of 0; a NaN stays one)
   sum *= m == wm ? 1.0 : (double)exp_of(m - wm);
-  sum = wave_join(sum, [](double p, double q) { return p + q; });
+  sum = lanes_join<64>(sum, Sum());
   if (lane == 0) {
     s_max[wv] = wm;
     s_sum[wv] = sum;
-    s_n[wv] = n;
   }
+  // ---- the best of all lists, up to 64 entries each
+  const unsigned long long e = lane < n ? list[lane] : 0;
+  const uint32_t least = max(block_bound<SEL_THREADS>((uint32_t)(e >> 32), K, s_bound), 1u);
+  const unsigned long long mask = __ballot((uint32_t)(e >> 32) >= least);
+  int to = 0;
+  if (lane == 0 && mask) to = atomicAdd(&s_count, __popcll(mask));     // (in any order)
+  to = __builtin_amdgcn_readfirstlane(to);
+  if ((uint32_t)(e >> 32) >= least) s_all[to + __popcll(mask & ((1ull << lane) - 1))] = e;
   __syncthreads();
-  // ---- the wavefronts' sums joined, and the best of their lists (up to 64 entries each), an entry a thread
-  const int64_t at = row * a.pieces + piece;
-  if (tid == 0) {
+  const int64_t to_row = row * a.pieces + piece;
+  const int all = s_count;
+  if (tid == SEL_THREADS - 1) {
     float M = s_max[0];
     for (int w = 1; w < NW; ++w) M = fmaxf(M, s_max[w]);
     double S = 0.0;
     for (int w = 0; w < NW; ++w) S += s_sum[w] * (s_max[w] == M ? 1.0 : (double)exp_of(s_max[w] - M));
-    a.part_m[at] = M;
-    a.part_s[at] = S;
+    a.part_m[to_row] = M;
+    a.part_s[to_row] = S;
   }
-  const unsigned long long e = lane < n ? list[lane] : 0;
-  int rank = 0, all = 0;
-  for (int w = 0; w < NW; ++w) {
-    const int nw = s_n[w];
-    for (int j = 0; j < nw; ++j) rank += s_list[w][j] > e;
-    all += nw;
-  }
-  if (lane < n && rank < K) a.keys[at * K + rank] = e;
-  for (int k = all + tid; k < K; k += SEL_THREADS) a.keys[at * K + k] = 0;
+  if (wv * 64 >= max(all, K)) return;
+  const unsigned long long own = s_all[tid];
+  const int rank = own ? above(s_all, all, own) : tid;       // (behind the entries: zeros)
+  if (rank < K) a.keys[to_row * K + rank] = own;
 }
 
-// A continuation: larger first.
-struct Cont { double score; int beam; unsigned long long key; };
-__device__ __forceinline__ bool before(const Cont& x, const Cont& y) {
-  return x.score > y.score || (x.score == y.score && (x.beam < y.beam || (x.beam == y.beam && x.key > y.key)));
+// A continuation as whole numbers, the first more significant; all 0: none.
+struct Cont {
+  unsigned long long score;            // of the order of the score in 64 bits
+  unsigned long long rest;             // 63 - beam, the logit, the complement of the token: 6, 32 and 24 bits
+};
+// (a subtraction of 128 bits, whose borrow is the answer)
+__device__ __forceinline__ bool over(const Cont& x, const Cont& y) {
+  unsigned c;
+  __builtin_subc((uint32_t)y.rest, (uint32_t)x.rest, 0u, &c);
+  __builtin_subc((uint32_t)(y.rest >> 32), (uint32_t)(x.rest >> 32), c, &c);
+  __builtin_subc((uint32_t)y.score, (uint32_t)x.score, c, &c);
+  __builtin_subc((uint32_t)(y.score >> 32), (uint32_t)(x.score >> 32), c, &c);
+  return c;
 }
-__device__ __forceinline__ Cont better(const Cont& x, const Cont& y) { return before(x, y) ? x : y; }
+__device__ __forceinline__ Cont higher(const Cont& x, const Cont& y) { return over(x, y) ? x : y; }
+__device__ __forceinline__ Cont cont_of(double score, int beam, unsigned long long key) {
+  if (!(score - score == 0.0)) return {0, 0};                // (only finite scores)
+  const long long b = __double_as_longlong(score + 0.0);     // (-0 counts as 0)
+  return {(unsigned long long)(b < 0 ? ~b : b | (long long)(1ull << 63)),
+          (unsigned long long)(63 - beam) << 56 | (key >> 32) << 24 | (key & 0xFFFFFFu)};
+}
+__device__ __forceinline__ double score_of(const Cont& x) {
+  const long long s = (long long)x.score;
+  return __longlong_as_double(s < 0 ? s ^ (long long)(1ull << 63) : ~s);
+}
 
 // A workgroup a request, a wavefront a row or a part of one.  Of the continuations that the rows' pieces have left, those that reach a
-// bound go into a list in LDS, and an entry's place in the answer is the number of entries before it.  The bound: of the wavefront that
-// has the highest, the n_out-th largest of its lanes' maxima.  Where more reach it than the list holds (scores that are all equal) the answer is
-// found one at a time.
+// bound go into a list in LDS, and an entry's place in the answer is the number of entries above it.  Of a long list (where one beam
+// is far ahead of the others, most threads' maxima tell little) the same bound is taken again over the list.  Where more reach it
+// than the list holds (scores that are all equal) the answer is found one at a time.
 constexpr int JOIN_WAVES = 16, JOIN_LIST = 64 * JOIN_WAVES, JOIN_AHEAD = 4;
 __global__ __launch_bounds__(JOIN_LIST) void k_select_join(SelectArgs a) {
   constexpr int NW = JOIN_WAVES;
   __shared__ double s_score[64], s_log[64];
   __shared__ float s_top[64];
-  __shared__ int s_end[64], s_count;
-  __shared__ uint32_t s_bar[NW];
-  __shared__ __align__(16) uint32_t s_floor[JOIN_LIST];
-  __shared__ Cont s_list[JOIN_LIST];
+  __shared__ int s_end[64], s_count[2];
+  __shared__ __align__(16) uint32_t s_bound[68];
+  __shared__ __align__(16) Cont s_list[JOIN_LIST + 4];
   const int B = a.b.n_beams, K = a.b.n_out, C = a.pieces, tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t g = blockIdx.x;
   const unsigned long long* const keys = a.keys + g * B * C * K;
-  // rows of this wavefront: row0, row0 + NW, ..; of such a row every `parts`-th 64 keys
-  const int parts = max(1, NW / B), row0 = wv / parts, part = wv % parts, per = C * K;
-  const Cont none = {-INFINITY, 1 << 30, 0};
-  // (none where the score is not finite)
+  // rows of this wavefront: row0, row0 + step, ..; of such a row every `parts`-th `wide` keys
+  const int parts = max(1, NW / B), step = NW / parts, row0 = wv / parts, part = wv % parts, per = C * K;
+  const int wide = min(64, (per + parts - 1) / parts), hop = wide * parts;
+  const int spread = (lane & 15) * 4 + (lane >> 4), at0 = spread < wide ? part * wide + spread : per;     // (neighbours to other groups)
   auto cont = [&](int b, unsigned long long key) {
-    const Cont x = {s_score[b] + (((double)logit_of(key) - (double)s_top[b]) - s_log[b]), b, key};
-    return key && x.score - x.score == 0.0 ? x : none;
+    return key ? cont_of(s_score[b] + (((double)logit_of(key) - (double)s_top[b]) - s_log[b]), b, key) : Cont{0, 0};
   };
-  auto ended = [&](int b) {
-    const Cont x = {s_score[b], b, (unsigned long long)(uint32_t)~a.b.end_token};
-    return x.score - x.score == 0.0 ? x : none;
-  };
-  // a score as a float that is not above it, as a whole number
-  auto floor_of = [](double s) {
-    const float f = (float)s;
-    const uint32_t k = float_key(f);
-    return s > -INFINITY ? ((double)f > s ? k - 1 : k) : 0u;
-  };
-  if (tid == 0) s_count = 0;
-  uint32_t top[1] = {0};
-  for (int b = row0; b < B; b += NW / parts) {
+  if (tid < 2) s_count[tid] = 0;
+  unsigned long long mine[JOIN_AHEAD];         // of row0
+  uint32_t top = 0;                            // (of the order of a score, 32 of 64 bits)
+  for (int b = row0; b < B; b += step) {
     const int64_t row = g * B + b;
     const bool end = a.finished && a.finished[row];
+    // (all that is read at once; of a beam that has ended it is not looked at)
     unsigned long long key[JOIN_AHEAD];
 #pragma unroll
     for (int u = 0; u < JOIN_AHEAD; ++u) {
-      const int i = (u * parts + part) * 64 + lane;
-      key[u] = !end && i < per ? keys[b * per + i] : 0;
+      const int i = at0 + u * hop;
+      key[u] = i < per ? keys[b * per + i] : 0;
+      if (b == row0) mine[u] = key[u];
     }
-    double S = 0.0;
-    float M = -INFINITY;
     const double score = a.scores[row];
+    float m = lane < C ? a.part_m[row * C + lane] : -INFINITY;
+    double S = 0.0, s = lane < C ? a.part_s[row * C + lane] : 0.0;
+    float M = -INFINITY;
     if (!end) {
-      float m = lane < C ? a.part_m[row * C + lane] : -INFINITY;
-      double s = lane < C ? a.part_s[row * C + lane] : 0.0;
       for (int c = lane + 64; c < C; c += 64) {
         const float mc = a.part_m[row * C + c], mx = fmaxf(m, mc);
         s = s * (m == mx ? 1.0 : (double)exp_of(m - mx)) + a.part_s[row * C + c] * (mc == mx ? 1.0 : (double)exp_of(mc - mx));
         m = mx;
       }
-      M = wave_join(m, [](float p, float q) { return fmaxf(p, q); });
-      S = wave_join(s * (m == M ? 1.0 : (double)exp_of(m - M)), [](double p, double q) { return p + q; });
+      M = lanes_join<64>(m, MaxF());
+      S = lanes_join<64>(s * (m == M ? 1.0 : (double)exp_of(m - M)), Sum());
     }
-    if (lane == 0 && part == 0) {
+    if (lane == 0) {                   // (the parts of a row write the same)
       s_end[b] = end;
-    }
-    if (lane == 0) {                   // (all parts write the same)
       s_score[b] = score;
       s_log[b] = log(S);
       s_top[b] = M;
     }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+    settle();
     if (end) {
-      if (lane == 0) top[0] = max(top[0], floor_of(ended(b).score));
+      if (lane == 0 && part == 0) top = max(top, (uint32_t)(cont_of(score, b, 0).score >> 32));
       continue;
     }
 #pragma unroll
-    for (int u = 0; u < JOIN_AHEAD; ++u) top[0] = max(top[0], floor_of(cont(b, key[u]).score));
-    for (int i = (JOIN_AHEAD * parts + part) * 64 + lane; i < per; i += parts * 64) top[0] = max(top[0], floor_of(cont(b, keys[b * per + i]).score));
+    for (int u = 0; u < JOIN_AHEAD; ++u) top = max(top, (uint32_t)(cont(b, key[u]).score >> 32));
+    for (int i = at0 + JOIN_AHEAD * hop; i < per; i += hop)
+      top = max(top, (uint32_t)(cont(b, keys[b * per + i]).score >> 32));
   }
-  const uint32_t own = kth<12>(top, K);
-  if (lane == 0) s_bar[wv] = own;
-  __syncthreads();
-  uint32_t bar = 1;
-  for (int w = 0; w < NW; ++w) bar = max(bar, s_bar[w]);
-  auto put_in = [&](const Cont& x) {
-    const uint32_t f = floor_of(x.score);
-    if (f < bar) return;
-    const int at = atomicAdd(&s_count, 1);             // (in any order)
-    if (at < JOIN_LIST) {
-      s_list[at] = x;
-      s_floor[at] = f;
-    }
+  uint32_t bar = max(block_bound<JOIN_LIST>(top, K, s_bound), 1u);
+  auto put_in = [&](const Cont& x, int which) {
+    const bool in = (uint32_t)(x.score >> 32) >= bar;
+    const unsigned long long mask = __ballot(in);
+    if (!mask) return;
+    int to = 0;
+    if (lane == __builtin_ctzll(mask)) to = atomicAdd(&s_count[which], __popcll(mask));      // (in any order)
+    to = __builtin_amdgcn_readlane(to, __builtin_ctzll(mask)) + __popcll(mask & ((1ull << lane) - 1));
+    if (in && to < JOIN_LIST) s_list[to] = x;
   };
-  for (int b = row0; b < B; b += NW / parts) {
+  for (int b = row0; b < B; b += step) {
     if (s_end[b]) {
-      if (part == 0 && lane == 0) put_in(ended(b));
+      if (part == 0) put_in(lane == 0 ? cont_of(s_score[b], b, 0) : Cont{0, 0}, 0);
       continue;
     }
-    for (int i = part * 64 + lane; i < per; i += parts * 64) put_in(cont(b, keys[b * per + i]));
+    int i = 0;                         // (the same for all lanes)
+    if (b == row0) {
+#pragma unroll
+      for (int u = 0; u < JOIN_AHEAD; ++u) put_in(cont(b, mine[u]), 0);
+      i += JOIN_AHEAD * hop;
+    }
+    for (; i < per; i += hop) put_in(cont(b, i + at0 < per ? keys[b * per + i + at0] : 0), 0);
   }
   __syncthreads();
-  const int n = s_count;
+  int n = s_count[0];
+  if (n > 128 && n <= JOIN_LIST) {
+    const int i = (tid & 15) * 64 + (tid >> 4);        // (neighbours to other groups)
+    const Cont x = i < n ? s_list[i] : Cont{0, 0};
+    bar = max(block_bound<JOIN_LIST>((uint32_t)(x.score >> 32), K, s_bound), 1u);
+    put_in(x, 1);
+    __syncthreads();
+    n = s_count[1];
+  }
   auto give = [&](int k, const Cont& x) {
-    const bool there = x.score > -INFINITY;
-    const int token = there ? (int)token_of(x.key) : -1;
-    a.new_scores[g * K + k] = (float)x.score;
-    a.parents[g * K + k] = there ? x.beam : -1;
+    const bool there = x.score != 0;
+    const int beam = 63 - (int)(x.rest >> 56);
+    const bool end = there && s_end[beam];
+    const int token = !there ? -1 : end ? a.b.end_token : (int)(~x.rest & 0xFFFFFFu);
+    a.new_scores[g * K + k] = there ? (float)score_of(x) : -INFINITY;
+    a.parents[g * K + k] = there ? beam : -1;
     a.tokens[g * K + k] = token;
-    if (a.new_finished) a.new_finished[g * K + k] = !there || token == a.b.end_token || s_end[x.beam];
+    if (a.new_finished) a.new_finished[g * K + k] = !there || end || token == a.b.end_token;
   };
   if (n <= JOIN_LIST) {
-    // (whole floats first: only scores that are equal as such are compared in 64 bits)
+    if (wv * 64 >= max(n, K)) return;
     if (tid < n) {
-      const uint32_t f = s_floor[tid];
-      int rank = 0, equal = 0;
-      for (int j = 0; j < n; ++j) {
-        rank += s_floor[j] > f;
-        equal += s_floor[j] == f;
-      }
       const Cont x = s_list[tid];
-      if (equal > 1)
-        for (int j = 0; j < n; ++j) rank += s_floor[j] == f && before(s_list[j], x);
+      int rank = 0;
+#pragma unroll 4
+      for (int j = 0; j < n; ++j) rank += over(s_list[j], x);
       if (rank < K) give(rank, x);
     }
-    for (int k = n + tid; k < K; k += JOIN_LIST) give(k, none);
+    if (tid >= n && tid < K) give(tid, {0, 0});
     return;
   }
-  Cont last = {INFINITY, -1, ~0ull};
-  Cont* const s_best = s_list;         // [2][NW]
+  Cont last = {~0ull, ~0ull};
   for (int k = 0; k < K; ++k) {
-    Cont best = none;
-    for (int b = row0; b < B; b += NW / parts) {
-      if (s_end[b]) {
-        const Cont x = ended(b);
-        if (before(last, x)) best = better(best, x);
-        continue;
-      }
-      for (int i = part * 64 + lane; i < per; i += parts * 64) {
-        const Cont x = cont(b, keys[b * per + i]);
-        if (before(last, x)) best = better(best, x);
-      }
+    Cont best = {0, 0};
+    auto look = [&](const Cont& x) {
+      if (over(last, x)) best = higher(best, x);
+    };
+    for (int b = row0; b < B; b += step) {
+      if (s_end[b]) look(cont_of(s_score[b], b, 0));
+      else
+        for (int i = at0; i < per; i += hop) look(cont(b, keys[b * per + i]));
     }
-    for (int d = 1; d < 64; d <<= 1) {
-      const Cont o = {__shfl_xor(best.score, d), __shfl_xor(best.beam, d), __shfl_xor(best.key, d)};
-      best = better(best, o);
-    }
-    if (lane == 0) s_best[(k & 1) * NW + wv] = best;
+    for (int d = 1; d < 64; d <<= 1) best = higher(best, Cont{__shfl_xor(best.score, d), __shfl_xor(best.rest, d)});
+    Cont* const s_best = s_list + (k & 1) * NW;
+    if (lane == 0) s_best[wv] = best;
     __syncthreads();
-    for (int w = 0; w < NW; ++w) best = better(best, s_best[(k & 1) * NW + w]);
+    for (int w = 0; w < NW; ++w) best = higher(best, s_best[w]);
     last = best;
     if (tid == 0) give(k, best);
   }
 }
 
-struct SelectPlan { int pieces, tiles; };
+struct SelectPlan { int pieces, blocks; };
 SelectPlan select_plan(const Beams& b) {
   const int vec = b.dtype == RESTKV_F32 ? 4 : 8;
-  const int all = (b.n_vocab / vec + 2 + SEL_TILE - 1) / SEL_TILE;       // (blocks of 16 bytes that a row may touch)
-  // workgroups for four on each compute unit, if there is as much
+  const int all = (b.n_vocab + vec - 1) / vec + 1;     // blocks of 16 bytes that a row may touch
+  // even pieces of a tile at least, as many as four workgroups on each compute unit take
   const int64_t rows = (int64_t)b.n_groups * b.n_beams, want = 4 * n_cu();
-  const int tiles = (int)std::max<int64_t>(1, rows * all / want);
-  return {(all + tiles - 1) / tiles, tiles};
+  const int pieces = (int)std::min<int64_t>((all + SEL_TILE - 1) / SEL_TILE, std::max<int64_t>(1, want / std::max<int64_t>(rows, 1)));
+  const int blocks = (all + pieces - 1) / pieces;
+  return {(all + blocks - 1) / blocks, blocks};
 }
 struct SelectWs { size_t s, m, keys, bytes; };
 SelectWs select_ws(const Beams& b) {
@@ -473,7 +557,7 @@ int launch_beam_select(const Beams& b, const void* logits, const float* scores, 
   a.logits = logits; a.scores = scores; a.finished = finished;
   a.new_scores = new_scores; a.parents = parents; a.tokens = tokens; a.new_finished = new_finished;
   const SelectPlan plan = select_plan(b);
-  a.pieces = plan.pieces; a.tiles = plan.tiles;
+  a.pieces = plan.pieces; a.blocks = plan.blocks;
   a.part_s = (double*)(ws + lay.s); a.part_m = (float*)(ws + lay.m); a.keys = (unsigned long long*)(ws + lay.keys);
   const dim3 grid = wide_grid((int64_t)b.n_groups * b.n_beams * a.pieces);
   if (b.dtype == RESTKV_F32) hipLaunchKernelGGL(k_select_rows<float>, grid, dim3(SEL_THREADS), 0, st, a);
