@@ -7,57 +7,18 @@ namespace restkv {
 
 namespace {
 
-// Sums of an entry's chunks joined into its output: a workgroup a row (new token, query head), 256 threads as 1024 / d
-// groups that take every so manyeth chunk, four channels a thread.  A chain of two reads (where the chunks are, what they
-// hold) and a launch: chunks are read four at a time, references with the sums.  3.6 to 5 us for decoding steps, 8.3 for the 33 MB of
-// 256 queries a KV head.
 template <int D>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
-  constexpr int TPR = D / 4, NGR = 256 / TPR, AHEAD = 4;
-  __shared__ float4 sm_x[NGR][TPR];
-  __shared__ float sm_m[NGR], sm_l[NGR];
   const Pages& pg = a.pg;
   const int i = blockIdx.x / pg.Hq, head = blockIdx.x % pg.Hq, h = head / pg.G, s = blockIdx.y;
   const int2 pl = a.plan[a.per_head ? s * pg.Hkv + h : s];       // (of a sequence without new tokens: whatever it is, not used)
   const NewRows nr = new_rows(pg, s);
   if (i >= nr.n || pl.y < 2) return;
   const int hy = a.per_head ? 0 : h, row = i * pg.G + head - h * pg.G, rows = pg.G * pg.max_new;
-  const int g = threadIdx.x / TPR, c = threadIdx.x % TPR;
-  float M = -INFINITY, L = 0.f;
-  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto take = [&](float m, float l, float4 y) {
-    // (a chunk of which the row sees nothing has a reference of -inf and sums of 0)
-    const float n = fmaxf(M, m);
-    const float fo = M == n ? 1.f : __builtin_amdgcn_exp2f(M - n), fn = m == n ? 1.f : __builtin_amdgcn_exp2f(m - n);
-    M = n;
-    L = L * fo + l * fn;
-    x.x = x.x * fo + y.x * fn; x.y = x.y * fo + y.y * fn; x.z = x.z * fo + y.z * fn; x.w = x.w * fo + y.w * fn;
-  };
-  for (int k = g; k < pl.y; k += NGR * AHEAD) {
-    float m[AHEAD], l[AHEAD];
-    float4 y[AHEAD];
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      const int kk = min(k + u * NGR, pl.y - 1);
-      const int64_t at = (int64_t)((pl.x + kk) * a.Hy + hy) * rows + row;
-      m[u] = a.part_m[at];
-      l[u] = a.part_l[at];
-      y[u] = *(const float4*)&a.part_o[at * D + c * 4];
-    }
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u)
-      if (k + u * NGR < pl.y) take(m[u], l[u], y[u]);
-  }
-  sm_x[g][c] = x;
-  if (c == 0) {
-    sm_m[g] = M;
-    sm_l[g] = L;
-  }
-  __syncthreads();
-  if (g) return;
-#pragma unroll
-  for (int k = 1; k < NGR; ++k) take(sm_m[k], sm_l[k], sm_x[k][c]);
-  store_out(a, nr.first + i, head, c * 4, x, M, L);
+  join_chunks<D>(a, pl.y, nr.first + i, head, [&](int k) {
+    const int64_t at = (int64_t)((pl.x + k) * a.Hy + hy) * rows + row;
+    return Part{a.part_m + at, a.part_l + at, a.part_o + at * D};
+  });
 }
 
 struct AttendPlan { int R, many, waves, c_min, target; int64_t row_blocks, entries, Hy, chunks, slots; };
@@ -121,28 +82,35 @@ AttendWs attend_ws(const Pages& pg, const AttendPlan& p) {
 
 size_t attend_ws_bytes(const Pages& pg) { return attend_ws(pg, attend_plan(pg)).bytes; }
 
+AttendArgs attend_args(const Pages& pg, const void* q, const void* k_pages, const void* v_pages, const void* k_scale,
+                       const void* v_scale, void* out, float* lse) {
+  AttendArgs a = {};
+  a.pg = pg;
+  a.q = q; a.k = (const char*)k_pages; a.v = (const char*)v_pages;
+  a.ks = (const uint32_t*)k_scale; a.vs = (const uint32_t*)v_scale;
+  a.out = out; a.lse = lse;
+  a.per_head = pg.lens_sh != 0;
+  const int qel = pg.dtype == RESTKV_F32 ? 4 : 8;
+  a.vec_q = !((uintptr_t)q & 15u) && !((pg.q_st | pg.q_sh) & (qel - 1));
+  const int oal = pg.out_dtype == RESTKV_F32 ? 15 : 7;
+  a.vec_out = !((uintptr_t)out & oal) && !((pg.o_st | pg.o_sh) & 3);
+  return a;
+}
+
 int launch_attend(const Pages& pg, const void* q, const void* k_pages, const void* v_pages, const void* k_scale,
                   const void* v_scale, void* out, float* lse, char* ws, hipStream_t st) {
   const AttendPlan p = attend_plan(pg);
   const AttendWs lay = attend_ws(pg, p);
   if (p.chunks * p.Hy > (int64_t)1 << 30 || p.row_blocks * p.waves > (1 << 22) || (p.slots && (int64_t)pg.max_new * pg.Hq >= (1 << 24)))
     return RESTKV_EUNSUPPORTED;
-  AttendArgs a = {};
-  a.pg = pg;
-  a.q = q; a.k = (const char*)k_pages; a.v = (const char*)v_pages;
-  a.ks = (const uint32_t*)k_scale; a.vs = (const uint32_t*)v_scale;
-  a.out = out; a.lse = lse;
+  AttendArgs a = attend_args(pg, q, k_pages, v_pages, k_scale, v_scale, out, lse);
   if (p.slots) {
     a.plan = (int2*)(ws + lay.plan);
     a.part_m = (float*)(ws + lay.m); a.part_l = (float*)(ws + lay.l); a.part_o = (float*)(ws + lay.o);
   }
-  a.entries = (int)p.entries; a.per_head = pg.lens_sh != 0; a.Hy = (int)p.Hy;
+  a.entries = (int)p.entries; a.Hy = (int)p.Hy;
   a.row_blocks = (int)p.row_blocks; a.units = (int)(p.chunks * p.Hy);
   a.c_min = p.c_min; a.chunks = (float)((double)p.target / (double)(p.Hy * p.row_blocks) * (1 - 0x1p-23));
-  const int qel = pg.dtype == RESTKV_F32 ? 4 : 8;
-  a.vec_q = !((uintptr_t)q & 15u) && !((pg.q_st | pg.q_sh) & (qel - 1));
-  const int oal = pg.out_dtype == RESTKV_F32 ? 15 : 7;
-  a.vec_out = !((uintptr_t)out & oal) && !((pg.o_st | pg.o_sh) & 3);
   const int rc = p.many ? run_attend_rows(a, p.R, p.waves, st) : pg.fmt == RESTKV_F32 ? run_attend_f32(a, p.R, st) : pg.fmt == RESTKV_BF16 ? run_attend_bf16(a, st) : run_attend_q4(a, p.R, st);
   if (rc || !p.slots) return rc;
   const dim3 grid(pg.max_new * pg.Hq, pg.n_seqs);

@@ -29,6 +29,12 @@ struct AttendArgs {
   int entries, per_head, Hy;        // an entry is a sequence, or with lengths per head a (sequence, head); Hy heads share it
   int row_blocks, units, c_min, vec_q, vec_out;
   float chunks;                     // workgroups wanted of each head and row block
+  // Beams (launch_attend_beams): entries 0 .. fronts-1 are the shared positions of groups of n_beams sequences (or of a group's
+  // head), the rows of all its beams for them; then each sequence's own positions behind these.  All chunks have a slot, those of fronts in
+  // front_*: [slots * Hy, n_beams rows], the others in part_*.
+  const int32_t* shared;
+  int n_beams, fronts;
+  float* front_m; float* front_l; float* front_o;
 };
 
 constexpr int ATT_TILE = 64;        // chunks are whole tiles of 64 keys
@@ -60,11 +66,53 @@ __device__ __forceinline__ int wave_scan(int x) {
 // passes: one sequence of 2048 tiles for 64 workgroups makes 63 chunks of up to 33, 24 sequences of 1 to 250 tiles (24.2 a workgroup) 61 of
 // up to 35, 256 entries of 9 to 33 tiles 497 of up to 13 for 512 workgroups (9.3 each).  Up to 64 entries a wavefront works this out by
 // itself, more are divided among the threads of the workgroup.
-struct Chunk { int e, tile0, tile1, index, count, slot0, told, first, n; };
-struct Entry { int told, first, n, tiles; };
+struct Chunk { int e, tile0, tile1, index, count, slot0, told, first, n, front; };
+struct Entry { int told, first, n, tiles, front; };      // front: tiles before the entry's first
+
+// Tiles of the positions that the beams of a group share, and all see: no more than any of them has in front of its new tokens.
+__device__ __forceinline__ int shared_tiles(const AttendArgs& a, int g, int h) {
+  const Pages& pg = a.pg;
+  constexpr int AHEAD = 8;
+  int room = (int)min((int64_t)max(a.shared[g], 0) << pg.lg_ps, (int64_t)pg.max_len), any = 0;
+  for (int b = 0; b < a.n_beams; b += AHEAD) {
+    int told[AHEAD], n[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int s = g * a.n_beams + min(b + u, a.n_beams - 1);
+      told[u] = told_len(pg, s, h);
+      n[u] = new_rows(pg, s).n;
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      if (n[u]) room = min(room, pg.causal ? max(told[u] - n[u], 0) : told[u]);
+      any |= n[u];
+    }
+  }
+  return any ? room / ATT_TILE : 0;
+}
+
+template <bool BEAMS>
 __device__ __forceinline__ Entry read_entry(const AttendArgs& a, int e) {
   const Pages& pg = a.pg;
-  Entry o = {0, 0, 0, 0};
+  Entry o = {0, 0, 0, 0, 0};
+  if constexpr (BEAMS) {
+    if (e < a.entries) {
+      const bool front = e < a.fronts;
+      const int x = front ? e : e - a.fronts, s = a.per_head ? x / pg.Hkv : x, h = a.per_head ? x - s * pg.Hkv : 0;
+      const int tiles = shared_tiles(a, front ? s : s / a.n_beams, h);
+      if (front) {
+        o = {tiles * ATT_TILE, 0, a.n_beams * pg.max_new, tiles, 0};
+      } else {
+        o.told = told_len(pg, s, h);
+        const NewRows nr = new_rows(pg, s);
+        o.first = nr.first;
+        o.n = nr.n;
+        o.front = tiles;
+        if (o.n) o.tiles = (min(o.told, pg.max_len) + ATT_TILE - 1) / ATT_TILE - tiles;
+      }
+    }
+    return o;
+  }
   if (e < a.entries) {
     const int s = a.per_head ? e / pg.Hkv : e, h = a.per_head ? e - s * pg.Hkv : 0;
     o.told = told_len(pg, s, h);
@@ -83,13 +131,13 @@ __device__ __forceinline__ int chunk_tiles(const AttendArgs& a, float total, int
 }
 __device__ __forceinline__ Chunk chunk_of(const Entry& x, int e, int index, int count, int slot0) {
   const int each = count == 1 ? x.tiles : (x.tiles + count - 1) / count, t0 = min(index * each, x.tiles);
-  return {e, t0, min(t0 + each, x.tiles), index, count, slot0, x.told, x.first, x.n};
+  return {e, x.front + t0, x.front + min(t0 + each, x.tiles), index, count, slot0, x.told, x.first, x.n, x.front};
 }
-template <int NW = 4>
+template <int NW = 4, bool BEAMS = false>
 __device__ __forceinline__ bool find_chunk(const AttendArgs& a, int x, int* lds, Chunk& o) {
   const int lane = threadIdx.x & 63;
   if (a.entries <= 64) {
-    const Entry en = read_entry(a, lane);
+    const Entry en = read_entry<BEAMS>(a, lane);
     int C = chunk_tiles(a, (float)wave_sum((uint32_t)en.tiles), __popcll(__ballot(en.tiles > 0)));
     int cnt = 0, inc = 0;
     for (int i = 0; i < 8; ++i) {       // (until they are fewer than the resident workgroups: a few too many cost a sixth of the time of 24 lengths)
@@ -98,21 +146,21 @@ __device__ __forceinline__ bool find_chunk(const AttendArgs& a, int x, int* lds,
       if (__builtin_amdgcn_readlane(inc, 63) <= a.chunks || a.entries >= a.chunks) break;
       C += C / 16 + 1;
     }
-    const int own = cnt > 1 ? cnt : 0, sl = wave_scan(own);
+    const int own = BEAMS || cnt > 1 ? cnt : 0, sl = BEAMS ? inc : wave_scan(own);
     const unsigned long long hit = __ballot(inc > x);
     if (!hit) return false;
     const int l = __builtin_ctzll(hit);
     auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
     const int count = of(cnt);
-    o = chunk_of({of(en.told), of(en.first), of(en.n), of(en.tiles)}, l, x - of(inc) + count, count, of(sl - own));
+    o = chunk_of({of(en.told), of(en.first), of(en.n), of(en.tiles), BEAMS ? of(en.front) : 0}, l, x - of(inc) + count, count, of(sl - own));
     return true;
   }
   const int tid = threadIdx.x, wv = tid >> 6;
-  Entry en = read_entry(a, tid);
+  Entry en = read_entry<BEAMS>(a, tid);
   int64_t tiles = en.tiles;
   int active = en.tiles > 0;
   for (int e = tid + 64 * NW; e < a.entries; e += 64 * NW) {
-    const int t = read_entry(a, e).tiles;
+    const int t = read_entry<BEAMS>(a, e).tiles;
     tiles += t;
     active += t > 0;
   }
@@ -138,8 +186,8 @@ __device__ __forceinline__ bool find_chunk(const AttendArgs& a, int x, int* lds,
   int run = 0, slots = 0;
   for (int base = 0; base < a.entries; base += 64 * NW) {
     const int e = base + tid;
-    if (base) en = read_entry(a, e);
-    const int cnt = e < a.entries ? max(1, (en.tiles + C - 1) / C) : 0, own = cnt > 1 ? cnt : 0;
+    if (base) en = read_entry<BEAMS>(a, e);
+    const int cnt = e < a.entries ? max(1, (en.tiles + C - 1) / C) : 0, own = BEAMS || cnt > 1 ? cnt : 0;
     int inc = wave_scan(cnt), sl = wave_scan(own);
     if (lane == 63) {
       lds[2 * NW + wv] = inc;
@@ -160,13 +208,13 @@ __device__ __forceinline__ bool find_chunk(const AttendArgs& a, int x, int* lds,
     if (inc > x && inc - cnt <= x) {
       const Chunk c = chunk_of(en, e, x - inc + cnt, cnt, sl - own);
       at[0] = c.e; at[1] = c.tile0; at[2] = c.tile1; at[3] = c.index; at[4] = c.count; at[5] = c.slot0;
-      at[6] = c.told; at[7] = c.first; at[8] = c.n;
+      at[6] = c.told; at[7] = c.first; at[8] = c.n; at[9] = c.front;
     }
     run += all;
     slots += all_slots;
     __syncthreads();
     const bool found = at[0] >= 0;
-    if (found) o = {at[0], at[1], at[2], at[3], at[4], at[5], at[6], at[7], at[8]};
+    if (found) o = {at[0], at[1], at[2], at[3], at[4], at[5], at[6], at[7], at[8], BEAMS ? at[9] : 0};
     __syncthreads();                  // (the scratch is used for other things from here on, or for the next entries)
     if (found) return true;
   }
@@ -239,6 +287,53 @@ __device__ __forceinline__ void store_out(const AttendArgs& a, int64_t t, int64_
     }
   }
   if (c == 0 && a.lse) a.lse[t * pg.lse_st + head * pg.lse_sh] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.693147180559945309f;
+}
+
+// Sums of a row's chunks joined into its output: a workgroup a row (new token, query head), 256 threads as 1024 / d
+// groups that take every so manyeth chunk, four channels a thread.  A chain of two reads (where the chunks are, what they
+// hold) and a launch: chunks are read four at a time, references with the sums.  3.6 to 5 us for decoding steps, 8.3 for the 33 MB of
+// 256 queries a KV head.
+struct Part { const float *m, *l, *o; };
+template <int D, typename F>
+__device__ __forceinline__ void join_chunks(const AttendArgs& a, int count, int64_t t, int head, F part) {
+  constexpr int TPR = D / 4, NGR = 256 / TPR, AHEAD = 4;
+  __shared__ float4 sm_x[NGR][TPR];
+  __shared__ float sm_m[NGR], sm_l[NGR];
+  const int g = threadIdx.x / TPR, c = threadIdx.x % TPR;
+  float M = -INFINITY, L = 0.f;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto take = [&](float m, float l, float4 y) {
+    // (a chunk of which the row sees nothing has a reference of -inf and sums of 0)
+    const float n = fmaxf(M, m);
+    const float fo = M == n ? 1.f : __builtin_amdgcn_exp2f(M - n), fn = m == n ? 1.f : __builtin_amdgcn_exp2f(m - n);
+    M = n;
+    L = L * fo + l * fn;
+    x.x = x.x * fo + y.x * fn; x.y = x.y * fo + y.y * fn; x.z = x.z * fo + y.z * fn; x.w = x.w * fo + y.w * fn;
+  };
+  for (int k = g; k < count; k += NGR * AHEAD) {
+    float m[AHEAD], l[AHEAD];
+    float4 y[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const Part p = part(min(k + u * NGR, count - 1));
+      m[u] = *p.m;
+      l[u] = *p.l;
+      y[u] = *(const float4*)(p.o + c * 4);
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (k + u * NGR < count) take(m[u], l[u], y[u]);
+  }
+  sm_x[g][c] = x;
+  if (c == 0) {
+    sm_m[g] = M;
+    sm_l[g] = L;
+  }
+  __syncthreads();
+  if (g) return;
+#pragma unroll
+  for (int k = 1; k < NGR; ++k) take(sm_m[k], sm_l[k], sm_x[k][c]);
+  store_out(a, t, head, c * 4, x, M, L);
 }
 
 enum { FMT_F32, FMT_BF16, FMT_Q4 };
@@ -340,7 +435,7 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t x, int i, uint32_t mask, 
 // SP + x, ...: its queries are zeros in the products of other blocks, which add up in one set of registers, and its weights
 // are zeros in those blocks' products with values.  The matrix pipe does as much as before, but a lane scales, exponentiates
 // and splits 1 / SP of the keys, which is what bounds this format: four rows, 128k tokens 47.7 -> 39.2 us.
-template <int FMT, typename T, int D, int NP, int R, int SP>
+template <int FMT, typename T, int D, int NP, int R, int SP, bool BEAMS>
 __global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(2)))
 void k_attend(AttendArgs a) {
   constexpr int UN = D / 16, NG = D / 32;
@@ -360,17 +455,20 @@ void k_attend(AttendArgs a) {
   if (unit >= a.units) return;
   const int hy = unit % a.Hy;
   Chunk ch;
-  if (!find_chunk(a, unit / a.Hy, (int*)sm, ch)) return;
+  if (!find_chunk<4, BEAMS>(a, unit / a.Hy, (int*)sm, ch)) return;
   const int e = __builtin_amdgcn_readfirstlane(ch.e);
-  const int s = a.per_head ? e / pg.Hkv : e, h = a.per_head ? e - s * pg.Hkv : hy;
+  const bool front = BEAMS && e < a.fronts;
+  const int x = BEAMS && !front ? e - a.fronts : e, sg = a.per_head ? x / pg.Hkv : x, h = a.per_head ? x - sg * pg.Hkv : hy;
+  const int s = front ? sg * a.n_beams : sg;          // (its tables, for a group)
   const NewRows nr = {__builtin_amdgcn_readfirstlane(ch.first), __builtin_amdgcn_readfirstlane(ch.n)};
   const int rows = pg.G * nr.n, row0 = rb * 16 * R;
   if (row0 >= rows) return;
-  if (a.plan && ch.index == 0 && hy == 0 && rb == 0 && threadIdx.x == 0) a.plan[e] = make_int2(ch.slot0, ch.count);
+  if (a.plan && ch.index == 0 && hy == 0 && rb == 0 && threadIdx.x == 0) a.plan[e] = make_int2(ch.slot0, front && ch.tile1 == 0 ? 0 : ch.count);
+  if (front && ch.tile1 == 0) return;                 // (nothing is shared)
 
   const int told = __builtin_amdgcn_readfirstlane(ch.told), len = min(told, pg.max_len);
   auto limit = [&](int row) {       // positions that a row sees
-    return pg.causal ? min(max(told - nr.n + row / pg.G + 1, 0), len) : len;
+    return pg.causal && !front ? min(max(told - nr.n + row / pg.G + 1, 0), len) : len;
   };
   const int last_row = min(row0 + 16 * R, rows) - 1;
   const int k_end = __builtin_amdgcn_readfirstlane(min(ch.tile1 * ATT_TILE, limit(last_row)));
@@ -476,7 +574,13 @@ void k_attend(AttendArgs a) {
     const int row = min(row0 + cb * 16 + (SP > 1 ? n % CW : n), rows - 1);
     lim[cb] = limit(row);
     const int tok = row / pg.G;
-    const T* p = (const T*)a.q + (nr.first + tok) * pg.q_st + (h * pg.G + row - tok * pg.G) * pg.q_sh;
+    int t = nr.first + tok;
+    if (front) {                     // (places of new tokens that a beam does not have hold another's; nobody reads what comes of them)
+      const int b = tok / pg.max_new;
+      const NewRows of = new_rows(pg, s + b);
+      t = min(of.first + min(tok - b * pg.max_new, max(of.n - 1, 0)), pg.n_tokens - 1);
+    }
+    const T* p = (const T*)a.q + (int64_t)t * pg.q_st + (h * pg.G + row - tok * pg.G) * pg.q_sh;
     if constexpr (FMT == FMT_F32) {
 #pragma unroll
       for (int c = 0; c < QC; ++c) {
@@ -1016,12 +1120,13 @@ void k_attend(AttendArgs a) {
       x.w = __builtin_fmaf(f, y.w, x.w);
     }
     const int row = row0 + r;
-    if (ch.count > 1) {
-      const int64_t at = (int64_t)((ch.slot0 + ch.index) * z.Hy + hy) * ((int64_t)z.pg.G * z.pg.max_new) + row;
-      *(float4*)&z.part_o[at * D + c] = x;
+    if (ch.count > 1 || (BEAMS && (front || ch.front))) {
+      const int64_t slot = (int64_t)((ch.slot0 + ch.index) * z.Hy + hy), each = (int64_t)z.pg.G * z.pg.max_new;
+      const int64_t at = slot * (front ? each * z.n_beams : each) + row;
+      *(float4*)&(front ? z.front_o : z.part_o)[at * D + c] = x;
       if (c == 0) {
-        z.part_m[at] = M;
-        z.part_l[at] = L;
+        (front ? z.front_m : z.part_m)[at] = M;
+        (front ? z.front_l : z.part_l)[at] = L;
       }
     } else {
       const int tok = row / z.pg.G, head = h * z.pg.G + row - tok * z.pg.G;
@@ -1030,11 +1135,11 @@ void k_attend(AttendArgs a) {
   }
 }
 
-template <int FMT, typename T, int D, int NP, int R, int SP = 1>
+template <int FMT, typename T, int D, int NP, int R, int SP = 1, bool BEAMS = false>
 int run_attend(const AttendArgs& a, hipStream_t st) {
   constexpr size_t join = (8 * 16 * R + (size_t)4 * 16 * R * (D + 4)) * 4, scales = FMT == FMT_Q4 ? 4 * 4 * 64 * (D / 32) * 4 : 0;
   constexpr size_t lds = join > scales ? join : scales;
-  auto kern = k_attend<FMT, T, D, NP, R, SP>;
+  auto kern = k_attend<FMT, T, D, NP, R, SP, BEAMS>;
   if constexpr (lds > 65536) {
     if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) return RESTKV_EHIP;
   }
@@ -1042,10 +1147,16 @@ int run_attend(const AttendArgs& a, hipStream_t st) {
   return hip_status();
 }
 
-// by format, and for many rows (attend_*.hip)
+// by format, and for many rows (attend_*.hip); for beams (attend_beams_*.hip)
 int run_attend_rows(const AttendArgs& a, int R, int waves, hipStream_t st);
 int run_attend_f32(const AttendArgs& a, int R, hipStream_t st);
 int run_attend_bf16(const AttendArgs& a, hipStream_t st);
 int run_attend_q4(const AttendArgs& a, int R, hipStream_t st);
+int run_attend_beams_f32(const AttendArgs& a, int R, hipStream_t st);
+int run_attend_beams_bf16(const AttendArgs& a, int R, hipStream_t st);
+int run_attend_beams_q4(const AttendArgs& a, int R, hipStream_t st);
+// What kernels and join share of the arguments.
+AttendArgs attend_args(const Pages& pg, const void* q, const void* k_pages, const void* v_pages, const void* k_scale,
+                       const void* v_scale, void* out, float* lse);
 
 }  // namespace restkv
