@@ -74,12 +74,12 @@ __device__ __forceinline__ int source(const Deal& d, const Open& open, int b, in
   return col < open.lo ? p : col <= open.hi ? w : b;
 }
 
-// Rows: a wavefront takes, of one layer, a few rows (16 KB) of one head in an open column of one child that takes pages, keys or values, eight
+// Rows: a wavefront takes, of one layer, a few rows (8 KB) of one head in an open column of one child that takes pages, keys or values, eight
 // 16-byte loads a lane in flight.  What a group and layer has to copy is dealt over its a.parts workgroups.  Bound by memory, where it is
 // short by the chain parents, pages, rows.  The first a.table_groups workgroups write the new tables (which are others than the old ones).
 template <int RB, int SB>
 __global__ __launch_bounds__(256) void k_reorder(ReorderArgs a, LayerPages layers) {
-  constexpr int U = 8, L = RB / 16, SEG = 16384 / RB;        // (lanes and rows of a piece)
+  constexpr int U = 8, L = RB / 16, SEG = 8192 / RB;        // (lanes and rows of a piece)
   const Pages& pg = a.pg;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int64_t id = wide_block();
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(256) void k_reorder(ReorderArgs a, LayerPages layer
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int x = i + 64 * u;
-        if (x < end * L) *(Words<4>*)(out + x / L * hop + x % L * 16) = w[u];
+        if (x < end * L) put<true>(out + x / L * hop + x % L * 16, w[u]);
       }
     }
     if constexpr (SB != 0) {
@@ -198,9 +198,9 @@ int launch_beam_reorder(const Pages& pg, int n_beams, const int32_t* parents, in
     a.n_layers = std::max(0, std::min(copied - at, LAYERS));
     for (int i = 0; i < a.n_layers; ++i) lp.at[i] = layers[at + i];
     a.table_groups = at || in_place ? 0 : tables;
-    // workgroups for eight on each compute unit, and no more than columns of a page, or eight where there may be more, have work for
+    // workgroups for four on each compute unit, and no more than columns of a page, or eight where there may be more, have work for
     const int64_t most = ((int64_t)(n_beams - 1) * 2 * pg.Hkv * (pg.lens_sh ? 8 : 1) + 3) / 4, pairs = std::max<int64_t>(1, (int64_t)a.n_layers * a.n_groups);
-    a.parts = (int)std::max<int64_t>(1, std::min(most, (8 * n_cu() + pairs - 1) / pairs));
+    a.parts = (int)std::max<int64_t>(1, std::min(most, (4 * n_cu() + pairs - 1) / pairs));
     const dim3 grid = wide_grid(a.table_groups + (int64_t)a.n_layers * a.n_groups * a.parts);
     auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, a, lp); };
     const bool wide = pg.d == 128;
