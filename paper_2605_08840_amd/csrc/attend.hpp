@@ -30,10 +30,12 @@ struct AttendArgs {
   int row_blocks, units, c_min, vec_q, vec_out;
   float chunks;                     // workgroups wanted of each head and row block
   // Beams (launch_attend_beams): entries 0 .. fronts-1 are the shared positions of groups of n_beams sequences (or of a group's
-  // head), the rows of all its beams for them; then each sequence's own positions behind these.  All chunks have a slot, those of fronts in
-  // front_*: [slots * Hy, n_beams rows], the others in part_*.
+  // head), the rows of all its beams for them; then each sequence's own positions behind these.  An entry times a block of rows is a
+  // part: front_blocks of each of the former, own_blocks of each of the latter.  plan[part] {first, last} slot (first > last: none);
+  // front_*: [slots of fronts * Hy, rows of a block], part_*: [slots * Hy, rows of a sequence].  spread: parts are cut evenly over
+  // the workgroups of a head, of which there are `chunks`; else workgroups go by chunks and blocks of rows.
   const int32_t* shared;
-  int n_beams, fronts;
+  int n_beams, fronts, front_blocks, own_blocks, front_slots, spread;
   float* front_m; float* front_l; float* front_o;
 };
 
@@ -66,7 +68,7 @@ __device__ __forceinline__ int wave_scan(int x) {
 // passes: one sequence of 2048 tiles for 64 workgroups makes 63 chunks of up to 33, 24 sequences of 1 to 250 tiles (24.2 a workgroup) 61 of
 // up to 35, 256 entries of 9 to 33 tiles 497 of up to 13 for 512 workgroups (9.3 each).  Up to 64 entries a wavefront works this out by
 // itself, more are divided among the threads of the workgroup.
-struct Chunk { int e, tile0, tile1, index, count, slot0, told, first, n, front; };
+struct Chunk { int e, tile0, tile1, index, count, slot0, told, first, n; };
 struct Entry { int told, first, n, tiles, front; };      // front: tiles before the entry's first
 
 // Tiles of the positions that the beams of a group share, and all see: no more than any of them has in front of its new tokens.
@@ -131,7 +133,7 @@ __device__ __forceinline__ int chunk_tiles(const AttendArgs& a, float total, int
 }
 __device__ __forceinline__ Chunk chunk_of(const Entry& x, int e, int index, int count, int slot0) {
   const int each = count == 1 ? x.tiles : (x.tiles + count - 1) / count, t0 = min(index * each, x.tiles);
-  return {e, x.front + t0, x.front + min(t0 + each, x.tiles), index, count, slot0, x.told, x.first, x.n, x.front};
+  return {e, x.front + t0, x.front + min(t0 + each, x.tiles), index, count, slot0, x.told, x.first, x.n};
 }
 template <int NW = 4, bool BEAMS = false>
 __device__ __forceinline__ bool find_chunk(const AttendArgs& a, int x, int* lds, Chunk& o) {
@@ -208,13 +210,13 @@ __device__ __forceinline__ bool find_chunk(const AttendArgs& a, int x, int* lds,
     if (inc > x && inc - cnt <= x) {
       const Chunk c = chunk_of(en, e, x - inc + cnt, cnt, sl - own);
       at[0] = c.e; at[1] = c.tile0; at[2] = c.tile1; at[3] = c.index; at[4] = c.count; at[5] = c.slot0;
-      at[6] = c.told; at[7] = c.first; at[8] = c.n; at[9] = c.front;
+      at[6] = c.told; at[7] = c.first; at[8] = c.n;
     }
     run += all;
     slots += all_slots;
     __syncthreads();
     const bool found = at[0] >= 0;
-    if (found) o = {at[0], at[1], at[2], at[3], at[4], at[5], at[6], at[7], at[8], BEAMS ? at[9] : 0};
+    if (found) o = {at[0], at[1], at[2], at[3], at[4], at[5], at[6], at[7], at[8]};
     __syncthreads();                  // (the scratch is used for other things from here on, or for the next entries)
     if (found) return true;
   }
@@ -435,9 +437,9 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t x, int i, uint32_t mask, 
 // SP + x, ...: its queries are zeros in the products of other blocks, which add up in one set of registers, and its weights
 // are zeros in those blocks' products with values.  The matrix pipe does as much as before, but a lane scales, exponentiates
 // and splits 1 / SP of the keys, which is what bounds this format: four rows, 128k tokens 47.7 -> 39.2 us.
+// A chunk of an entry for block rb of its rows.  Beams: the entry is a group's shared positions (front) or not, `slot` takes the sums.
 template <int FMT, typename T, int D, int NP, int R, int SP, bool BEAMS>
-__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(2)))
-void k_attend(AttendArgs a) {
+__device__ __forceinline__ void attend_chunk(const AttendArgs& a, const Chunk& ch, int hy, int rb, bool front, int slot, float* sm) {
   constexpr int UN = D / 16, NG = D / 32;
   constexpr int QP = FMT == FMT_Q4 ? planes_of<T> : 1;
   constexpr int TK = FMT == FMT_F32 ? 16 : FMT == FMT_BF16 ? 32 : 64, NB = TK / 16;
@@ -446,25 +448,17 @@ void k_attend(AttendArgs a) {
   constexpr float BASE = CENTRED ? 8.f : -16.f;    // of a code, from its operand
   constexpr int CW = 16 / SP, NBS = NB / SP;       // columns of a copy, blocks of a copy
   constexpr int LDO = D + 4, QC = FMT == FMT_F32 ? D / 16 : D / 32;
-  extern __shared__ __align__(16) float sm[];
   const Pages& pg = a.pg;
   const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4, copy = SP > 1 ? n / CW : 0;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  const int unit = unit_of_block(), rb = blockIdx.x >> 3;
-  if (unit >= a.units) return;
-  const int hy = unit % a.Hy;
-  Chunk ch;
-  if (!find_chunk<4, BEAMS>(a, unit / a.Hy, (int*)sm, ch)) return;
   const int e = __builtin_amdgcn_readfirstlane(ch.e);
-  const bool front = BEAMS && e < a.fronts;
   const int x = BEAMS && !front ? e - a.fronts : e, sg = a.per_head ? x / pg.Hkv : x, h = a.per_head ? x - sg * pg.Hkv : hy;
   const int s = front ? sg * a.n_beams : sg;          // (its tables, for a group)
   const NewRows nr = {__builtin_amdgcn_readfirstlane(ch.first), __builtin_amdgcn_readfirstlane(ch.n)};
   const int rows = pg.G * nr.n, row0 = rb * 16 * R;
   if (row0 >= rows) return;
-  if (a.plan && ch.index == 0 && hy == 0 && rb == 0 && threadIdx.x == 0) a.plan[e] = make_int2(ch.slot0, front && ch.tile1 == 0 ? 0 : ch.count);
-  if (front && ch.tile1 == 0) return;                 // (nothing is shared)
+  if (!BEAMS && a.plan && ch.index == 0 && hy == 0 && rb == 0 && threadIdx.x == 0) a.plan[e] = make_int2(ch.slot0, ch.count);
 
   const int told = __builtin_amdgcn_readfirstlane(ch.told), len = min(told, pg.max_len);
   auto limit = [&](int row) {       // positions that a row sees
@@ -1120,17 +1114,106 @@ void k_attend(AttendArgs a) {
       x.w = __builtin_fmaf(f, y.w, x.w);
     }
     const int row = row0 + r;
-    if (ch.count > 1 || (BEAMS && (front || ch.front))) {
-      const int64_t slot = (int64_t)((ch.slot0 + ch.index) * z.Hy + hy), each = (int64_t)z.pg.G * z.pg.max_new;
-      const int64_t at = slot * (front ? each * z.n_beams : each) + row;
-      *(float4*)&(front ? z.front_o : z.part_o)[at * D + c] = x;
+    if (BEAMS || ch.count > 1) {
+      const int64_t each = (int64_t)z.pg.G * z.pg.max_new;
+      const int64_t at = BEAMS && front ? ((int64_t)slot * z.Hy + hy) * (16 * R) + r
+                                        : (int64_t)((BEAMS ? slot : ch.slot0 + ch.index) * z.Hy + hy) * each + row;
+      float* const po = BEAMS && front ? z.front_o : z.part_o;
+      *(float4*)&po[at * D + c] = x;
       if (c == 0) {
-        (front ? z.front_m : z.part_m)[at] = M;
-        (front ? z.front_l : z.part_l)[at] = L;
+        (BEAMS && front ? z.front_m : z.part_m)[at] = M;
+        (BEAMS && front ? z.front_l : z.part_l)[at] = L;
       }
     } else {
       const int tok = row / z.pg.G, head = h * z.pg.G + row - tok * z.pg.G;
       store_out(z, nr.first + tok, head, c, x, M, L);
+    }
+  }
+}
+
+// What a workgroup of a launch for beams takes, one part after the other.
+struct BeamsWork {
+  unsigned long long todo;       // parts (spread), or one
+  Entry en; int seg0, seg1;      // of the lane's part: tiles of this workgroup
+  Chunk ch;
+  int u, rb;
+};
+// Parts cut evenly (up to 64 of them, a lane each): the tiles of all follow each other, with PART_COST tiles more for each part, which
+// is what its beginning and end take, and workgroup u takes the u-th share.
+constexpr int PART_COST = 2;
+template <int NW>
+__device__ __forceinline__ bool beams_work(const AttendArgs& a, int unit, int rb, int* lds, BeamsWork& o) {
+  const int lane = threadIdx.x & 63, hy = unit % a.Hy, all_fronts = a.fronts * a.front_blocks;
+  o.u = unit / a.Hy;
+  o.rb = rb;
+  if (a.spread) {
+    const int parts = all_fronts + (a.entries - a.fronts) * a.own_blocks;
+    const int e = lane >= parts ? a.entries : lane < all_fronts ? lane / a.front_blocks : a.fronts + (lane - all_fronts) / a.own_blocks;
+    o.en = read_entry<true>(a, e);
+    const int cost = o.en.tiles ? o.en.tiles + PART_COST : 0, upto = wave_scan(cost), total = __builtin_amdgcn_readlane(upto, 63);
+    const int groups = max(1, min((int)a.chunks, total / max(a.c_min, PART_COST + 1)));
+    if (o.u >= groups) return false;
+    const int q = total / groups, r = total % groups;
+    const int begin = o.u * q + min(o.u, r) - (upto - cost) - PART_COST, end = begin + q + (o.u < r ? 1 : 0);
+    o.seg0 = min(max(begin, 0), o.en.tiles);
+    o.seg1 = min(max(end, 0), o.en.tiles);
+    o.todo = __ballot(o.seg1 > o.seg0);
+    if (hy == 0 && threadIdx.x < 64 && lane < parts) {
+      if (o.seg1 > o.seg0 && o.seg0 == 0) a.plan[lane].x = o.u + lane;
+      if (o.seg1 > o.seg0 && o.seg1 == o.en.tiles) a.plan[lane].y = o.u + lane;
+      if (o.u == 0 && o.en.tiles == 0) a.plan[lane] = make_int2(1, 0);
+    }
+    return true;
+  }
+  if (!find_chunk<NW, true>(a, o.u, lds, o.ch)) return false;
+  const bool front = o.ch.e < a.fronts, none = front && o.ch.tile1 == 0;
+  if (rb >= (front ? a.front_blocks : a.own_blocks)) return false;
+  if (o.ch.index == 0 && hy == 0 && threadIdx.x == 0) {
+    const int slot0 = front ? rb * a.front_slots + o.ch.slot0 : o.ch.slot0;
+    a.plan[front ? o.ch.e * a.front_blocks + rb : all_fronts + (o.ch.e - a.fronts) * a.own_blocks + rb] =
+        none ? make_int2(1, 0) : make_int2(slot0, slot0 + o.ch.count - 1);
+  }
+  o.todo = none ? 0 : 1;
+  return true;
+}
+// The next part: its chunk, whether it is a front, and the slot of its sums.
+__device__ __forceinline__ void next_part(const AttendArgs& a, BeamsWork& o, bool& front, int& slot) {
+  if (a.spread) {
+    const int l = __builtin_ctzll(o.todo), all_fronts = a.fronts * a.front_blocks;
+    auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+    front = l < all_fronts;
+    o.rb = front ? l % a.front_blocks : (l - all_fronts) % a.own_blocks;
+    const int before = of(o.en.front);
+    o.ch = {front ? l / a.front_blocks : a.fronts + (l - all_fronts) / a.own_blocks, before + of(o.seg0), before + of(o.seg1), 0, 0, 0,
+            of(o.en.told), of(o.en.first), of(o.en.n)};
+    slot = o.u + l;
+  } else {
+    front = o.ch.e < a.fronts;
+    slot = o.ch.slot0 + o.ch.index + (front ? o.rb * a.front_slots : 0);
+  }
+  o.todo &= o.todo - 1;
+}
+
+template <int FMT, typename T, int D, int NP, int R, int SP, bool BEAMS>
+__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(2)))
+void k_attend(AttendArgs a) {
+  extern __shared__ __align__(16) float sm[];
+  const int unit = unit_of_block(), rb = blockIdx.x >> 3;
+  if (unit >= a.units) return;
+  const int hy = unit % a.Hy;
+  if constexpr (!BEAMS) {
+    Chunk ch;
+    if (!find_chunk(a, unit / a.Hy, (int*)sm, ch)) return;
+    attend_chunk<FMT, T, D, NP, R, SP, false>(a, ch, hy, rb, false, 0, sm);
+  } else {
+    BeamsWork w;
+    if (!beams_work<4>(a, unit, rb, (int*)sm, w)) return;
+    while (w.todo) {
+      bool front;
+      int slot;
+      next_part(a, w, front, slot);
+      attend_chunk<FMT, T, D, NP, R, SP, true>(a, w.ch, hy, w.rb, front, slot, sm);
+      if (w.todo) __syncthreads();       // (the sums of this part are read, before the next one's scales or sums come there)
     }
   }
 }
