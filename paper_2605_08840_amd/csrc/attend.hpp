@@ -35,7 +35,8 @@ struct AttendArgs {
   // front_*: [slots of fronts * Hy, rows of a block], part_*: [slots * Hy, rows of a sequence].  spread: parts are cut evenly over
   // the workgroups of a head, of which there are `chunks`; else workgroups go by chunks and blocks of rows.
   const int32_t* shared;
-  int n_beams, fronts, front_blocks, own_blocks, front_slots, spread;
+  int n_beams, fronts, front_blocks, own_blocks, front_slots, spread, front_rows, own_rows;
+  uint32_t part_cost, front_cost, front_tiles;
   float* front_m; float* front_l; float* front_o;
 };
 
@@ -437,6 +438,14 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t x, int i, uint32_t mask, 
 // SP + x, ...: its queries are zeros in the products of other blocks, which add up in one set of registers, and its weights
 // are zeros in those blocks' products with values.  The matrix pipe does as much as before, but a lane scales, exponentiates
 // and splits 1 / SP of the keys, which is what bounds this format: four rows, 128k tokens 47.7 -> 39.2 us.
+// Row of the token tensors for place `tok` of a group's new tokens, max_new for each beam from sequence s on (places that a beam does not
+// have hold another's; nobody reads what comes of them).
+__device__ __forceinline__ int front_token(const Pages& pg, int s, int tok) {
+  const int b = tok / pg.max_new;
+  const NewRows of = new_rows(pg, s + b);
+  return min(of.first + min(tok - b * pg.max_new, max(of.n - 1, 0)), pg.n_tokens - 1);
+}
+
 // A chunk of an entry for block rb of its rows.  Beams: the entry is a group's shared positions (front) or not, `slot` takes the sums.
 template <int FMT, typename T, int D, int NP, int R, int SP, bool BEAMS>
 __device__ __forceinline__ void attend_chunk(const AttendArgs& a, const Chunk& ch, int hy, int rb, bool front, int slot, float* sm) {
@@ -569,11 +578,7 @@ __device__ __forceinline__ void attend_chunk(const AttendArgs& a, const Chunk& c
     lim[cb] = limit(row);
     const int tok = row / pg.G;
     int t = nr.first + tok;
-    if (front) {                     // (places of new tokens that a beam does not have hold another's; nobody reads what comes of them)
-      const int b = tok / pg.max_new;
-      const NewRows of = new_rows(pg, s + b);
-      t = min(of.first + min(tok - b * pg.max_new, max(of.n - 1, 0)), pg.n_tokens - 1);
-    }
+    if (front) t = front_token(pg, s, tok);
     const T* p = (const T*)a.q + (int64_t)t * pg.q_st + (h * pg.G + row - tok * pg.G) * pg.q_sh;
     if constexpr (FMT == FMT_F32) {
 #pragma unroll
@@ -1138,25 +1143,52 @@ struct BeamsWork {
   Chunk ch;
   int u, rb;
 };
-// Parts cut evenly (up to 64 of them, a lane each): the tiles of all follow each other, with PART_COST tiles more for each part, which
-// is what its beginning and end take, and workgroup u takes the u-th share.
-constexpr int PART_COST = 2;
+// Parts cut evenly (up to 64 of them, a lane each): the rounds of all follow each other, with a.part_cost half rounds more for each
+// part, which is what its beginning and end take, and workgroup u takes the u-th share.  A round is what the wavefronts of a workgroup
+// take at a time, a.c_min tiles.
 template <int NW>
 __device__ __forceinline__ bool beams_work(const AttendArgs& a, int unit, int rb, int* lds, BeamsWork& o) {
+  const Pages& pg = a.pg;
   const int lane = threadIdx.x & 63, hy = unit % a.Hy, all_fronts = a.fronts * a.front_blocks;
   o.u = unit / a.Hy;
   o.rb = rb;
   if (a.spread) {
-    const int parts = all_fronts + (a.entries - a.fronts) * a.own_blocks;
-    const int e = lane >= parts ? a.entries : lane < all_fronts ? lane / a.front_blocks : a.fronts + (lane - all_fronts) / a.own_blocks;
-    o.en = read_entry<true>(a, e);
-    const int cost = o.en.tiles ? o.en.tiles + PART_COST : 0, upto = wave_scan(cost), total = __builtin_amdgcn_readlane(upto, 63);
-    const int groups = max(1, min((int)a.chunks, total / max(a.c_min, PART_COST + 1)));
-    if (o.u >= groups) return false;
-    const int q = total / groups, r = total % groups;
-    const int begin = o.u * q + min(o.u, r) - (upto - cost) - PART_COST, end = begin + q + (o.u < r ? 1 : 0);
-    o.seg0 = min(max(begin, 0), o.en.tiles);
-    o.seg1 = min(max(end, 0), o.en.tiles);
+    // lane = sequence (and head) first, then a part: what each sequence has in front of its new tokens, the least of each group
+    const int owns = a.entries - a.fronts, parts = all_fronts + owns * a.own_blocks;
+    const int y = min(lane, owns - 1), s = a.per_head ? y / pg.Hkv : y;
+    const int told = told_len(pg, s, a.per_head ? y - s * pg.Hkv : 0);
+    const NewRows nr = new_rows(pg, s);
+    const int want = max(a.shared[s / a.n_beams], 0), room = !nr.n ? -1 : pg.causal ? max(told - nr.n, 0) : told;
+    const bool is_front = lane < all_fronts;
+    const int x = min(is_front ? lane / a.front_blocks : (lane - all_fronts) / a.own_blocks, is_front ? a.fronts - 1 : owns - 1);
+    // first sequence (and head) of the part's group
+    const int step = a.per_head ? pg.Hkv : 1, h = a.per_head ? x % pg.Hkv : 0, group = is_front ? x / step : x / step / a.n_beams;
+    const int seq0 = group * a.n_beams * step + h;
+    int least = 0x7FFFFFFF;
+#pragma unroll 4
+    for (int b = 0; b < a.n_beams; ++b) {
+      const int r = __shfl(room, seq0 + b * step);
+      least = r >= 0 ? min(least, r) : least;
+    }
+    const int shared = (int)min((int64_t)__shfl(want, seq0) << pg.lg_ps, (int64_t)pg.max_len);
+    const int tiles = least == 0x7FFFFFFF ? 0 : min(shared, least) / ATT_TILE;
+    const int own = is_front ? 0 : x, t = __shfl(told, own), first = __shfl(nr.first, own), n = __shfl(nr.n, own);
+    if (lane >= parts) o.en = {0, 0, 0, 0, 0};
+    else if (is_front) o.en = {tiles * ATT_TILE, 0, a.n_beams * pg.max_new, tiles, 0};
+    else o.en = {t, first, n, n ? (min(t, pg.max_len) + ATT_TILE - 1) / ATT_TILE - tiles : 0, tiles};
+
+    // (fronts of many rows go by tiles, of a.front_cost each)
+    const uint32_t per = is_front ? a.front_tiles : a.c_min, price = is_front ? a.front_cost : 2u;
+    const uint32_t rounds = ((uint32_t)o.en.tiles + per - 1) / per;
+    const uint32_t cost = rounds ? price * rounds + a.part_cost : 0, upto = (uint32_t)wave_scan((int)cost), total = __builtin_amdgcn_readlane(upto, 63);
+    const uint32_t groups = max(1u, min((uint32_t)a.chunks, total / (a.part_cost + max(2u, a.front_cost))));
+    if ((uint32_t)o.u >= groups) return false;
+    const uint32_t q = total / groups, r = total % groups, at = o.u * q + min((uint32_t)o.u, r), end = at + q + ((uint32_t)o.u < r ? 1 : 0);
+    const uint32_t begins = upto - cost + a.part_cost;       // of the part's rounds
+    auto tile_of = [&](uint32_t c) { return c <= begins ? 0 : (int)min((c - begins) / price * per, (uint32_t)o.en.tiles); };
+    o.seg0 = tile_of(at);
+    o.seg1 = end >= upto ? o.en.tiles : tile_of(end);
+    if (at >= upto) o.seg0 = o.en.tiles;
     o.todo = __ballot(o.seg1 > o.seg0);
     if (hy == 0 && threadIdx.x < 64 && lane < parts) {
       if (o.seg1 > o.seg0 && o.seg0 == 0) a.plan[lane].x = o.u + lane;
@@ -1238,6 +1270,7 @@ int run_attend_q4(const AttendArgs& a, int R, hipStream_t st);
 int run_attend_beams_f32(const AttendArgs& a, int R, hipStream_t st);
 int run_attend_beams_bf16(const AttendArgs& a, int R, hipStream_t st);
 int run_attend_beams_q4(const AttendArgs& a, int R, hipStream_t st);
+int run_attend_beams_rows(const AttendArgs& a, int R, hipStream_t st);
 // What kernels and join share of the arguments.
 AttendArgs attend_args(const Pages& pg, const void* q, const void* k_pages, const void* v_pages, const void* k_scale,
                        const void* v_scale, void* out, float* lse);

@@ -12,46 +12,48 @@ namespace restkv {
 namespace {
 
 template <int D>
-__global__ __launch_bounds__(256) void k_beams_join(AttendArgs a, int block) {
+__global__ __launch_bounds__(256) void k_beams_join(AttendArgs a) {
   const Pages& pg = a.pg;
   const int i = blockIdx.x / pg.Hq, head = blockIdx.x % pg.Hq, h = head / pg.G, s = blockIdx.y, g = s / a.n_beams;
   const int hy = a.per_head ? 0 : h, row = i * pg.G + head - h * pg.G, rows = pg.G * pg.max_new;
-  const int of_group = (s - g * a.n_beams) * rows + row, rb = of_group / block;
+  const int of_group = (s - g * a.n_beams) * rows + row, rb = of_group / a.front_rows;
   const int2 pf = a.plan[(a.per_head ? g * pg.Hkv + h : g) * a.front_blocks + rb];
-  const int2 pl = a.plan[a.fronts * a.front_blocks + (a.per_head ? s * pg.Hkv + h : s) * a.own_blocks + row / block];
+  const int2 pl = a.plan[a.fronts * a.front_blocks + (a.per_head ? s * pg.Hkv + h : s) * a.own_blocks + row / a.own_rows];
   const NewRows nr = new_rows(pg, s);
   if (i >= nr.n) return;
   const int n = pf.y - pf.x + 1;
   join_chunks<D>(a, n + pl.y - pl.x + 1, nr.first + i, head, [&](int k) {
     const bool front = k < n;
     const int64_t slot = (int64_t)(front ? pf.x + k : pl.x + k - n) * a.Hy + hy;
-    const int64_t at = front ? slot * block + (of_group - rb * block) : slot * rows + row;
+    const int64_t at = front ? slot * a.front_rows + (of_group - rb * a.front_rows) : slot * rows + row;
     return Part{(front ? a.front_m : a.part_m) + at, (front ? a.front_l : a.part_l) + at, (front ? a.front_o : a.part_o) + at * D};
   });
 }
 
-struct BeamsPlan { int R, c_min, target, spread; int64_t front_blocks, own_blocks, fronts, entries, parts, Hy, groups, slots, front_slots; };
+struct BeamsPlan { int many, R, front_rows, own_rows, c_min, target, spread; int64_t front_blocks, own_blocks, fronts, entries, parts, Hy, groups, slots, front_slots; };
 BeamsPlan beams_plan(const Pages& pg, int n_beams) {
   BeamsPlan p;
   const int64_t rows = (int64_t)pg.G * pg.max_new;
   const bool wide_q = pg.fmt == RESTKV_Q4 && pg.dtype == RESTKV_F32 && pg.d == 128;      // (see attend_plan)
-  p.R = rows * n_beams <= 16 || wide_q ? 1 : 2;
-  const int block = 16 * p.R;
-  p.front_blocks = (rows * n_beams + block - 1) / block;
-  p.own_blocks = (rows + block - 1) / block;
+  p.many = pg.fmt == RESTKV_BF16 && rows * n_beams > 32;
+  p.R = p.many ? (rows * n_beams <= 64 ? 1 : 2) : rows * n_beams <= 16 || wide_q ? 1 : 2;
+  p.front_rows = p.many ? 64 * p.R : 16 * p.R;
+  p.own_rows = p.many ? 16 : 16 * p.R;
+  p.front_blocks = (rows * n_beams + p.front_rows - 1) / p.front_rows;
+  p.own_blocks = (rows + p.own_rows - 1) / p.own_rows;
   const bool per_head = pg.lens_sh != 0;
   p.Hy = per_head ? 1 : pg.Hkv;
   p.fronts = (int64_t)(pg.n_seqs / n_beams) * (per_head ? pg.Hkv : 1);
   p.entries = p.fronts + (int64_t)pg.n_seqs * (per_head ? pg.Hkv : 1);
   p.parts = p.fronts * p.front_blocks + (p.entries - p.fronts) * p.own_blocks;
-  p.c_min = pg.fmt == RESTKV_Q4 ? 4 : 2;
+  p.c_min = pg.fmt == RESTKV_Q4 ? 4 : pg.fmt == RESTKV_BF16 ? 2 : 1;      // (tiles of a round: one of the keys of each wavefront)
   p.target = n_cu() * 2;
   p.spread = p.parts <= 64;
   if (p.spread) {
     p.groups = std::max<int64_t>(1, p.target / p.Hy);
     p.slots = p.front_slots = p.groups + p.parts;
   } else {
-    const int64_t tiles = (pg.max_len + ATT_TILE - 1) / ATT_TILE, each = p.Hy * p.front_blocks;
+    const int64_t tiles = (pg.max_len + ATT_TILE - 1) / ATT_TILE, each = p.Hy * std::max(p.front_blocks, p.own_blocks);
     const int64_t more = std::min<int64_t>(p.target / each + 1, p.entries * ((tiles + p.c_min - 1) / p.c_min));
     p.groups = p.slots = p.front_slots = p.entries + (each >= p.target || tiles <= p.c_min ? 0 : more);
   }
@@ -63,7 +65,7 @@ BeamsWs beams_ws(const Pages& pg, const BeamsPlan& p) {
   BeamsWs w = {};
   auto take = [&](size_t bytes) { size_t o = w.bytes; w.bytes = align_up(w.bytes + bytes); return o; };
   const size_t rows = (size_t)p.slots * p.Hy * pg.G * pg.max_new;
-  const size_t front = (size_t)p.front_slots * (p.spread ? 1 : p.front_blocks) * p.Hy * (16 * p.R);
+  const size_t front = (size_t)p.front_slots * (p.spread ? 1 : p.front_blocks) * p.Hy * p.front_rows;
   w.plan = take((size_t)p.parts * 8);
   w.m = take(rows * 4);
   w.l = take(rows * 4);
@@ -82,7 +84,7 @@ int launch_attend_beams(const Pages& pg, int n_beams, const int32_t* shared, con
                         const void* k_scale, const void* v_scale, void* out, float* lse, char* ws, hipStream_t st) {
   const BeamsPlan p = beams_plan(pg, n_beams);
   const BeamsWs lay = beams_ws(pg, p);
-  if (p.groups * p.Hy > (int64_t)1 << 30 || p.front_slots * p.front_blocks > (int64_t)1 << 30 || p.front_blocks > (1 << 20) || (int64_t)pg.max_new * pg.Hq >= (1 << 24)) return RESTKV_EUNSUPPORTED;
+  if (p.groups * p.Hy > (int64_t)1 << 30 || p.front_slots * p.front_blocks > (int64_t)1 << 30 || std::max(p.front_blocks, p.own_blocks) > (1 << 20) || (int64_t)pg.max_new * pg.Hq >= (1 << 24)) return RESTKV_EUNSUPPORTED;
   AttendArgs a = attend_args(pg, q, k_pages, v_pages, k_scale, v_scale, out, lse);
   a.plan = (int2*)(ws + lay.plan);
   a.part_m = (float*)(ws + lay.m); a.part_l = (float*)(ws + lay.l); a.part_o = (float*)(ws + lay.o);
@@ -90,13 +92,15 @@ int launch_attend_beams(const Pages& pg, int n_beams, const int32_t* shared, con
   a.entries = (int)p.entries; a.Hy = (int)p.Hy;
   a.shared = shared; a.n_beams = n_beams; a.fronts = (int)p.fronts;
   a.front_blocks = (int)p.front_blocks; a.own_blocks = (int)p.own_blocks; a.front_slots = (int)p.front_slots; a.spread = p.spread;
-  a.row_blocks = p.spread ? 1 : (int)p.front_blocks; a.units = (int)(p.groups * p.Hy); a.c_min = p.c_min;
-  a.chunks = p.spread ? (float)p.groups : (float)((double)p.target / (double)(p.Hy * p.front_blocks) * (1 - 0x1p-23));
-  const int rc = pg.fmt == RESTKV_F32 ? run_attend_beams_f32(a, p.R, st) : pg.fmt == RESTKV_BF16 ? run_attend_beams_bf16(a, p.R, st) : run_attend_beams_q4(a, p.R, st);
+  a.front_rows = p.front_rows; a.own_rows = p.own_rows;
+  a.part_cost = 3; a.front_tiles = p.many ? 1 : p.c_min; a.front_cost = 2;
+  a.row_blocks = p.spread ? 1 : (int)std::max(p.front_blocks, p.own_blocks); a.units = (int)(p.groups * p.Hy); a.c_min = p.c_min;
+  a.chunks = p.spread ? (float)p.groups : (float)((double)p.target / (double)(p.Hy * std::max(p.front_blocks, p.own_blocks)) * (1 - 0x1p-23));
+  const int rc = p.many ? run_attend_beams_rows(a, p.R, st) : pg.fmt == RESTKV_F32 ? run_attend_beams_f32(a, p.R, st) : pg.fmt == RESTKV_BF16 ? run_attend_beams_bf16(a, p.R, st) : run_attend_beams_q4(a, p.R, st);
   if (rc) return rc;
   const dim3 grid(pg.max_new * pg.Hq, pg.n_seqs);
-  if (pg.d == 128) hipLaunchKernelGGL(k_beams_join<128>, grid, dim3(256), 0, st, a, 16 * p.R);
-  else hipLaunchKernelGGL(k_beams_join<64>, grid, dim3(256), 0, st, a, 16 * p.R);
+  if (pg.d == 128) hipLaunchKernelGGL(k_beams_join<128>, grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(k_beams_join<64>, grid, dim3(256), 0, st, a);
   return hip_status();
 }
 
