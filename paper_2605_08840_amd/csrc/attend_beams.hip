@@ -36,8 +36,8 @@ BeamsPlan beams_plan(const Pages& pg, int n_beams) {
   const int64_t rows = (int64_t)pg.G * pg.max_new;
   const bool wide_q = pg.fmt == RESTKV_Q4 && pg.dtype == RESTKV_F32 && pg.d == 128;      // (see attend_plan)
   p.many = pg.fmt == RESTKV_BF16 && rows * n_beams > 32;
-  p.R = p.many ? (rows * n_beams <= 64 ? 1 : 2) : rows * n_beams <= 16 || wide_q ? 1 : 2;
-  p.front_rows = p.many ? 64 * p.R : 16 * p.R;
+  p.R = p.many ? 1 : rows * n_beams <= 16 || wide_q ? 1 : 2;
+  p.front_rows = p.many ? 64 : 16 * p.R;
   p.own_rows = p.many ? 16 : 16 * p.R;
   p.front_blocks = (rows * n_beams + p.front_rows - 1) / p.front_rows;
   p.own_blocks = (rows + p.own_rows - 1) / p.own_rows;
@@ -96,7 +96,7 @@ int launch_attend_beams(const Pages& pg, int n_beams, const int32_t* shared, con
   a.part_cost = 3; a.front_tiles = p.many ? 1 : p.c_min; a.front_cost = 2;
   a.row_blocks = p.spread ? 1 : (int)std::max(p.front_blocks, p.own_blocks); a.units = (int)(p.groups * p.Hy); a.c_min = p.c_min;
   a.chunks = p.spread ? (float)p.groups : (float)((double)p.target / (double)(p.Hy * std::max(p.front_blocks, p.own_blocks)) * (1 - 0x1p-23));
-  const int rc = p.many ? run_attend_beams_rows(a, p.R, st) : pg.fmt == RESTKV_F32 ? run_attend_beams_f32(a, p.R, st) : pg.fmt == RESTKV_BF16 ? run_attend_beams_bf16(a, p.R, st) : run_attend_beams_q4(a, p.R, st);
+  const int rc = p.many ? run_attend_beams_rows(a, st) : pg.fmt == RESTKV_F32 ? run_attend_beams_f32(a, p.R, st) : pg.fmt == RESTKV_BF16 ? run_attend_beams_bf16(a, p.R, st) : run_attend_beams_q4(a, p.R, st);
   if (rc) return rc;
   const dim3 grid(pg.max_new * pg.Hq, pg.n_seqs);
   if (pg.d == 128) hipLaunchKernelGGL(k_beams_join<128>, grid, dim3(256), 0, st, a);

@@ -16,19 +16,46 @@ namespace restkv {
 // (matrix 36 % busy, vector issue 41 %): the two wavefronts of a SIMD do the same at the same time, behind one barrier a tile, so that products
 // and softmax follow each other (a wavefront alone takes 4500 cycles a tile, 2048 of them products); 31 chunks of up to 17 tiles stand
 // for 32 of 16, and 33 MB of chunk sums are written and read again.
-// Beams: a front, whose sums go to `slot`.
+// Beams: the workgroup's parts one after the other, the fronts so, what a beam has behind them as for few rows.
 template <int D, int NP, int R, int NW, bool BEAMS>
-__device__ __forceinline__ void rows_chunk(const AttendArgs& a, Chunk ch, int hy, int rb, int slot, char* lds) {
+__global__ __attribute__((amdgpu_flat_work_group_size(64 * NW, 64 * NW), amdgpu_waves_per_eu(2)))
+void k_attend_rows(AttendArgs a) {
   constexpr int UN = D / 16, QC = D / 32, ROWB = D * 2, TK = 64, NB = 4, CH = ROWB / 16, TILE = TK * ROWB;
+  extern __shared__ __align__(16) char lds[];        // [2][keys | values][TILE]
   const Pages& pg = a.pg;
   const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+  const int unit = unit_of_block();
+  int rb = blockIdx.x >> 3, slot = 0;
+  if (unit >= a.units) return;
+  const int hy = unit % a.Hy;
+  Chunk ch;
+  BeamsWork work;
+  if constexpr (BEAMS) {
+    if (!beams_work<NW>(a, unit, rb, (int*)lds, work)) return;
+  } else {
+    if (!find_chunk<NW>(a, unit / a.Hy, (int*)lds, ch)) return;
+  }
+  do {
+  if constexpr (BEAMS) {
+    if (!work.todo) return;
+    bool front;
+    next_part(a, work, front, slot);
+    ch = work.ch;
+    rb = work.rb;
+    if (!front) {
+      attend_chunk<FMT_BF16, bf16_t, D, NP, 1, 1, true>(a, ch, hy, rb, false, slot, (float*)lds);
+      __syncthreads();
+      continue;
+    }
+  }
   ch.n = __builtin_amdgcn_readfirstlane(ch.n);
   ch.first = __builtin_amdgcn_readfirstlane(ch.first);
   const int e = __builtin_amdgcn_readfirstlane(ch.e);
   const int sg = a.per_head ? e / pg.Hkv : e, h = a.per_head ? e - sg * pg.Hkv : hy, s = BEAMS ? sg * a.n_beams : sg;
   const int rows = pg.G * ch.n, block0 = rb * 16 * NW * R, row0 = block0 + wv * 16 * R;
-  if (block0 >= rows) return;
+  if (block0 >= rows) return;          // (not of a front: its blocks all have rows)
   if (!BEAMS && a.plan && ch.index == 0 && hy == 0 && rb == 0 && threadIdx.x == 0) a.plan[e] = make_int2(ch.slot0, ch.count);
 
   const int told = __builtin_amdgcn_readfirstlane(ch.told), len = min(told, pg.max_len);
@@ -72,7 +99,7 @@ __device__ __forceinline__ void rows_chunk(const AttendArgs& a, Chunk ch, int hy
 #pragma unroll
     for (int x = 0; x < PIECES; ++x) dma_1k(vh + (uint64_t)row * ROWB, off[x], to + TILE + x * 1024);
   };
-  if (k_begin < k_end) copy(k_begin, 0);
+  if (!BEAMS && k_begin < k_end) copy(k_begin, 0);
 
   // ---- queries
   int lim[R];
@@ -91,6 +118,8 @@ __device__ __forceinline__ void rows_chunk(const AttendArgs& a, Chunk ch, int hy
       qo[cb][c] = split8<1>(x);
     }
   }
+  // (queries of a front are many loads behind another: the tile's would go before them in the queue)
+  if (BEAMS && k_begin < k_end) copy(k_begin, 0);
   f32x4 o[UN][R];
   float ref[R], l[R];
 #pragma unroll
@@ -292,6 +321,8 @@ __device__ __forceinline__ void rows_chunk(const AttendArgs& a, Chunk ch, int hy
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
+  if (BEAMS) __syncthreads();          // (the next part's tiles come where these rows were)
+  } while (BEAMS);
 }
 
 }  // namespace restkv
