@@ -33,10 +33,11 @@ struct AttendArgs {
   // head), the rows of all its beams for them; then each sequence's own positions behind these.  An entry times a block of rows is a
   // part: front_blocks of each of the former, own_blocks of each of the latter.  plan[part] {first, last} slot (first > last: none);
   // front_*: [slots of fronts * Hy, rows of a block], part_*: [slots * Hy, rows of a sequence].  spread: parts are cut evenly over
-  // the workgroups of a head, of which there are `chunks`; else workgroups go by chunks and blocks of rows.
+  // the teams of workgroups of a head, of which there are `chunks` (beams_work); else workgroups go by chunks and blocks of rows.
   const int32_t* shared;
-  int n_beams, fronts, front_blocks, own_blocks, front_slots, spread, front_rows, own_rows;
-  uint32_t part_cost, front_cost, front_tiles;
+  int n_beams, fronts, front_blocks, own_blocks, front_slots, spread, front_rows, own_rows, front_tiles, coarse;
+  uint32_t part_cost;
+  float first_more;
   float* front_m; float* front_l; float* front_o;
 };
 
@@ -1139,30 +1140,39 @@ __device__ __forceinline__ void attend_chunk(const AttendArgs& a, const Chunk& c
 // What a workgroup of a launch for beams takes, one part after the other.
 struct BeamsWork {
   unsigned long long todo;       // parts (spread), or one
-  Entry en; int seg0, seg1;      // of the lane's part: tiles of this workgroup
+  int (*lds)[8];                 // of a part: positions, first row, new tokens, first and last tile of this workgroup (spread)
   Chunk ch;
-  int u, rb;
+  int u, rb, team_rb, slot0;
 };
-// Parts cut evenly (up to 64 of them, a lane each): the rounds of all follow each other, with a.part_cost half rounds more for each
-// part, which is what its beginning and end take, and workgroup u takes the u-th share.  A round is what the wavefronts of a workgroup
-// take at a time, a.c_min tiles.
+// Parts (up to 64, a lane each; a front with all its blocks of rows is one) cut evenly: the rounds of all follow each other, with
+// a.part_cost half rounds more for each part, which is what its beginning and end take.  Workgroups come in teams of front_blocks.  Some teams take the fronts, one front each and all about as many rounds, each of a team's workgroups the same tiles for a block of rows
+// (at the same time on one XCD, whose L2 reads them once); the workgroups of the other teams cut what is left, one by one.  A round is what
+// the wavefronts of a workgroup take at a time, a.c_min tiles.
+// (What comes of it is in LDS, so that the loops between have the registers.)
+// Quotients of small whole numbers (below 2^15), where a division of 32 bits would take forty instructions.
+__device__ __forceinline__ int quotient(int x, float one_over) { return (int)(((float)x + 0.5f) * one_over); }
 template <int NW>
 __device__ __forceinline__ bool beams_work(const AttendArgs& a, int unit, int rb, int* lds, BeamsWork& o) {
   const Pages& pg = a.pg;
-  const int lane = threadIdx.x & 63, hy = unit % a.Hy, all_fronts = a.fronts * a.front_blocks;
-  o.u = unit / a.Hy;
-  o.rb = rb;
+  const int lane = threadIdx.x & 63, all_fronts = a.fronts * a.front_blocks;
+  o.u = a.spread ? quotient(unit, __builtin_amdgcn_rcpf((float)a.Hy)) : unit / a.Hy;
+  const int hy = unit - o.u * a.Hy;
+  __shared__ int s_parts[64][8];
+  o.lds = s_parts;
+  o.rb = o.team_rb = rb;
   if (a.spread) {
     // lane = sequence (and head) first, then a part: what each sequence has in front of its new tokens, the least of each group
-    const int owns = a.entries - a.fronts, parts = all_fronts + owns * a.own_blocks;
-    const int y = min(lane, owns - 1), s = a.per_head ? y / pg.Hkv : y;
+    const int owns = a.entries - a.fronts, parts = a.fronts + owns * a.own_blocks;
+    const float one_beams = __builtin_amdgcn_rcpf((float)a.n_beams), one_heads = __builtin_amdgcn_rcpf((float)pg.Hkv);
+    const int y = min(lane, owns - 1), s = a.per_head ? quotient(y, one_heads) : y;
     const int told = told_len(pg, s, a.per_head ? y - s * pg.Hkv : 0);
     const NewRows nr = new_rows(pg, s);
-    const int want = max(a.shared[s / a.n_beams], 0), room = !nr.n ? -1 : pg.causal ? max(told - nr.n, 0) : told;
-    const bool is_front = lane < all_fronts;
-    const int x = min(is_front ? lane / a.front_blocks : (lane - all_fronts) / a.own_blocks, is_front ? a.fronts - 1 : owns - 1);
+    const int want = max(a.shared[quotient(s, one_beams)], 0), room = !nr.n ? -1 : pg.causal ? max(told - nr.n, 0) : told;
+    const bool is_front = lane < a.fronts;
+    const int x = is_front ? lane : min(quotient(lane - a.fronts, __builtin_amdgcn_rcpf((float)a.own_blocks)), owns - 1);
     // first sequence (and head) of the part's group
-    const int step = a.per_head ? pg.Hkv : 1, h = a.per_head ? x % pg.Hkv : 0, group = is_front ? x / step : x / step / a.n_beams;
+    const int step = a.per_head ? pg.Hkv : 1, of = a.per_head ? quotient(x, one_heads) : x, h = x - of * step;
+    const int group = is_front ? of : quotient(of, one_beams);
     const int seq0 = group * a.n_beams * step + h;
     int least = 0x7FFFFFFF;
 #pragma unroll 4
@@ -1173,28 +1183,75 @@ __device__ __forceinline__ bool beams_work(const AttendArgs& a, int unit, int rb
     const int shared = (int)min((int64_t)__shfl(want, seq0) << pg.lg_ps, (int64_t)pg.max_len);
     const int tiles = least == 0x7FFFFFFF ? 0 : min(shared, least) / ATT_TILE;
     const int own = is_front ? 0 : x, t = __shfl(told, own), first = __shfl(nr.first, own), n = __shfl(nr.n, own);
-    if (lane >= parts) o.en = {0, 0, 0, 0, 0};
-    else if (is_front) o.en = {tiles * ATT_TILE, 0, a.n_beams * pg.max_new, tiles, 0};
-    else o.en = {t, first, n, n ? (min(t, pg.max_len) + ATT_TILE - 1) / ATT_TILE - tiles : 0, tiles};
-
-    // (fronts of many rows go by tiles, of a.front_cost each)
-    const uint32_t per = is_front ? a.front_tiles : a.c_min, price = is_front ? a.front_cost : 2u;
-    const uint32_t rounds = ((uint32_t)o.en.tiles + per - 1) / per;
-    const uint32_t cost = rounds ? price * rounds + a.part_cost : 0, upto = (uint32_t)wave_scan((int)cost), total = __builtin_amdgcn_readlane(upto, 63);
-    const uint32_t groups = max(1u, min((uint32_t)a.chunks, total / (a.part_cost + max(2u, a.front_cost))));
-    if ((uint32_t)o.u >= groups) return false;
-    const uint32_t q = total / groups, r = total % groups, at = o.u * q + min((uint32_t)o.u, r), end = at + q + ((uint32_t)o.u < r ? 1 : 0);
-    const uint32_t begins = upto - cost + a.part_cost;       // of the part's rounds
-    auto tile_of = [&](uint32_t c) { return c <= begins ? 0 : (int)min((c - begins) / price * per, (uint32_t)o.en.tiles); };
-    o.seg0 = tile_of(at);
-    o.seg1 = end >= upto ? o.en.tiles : tile_of(end);
-    if (at >= upto) o.seg0 = o.en.tiles;
-    o.todo = __ballot(o.seg1 > o.seg0);
-    if (hy == 0 && threadIdx.x < 64 && lane < parts) {
-      if (o.seg1 > o.seg0 && o.seg0 == 0) a.plan[lane].x = o.u + lane;
-      if (o.seg1 > o.seg0 && o.seg1 == o.en.tiles) a.plan[lane].y = o.u + lane;
-      if (o.u == 0 && o.en.tiles == 0) a.plan[lane] = make_int2(1, 0);
+    Entry en = {0, 0, 0, 0, 0};
+    if (lane < parts) {
+      if (is_front) en = {tiles * ATT_TILE, 0, a.n_beams * pg.max_new, tiles, 0};
+      else en = {t, first, n, n ? (min(t, pg.max_len) + ATT_TILE - 1) / ATT_TILE - tiles : 0, tiles};
     }
+    // (fronts of many rows go by tiles; of very long caches 2^coarse rounds are one)
+    const uint32_t team = a.front_blocks, per = (uint32_t)(is_front ? a.front_tiles : a.c_min) << a.coarse;
+    const uint32_t rounds = ((uint32_t)en.tiles + per - 1) / per, cost = rounds ? 2 * rounds + a.part_cost : 0;
+    const uint32_t upto = (uint32_t)wave_scan((int)cost), all = __builtin_amdgcn_readlane(upto, 63);
+    const uint32_t of_fronts = __builtin_amdgcn_readlane(upto, a.fronts - 1), of_own = all - of_fronts;
+    // teams for fronts: as many as their cost asks for, and one each at least
+    const uint32_t used = __popcll(__ballot(is_front && rounds > 0)), least_teams = used + (of_own > 0);
+    const float weight = (float)of_fronts * team, every = weight + (float)of_own;      // (half rounds of all workgroups)
+    const uint32_t teams = max(least_teams, (uint32_t)fminf(a.chunks, every * __builtin_amdgcn_rcpf((float)((a.part_cost + 2u) * team))));
+    const float due = (float)teams * weight * __builtin_amdgcn_rcpf(fmaxf(every, 1.f));
+    const uint32_t most = min(max((uint32_t)(due + 0.5f), used), teams - (of_own > 0 ? 1u : 0u));
+    // the fewest rounds a team (sixteenths of them) for which those are enough
+    const uint32_t of_front = is_front ? rounds : 0, all_rounds = wave_sum(of_front);
+    uint32_t n_teams, upto_teams, front_teams;
+    for (float each = fmaxf(1.f, 16.f * (float)all_rounds * __builtin_amdgcn_rcpf((float)max(most, 1u)));; each += each * 0.0625f + 1.f) {
+      n_teams = min((uint32_t)(fmaxf(16.f * (float)of_front - 0.5f, 0.f) * __builtin_amdgcn_rcpf(each)) + (of_front > 0), of_front);
+      upto_teams = (uint32_t)wave_scan((int)n_teams);
+      front_teams = __builtin_amdgcn_readlane(upto_teams, 63);
+      if (front_teams <= most) break;
+    }
+    if ((uint32_t)o.u >= max(teams, 1u)) return false;
+    const bool at_fronts = (uint32_t)o.u < front_teams;
+    uint32_t u = at_fronts ? o.u : (o.u - front_teams) * team + rb;
+    int seg0 = 0, seg1 = 0;
+    if (at_fronts) {
+      // Of two workgroups of a compute unit the one that came first is served first, and ends first (4 bits: five rounds 23 us, then
+      // 25 us): so it takes more.  Teams in the order first, second, first, .., then those whose second is no front's.
+      const uint32_t firsts = (teams + 1) / 2, seconds = front_teams > firsts ? front_teams - firsts : 0;
+      u = u >= firsts ? 2 * (u - firsts) + 1 : u < seconds ? 2 * u : u + seconds;
+      auto upto_team = [&](uint32_t x) {
+        return x < 2 * seconds ? (float)x + (x & 1 ? a.first_more : 0.f) : (float)x + (float)(x - 2 * seconds) * (seconds ? a.first_more : 0.f);
+      };
+      const uint32_t from = upto_teams - n_teams, i = u - from;
+      if (is_front && i < n_teams) {
+        const float base = upto_team(from), unit = (float)rounds * __builtin_amdgcn_rcpf(upto_team(from + n_teams) - base);
+        // (of few rounds each takes as many, so that none is without)
+        auto cut = [&](uint32_t k) {
+          return k == n_teams ? rounds : rounds < 2 * n_teams ? (uint32_t)(((float)(k * rounds) + 0.5f) * __builtin_amdgcn_rcpf((float)n_teams)) : (uint32_t)((upto_team(from + k) - base) * unit);
+        };
+        seg0 = (int)min(cut(i) * per, (uint32_t)en.tiles);
+        seg1 = (int)min(cut(i + 1) * per, (uint32_t)en.tiles);
+      }
+    } else if (!is_front && of_own) {
+      // (a share of two half rounds at least: no workgroup between others of a part is without a tile of it)
+      const uint32_t groups = max(1u, min((teams - front_teams) * team, of_own / 2)), q = of_own / groups, r = of_own % groups;
+      const uint32_t at = u * q + min(u, r), end = at + q + (u < r ? 1 : 0), ends = upto - of_fronts, begins = ends - cost + a.part_cost;
+      auto tile_of = [&](uint32_t c) { return c >= ends ? en.tiles : c <= begins ? 0 : (int)min((c - begins) / 2 * per, (uint32_t)en.tiles); };
+      seg0 = tile_of(at);
+      seg1 = tile_of(end);
+    }
+    const bool some = seg1 > seg0;
+    o.todo = __ballot(some);
+    o.slot0 = u + (at_fronts ? rb * a.front_slots : 0);
+    if (hy == 0 && threadIdx.x < 64 && lane < parts) {
+      int2* const plan = a.plan + (is_front ? lane * a.front_blocks + rb : all_fronts + lane - a.fronts);
+      if (some && seg0 == 0) plan->x = o.slot0 + lane;
+      if (some && seg1 == en.tiles) plan->y = o.slot0 + lane;
+      if (o.u == 0 && en.tiles == 0 && (is_front || rb == 0)) *plan = make_int2(1, 0);
+    }
+    if (threadIdx.x < 64) {
+      *(int4*)s_parts[lane] = make_int4(en.told, en.first, en.n, en.front + seg0);
+      s_parts[lane][4] = en.front + seg1;
+    }
+    __syncthreads();
     return true;
   }
   if (!find_chunk<NW, true>(a, o.u, lds, o.ch)) return false;
@@ -1211,14 +1268,12 @@ __device__ __forceinline__ bool beams_work(const AttendArgs& a, int unit, int rb
 // The next part: its chunk, whether it is a front, and the slot of its sums.
 __device__ __forceinline__ void next_part(const AttendArgs& a, BeamsWork& o, bool& front, int& slot) {
   if (a.spread) {
-    const int l = __builtin_ctzll(o.todo), all_fronts = a.fronts * a.front_blocks;
-    auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
-    front = l < all_fronts;
-    o.rb = front ? l % a.front_blocks : (l - all_fronts) % a.own_blocks;
-    const int before = of(o.en.front);
-    o.ch = {front ? l / a.front_blocks : a.fronts + (l - all_fronts) / a.own_blocks, before + of(o.seg0), before + of(o.seg1), 0, 0, 0,
-            of(o.en.told), of(o.en.first), of(o.en.n)};
-    slot = o.u + l;
+    const int l = __builtin_ctzll(o.todo);
+    front = l < a.fronts;
+    const int* p = o.lds[l];
+    o.ch = {front ? l : a.fronts + (l - a.fronts) / a.own_blocks, p[3], p[4], 0, 0, 0, p[0], p[1], p[2]};
+    slot = o.slot0 + l;
+    o.rb = front ? o.team_rb : (l - a.fronts) % a.own_blocks;
   } else {
     front = o.ch.e < a.fronts;
     slot = o.ch.slot0 + o.ch.index + (front ? o.rb * a.front_slots : 0);

@@ -30,7 +30,7 @@ __global__ __launch_bounds__(256) void k_beams_join(AttendArgs a) {
   });
 }
 
-struct BeamsPlan { int many, R, front_rows, own_rows, c_min, target, spread; int64_t front_blocks, own_blocks, fronts, entries, parts, Hy, groups, slots, front_slots; };
+struct BeamsPlan { int many, R, front_rows, own_rows, c_min, target, spread, coarse; int64_t front_blocks, own_blocks, fronts, entries, parts, Hy, groups, slots, front_slots; };
 BeamsPlan beams_plan(const Pages& pg, int n_beams) {
   BeamsPlan p;
   const int64_t rows = (int64_t)pg.G * pg.max_new;
@@ -48,10 +48,14 @@ BeamsPlan beams_plan(const Pages& pg, int n_beams) {
   p.parts = p.fronts * p.front_blocks + (p.entries - p.fronts) * p.own_blocks;
   p.c_min = pg.fmt == RESTKV_Q4 ? 4 : pg.fmt == RESTKV_BF16 ? 2 : 1;      // (tiles of a round: one of the keys of each wavefront)
   p.target = n_cu() * 2;
-  p.spread = p.parts <= 64;
+  p.spread = p.fronts + (p.entries - p.fronts) * p.own_blocks <= 64 && (p.fronts + 1) * p.Hy * p.front_blocks <= p.target;
+  p.coarse = 0;
   if (p.spread) {
-    p.groups = std::max<int64_t>(1, p.target / p.Hy);
-    p.slots = p.front_slots = p.groups + p.parts;
+    p.groups = p.target / (p.Hy * p.front_blocks);
+    p.front_slots = p.groups + 64;
+    p.slots = p.groups * p.front_blocks + 64;
+    // (what 64 parts cost has to be below 2^32)
+    while (((pg.max_len / ATT_TILE >> p.coarse) + 4) * 2 * 64 * p.front_blocks > (int64_t)1 << 31) ++p.coarse;
   } else {
     const int64_t tiles = (pg.max_len + ATT_TILE - 1) / ATT_TILE, each = p.Hy * std::max(p.front_blocks, p.own_blocks);
     const int64_t more = std::min<int64_t>(p.target / each + 1, p.entries * ((tiles + p.c_min - 1) / p.c_min));
@@ -65,7 +69,7 @@ BeamsWs beams_ws(const Pages& pg, const BeamsPlan& p) {
   BeamsWs w = {};
   auto take = [&](size_t bytes) { size_t o = w.bytes; w.bytes = align_up(w.bytes + bytes); return o; };
   const size_t rows = (size_t)p.slots * p.Hy * pg.G * pg.max_new;
-  const size_t front = (size_t)p.front_slots * (p.spread ? 1 : p.front_blocks) * p.Hy * p.front_rows;
+  const size_t front = (size_t)p.front_slots * p.front_blocks * p.Hy * p.front_rows;
   w.plan = take((size_t)p.parts * 8);
   w.m = take(rows * 4);
   w.l = take(rows * 4);
@@ -93,8 +97,9 @@ int launch_attend_beams(const Pages& pg, int n_beams, const int32_t* shared, con
   a.shared = shared; a.n_beams = n_beams; a.fronts = (int)p.fronts;
   a.front_blocks = (int)p.front_blocks; a.own_blocks = (int)p.own_blocks; a.front_slots = (int)p.front_slots; a.spread = p.spread;
   a.front_rows = p.front_rows; a.own_rows = p.own_rows;
-  a.part_cost = 3; a.front_tiles = p.many ? 1 : p.c_min; a.front_cost = 2;
-  a.row_blocks = p.spread ? 1 : (int)std::max(p.front_blocks, p.own_blocks); a.units = (int)(p.groups * p.Hy); a.c_min = p.c_min;
+  a.part_cost = p.many ? 4 : 3; a.front_tiles = p.many ? 1 : p.c_min; a.coarse = p.coarse;
+  a.first_more = 0.1f;
+  a.row_blocks = (int)(p.spread ? p.front_blocks : std::max(p.front_blocks, p.own_blocks)); a.units = (int)(p.groups * p.Hy); a.c_min = p.c_min;
   a.chunks = p.spread ? (float)p.groups : (float)((double)p.target / (double)(p.Hy * std::max(p.front_blocks, p.own_blocks)) * (1 - 0x1p-23));
   const int rc = p.many ? run_attend_beams_rows(a, st) : pg.fmt == RESTKV_F32 ? run_attend_beams_f32(a, p.R, st) : pg.fmt == RESTKV_BF16 ? run_attend_beams_bf16(a, p.R, st) : run_attend_beams_q4(a, p.R, st);
   if (rc) return rc;
