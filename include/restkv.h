@@ -510,6 +510,12 @@ int restkv_debug_score_plan(const restkv_params* p, int32_t* plan);
  */
 int restkv_debug_fp32_plan(const restkv_params* p, int32_t* plan);
 
+/*
+ * Debug aid: with on != 0 restkv_attend_beams reads shared pages once for all beams however short the caches are (short ones are
+ * otherwise read as restkv_attend does).  Process-wide; its workspace size follows.
+ */
+int restkv_debug_force_shared(int on);
+
 /* Static description of an error code. */
 const char* restkv_strerror(int code);
 

@@ -121,6 +121,8 @@ def lib() -> ctypes.CDLL:
         L.restkv_beam_reorder.restype = ctypes.c_int
         L.restkv_attend_beams_workspace_bytes.argtypes = [C, i32]
         L.restkv_attend_beams_workspace_bytes.restype = sz
+        L.restkv_debug_force_shared.argtypes = [ctypes.c_int]
+        L.restkv_debug_force_shared.restype = ctypes.c_int
         L.restkv_attend_beams.argtypes = [C, i32] + [vp] * 12 + [sz, vp]
         L.restkv_attend_beams.restype = ctypes.c_int
         L.restkv_strerror.restype = ctypes.c_char_p
@@ -722,6 +724,10 @@ def alloc_attend_beams_workspace(c: RestkvCache, n_beams, device="cuda") -> Opti
     """Scratch of restkv_attend_beams, or None where it needs none."""
     n = restkv_attend_beams_workspace_bytes(c, n_beams)
     return torch.empty(n + 256, dtype=torch.uint8, device=device) if n else None
+
+
+def restkv_debug_force_shared(on: bool):
+    _chk(lib().restkv_debug_force_shared(int(bool(on))), "restkv_debug_force_shared")
 
 
 def restkv_attend_beams(c: RestkvCache, n_beams, shared, q, pages: CachePages, table, lens, out, lse=None, workspace=None, *,

@@ -3,6 +3,7 @@
 // them, to a whole tile, is another.  The kernels are those of attend.hpp, on chunks of both kinds in one launch, and a row's output is
 // joined from the chunks of its group's entry and of its own.
 #include <algorithm>
+#include <atomic>
 
 #include "attend.hpp"
 #include "beams.hpp"
@@ -80,12 +81,27 @@ BeamsWs beams_ws(const Pages& pg, const BeamsPlan& p) {
   return w;
 }
 
+// Short caches are read as if nothing were shared: one launch where each is one chunk, and no join of two kinds of chunks.  By what all
+// caches may hold together.  So / by parts, us, 8 KV heads of 128, pages that the last call has read too: bf16, 4 beams 33 MB 14.2 / 15.7
+// and 64 MB 16.3 / 16.3, four groups of them 33 MB 13.7 / 14.8, 65 MB 16.3 / 16.4, 129 MB 23.6 / 17.4, two groups of 16 beams 66 MB 14.6 / 18.1, 130 MB
+// 19.1 / 19.6; 4 bits 40 MB 19.4 / 21.1, 80 MB 28.5 / 21.7; float32 33 MB 15.9 / 17.0, 65 MB 19.3 / 17.2.
+std::atomic<int> g_force_shared{0};
+bool as_if_alone(const Pages& pg, int n_beams) {
+  const int64_t row = pg.fmt == RESTKV_Q4 ? pg.d / 2 + pg.d / 8 : pg.fmt == RESTKV_BF16 ? pg.d * 2 : pg.d * 4;
+  return n_beams == 1 || (!g_force_shared && 2 * row * pg.Hkv * pg.n_seqs <= ((int64_t)48 << 20) / pg.max_len);
+}
+
 }  // namespace
 
-size_t attend_beams_ws_bytes(const Pages& pg, int n_beams) { return beams_ws(pg, beams_plan(pg, n_beams)).bytes; }
+void force_shared(bool on) { g_force_shared = on; }
+
+size_t attend_beams_ws_bytes(const Pages& pg, int n_beams) {
+  return as_if_alone(pg, n_beams) ? attend_ws_bytes(pg) : beams_ws(pg, beams_plan(pg, n_beams)).bytes;
+}
 
 int launch_attend_beams(const Pages& pg, int n_beams, const int32_t* shared, const void* q, const void* k_pages, const void* v_pages,
                         const void* k_scale, const void* v_scale, void* out, float* lse, char* ws, hipStream_t st) {
+  if (as_if_alone(pg, n_beams)) return launch_attend(pg, q, k_pages, v_pages, k_scale, v_scale, out, lse, ws, st);
   const BeamsPlan p = beams_plan(pg, n_beams);
   const BeamsWs lay = beams_ws(pg, p);
   if (p.groups * p.Hy > (int64_t)1 << 30 || p.front_slots * p.front_blocks > (int64_t)1 << 30 || std::max(p.front_blocks, p.own_blocks) > (1 << 20) || (int64_t)pg.max_new * pg.Hq >= (1 << 24)) return RESTKV_EUNSUPPORTED;

@@ -172,6 +172,11 @@ int restkv_attend_beams(const restkv_cache* c, int32_t n_beams, const int32_t* s
                              (hipStream_t)stream);
 }
 
+int restkv_debug_force_shared(int on) {
+  force_shared(on != 0);
+  return RESTKV_OK;
+}
+
 size_t restkv_beam_workspace_bytes(const restkv_beams* b) {
   Beams o;
   return resolve_beams(b, &o) == RESTKV_OK ? beam_ws_bytes(o) : 0;

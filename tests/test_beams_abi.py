@@ -101,6 +101,15 @@ def test_attend_beams_refusals(rk):  # noqa: F811
     need = rk.restkv_attend_beams_workspace_bytes(big, 3)
     assert need > 0
     assert attend(rk, big, ws=None) == -3 and attend(rk, big, ws_n=need - 1) == -3 and attend(rk, big, ws=ctypes.c_void_p(264)) == -3
+    # short caches need what restkv_attend does, others (or all, where told so) more
+    assert need == rk.restkv_attend_workspace_bytes(big)
+    rk.restkv_debug_force_shared(True)
+    more = rk.restkv_attend_beams_workspace_bytes(big, 3)
+    assert more > need and attend(rk, big, ws_n=need) == -3
+    rk.restkv_debug_force_shared(False)
+    large = good(rk, max_pages=6000, n_pages=4000)
+    assert rk.restkv_attend_beams_workspace_bytes(large, 3) != rk.restkv_attend_workspace_bytes(large)
+    assert rk.restkv_attend_beams_workspace_bytes(large, 1) == rk.restkv_attend_workspace_bytes(large)
     assert attend(rk, good(rk, n_seqs=0), shared=None, q=None) == 0
     assert attend(rk, good(rk, n_tokens=0), new_start=ONE, shared=None, q=None) == 0
 

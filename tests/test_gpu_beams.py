@@ -282,6 +282,14 @@ def test_binding_refuses_wrong_reorder_tensors():
 FORMATS = [("f32", None, None), ("bf16", None, None), ("bf16", None, "f32"), ("bf16", "q4", None), ("f32", "q4", None)]
 
 
+@pytest.fixture
+def shared_once():
+    """Shared pages read once, however short the caches are."""
+    rk.restkv_debug_force_shared(True)
+    yield
+    rk.restkv_debug_force_shared(False)
+
+
 def share(p, n_beams, shared):
     """The first shared[g] pages of each group (per head, with tables per head): those of its longest sequence, in all tables."""
     for g, n in enumerate(shared):
@@ -344,7 +352,7 @@ ATTENDS = [
 
 @pytest.mark.parametrize("dtype,fmt,out", FORMATS)
 @pytest.mark.parametrize("lens,new,n_beams,shared,more", ATTENDS)
-def test_attend_beams(lens, new, n_beams, shared, more, dtype, fmt, out):
+def test_attend_beams(lens, new, n_beams, shared, more, dtype, fmt, out, shared_once):
     p = Plain(rk, lens=lens, new=new, dtype=dtype, fmt=fmt, out_dtype=out, seed=sum(new), **more)
     out_type = torch.float32 if "f32" in (dtype, out) else torch.bfloat16
     sh = share(p, n_beams, [min(n, p.width) for n in shared])
@@ -352,10 +360,13 @@ def test_attend_beams(lens, new, n_beams, shared, more, dtype, fmt, out):
         sh.fill_(shared[0])
     q = (p.normal(p.tokens, p.hq, p.d) * 2).to(p.type)
     check_beams(p, n_beams, sh, q, out_type, causal=more.get("causal", True), scale=more.get("scale"))
+    if sum(new) % 3 == 0:                                  # and as the sizes have it
+        rk.restkv_debug_force_shared(False)
+        check_beams(p, n_beams, sh, q, out_type, causal=more.get("causal", True), scale=more.get("scale"))
 
 
 @pytest.mark.parametrize("dtype,fmt,out", FORMATS)
-def test_attend_beams_long(dtype, fmt, out):
+def test_attend_beams_long(dtype, fmt, out, shared_once):
     """Many chunks of the shared pages and of the beams' own, against restkv_attend, which reads every beam's."""
     for lens, n_beams, new, hq, hkv in (([5000, 5100, 6000, 4999], 4, 1, 8, 2), ([3000 + 37 * i for i in range(24)], 12, 2, 8, 2),
                                         ([9000] * 3 + [700] * 3, 3, 1, 4, 1)):
@@ -394,7 +405,7 @@ def test_attend_beams_long(dtype, fmt, out):
 
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
 @pytest.mark.parametrize("dtype,fmt", [("f32", None), ("bf16", None), ("bf16", "q4")])
-def test_what_beams_do_not_see_has_no_influence(dtype, fmt, bad):
+def test_what_beams_do_not_see_has_no_influence(dtype, fmt, bad, shared_once):
     """Junk behind the lengths, in the same pages as what is seen; a page that is not there, in front and behind."""
     p = Plain(rk, lens=[133, 140, 150, 129], new=[1, 3, 1, 1], dtype=dtype, fmt=fmt, junk=bad, hq=8, hkv=2)
     sh = share(p, 4, [8])
@@ -404,7 +415,7 @@ def test_what_beams_do_not_see_has_no_influence(dtype, fmt, bad):
     check_beams(p, 4, sh, p.normal(p.tokens, 8, 64).to(p.type), p.type)
 
 
-def test_attend_beams_strided_and_without_lse():
+def test_attend_beams_strided_and_without_lse(shared_once):
     p = Plain(rk, lens=[133, 140, 150, 129], new=[1, 3, 1, 1], hq=8, hkv=2, d=128)
     sh = share(p, 2, [8, 6])
     wide = p.normal(p.tokens, 1 + 8 * 128 + 7).bfloat16()
@@ -418,7 +429,7 @@ def test_attend_beams_strided_and_without_lse():
     assert torch.equal(out.cpu(), want) and (back[:, :, 0] == 5.0).all()
 
 
-def test_attend_beams_two_calls_at_once_and_on_another_stream():
+def test_attend_beams_two_calls_at_once_and_on_another_stream(shared_once):
     p = Plain(rk, lens=[700, 720, 650, 900], new=[2, 1, 1, 1], d=128, hq=8, hkv=2)
     sh = share(p, 2, [40, 39])
     q = p.normal(p.tokens, 8, 128).bfloat16().cuda()
@@ -498,7 +509,7 @@ class Search:
 
 
 @pytest.mark.parametrize("fmt", [None, "q4"])
-def test_a_search_follows_its_histories(fmt):
+def test_a_search_follows_its_histories(fmt, shared_once):
     """Every step's attention is that of the tokens that a beam stands for, whatever pages they lie in; selections follow its logits."""
     m = Search(fmt)
     m.start()
@@ -528,7 +539,7 @@ def test_a_search_follows_its_histories(fmt):
 
 
 @pytest.mark.parametrize("fmt", [None, "q4"])
-def test_a_search_replayed_from_a_hip_graph(fmt):
+def test_a_search_replayed_from_a_hip_graph(fmt, shared_once):
     """A step captured once, in two graphs that share the workspaces, against eager steps: the same tokens, scores, tables and pages."""
     a, b = Search(fmt, seed=3), Search(fmt, seed=3)
     s = torch.cuda.Stream()
