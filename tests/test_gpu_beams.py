@@ -88,6 +88,18 @@ def test_select_ties(dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_select_beams_far_apart(dtype):
+    """One beam far ahead of many others, over many pieces of its row: nearly all is its own; and two that overlap."""
+    g = torch.Generator().manual_seed(11)
+    x = torch.randn((32, 60000), generator=g).to(dtype)
+    scores = -50 - 10 * torch.rand((2, 16), generator=g)
+    scores[0, 3], scores[1, 5], scores[1, 9] = 0, 0, -0.5
+    for n_out in (5, 64):
+        got = check_select(x, scores, None, n_out)
+        assert (got[1][0] == 3).all() and set(got[1][1].tolist()) <= {5, 9}
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_select_masks_and_unusual_values(dtype):
     g = torch.Generator().manual_seed(3)
     vocab, low = 6000, torch.finfo(dtype).min
