@@ -540,19 +540,21 @@ __global__ __launch_bounds__(JOIN_LIST) void k_select_join(SelectArgs a) {
 }
 
 struct SelectPlan { int pieces, blocks; };
-SelectPlan select_plan(const Beams& b) {
-  const int vec = b.dtype == RESTKV_F32 ? 4 : 8;
-  const int all = (b.n_vocab + vec - 1) / vec + 1;     // blocks of 16 bytes that a row may touch
-  // even pieces of a tile at least, as many as four workgroups on each compute unit take
+// logits: null for the most pieces that there may be.
+SelectPlan select_plan(const Beams& b, const void* logits) {
+  const int size = b.dtype == RESTKV_F32 ? 4 : 2, vec = 16 / size;
+  // blocks of 16 bytes that a row may touch; even pieces of them, a tile at least, as many as four workgroups on each compute unit take
+  const bool aligned = logits && !(((uintptr_t)logits | (uint64_t)b.stride * size) & 15u);
+  const int most = (b.n_vocab + vec - 1 + vec - 1) / vec, all = aligned ? (b.n_vocab + vec - 1) / vec : most;
   const int64_t rows = (int64_t)b.n_groups * b.n_beams, want = 4 * n_cu();
-  const int pieces = (int)std::min<int64_t>((all + SEL_TILE - 1) / SEL_TILE, std::max<int64_t>(1, want / std::max<int64_t>(rows, 1)));
+  const int pieces = (int)std::min<int64_t>((most + SEL_TILE - 1) / SEL_TILE, std::max<int64_t>(1, want / std::max<int64_t>(rows, 1)));
   const int blocks = (all + pieces - 1) / pieces;
-  return {(all + blocks - 1) / blocks, blocks};
+  return {logits ? (all + blocks - 1) / blocks : pieces, blocks};
 }
 struct SelectWs { size_t s, m, keys, bytes; };
 SelectWs select_ws(const Beams& b) {
   SelectWs w = {};
-  const size_t n = (size_t)b.n_groups * b.n_beams * select_plan(b).pieces;
+  const size_t n = (size_t)b.n_groups * b.n_beams * select_plan(b, nullptr).pieces;
   auto take = [&](size_t bytes) { size_t o = w.bytes; w.bytes = align_up(w.bytes + bytes); return o; };
   w.s = take(n * 8);
   w.m = take(n * 4);
@@ -571,7 +573,7 @@ int launch_beam_select(const Beams& b, const void* logits, const float* scores, 
   a.b = b;
   a.logits = logits; a.scores = scores; a.finished = finished;
   a.new_scores = new_scores; a.parents = parents; a.tokens = tokens; a.new_finished = new_finished;
-  const SelectPlan plan = select_plan(b);
+  const SelectPlan plan = select_plan(b, logits);
   a.pieces = plan.pieces; a.blocks = plan.blocks;
   a.part_s = (double*)(ws + lay.s); a.part_m = (float*)(ws + lay.m); a.keys = (unsigned long long*)(ws + lay.keys);
   const dim3 grid = wide_grid((int64_t)b.n_groups * b.n_beams * a.pieces);
