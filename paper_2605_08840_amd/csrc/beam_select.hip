@@ -384,9 +384,10 @@ __device__ __forceinline__ double score_of(const Cont& x) {
 // bound go into a list in LDS, and an entry's place in the answer is the number of entries above it.  Of a long list (where one beam
 // is far ahead of the others, most threads' maxima tell little) the same bound is taken again over the list.  Where more than the list
 // holds reach it all the same (scores that are all equal) the answer is found one at a time.
-constexpr int JOIN_WAVES = 16, JOIN_LIST = 64 * JOIN_WAVES, JOIN_AHEAD = 4, JOIN_ROUNDS = 5;
-__global__ __launch_bounds__(JOIN_LIST) void k_select_join(SelectArgs a) {
-  constexpr int NW = JOIN_WAVES;
+constexpr int JOIN_AHEAD = 4, JOIN_ROUNDS = 5;
+template <int NW>
+__global__ __launch_bounds__(64 * NW) void k_select_join(SelectArgs a) {
+  constexpr int JOIN_LIST = 64 * NW;
   __shared__ double s_score[64], s_log[64];
   __shared__ float s_top[64];
   __shared__ int s_end[64], s_count[JOIN_ROUNDS];
@@ -400,7 +401,7 @@ __global__ __launch_bounds__(JOIN_LIST) void k_select_join(SelectArgs a) {
   // rows of this wavefront: row0, row0 + step, ..; of such a row every `parts`-th `wide` keys
   const int parts = max(1, NW / B), step = NW / parts, row0 = wv / parts, part = wv % parts, per = C * K;
   const int wide = min(64, (per + parts - 1) / parts), hop = wide * parts;
-  const int spread = (lane & 15) * 4 + (lane >> 4), at0 = spread < wide ? part * wide + spread : per;     // (neighbours to other groups)
+  const int spread = lane % NW * (64 / NW) + lane / NW, at0 = spread < wide ? part * wide + spread : per;     // (neighbours to other groups)
   auto cont = [&](int b, unsigned long long key) {
     return key ? cont_of(s_score[b] + (((double)logit_of(key) - (double)s_top[b]) - s_log[b]), b, key) : Cont{0, 0};
   };
@@ -480,7 +481,7 @@ __global__ __launch_bounds__(JOIN_LIST) void k_select_join(SelectArgs a) {
   int n = s_count[0];
   for (int round = 1; n > 128 && round < JOIN_ROUNDS; ++round) {
     // (of a list that has overflowed what is in it will do: as many reach the bound)
-    const int i = (tid & 15) * 64 + (tid >> 4);        // (neighbours to other groups)
+    const int i = tid % NW * 64 + tid / NW;            // (neighbours to other groups)
     const Cont x = i < n ? Cont{s_scores[i], s_rests[i]} : Cont{0, 0};
     const uint32_t next = block_bound<JOIN_LIST>((uint32_t)(x.score >> 32), K, s_bound);
     if (next <= bar) break;
@@ -579,7 +580,9 @@ int launch_beam_select(const Beams& b, const void* logits, const float* scores, 
   const dim3 grid = wide_grid((int64_t)b.n_groups * b.n_beams * a.pieces);
   if (b.dtype == RESTKV_F32) hipLaunchKernelGGL(k_select_rows<float>, grid, dim3(SEL_THREADS), 0, st, a);
   else hipLaunchKernelGGL(k_select_rows<bf16_t>, grid, dim3(SEL_THREADS), 0, st, a);
-  hipLaunchKernelGGL(k_select_join, dim3(b.n_groups), dim3(JOIN_LIST), 0, st, a);
+  // (four / sixteen wavefronts, us a call: 112 continuations left by the pieces 11.8 / 13.4, 504 of them 22.1 / 23.2, 2048 39.5 / 33.9)
+  if ((int64_t)b.n_beams * a.pieces * b.n_out <= 1024) hipLaunchKernelGGL(k_select_join<4>, dim3(b.n_groups), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(k_select_join<16>, dim3(b.n_groups), dim3(1024), 0, st, a);
   return hip_status();
 }
 
