@@ -61,6 +61,10 @@ class RestkvBeams(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("n_groups", "n_beams", "n_vocab", "n_out", "dtype", "end_token")] + [
         ("logit_stride", ctypes.c_int64)]
 
+    def __setattr__(self, name, value):
+        self.__dict__.pop("told", None)      # what the binding has worked out from the fields
+        super().__setattr__(name, value)
+
 
 class RestkvLayerPages(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("k_pages", "v_pages", "k_scale", "v_scale")]
@@ -663,27 +667,48 @@ def alloc_beam_workspace(b: RestkvBeams, device="cuda") -> torch.Tensor:
     return torch.empty(restkv_beam_workspace_bytes(b) + 256, dtype=torch.uint8, device=device)
 
 
+class _BeamsTold:
+    """What a description says of the tensors of restkv_beam_select, worked out once (a field that is set makes it new)."""
+
+    def __init__(self, b: RestkvBeams):
+        self.ref, self.dtype = ctypes.byref(b), _TORCH.get(b.dtype)
+        rows, stride = b.n_groups * b.n_beams, b.logit_stride or b.n_vocab
+        self.flat, self.flat_strides = (rows, b.n_vocab), (stride, 1)
+        self.grouped, self.stride, self.many = (b.n_groups, b.n_beams, b.n_vocab), stride, (b.n_groups > 1, b.n_beams > 1, b.n_vocab > 1)
+        into, of = (b.n_groups, b.n_out), (b.n_groups, b.n_beams)
+        self.scores, self.finished = (of, torch.float32, "scores", None), (of, torch.int32, "finished", None)
+        self.new_scores, self.new_finished = (into, torch.float32, "new_scores", None), (into, torch.int32, "new_finished", None)
+        self.parents, self.tokens = (into, torch.int32, "parents", None), (into, torch.int32, "tokens", None)
+
+    def takes(self, shape, strides) -> bool:
+        """Whether logits of this shape are rows at the described distance (a stride along one entry says nothing)."""
+        groups, beams, vocab = self.many
+        if strides[-1] != 1 and vocab:
+            return False
+        if shape == self.flat:
+            return strides[0] == self.stride or shape[0] <= 1
+        return shape == self.grouped and (strides[1] == self.stride or not beams) and \
+            (strides[0] == self.grouped[1] * self.stride or not groups)
+
+
 def restkv_beam_select(b: RestkvBeams, logits, scores, new_scores, parents, tokens, workspace, *, finished=None, new_finished=None,
                        stream=None):
     """The n_out best continuations of each request, best first: new_scores, parents (beams), tokens [n_groups, n_out] from logits
     [n_groups * n_beams, n_vocab] (or [n_groups, n_beams, n_vocab]) and scores [n_groups, n_beams]; finished and new_finished
     (int32, nonzero: ended) beside them.  new_scores may be scores and new_finished finished, where n_out = n_beams."""
     what, dev = "restkv_beam_select", logits.get_device()
-    rows, stride = b.n_groups * b.n_beams, b.logit_stride or b.n_vocab
-    shape, strides = logits.shape, logits.stride()
-    if dev < 0 or logits.dtype is not _TORCH.get(b.dtype) or \
-            not (shape == (rows, b.n_vocab) or shape == (b.n_groups, b.n_beams, b.n_vocab)) or \
-            (strides[-1] != 1 and b.n_vocab > 1) or (strides[-2] != stride and shape[-2] > 1) or \
-            (len(shape) == 3 and strides[0] != b.n_beams * stride and b.n_groups > 1):
-        raise RestkvError(-1, f"{what}: logits have to be {_TORCH.get(b.dtype)} [{rows}, {b.n_vocab}], rows {stride} apart, on a GPU")
-    into, of = (b.n_groups, b.n_out), (b.n_groups, b.n_beams)
-    sc = _check_flat(what, dev, scores, (of, torch.float32, "scores", None))
-    ns = _check_flat(what, dev, new_scores, (into, torch.float32, "new_scores", None))
-    ps, tk = _check_flat(what, dev, parents, (into, torch.int32, "parents", None)), _check_flat(what, dev, tokens, (into, torch.int32, "tokens", None))
-    fn = None if finished is None else _check_flat(what, dev, finished, (of, torch.int32, "finished", None))
-    nf = None if new_finished is None else _check_flat(what, dev, new_finished, (into, torch.int32, "new_finished", None))
+    told = b.__dict__.get("told")
+    if told is None:
+        told = b.__dict__["told"] = _BeamsTold(b)
+    if dev < 0 or logits.dtype is not told.dtype or \
+            ((logits.shape != told.flat or logits.stride() != told.flat_strides) and not told.takes(logits.shape, logits.stride())):
+        raise RestkvError(-1, f"{what}: logits have to be {told.dtype} {told.flat}, rows {told.stride} apart, on a GPU")
+    sc, ns = _check_flat(what, dev, scores, told.scores), _check_flat(what, dev, new_scores, told.new_scores)
+    ps, tk = _check_flat(what, dev, parents, told.parents), _check_flat(what, dev, tokens, told.tokens)
+    fn = None if finished is None else _check_flat(what, dev, finished, told.finished)
+    nf = None if new_finished is None else _check_flat(what, dev, new_finished, told.new_finished)
     wp, wn = _take_workspace(what, dev, workspace)
-    _on_gpu(dev, stream, what, lib().restkv_beam_select, ctypes.byref(b), logits.data_ptr(), sc, fn, ns, ps, tk, nf, wp, wn)
+    _on_gpu(dev, stream, what, lib().restkv_beam_select, told.ref, logits.data_ptr(), sc, fn, ns, ps, tk, nf, wp, wn)
 
 
 class CacheLayers:
