@@ -45,7 +45,7 @@ void k_attend_rows(AttendArgs a) {
     ch = work.ch;
     rb = work.rb;
     if (!front) {
-      attend_chunk<FMT_BF16, bf16_t, D, NP, 1, 1, true>(a, ch, hy, rb, false, slot, (float*)lds);
+      attend_own<FMT_BF16, bf16_t, D, NP, 1, 1, true>(a, ch, hy, rb, slot, (float*)lds);
       __syncthreads();
       continue;
     }
