@@ -33,8 +33,12 @@ struct AttendArgs {
   // head), the rows of all its beams for them; then each sequence's own positions behind these.  An entry times a block of rows is a
   // part: front_blocks of each of the former, own_blocks of each of the latter.  plan[part] {first, last} slot (first > last: none);
   // front_*: [slots of fronts * Hy, rows of a block], part_*: [slots * Hy, rows of a sequence].  spread: parts are cut evenly over
-  // the teams of workgroups of a head, of which there are `chunks` (beams_work); else workgroups go by chunks and blocks of rows.
+  // the teams of workgroups of a head, of which there are `chunks` (beams_work); else a workgroup takes a chunk of an entry
+  // for a block of rows, and k_beams_list has written which: list[2 u], [2 u + 1] {entry (-1: none), tiles from, to, slot}, {positions, first
+  // row, new tokens}, of up to front_chunks chunks of fronts, then up to own_chunks of the rest.
   const int32_t* shared;
+  int4* list; int* front_tiles_of;
+  int front_chunks, own_chunks;
   int n_beams, fronts, front_blocks, own_blocks, front_slots, spread, front_rows, own_rows, front_tiles, coarse;
   uint32_t part_cost;
   float first_more;
@@ -71,52 +75,10 @@ __device__ __forceinline__ int wave_scan(int x) {
 // up to 35, 256 entries of 9 to 33 tiles 497 of up to 13 for 512 workgroups (9.3 each).  Up to 64 entries a wavefront works this out by
 // itself, more are divided among the threads of the workgroup.
 struct Chunk { int e, tile0, tile1, index, count, slot0, told, first, n; };
-struct Entry { int told, first, n, tiles, front; };      // front: tiles before the entry's first
-
-// Tiles of the positions that the beams of a group share, and all see: no more than any of them has in front of its new tokens.
-__device__ __forceinline__ int shared_tiles(const AttendArgs& a, int g, int h) {
-  const Pages& pg = a.pg;
-  constexpr int AHEAD = 8;
-  int room = (int)min((int64_t)max(a.shared[g], 0) << pg.lg_ps, (int64_t)pg.max_len), any = 0;
-  for (int b = 0; b < a.n_beams; b += AHEAD) {
-    int told[AHEAD], n[AHEAD];
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      const int s = g * a.n_beams + min(b + u, a.n_beams - 1);
-      told[u] = told_len(pg, s, h);
-      n[u] = new_rows(pg, s).n;
-    }
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      if (n[u]) room = min(room, pg.causal ? max(told[u] - n[u], 0) : told[u]);
-      any |= n[u];
-    }
-  }
-  return any ? room / ATT_TILE : 0;
-}
-
-template <bool BEAMS>
+struct Entry { int told, first, n, tiles; };
 __device__ __forceinline__ Entry read_entry(const AttendArgs& a, int e) {
   const Pages& pg = a.pg;
-  Entry o = {0, 0, 0, 0, 0};
-  if constexpr (BEAMS) {
-    if (e < a.entries) {
-      const bool front = e < a.fronts;
-      const int x = front ? e : e - a.fronts, s = a.per_head ? x / pg.Hkv : x, h = a.per_head ? x - s * pg.Hkv : 0;
-      const int tiles = shared_tiles(a, front ? s : s / a.n_beams, h);
-      if (front) {
-        o = {tiles * ATT_TILE, 0, a.n_beams * pg.max_new, tiles, 0};
-      } else {
-        o.told = told_len(pg, s, h);
-        const NewRows nr = new_rows(pg, s);
-        o.first = nr.first;
-        o.n = nr.n;
-        o.front = tiles;
-        if (o.n) o.tiles = (min(o.told, pg.max_len) + ATT_TILE - 1) / ATT_TILE - tiles;
-      }
-    }
-    return o;
-  }
+  Entry o = {0, 0, 0, 0};
   if (e < a.entries) {
     const int s = a.per_head ? e / pg.Hkv : e, h = a.per_head ? e - s * pg.Hkv : 0;
     o.told = told_len(pg, s, h);
@@ -135,13 +97,13 @@ __device__ __forceinline__ int chunk_tiles(const AttendArgs& a, float total, int
 }
 __device__ __forceinline__ Chunk chunk_of(const Entry& x, int e, int index, int count, int slot0) {
   const int each = count == 1 ? x.tiles : (x.tiles + count - 1) / count, t0 = min(index * each, x.tiles);
-  return {e, x.front + t0, x.front + min(t0 + each, x.tiles), index, count, slot0, x.told, x.first, x.n};
+  return {e, t0, min(t0 + each, x.tiles), index, count, slot0, x.told, x.first, x.n};
 }
-template <int NW = 4, bool BEAMS = false>
+template <int NW = 4>
 __device__ __forceinline__ bool find_chunk(const AttendArgs& a, int x, int* lds, Chunk& o) {
   const int lane = threadIdx.x & 63;
   if (a.entries <= 64) {
-    const Entry en = read_entry<BEAMS>(a, lane);
+    const Entry en = read_entry(a, lane);
     int C = chunk_tiles(a, (float)wave_sum((uint32_t)en.tiles), __popcll(__ballot(en.tiles > 0)));
     int cnt = 0, inc = 0;
     for (int i = 0; i < 8; ++i) {       // (until they are fewer than the resident workgroups: a few too many cost a sixth of the time of 24 lengths)
@@ -150,21 +112,21 @@ __device__ __forceinline__ bool find_chunk(const AttendArgs& a, int x, int* lds,
       if (__builtin_amdgcn_readlane(inc, 63) <= a.chunks || a.entries >= a.chunks) break;
       C += C / 16 + 1;
     }
-    const int own = BEAMS || cnt > 1 ? cnt : 0, sl = BEAMS ? inc : wave_scan(own);
+    const int own = cnt > 1 ? cnt : 0, sl = wave_scan(own);
     const unsigned long long hit = __ballot(inc > x);
     if (!hit) return false;
     const int l = __builtin_ctzll(hit);
     auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
     const int count = of(cnt);
-    o = chunk_of({of(en.told), of(en.first), of(en.n), of(en.tiles), BEAMS ? of(en.front) : 0}, l, x - of(inc) + count, count, of(sl - own));
+    o = chunk_of({of(en.told), of(en.first), of(en.n), of(en.tiles)}, l, x - of(inc) + count, count, of(sl - own));
     return true;
   }
   const int tid = threadIdx.x, wv = tid >> 6;
-  Entry en = read_entry<BEAMS>(a, tid);
+  Entry en = read_entry(a, tid);
   int64_t tiles = en.tiles;
   int active = en.tiles > 0;
   for (int e = tid + 64 * NW; e < a.entries; e += 64 * NW) {
-    const int t = read_entry<BEAMS>(a, e).tiles;
+    const int t = read_entry(a, e).tiles;
     tiles += t;
     active += t > 0;
   }
@@ -190,8 +152,8 @@ __device__ __forceinline__ bool find_chunk(const AttendArgs& a, int x, int* lds,
   int run = 0, slots = 0;
   for (int base = 0; base < a.entries; base += 64 * NW) {
     const int e = base + tid;
-    if (base) en = read_entry<BEAMS>(a, e);
-    const int cnt = e < a.entries ? max(1, (en.tiles + C - 1) / C) : 0, own = BEAMS || cnt > 1 ? cnt : 0;
+    if (base) en = read_entry(a, e);
+    const int cnt = e < a.entries ? max(1, (en.tiles + C - 1) / C) : 0, own = cnt > 1 ? cnt : 0;
     int inc = wave_scan(cnt), sl = wave_scan(own);
     if (lane == 63) {
       lds[2 * NW + wv] = inc;
@@ -452,7 +414,7 @@ struct BeamsWork {
   unsigned long long todo;       // parts (spread), or one
   int (*lds)[8];                 // of a part: positions, first row, new tokens, first and last tile of this workgroup (spread)
   Chunk ch;
-  int u, rb, team_rb, slot0;
+  int u, hy, rb, team_rb, slot0;
 };
 // Parts (up to 64, a lane each; a front with all its blocks of rows is one) cut evenly: the rounds of all follow each other, with
 // a.part_cost half rounds more for each part, which is what its beginning and end take.  Workgroups come in teams of front_blocks.  Some teams take the fronts, one front each and all about as many rounds, each of a team's workgroups the same tiles for a block of rows
@@ -461,16 +423,34 @@ struct BeamsWork {
 // (What comes of it is in LDS, so that the loops between have the registers.)
 // Quotients of small whole numbers (below 2^15), where a division of 32 bits would take forty instructions.
 __device__ __forceinline__ int quotient(int x, float one_over) { return (int)(((float)x + 0.5f) * one_over); }
-template <int NW>
-__device__ __forceinline__ bool beams_work(const AttendArgs& a, int unit, int rb, int* lds, BeamsWork& o) {
+__device__ __forceinline__ bool beams_work(const AttendArgs& a, BeamsWork& o) {
   const Pages& pg = a.pg;
   const int lane = threadIdx.x & 63, all_fronts = a.fronts * a.front_blocks;
-  o.u = a.spread ? quotient(unit, __builtin_amdgcn_rcpf((float)a.Hy)) : unit / a.Hy;
-  const int hy = unit - o.u * a.Hy;
+  const int id = unit_of_block();
+  if (id >= a.units) return false;
+  if (!a.spread) {
+    // blocks of eight units, all row blocks of theirs after each other (so on one XCD)
+    const int front_ids = (a.front_chunks * a.Hy + 7) / 8 * 8 * a.front_blocks;
+    const bool front = id < front_ids;
+    const int x = front ? id : id - front_ids, blocks = front ? a.front_blocks : a.own_blocks, eight = x / (8 * blocks);
+    const int unit = eight * 8 + (x & 7), u = unit / a.Hy;
+    if (u >= (front ? a.front_chunks : a.own_chunks)) return false;
+    const int at = front ? u : u + a.front_chunks;
+    const int4 p = a.list[2 * at], q = a.list[2 * at + 1];
+    if (p.x < 0) return false;
+    o.ch = {p.x, p.y, p.z, 0, 0, p.w, q.x, q.y, q.z};
+    o.hy = unit - u * a.Hy;
+    o.rb = (x - eight * 8 * blocks) >> 3;
+    o.todo = 1;
+    return true;
+  }
+  const int rb = blockIdx.x >> 3;
+  o.u = quotient(id, __builtin_amdgcn_rcpf((float)a.Hy));
+  const int hy = o.hy = id - o.u * a.Hy;
   __shared__ int s_parts[64][8];
   o.lds = s_parts;
   o.rb = o.team_rb = rb;
-  if (a.spread) {
+  {
     // lane = sequence (and head) first, then a part: what each sequence has in front of its new tokens, the least of each group
     const int owns = a.entries - a.fronts, parts = a.fronts + owns * a.own_blocks;
     const float one_beams = __builtin_amdgcn_rcpf((float)a.n_beams), one_heads = __builtin_amdgcn_rcpf((float)pg.Hkv);
@@ -493,11 +473,12 @@ __device__ __forceinline__ bool beams_work(const AttendArgs& a, int unit, int rb
     const int shared = (int)min((int64_t)__shfl(want, seq0) << pg.lg_ps, (int64_t)pg.max_len);
     const int tiles = least == 0x7FFFFFFF ? 0 : min(shared, least) / ATT_TILE;
     const int own = is_front ? 0 : x, t = __shfl(told, own), first = __shfl(nr.first, own), n = __shfl(nr.n, own);
-    Entry en = {0, 0, 0, 0, 0};
+    Entry en = {0, 0, 0, 0};
     if (lane < parts) {
-      if (is_front) en = {tiles * ATT_TILE, 0, a.n_beams * pg.max_new, tiles, 0};
-      else en = {t, first, n, n ? (min(t, pg.max_len) + ATT_TILE - 1) / ATT_TILE - tiles : 0, tiles};
+      if (is_front) en = {tiles * ATT_TILE, 0, a.n_beams * pg.max_new, tiles};
+      else en = {t, first, n, n ? (min(t, pg.max_len) + ATT_TILE - 1) / ATT_TILE - tiles : 0};
     }
+    const int tile0 = is_front ? 0 : tiles;
     // (fronts of many rows go by tiles; of very long caches 2^coarse rounds are one)
     const uint32_t team = a.front_blocks, per = (uint32_t)(is_front ? a.front_tiles : a.c_min) << a.coarse;
     const uint32_t rounds = ((uint32_t)en.tiles + per - 1) / per, cost = rounds ? 2 * rounds + a.part_cost : 0;
@@ -558,22 +539,12 @@ __device__ __forceinline__ bool beams_work(const AttendArgs& a, int unit, int rb
       if (o.u == 0 && en.tiles == 0 && (is_front || rb == 0)) *plan = make_int2(1, 0);
     }
     if (threadIdx.x < 64) {
-      *(int4*)s_parts[lane] = make_int4(en.told, en.first, en.n, en.front + seg0);
-      s_parts[lane][4] = en.front + seg1;
+      *(int4*)s_parts[lane] = make_int4(en.told, en.first, en.n, tile0 + seg0);
+      s_parts[lane][4] = tile0 + seg1;
     }
     __syncthreads();
     return true;
   }
-  if (!find_chunk<NW, true>(a, o.u, lds, o.ch)) return false;
-  const bool front = o.ch.e < a.fronts, none = front && o.ch.tile1 == 0;
-  if (rb >= (front ? a.front_blocks : a.own_blocks)) return false;
-  if (o.ch.index == 0 && hy == 0 && threadIdx.x == 0) {
-    const int slot0 = front ? rb * a.front_slots + o.ch.slot0 : o.ch.slot0;
-    a.plan[front ? o.ch.e * a.front_blocks + rb : all_fronts + (o.ch.e - a.fronts) * a.own_blocks + rb] =
-        none ? make_int2(1, 0) : make_int2(slot0, slot0 + o.ch.count - 1);
-  }
-  o.todo = none ? 0 : 1;
-  return true;
 }
 // The next part: its chunk, whether it is a front, and the slot of its sums.
 __device__ __forceinline__ void next_part(const AttendArgs& a, BeamsWork& o, bool& front, int& slot) {
@@ -586,7 +557,7 @@ __device__ __forceinline__ void next_part(const AttendArgs& a, BeamsWork& o, boo
     o.rb = front ? o.team_rb : (l - a.fronts) % a.own_blocks;
   } else {
     front = o.ch.e < a.fronts;
-    slot = o.ch.slot0 + o.ch.index + (front ? o.rb * a.front_slots : 0);
+    slot = o.ch.slot0 + (front ? o.rb * a.front_slots : 0);
   }
   o.todo &= o.todo - 1;
 }
@@ -597,13 +568,14 @@ void k_attend(AttendArgs a) {
   extern __shared__ __align__(16) float sm[];
   const int unit = unit_of_block();
   int rb = blockIdx.x >> 3, slot = 0;
-  if (unit >= a.units) return;
-  const int hy = unit % a.Hy;
+  if (!BEAMS && unit >= a.units) return;
+  int hy = BEAMS ? 0 : unit % a.Hy;
   bool front = false;
   Chunk ch;
   BeamsWork work;
   if constexpr (BEAMS) {
-    if (!beams_work<4>(a, unit, rb, (int*)sm, work)) return;
+    if (!beams_work(a, work)) return;
+    hy = work.hy;
   } else {
     if (!find_chunk(a, unit / a.Hy, (int*)sm, ch)) return;
   }

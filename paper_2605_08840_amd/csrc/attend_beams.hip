@@ -31,9 +31,109 @@ __global__ __launch_bounds__(256) void k_beams_join(AttendArgs a) {
   });
 }
 
-struct BeamsPlan { int many, R, front_rows, own_rows, c_min, target, spread, coarse; int64_t front_blocks, own_blocks, fronts, entries, parts, Hy, groups, slots, front_slots; };
+constexpr int PART_ROUNDS = 2;         // what a part's beginning and end take, in rounds
+
+// Sum over the 1024 threads; lds: 16 words, free to be written.
+template <typename V>
+__device__ __forceinline__ V block_sum(V x, V* lds) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+  __syncthreads();
+  x = lds[0];
+#pragma unroll
+  for (int w = 1; w < 16; ++w) x += lds[w];
+  return x;
+}
+
+// Where there are many parts, or many rows: which workgroup takes what, worked out once, by one workgroup.  Entries are cut into chunks of at
+// most C tiles, C being an even share of all rounds with what parts cost beside them, but more where the chunks of fronts would be
+// more than run at a time.  Fronts come first: they are the long ones, and what the beams have of their own fills the end.
+// (Each workgroup for itself, as restkv_attend has it, looks at all beams of all groups: 256 groups of four beams 472 us in place of 312.)
+__global__ __launch_bounds__(1024) void k_beams_list(AttendArgs a, int at_a_time) {
+  __shared__ long long s_sum[16];
+  __shared__ int s_count[16];
+  const Pages& pg = a.pg;
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, heads = a.per_head ? pg.Hkv : 1;
+  // tiles that a group (and head) shares: `seg` lanes each, one a beam
+  const int seg = 1 << (32 - __clz(a.n_beams - 1)), b = tid & (seg - 1);
+  long long cost = 0;
+  auto cost_of = [&](int tiles, int blocks) { return tiles ? (long long)((tiles + a.c_min - 1) / a.c_min + PART_ROUNDS) * blocks : 0; };
+  for (int base = 0; base < a.fronts; base += 1024 / seg) {
+    const int x = base + tid / seg, y = min(x, a.fronts - 1), g = y / heads, h = y - g * heads, s = g * a.n_beams + min(b, a.n_beams - 1);
+    const int told = told_len(pg, s, h), n = new_rows(pg, s).n;
+    int least = !n ? 0x7FFFFFFF : pg.causal ? max(told - n, 0) : told;
+    for (int d = 1; d < seg; d <<= 1) least = min(least, __shfl_xor(least, d));
+    const int shared = (int)min((int64_t)max(a.shared[g], 0) << pg.lg_ps, (int64_t)pg.max_len);
+    const int tiles = least == 0x7FFFFFFF ? 0 : min(shared, least) / ATT_TILE;
+    if (x >= a.fronts || b >= a.n_beams) continue;
+    if (b == 0) {
+      a.front_tiles_of[x] = tiles;
+      cost += cost_of(tiles, a.front_blocks);
+    }
+    if (n) cost += cost_of((min(told, pg.max_len) + ATT_TILE - 1) / ATT_TILE - tiles, a.own_blocks);
+  }
+  cost = block_sum(cost, s_sum);       // (and front_tiles_of is there for the whole workgroup)
+  long long rounds = max((cost + at_a_time - 1) / at_a_time, 1ll);
+  for (int i = 0; i < 16 && (int64_t)a.fronts * a.front_blocks < at_a_time; ++i) {
+    int chunks = 0;
+    for (int x = tid; x < a.fronts; x += 1024) chunks += (int)((a.front_tiles_of[x] + rounds * a.c_min - 1) / (rounds * a.c_min)) * a.front_blocks;
+    if (block_sum(chunks, s_count) <= at_a_time) break;
+    rounds += rounds / 16 + 1;
+  }
+  const int C = (int)min((long long)1 << 25, rounds * a.c_min);
+  auto list = [&](bool front) {
+    const int count = front ? a.fronts : a.entries - a.fronts, blocks = front ? a.front_blocks : a.own_blocks;
+    int2* const plan = a.plan + (front ? 0 : (int64_t)a.fronts * a.front_blocks);
+    int4* const to = a.list + (front ? 0 : 2 * (int64_t)a.front_chunks);
+    int run = 0;
+    for (int base = 0; base < count; base += 1024) {
+      const int x = base + tid;
+      int cnt = 0, tiles = 0, tile0 = 0, told = 0;
+      NewRows nr = {0, a.n_beams * pg.max_new};
+      if (x < count) {
+        const int s = a.per_head ? x / pg.Hkv : x, h = a.per_head ? x - s * pg.Hkv : 0;
+        tiles = a.front_tiles_of[front ? x : s / a.n_beams * heads + h];
+        told = tiles * ATT_TILE;
+        if (!front) {
+          tile0 = tiles;
+          told = told_len(pg, s, h);
+          nr = new_rows(pg, s);
+          tiles = nr.n ? (min(told, pg.max_len) + ATT_TILE - 1) / ATT_TILE - tile0 : 0;
+        }
+        cnt = (tiles + C - 1) / C;
+      }
+      const int inc = wave_scan(cnt);
+      __syncthreads();
+      if (lane == 63) s_count[wv] = inc;
+      __syncthreads();
+      int from = run + inc - cnt;
+      for (int w = 0; w < 16; ++w) {
+        from += w < wv ? s_count[w] : 0;
+        run += s_count[w];
+      }
+      if (x >= count) continue;
+      for (int rb = 0; rb < blocks; ++rb) {
+        const int slot = from + (front ? rb * a.front_slots : 0);
+        plan[(int64_t)x * blocks + rb] = cnt ? make_int2(slot, slot + cnt - 1) : make_int2(1, 0);
+      }
+      const int each = cnt > 1 ? (tiles + cnt - 1) / cnt : tiles;
+      for (int i = 0; i < cnt; ++i) {
+        const int t0 = min(i * each, tiles), u = from + i;
+        to[2 * u] = make_int4(front ? x : a.fronts + x, tile0 + t0, tile0 + min(t0 + each, tiles), u);
+        to[2 * u + 1] = make_int4(told, nr.first, nr.n, 0);
+      }
+    }
+    for (int u = run + tid; u < (front ? a.front_chunks : a.own_chunks); u += 1024) to[2 * u] = make_int4(-1, 0, 0, 0);
+  };
+  list(true);
+  list(false);
+}
+
+struct BeamsPlan { int many, R, front_rows, own_rows, c_min, target, spread, coarse; int64_t front_blocks, own_blocks, fronts, entries, parts, Hy, groups, at_a_time, slots, front_slots; };
 BeamsPlan beams_plan(const Pages& pg, int n_beams) {
-  BeamsPlan p;
+  BeamsPlan p = {};
   const int64_t rows = (int64_t)pg.G * pg.max_new;
   const bool wide_q = pg.fmt == RESTKV_Q4 && pg.dtype == RESTKV_F32 && pg.d == 128;      // (see attend_plan)
   p.many = pg.fmt == RESTKV_BF16 && rows * n_beams > 32;
@@ -58,20 +158,23 @@ BeamsPlan beams_plan(const Pages& pg, int n_beams) {
     // (what 64 parts cost has to be below 2^32)
     while (((pg.max_len / ATT_TILE >> p.coarse) + 4) * 2 * 64 * p.front_blocks > (int64_t)1 << 31) ++p.coarse;
   } else {
-    const int64_t tiles = (pg.max_len + ATT_TILE - 1) / ATT_TILE, each = p.Hy * std::max(p.front_blocks, p.own_blocks);
-    const int64_t more = std::min<int64_t>(p.target / each + 1, p.entries * ((tiles + p.c_min - 1) / p.c_min));
-    p.groups = p.slots = p.front_slots = p.entries + (each >= p.target || tiles <= p.c_min ? 0 : more);
+    // chunks: one for each entry with tiles, and as many more as make up what runs at a time
+    p.at_a_time = std::max<int64_t>(1, p.target / p.Hy);
+    p.front_slots = p.fronts + p.at_a_time / p.front_blocks;
+    p.slots = p.entries - p.fronts + p.at_a_time / p.own_blocks;
   }
   return p;
 }
 
-struct BeamsWs { size_t plan, m, l, o, fm, fl, fo, bytes; };
+struct BeamsWs { size_t plan, list, tiles, m, l, o, fm, fl, fo, bytes; };
 BeamsWs beams_ws(const Pages& pg, const BeamsPlan& p) {
   BeamsWs w = {};
   auto take = [&](size_t bytes) { size_t o = w.bytes; w.bytes = align_up(w.bytes + bytes); return o; };
   const size_t rows = (size_t)p.slots * p.Hy * pg.G * pg.max_new;
   const size_t front = (size_t)p.front_slots * p.front_blocks * p.Hy * p.front_rows;
   w.plan = take((size_t)p.parts * 8);
+  w.list = take(p.spread ? 0 : (size_t)(p.front_slots + p.slots) * 32);
+  w.tiles = take(p.spread ? 0 : (size_t)p.fronts * 4);
   w.m = take(rows * 4);
   w.l = take(rows * 4);
   w.o = take(rows * pg.d * 4);
@@ -104,9 +207,11 @@ int launch_attend_beams(const Pages& pg, int n_beams, const int32_t* shared, con
   if (as_if_alone(pg, n_beams)) return launch_attend(pg, q, k_pages, v_pages, k_scale, v_scale, out, lse, ws, st);
   const BeamsPlan p = beams_plan(pg, n_beams);
   const BeamsWs lay = beams_ws(pg, p);
-  if (p.groups * p.Hy > (int64_t)1 << 30 || p.front_slots * p.front_blocks > (int64_t)1 << 30 || std::max(p.front_blocks, p.own_blocks) > (1 << 20) || (int64_t)pg.max_new * pg.Hq >= (1 << 24)) return RESTKV_EUNSUPPORTED;
+  const int64_t ids = p.spread ? p.groups * p.Hy : (p.front_slots * p.Hy + 7) / 8 * 8 * p.front_blocks + (p.slots * p.Hy + 7) / 8 * 8 * p.own_blocks;
+  if (ids > (int64_t)1 << 30 || p.front_slots * p.front_blocks > (int64_t)1 << 30 || std::max(p.front_blocks, p.own_blocks) > (1 << 20) || (int64_t)pg.max_new * pg.Hq >= (1 << 24)) return RESTKV_EUNSUPPORTED;
   AttendArgs a = attend_args(pg, q, k_pages, v_pages, k_scale, v_scale, out, lse);
   a.plan = (int2*)(ws + lay.plan);
+  a.list = (int4*)(ws + lay.list); a.front_tiles_of = (int*)(ws + lay.tiles);
   a.part_m = (float*)(ws + lay.m); a.part_l = (float*)(ws + lay.l); a.part_o = (float*)(ws + lay.o);
   a.front_m = (float*)(ws + lay.fm); a.front_l = (float*)(ws + lay.fl); a.front_o = (float*)(ws + lay.fo);
   a.entries = (int)p.entries; a.Hy = (int)p.Hy;
@@ -115,8 +220,12 @@ int launch_attend_beams(const Pages& pg, int n_beams, const int32_t* shared, con
   a.front_rows = p.front_rows; a.own_rows = p.own_rows;
   a.part_cost = p.many ? 4 : 3; a.front_tiles = p.many ? 1 : p.c_min; a.coarse = p.coarse;
   a.first_more = 0.1f;
-  a.row_blocks = (int)(p.spread ? p.front_blocks : std::max(p.front_blocks, p.own_blocks)); a.units = (int)(p.groups * p.Hy); a.c_min = p.c_min;
-  a.chunks = p.spread ? (float)p.groups : (float)((double)p.target / (double)(p.Hy * std::max(p.front_blocks, p.own_blocks)) * (1 - 0x1p-23));
+  a.row_blocks = (int)(p.spread ? p.front_blocks : 1); a.units = (int)ids; a.c_min = p.c_min;
+  a.chunks = (float)p.groups;
+  if (!p.spread) {
+    a.front_chunks = (int)p.front_slots; a.own_chunks = (int)p.slots;
+    hipLaunchKernelGGL(k_beams_list, dim3(1), dim3(1024), 0, st, a, (int)p.at_a_time);
+  }
   const int rc = p.many ? run_attend_beams_rows(a, st) : pg.fmt == RESTKV_F32 ? run_attend_beams_f32(a, p.R, st) : pg.fmt == RESTKV_BF16 ? run_attend_beams_bf16(a, p.R, st) : run_attend_beams_q4(a, p.R, st);
   if (rc) return rc;
   const dim3 grid(pg.max_new * pg.Hq, pg.n_seqs);

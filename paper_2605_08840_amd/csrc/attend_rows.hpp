@@ -28,12 +28,13 @@ void k_attend_rows(AttendArgs a) {
 
   const int unit = unit_of_block();
   int rb = blockIdx.x >> 3, slot = 0;
-  if (unit >= a.units) return;
-  const int hy = unit % a.Hy;
+  if (!BEAMS && unit >= a.units) return;
+  int hy = BEAMS ? 0 : unit % a.Hy;
   Chunk ch;
   BeamsWork work;
   if constexpr (BEAMS) {
-    if (!beams_work<NW>(a, unit, rb, (int*)lds, work)) return;
+    if (!beams_work(a, work)) return;
+    hy = work.hy;
   } else {
     if (!find_chunk<NW>(a, unit / a.Hy, (int*)lds, ch)) return;
   }
