@@ -260,46 +260,56 @@ __device__ __forceinline__ void store_out(const AttendArgs& a, int64_t t, int64_
 // hold) and a launch: chunks are read four at a time, references with the sums.  3.6 to 5 us for decoding steps, 8.3 for the 33 MB of
 // 256 queries a KV head.
 struct Part { const float *m, *l, *o; };
-template <int D, typename F>
-__device__ __forceinline__ void join_chunks(const AttendArgs& a, int count, int64_t t, int head, F part) {
-  constexpr int TPR = D / 4, NGR = 256 / TPR, AHEAD = 4;
-  __shared__ float4 sm_x[NGR][TPR];
-  __shared__ float sm_m[NGR], sm_l[NGR];
-  const int g = threadIdx.x / TPR, c = threadIdx.x % TPR;
+struct Sums {
   float M = -INFINITY, L = 0.f;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto take = [&](float m, float l, float4 y) {
+  __device__ __forceinline__ void take(float m, float l, float4 y) {
     // (a chunk of which the row sees nothing has a reference of -inf and sums of 0)
     const float n = fmaxf(M, m);
     const float fo = M == n ? 1.f : __builtin_amdgcn_exp2f(M - n), fn = m == n ? 1.f : __builtin_amdgcn_exp2f(m - n);
     M = n;
     L = L * fo + l * fn;
     x.x = x.x * fo + y.x * fn; x.y = x.y * fo + y.y * fn; x.z = x.z * fo + y.z * fn; x.w = x.w * fo + y.w * fn;
-  };
-  for (int k = g; k < count; k += NGR * AHEAD) {
+  }
+};
+// Channels c to c + 3 of every `step`-th chunk from the first'th on, four chunks at a time.
+template <typename F>
+__device__ __forceinline__ Sums sum_chunks(int first, int step, int count, int c, F part) {
+  constexpr int AHEAD = 4;
+  Sums s;
+  for (int k = first; k < count; k += step * AHEAD) {
     float m[AHEAD], l[AHEAD];
     float4 y[AHEAD];
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
-      const Part p = part(min(k + u * NGR, count - 1));
+      const Part p = part(min(k + u * step, count - 1));
       m[u] = *p.m;
       l[u] = *p.l;
-      y[u] = *(const float4*)(p.o + c * 4);
+      y[u] = *(const float4*)(p.o + c);
     }
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
-      if (k + u * NGR < count) take(m[u], l[u], y[u]);
+      if (k + u * step < count) s.take(m[u], l[u], y[u]);
   }
-  sm_x[g][c] = x;
+  return s;
+}
+template <int D, typename F>
+__device__ __forceinline__ void join_chunks(const AttendArgs& a, int count, int64_t t, int head, F part) {
+  constexpr int TPR = D / 4, NGR = 256 / TPR;
+  __shared__ float4 sm_x[NGR][TPR];
+  __shared__ float sm_m[NGR], sm_l[NGR];
+  const int g = threadIdx.x / TPR, c = threadIdx.x % TPR;
+  Sums s = sum_chunks(g, NGR, count, c * 4, part);
+  sm_x[g][c] = s.x;
   if (c == 0) {
-    sm_m[g] = M;
-    sm_l[g] = L;
+    sm_m[g] = s.M;
+    sm_l[g] = s.L;
   }
   __syncthreads();
   if (g) return;
 #pragma unroll
-  for (int k = 1; k < NGR; ++k) take(sm_m[k], sm_l[k], sm_x[k][c]);
-  store_out(a, t, head, c * 4, x, M, L);
+  for (int k = 1; k < NGR; ++k) s.take(sm_m[k], sm_l[k], sm_x[k][c]);
+  store_out(a, t, head, c * 4, s.x, s.M, s.L);
 }
 
 enum { FMT_F32, FMT_BF16, FMT_Q4 };

@@ -12,28 +12,66 @@ namespace restkv {
 
 namespace {
 
-template <int D>
-__global__ __launch_bounds__(256) void k_beams_join(AttendArgs a) {
-  const Pages& pg = a.pg;
-  const int i = blockIdx.x / pg.Hq, head = blockIdx.x % pg.Hq, h = head / pg.G, s = blockIdx.y, g = s / a.n_beams;
-  const int hy = a.per_head ? 0 : h, row = i * pg.G + head - h * pg.G, rows = pg.G * pg.max_new;
-  const int of_group = (s - g * a.n_beams) * rows + row, rb = of_group / a.front_rows;
-  const int2 pf = a.plan[(a.per_head ? g * pg.Hkv + h : g) * a.front_blocks + rb];
-  const int2 pl = a.plan[a.fronts * a.front_blocks + (a.per_head ? s * pg.Hkv + h : s) * a.own_blocks + row / a.own_rows];
-  const NewRows nr = new_rows(pg, s);
-  if (i >= nr.n) return;
-  const int n = pf.y - pf.x + 1;
-  join_chunks<D>(a, n + pl.y - pl.x + 1, nr.first + i, head, [&](int k) {
+// Where the chunks of a row are (new token i, query head `head` of sequence s).
+struct RowParts {
+  const AttendArgs& a;
+  int n, count, of_group, row, first, own;       // chunks of the front, and of both
+  int hy, rb;
+  __device__ __forceinline__ RowParts(const AttendArgs& a, int s, int i, int head) : a(a) {
+    const Pages& pg = a.pg;
+    const int h = head / pg.G, g = s / a.n_beams, rows = pg.G * pg.max_new;
+    hy = a.per_head ? 0 : h;
+    row = i * pg.G + head - h * pg.G;
+    of_group = (s - g * a.n_beams) * rows + row;
+    rb = of_group / a.front_rows;
+    const int2 pf = a.plan[(int64_t)(a.per_head ? g * pg.Hkv + h : g) * a.front_blocks + rb];
+    const int2 pl = a.plan[(int64_t)a.fronts * a.front_blocks + (int64_t)(a.per_head ? s * pg.Hkv + h : s) * a.own_blocks + row / a.own_rows];
+    n = pf.y - pf.x + 1;
+    count = n + pl.y - pl.x + 1;
+    first = pf.x;
+    own = pl.x;
+  }
+  template <int D>
+  __device__ __forceinline__ Part at(int k) const {
     const bool front = k < n;
-    const int64_t slot = (int64_t)(front ? pf.x + k : pl.x + k - n) * a.Hy + hy;
-    const int64_t at = front ? slot * a.front_rows + (of_group - rb * a.front_rows) : slot * rows + row;
-    return Part{(front ? a.front_m : a.part_m) + at, (front ? a.front_l : a.part_l) + at, (front ? a.front_o : a.part_o) + at * D};
-  });
+    const int64_t slot = (int64_t)(front ? first + k : own + k - n) * a.Hy + hy;
+    const int64_t at = front ? slot * a.front_rows + (of_group - rb * a.front_rows) : slot * (a.pg.G * a.pg.max_new) + row;
+    return {(front ? a.front_m : a.part_m) + at, (front ? a.front_l : a.part_l) + at, (front ? a.front_o : a.part_o) + at * D};
+  }
+};
+
+// A workgroup a row; or (ALONE, where there are many) as many rows as it has groups of d / 4 threads, each joined by one of these if
+// none has many chunks.  256 groups of four beams, 32 heads of 128: 50 -> 19 us.
+template <int D, bool ALONE>
+__global__ __launch_bounds__(256) void k_beams_join(AttendArgs a) {
+  constexpr int TPR = D / 4, NGR = 256 / TPR, FEW = 8;
+  const Pages& pg = a.pg;
+  const int s = blockIdx.y, all = pg.max_new * pg.Hq;
+  if constexpr (ALONE) {
+    const int x = min((int)blockIdx.x * NGR + (int)threadIdx.x / TPR, all - 1), c = threadIdx.x % TPR * 4;
+    const RowParts p(a, s, x / pg.Hq, x % pg.Hq);
+    const NewRows nr = new_rows(pg, s);
+    const bool there = (int)blockIdx.x * NGR + (int)threadIdx.x / TPR < all && x / pg.Hq < nr.n;
+    if (!__syncthreads_or(there && p.count > FEW)) {
+      if (!there) return;
+      const Sums sums = sum_chunks(0, 1, p.count, c, [&](int k) { return p.at<D>(k); });
+      store_out(a, nr.first + x / pg.Hq, x % pg.Hq, c, sums.x, sums.M, sums.L);
+      return;
+    }
+  }
+  for (int x = blockIdx.x * (ALONE ? NGR : 1), end = ALONE ? min(x + NGR, all) : x + 1; x < end; ++x) {
+    const int i = x / pg.Hq, head = x % pg.Hq;
+    const RowParts p(a, s, i, head);
+    const NewRows nr = new_rows(pg, s);
+    if (i >= nr.n) return;
+    join_chunks<D>(a, p.count, nr.first + i, head, [&](int k) { return p.at<D>(k); });
+    if (ALONE) __syncthreads();
+  }
 }
 
 constexpr int PART_ROUNDS = 2;         // what a part's beginning and end take, in rounds
 
-// Sum over the 1024 threads; lds: 16 words, free to be written.
+// Sum over the workgroup; lds: 16 words, free to be written.
 template <typename V>
 __device__ __forceinline__ V block_sum(V x, V* lds) {
 #pragma unroll
@@ -42,8 +80,7 @@ __device__ __forceinline__ V block_sum(V x, V* lds) {
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
   __syncthreads();
   x = lds[0];
-#pragma unroll
-  for (int w = 1; w < 16; ++w) x += lds[w];
+  for (int w = 1; w < (int)blockDim.x / 64; ++w) x += lds[w];
   return x;
 }
 
@@ -55,12 +92,12 @@ __global__ __launch_bounds__(1024) void k_beams_list(AttendArgs a, int at_a_time
   __shared__ long long s_sum[16];
   __shared__ int s_count[16];
   const Pages& pg = a.pg;
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, heads = a.per_head ? pg.Hkv : 1;
+  const int tid = threadIdx.x, T = blockDim.x, lane = tid & 63, wv = tid >> 6, heads = a.per_head ? pg.Hkv : 1;
   // tiles that a group (and head) shares: `seg` lanes each, one a beam
   const int seg = 1 << (32 - __clz(a.n_beams - 1)), b = tid & (seg - 1);
   long long cost = 0;
   auto cost_of = [&](int tiles, int blocks) { return tiles ? (long long)((tiles + a.c_min - 1) / a.c_min + PART_ROUNDS) * blocks : 0; };
-  for (int base = 0; base < a.fronts; base += 1024 / seg) {
+  for (int base = 0; base < a.fronts; base += T / seg) {
     const int x = base + tid / seg, y = min(x, a.fronts - 1), g = y / heads, h = y - g * heads, s = g * a.n_beams + min(b, a.n_beams - 1);
     const int told = told_len(pg, s, h), n = new_rows(pg, s).n;
     int least = !n ? 0x7FFFFFFF : pg.causal ? max(told - n, 0) : told;
@@ -78,7 +115,7 @@ __global__ __launch_bounds__(1024) void k_beams_list(AttendArgs a, int at_a_time
   long long rounds = max((cost + at_a_time - 1) / at_a_time, 1ll);
   for (int i = 0; i < 16 && (int64_t)a.fronts * a.front_blocks < at_a_time; ++i) {
     int chunks = 0;
-    for (int x = tid; x < a.fronts; x += 1024) chunks += (int)((a.front_tiles_of[x] + rounds * a.c_min - 1) / (rounds * a.c_min)) * a.front_blocks;
+    for (int x = tid; x < a.fronts; x += T) chunks += (int)((a.front_tiles_of[x] + rounds * a.c_min - 1) / (rounds * a.c_min)) * a.front_blocks;
     if (block_sum(chunks, s_count) <= at_a_time) break;
     rounds += rounds / 16 + 1;
   }
@@ -88,7 +125,7 @@ __global__ __launch_bounds__(1024) void k_beams_list(AttendArgs a, int at_a_time
     int2* const plan = a.plan + (front ? 0 : (int64_t)a.fronts * a.front_blocks);
     int4* const to = a.list + (front ? 0 : 2 * (int64_t)a.front_chunks);
     int run = 0;
-    for (int base = 0; base < count; base += 1024) {
+    for (int base = 0; base < count; base += T) {
       const int x = base + tid;
       int cnt = 0, tiles = 0, tile0 = 0, told = 0;
       NewRows nr = {0, a.n_beams * pg.max_new};
@@ -109,7 +146,7 @@ __global__ __launch_bounds__(1024) void k_beams_list(AttendArgs a, int at_a_time
       if (lane == 63) s_count[wv] = inc;
       __syncthreads();
       int from = run + inc - cnt;
-      for (int w = 0; w < 16; ++w) {
+      for (int w = 0; w < T / 64; ++w) {
         from += w < wv ? s_count[w] : 0;
         run += s_count[w];
       }
@@ -125,7 +162,7 @@ __global__ __launch_bounds__(1024) void k_beams_list(AttendArgs a, int at_a_time
         to[2 * u + 1] = make_int4(told, nr.first, nr.n, 0);
       }
     }
-    for (int u = run + tid; u < (front ? a.front_chunks : a.own_chunks); u += 1024) to[2 * u] = make_int4(-1, 0, 0, 0);
+    for (int u = run + tid; u < (front ? a.front_chunks : a.own_chunks); u += T) to[2 * u] = make_int4(-1, 0, 0, 0);
   };
   list(true);
   list(false);
@@ -224,13 +261,17 @@ int launch_attend_beams(const Pages& pg, int n_beams, const int32_t* shared, con
   a.chunks = (float)p.groups;
   if (!p.spread) {
     a.front_chunks = (int)p.front_slots; a.own_chunks = (int)p.slots;
-    hipLaunchKernelGGL(k_beams_list, dim3(1), dim3(1024), 0, st, a, (int)p.at_a_time);
+    // (lanes for every beam of every group)
+    const int64_t lanes = p.fronts << (32 - __builtin_clz(n_beams - 1)), threads = std::min<int64_t>(1024, (std::max(lanes, p.entries - p.fronts) + 63) / 64 * 64);
+    hipLaunchKernelGGL(k_beams_list, dim3(1), dim3(threads), 0, st, a, (int)p.at_a_time);
   }
   const int rc = p.many ? run_attend_beams_rows(a, st) : pg.fmt == RESTKV_F32 ? run_attend_beams_f32(a, p.R, st) : pg.fmt == RESTKV_BF16 ? run_attend_beams_bf16(a, p.R, st) : run_attend_beams_q4(a, p.R, st);
   if (rc) return rc;
-  const dim3 grid(pg.max_new * pg.Hq, pg.n_seqs);
-  if (pg.d == 128) hipLaunchKernelGGL(k_beams_join<128>, grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(k_beams_join<64>, grid, dim3(256), 0, st, a);
+  const int each = p.spread ? 1 : 1024 / pg.d;
+  const dim3 grid((pg.max_new * pg.Hq + each - 1) / each, pg.n_seqs);
+  auto join = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, a); };
+  if (pg.d == 128) p.spread ? join(k_beams_join<128, false>) : join(k_beams_join<128, true>);
+  else p.spread ? join(k_beams_join<64, false>) : join(k_beams_join<64, true>);
   return hip_status();
 }
 
