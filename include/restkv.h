@@ -404,16 +404,16 @@ typedef struct restkv_beams {
  * The best continuations of each request's beams.  With logits x[b, v] and the score c[b] that beam b has so far,
  *     score(b, v) = c[b] + (x[b, v] - m_b) - ln(sum over v' of exp(x[b, v'] - m_b)),   m_b the largest logit of b,
  * and a beam that has ended has one continuation, (b, end_token) of score c[b].  The n_out largest are taken; of equal
- * scores the lower beam's is the larger, then the one of the larger logit, then the lower token's.  Only finite scores are
- * taken: a logit of -inf (a token that is masked out) is none, a beam with a score that is not finite has none, nor has one
+ * scores the lower beam's is the larger, then the one of the larger logit, then the lower token's.  Only scores that are
+ * finite as float32 are taken: a logit of -inf (a token that is masked out) is none, a beam with a score that is not finite has none, nor has one
  * with a NaN or +inf among its logits.  Places that are left get -inf, -1, -1 and 1.
  *   logits   [n_groups * n_beams, n_vocab] dtype (logit_stride), any alignment of that type
  *   scores   [n_groups, n_beams] float32;  finished [n_groups, n_beams] int32 (nonzero: ended) or NULL
  *   new_scores [n_groups, n_out] float32, parents (the beam, 0 .. n_beams-1), tokens [n_groups, n_out] int32 out, best first
  *   new_finished [n_groups, n_out] int32 out, may be NULL: 1 where the token is end_token or the beam had ended
  * new_scores may be scores, and new_finished may be finished, if n_out = n_beams.
- * Exponentials and their sums over up to 2048 neighbouring logits are float32 (sums of these, logarithms and scores 64 bits);
- * scores are ordered in 64 bits and rounded once.  Results do not depend on timing: no atomics.
+ * Exponentials are float32, and summed in float32 up to 32 at a time (sums of these, logarithms and scores 64 bits); scores are ordered
+ * in 64 bits and rounded once.  Results do not depend on timing: no atomics.
  * Workspace: restkv_beam_workspace_bytes(b), 256-byte aligned, whatever it holds; calls that run at the same time need one each.
  */
 size_t restkv_beam_workspace_bytes(const restkv_beams* b);
@@ -432,7 +432,8 @@ int restkv_beam_select(const restkv_beams* b, const void* logits, const float* s
  * A column is full if every KV head that shares the table has filled its page, and open from there to the last page in use.  In
  * an open column the pages of the parents go to one child each (the parent itself where it is its own child, else its first
  * child), those of beams without a child to the other children, in order of the beams; into these the rows in use are
- * copied.  Columns behind the open ones stay as they are.  So no page is lost or doubled, and a step needs none.
+ * copied.  Columns behind the open ones stay as they are.  So in columns that are, or will be, written to no page is lost or doubled,
+ * and a step needs none.  (In a full column the pages of beams that nobody goes on from are in no table any more.)
  * In open columns the beams of a group must have pages that differ.  An entry outside [0, n_pages) is dealt like any, and no row
  * of it is read or written.  Rows behind the lengths are left as they were.
  */
@@ -446,8 +447,8 @@ int restkv_beam_reorder(const restkv_cache* c, int32_t n_beams, const int32_t* p
  *   shared [n_seqs / n_beams] int32: so many table entries in front are the same for all sequences of the group (of each KV
  *          head, with tables per head).  Values below 0 count as 0; pages beyond what every beam of the group with new tokens
  *          has seen before them are each beam's own.
- * Everything else, the result too, as restkv_attend says (n_beams 1 .. 64); where the tables differ after all, the first beam's
- * pages count for the others.  Workspace: restkv_attend_beams_workspace_bytes(c, n_beams).
+ * Everything else, the result too, as restkv_attend says (n_beams 1 .. 64).  Where the tables differ after all, a beam sees its own
+ * pages there or the first beam's, by sizes.  Workspace: restkv_attend_beams_workspace_bytes(c, n_beams).
  */
 size_t restkv_attend_beams_workspace_bytes(const restkv_cache* c, int32_t n_beams);
 int restkv_attend_beams(const restkv_cache* c, int32_t n_beams, const int32_t* shared, const void* q, const void* k_pages,

@@ -370,7 +370,8 @@ __device__ __forceinline__ bool over(const Cont& x, const Cont& y) {
 }
 __device__ __forceinline__ Cont higher(const Cont& x, const Cont& y) { return over(x, y) ? x : y; }
 __device__ __forceinline__ Cont cont_of(double score, int beam, unsigned long long key) {
-  if (!(score - score == 0.0)) return {0, 0};                // (only finite scores)
+  const float f = (float)score;
+  if (!(f - f == 0.f)) return {0, 0};                        // (only finite scores, as they are given out)
   const long long b = __double_as_longlong(score + 0.0);     // (-0 counts as 0)
   return {(unsigned long long)(b < 0 ? ~b : b | (long long)(1ull << 63)),
           (unsigned long long)(63 - beam) << 56 | (key >> 32) << 24 | (key & 0xFFFFFFu)};

@@ -26,7 +26,7 @@ def select(logits, scores, finished, n_out, end):
             x = logits[g, b].double()
             m = x.max()
             s = c + ((x - m) - torch.log(torch.exp(x - m).sum()))
-            v = torch.nonzero(torch.isfinite(s))[:, 0]
+            v = torch.nonzero(torch.isfinite(s.float()))[:, 0]     # (finite as they are given out)
             if len(v) > n_out + 1:                             # (more cannot be taken: ties with the last one kept)
                 v = v[s[v] >= s[v].topk(n_out + 1)[0][-1]]
             every += [(-float(s[i]), b, -float(x[i]), int(i)) for i in v]

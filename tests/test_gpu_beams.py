@@ -129,6 +129,50 @@ def test_select_masks_and_unusual_values(dtype):
     check_select(x, first, None, 8)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_select_scores_that_float32_does_not_hold(dtype):
+    """Logits so far apart that a score is finite in 64 bits, and none as it is given out: such a token is not taken."""
+    low, top = torch.finfo(dtype).min, torch.finfo(dtype).max
+    x = torch.full((4, 100), low, dtype=dtype)
+    x[0, 5], x[1, 50], x[2, 7], x[3, 99] = top, top / 2, 0.0, top
+    scores = torch.tensor([[0.0, -1.0], [-2.0, -3e38]])
+    got = check_select(x, scores, None, 6)
+    assert got[2][0].tolist() == [5, 50, -1, -1, -1, -1] and got[1][0].tolist() == [0, 1, -1, -1, -1, -1]
+
+
+def test_select_largest_vocabulary_and_two_calls_at_once():
+    vocab = 1 << 24
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn((3, vocab), generator=g, device="cuda").bfloat16()
+    x[2, vocab - 1] = 40.0
+    check_select(x[:1], torch.zeros((1, 1)), None, 64)
+    got = check_select(x[1:], torch.tensor([[-0.5, -0.25]]), None, 64, end=vocab - 1)
+    assert got[2][0, 0] == vocab - 1 and got[3][0, 0] == 1
+    rows = [torch.randn((8, 5000), generator=g, device="cuda") for _ in range(2)]
+    scores = -torch.rand((2, 4), generator=torch.Generator().manual_seed(1))
+    want = [run_select(r, scores, None, 16) for r in rows]
+    b = rk.make_beams(n_groups=2, n_beams=4, n_vocab=5000, n_out=16, dtype="f32", end_token=2)
+    streams, outs = [torch.cuda.Stream() for _ in rows], []
+    for _ in rows:
+        outs.append((torch.empty((2, 16), device="cuda"), *(torch.empty((2, 16), dtype=torch.int32, device="cuda") for _ in range(2)),
+                     rk.alloc_beam_workspace(b)))
+    sc = scores.cuda()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for r, s, o in zip(rows, streams, outs):
+            rk.restkv_beam_select(b, r, sc, *o, stream=s)
+    torch.cuda.synchronize()
+    for o, w in zip(outs, want):
+        assert all(torch.equal(x.cpu(), y) for x, y in zip(o[:3], w))
+
+
+def test_select_of_no_groups():
+    b = rk.make_beams(n_groups=0, n_beams=4, n_vocab=50, dtype="f32")
+    f, i = torch.empty((0, 4), device="cuda"), torch.empty((0, 4), dtype=torch.int32, device="cuda")
+    rk.restkv_beam_select(b, torch.empty((0, 50), device="cuda"), f, f.clone(), i, i.clone(), rk.alloc_beam_workspace(b))
+    torch.cuda.synchronize()
+
+
 def test_select_in_place_and_on_another_stream():
     g = torch.Generator().manual_seed(5)
     x, scores = torch.randn((12, 3001), generator=g), -torch.rand((3, 4), generator=g)
@@ -232,6 +276,7 @@ REORDERS = [
     ([[5, 40], [33, 20], [16, 16]], 4, [[0, 0, 0, 0], [3, 3, 1, 1], [1, 0, 0, 2]], dict(head_lens=True, room=1)),
     ([[50, 0, 3], [17, 32, 90]], 3, [[1, 1, 1], [2, 2, 0]], dict(hq=6, hkv=3, d=128, head_lens=True)),
     ([[50, 0, 3], [17, 32, 90]], 3, [[1, 1, 1], [2, 2, 0]], dict(hq=3, hkv=3, head_lens=True, head_tables=True, room=1)),
+    ([[50, 50, 50], [17, 17, 17]], 3, [[1, 1, 1], [2, 2, 0]], dict(hq=3, hkv=3, head_tables=True, room=1)),
     ([37], 64, [[(7 * b) % 11 for b in range(64)]], dict(hkv=1, hq=1)),
     ([200], 2, [[0, 0]], dict(max_len=150, ps=64)),                                            # longer than the room
     ([90, 3], 2, [[1, 1], [0, 0]], dict(hkv=8, hq=8, d=128, ps=64)),
@@ -353,12 +398,18 @@ ATTENDS = [
     ([150, 170], [40, 60], 2, [9], dict(hq=6, hkv=2, causal=False)),
     ([[90, 240], [95, 250], [333, 20], [340, 30]], [1] * 4, 2, [5, 20], dict(head_lens=True)),
     ([[90, 40, 300], [99, 45, 310]], [1, 2], 2, [17], dict(hq=6, hkv=3, d=128, head_lens=True, head_tables=True)),
+    ([90, 140, 130], [1, 2, 1], 3, [5], dict(hq=6, hkv=3, head_tables=True)),
     ([200, 220], [1, 1], 2, [12], dict(scale=0.31, max_len=150)),                       # longer than the room
     ([200, 260], [90, 20], 2, [6], dict(max_new=33, room=3)),                           # the first 33 of 90
     ([170, 200], [2, 2], 2, [-3], dict(extra_tokens=3)),                                # a count below 0
     ([300] * 2, [1] * 2, 2, [2 ** 31 - 1], dict(d=128)),
     ([100] * 140, [1] * 140, 2, [6] * 70, dict(hq=2, hkv=1)),                           # more groups than lanes
     ([130] * 40, [1] * 40, 4, [8] * 10, dict(hq=4, hkv=4, d=128)),
+    ([90 + 7 * i for i in range(96)], [i % 3 for i in range(96)], 3, [i % 9 for i in range(32)], dict(hq=6, hkv=2)),     # lengths that differ
+    ([[90 + i, 300 - 3 * i] for i in range(40)], [1] * 40, 5, [5, 0, 9, 3, 1, 2, 4, 8], dict(head_lens=True, head_tables=True)),
+    ([260 + i for i in range(66)], [1] * 66, 33, [16, 12], dict(hq=8, hkv=2, d=128)),                                    # 132 rows
+    ([200, 290] * 20, [20, 31] * 20, 2, [8] * 20, dict(hq=4, hkv=2)),                                                    # blocks of rows of both kinds
+    ([900] * 3 + [5] * 66, [1] * 69, 3, [50] + [0] * 22, dict(hq=4, hkv=2)),                                             # one long group among short ones
 ]
 
 
@@ -413,6 +464,66 @@ def test_attend_beams_long(dtype, fmt, out, shared_once):
         tol = 2 * half * want.abs().float() + 2 * 6 * (300 * 2.0 ** -24 + (2.0 ** -17 if out_type == torch.bfloat16 else 2.0 ** -24))
         assert ((got.float() - want.float()).abs() <= tol).all(), ((got.float() - want.float()).abs() - tol).max().item()
         assert ((l1 - l2).abs() <= 2 * 300 * 2.0 ** -24 + 2.0 ** -23 * l2.abs()).all()
+
+
+def long_case(fmt, n_beams, lens, width, ps, n_pages, hq, hkv, shared, d=64, seed=7):
+    """restkv_attend_beams beside restkv_attend over pages of 65536 positions or so, made on the GPU."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    c = rk.make_cache(n_seqs=len(lens), n_q_heads=hq, n_kv_heads=hkv, head_dim=d, page_size=ps, n_pages=n_pages, max_pages=width, dtype="bf16",
+                      format=fmt)
+    pages = rk.alloc_cache_pages(c)
+    for x in (pages.k, pages.v):
+        x.random_(0, 256, generator=g) if fmt else x.normal_(generator=g)
+    if fmt:
+        for x in (pages.k_scale, pages.v_scale):
+            x.copy_(torch.tensor([0.25, -2.0], dtype=torch.bfloat16))
+    table = torch.full((len(lens), width), -1, dtype=torch.int32)
+    free = list(range(n_pages - 1, -1, -1))
+    for s, n in enumerate(lens):
+        for i in range(-(-n // ps)):
+            first = s // n_beams * n_beams
+            table[s, i] = table[first, i] if s != first and i < shared[s // n_beams] else free.pop()
+    table, ln = table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda()
+    q = torch.randn((len(lens), hq, d), generator=g, device="cuda").bfloat16()
+    outs, lses = [torch.empty(q.shape, dtype=q.dtype, device="cuda") for _ in range(2)], [torch.empty(q.shape[:2], device="cuda") for _ in range(2)]
+    sh = torch.tensor(shared, dtype=torch.int32).cuda()
+    rk.restkv_attend_beams(c, n_beams, sh, q, pages, table, ln, outs[0], lses[0], rk.alloc_attend_beams_workspace(c, n_beams))
+    rk.restkv_attend(c, q, pages, table, ln, outs[1], lses[1], rk.alloc_attend_workspace(c))
+    a, b = (x.float() for x in outs)
+    # outputs of below 2^2 in size: half a step each, weights to 2^-17, sums of some thousand tiles to 2^-13 of values below 8 at the most
+    assert ((a - b).abs() <= 2.0 ** -7 * b.abs() + 2 * 8 * (2.0 ** -17 + 2.0 ** -13)).all(), (a - b).abs().max().item()
+    assert ((lses[0] - lses[1]).abs() <= 2 * 2.0 ** -13 + 2.0 ** -22 * lses[1].abs()).all()
+
+
+@pytest.mark.parametrize("fmt", [None, "q4"])
+def test_attend_beams_with_room_for_a_billion_positions(fmt, shared_once):
+    """Tables that could hold 2^30 positions: the work is cut by what is there."""
+    long_case(fmt, 2, [200001, 333333, 70, 65], 16384, 65536, 12, 4, 1, [2, 0])
+    long_case(fmt, 40, [140000 + 31 * i for i in range(40)], 16384, 65536, 44 + 41, 8, 1, [2])
+    long_case(fmt, 20, [70000] * 20 + [66000 + i for i in range(20)] + [3] * 20, 16384, 65536, 62 + 42, 2, 1, [1, 1, 0])
+
+
+@pytest.mark.parametrize("fmt", [None, "q4"])
+def test_beams_pages_that_pass_four_gigabytes(fmt, shared_once):
+    """The last pages of arrays of more than 2^32 bytes: attention over them, and rows copied between them."""
+    ps, d = 65536, 64
+    many = (1 << 32) // (ps * (d // 2 if fmt else 2 * d)) + 6
+    long_case(fmt, 2, [140000, 150000], 4, ps, many, 4, 1, [2])
+    c = rk.make_cache(n_seqs=2, n_q_heads=1, n_kv_heads=1, head_dim=d, page_size=ps, n_pages=many, max_pages=2, dtype="bf16", format=fmt)
+    pages = rk.alloc_cache_pages(c)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    every = [x for x in (pages.k, pages.v, pages.k_scale, pages.v_scale) if x is not None]
+    for x in every:
+        for at in (many - 1, many - 2, 0, 1):
+            x[at].random_(0, 100, generator=g) if x.dtype is torch.uint8 else x[at].normal_(generator=g)
+    before = [x[[many - 1, many - 2, 0, 1]].clone() for x in every]
+    table = torch.tensor([[0, many - 2], [1, many - 1]], dtype=torch.int32).cuda()
+    n = 65536 + 12345
+    rk.restkv_beam_reorder(c, 2, torch.tensor([[0, 0]], dtype=torch.int32).cuda(), table, torch.tensor([n, n], dtype=torch.int32).cuda(), [pages])
+    assert table.tolist() == [[0, many - 2], [0, many - 1]]
+    for x, b in zip(every, before):
+        b[0][:, :n - ps] = b[1][:, :n - ps]
+        assert torch.equal(x[[many - 1, many - 2, 0, 1]].view(torch.uint8), b.view(torch.uint8))
 
 
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
