@@ -419,12 +419,12 @@ __device__ __forceinline__ int front_token(const Pages& pg, int s, int tok) {
   return min(of.first + min(tok - b * pg.max_new, max(of.n - 1, 0)), pg.n_tokens - 1);
 }
 
-// What a workgroup of a launch for beams takes, one part after the other.
+// How a workgroup of a launch for beams comes by its work: parts cut evenly, one after the other, or one of a list.
+enum { NO_BEAMS, BEAMS_PARTS, BEAMS_LIST };
 struct BeamsWork {
   unsigned long long todo;       // parts (spread), or one
   int (*lds)[8];                 // of a part: positions, first row, new tokens, first and last tile of this workgroup (spread)
-  Chunk ch;
-  int u, hy, rb, team_rb, slot0;
+  int u, hy, team_rb, slot0;
 };
 // Parts (up to 64, a lane each; a front with all its blocks of rows is one) cut evenly: the rounds of all follow each other, with
 // a.part_cost half rounds more for each part, which is what its beginning and end take.  Workgroups come in teams of front_blocks.  Some teams take the fronts, one front each and all about as many rounds, each of a team's workgroups the same tiles for a block of rows
@@ -433,146 +433,141 @@ struct BeamsWork {
 // (What comes of it is in LDS, so that the loops between have the registers.)
 // Quotients of small whole numbers (below 2^15), where a division of 32 bits would take forty instructions.
 __device__ __forceinline__ int quotient(int x, float one_over) { return (int)(((float)x + 0.5f) * one_over); }
-__device__ __forceinline__ bool beams_work(const AttendArgs& a, BeamsWork& o) {
+__device__ __forceinline__ bool cut_parts(const AttendArgs& a, BeamsWork& o) {
   const Pages& pg = a.pg;
   const int lane = threadIdx.x & 63, all_fronts = a.fronts * a.front_blocks;
   const int id = unit_of_block();
   if (id >= a.units) return false;
-  if (!a.spread) {
-    // blocks of eight units, all row blocks of theirs after each other (so on one XCD)
-    const int front_ids = (a.front_chunks * a.Hy + 7) / 8 * 8 * a.front_blocks;
-    const bool front = id < front_ids;
-    const int x = front ? id : id - front_ids, blocks = front ? a.front_blocks : a.own_blocks, eight = x / (8 * blocks);
-    const int unit = eight * 8 + (x & 7), u = unit / a.Hy;
-    if (u >= (front ? a.front_chunks : a.own_chunks)) return false;
-    const int at = front ? u : u + a.front_chunks;
-    const int4 p = a.list[2 * at], q = a.list[2 * at + 1];
-    if (p.x < 0) return false;
-    o.ch = {p.x, p.y, p.z, 0, 0, p.w, q.x, q.y, q.z};
-    o.hy = unit - u * a.Hy;
-    o.rb = (x - eight * 8 * blocks) >> 3;
-    o.todo = 1;
-    return true;
-  }
   const int rb = blockIdx.x >> 3;
-  o.u = quotient(id, __builtin_amdgcn_rcpf((float)a.Hy));
+  o.u = __builtin_amdgcn_readfirstlane(quotient(id, __builtin_amdgcn_rcpf((float)a.Hy)));
   const int hy = o.hy = id - o.u * a.Hy;
   __shared__ int s_parts[64][8];
   o.lds = s_parts;
-  o.rb = o.team_rb = rb;
-  {
-    // lane = sequence (and head) first, then a part: what each sequence has in front of its new tokens, the least of each group
-    const int owns = a.entries - a.fronts, parts = a.fronts + owns * a.own_blocks;
-    const float one_beams = __builtin_amdgcn_rcpf((float)a.n_beams), one_heads = __builtin_amdgcn_rcpf((float)pg.Hkv);
-    const int y = min(lane, owns - 1), s = a.per_head ? quotient(y, one_heads) : y;
-    const int told = told_len(pg, s, a.per_head ? y - s * pg.Hkv : 0);
-    const NewRows nr = new_rows(pg, s);
-    const int want = max(a.shared[quotient(s, one_beams)], 0), room = !nr.n ? -1 : pg.causal ? max(told - nr.n, 0) : told;
-    const bool is_front = lane < a.fronts;
-    const int x = is_front ? lane : min(quotient(lane - a.fronts, __builtin_amdgcn_rcpf((float)a.own_blocks)), owns - 1);
-    // first sequence (and head) of the part's group
-    const int step = a.per_head ? pg.Hkv : 1, of = a.per_head ? quotient(x, one_heads) : x, h = x - of * step;
-    const int group = is_front ? of : quotient(of, one_beams);
-    const int seq0 = group * a.n_beams * step + h;
-    int least = 0x7FFFFFFF;
+  o.team_rb = rb;
+  // lane = sequence (and head) first, then a part: what each sequence has in front of its new tokens, the least of each group
+  const int owns = a.entries - a.fronts, parts = a.fronts + owns * a.own_blocks;
+  const float one_beams = __builtin_amdgcn_rcpf((float)a.n_beams), one_heads = __builtin_amdgcn_rcpf((float)pg.Hkv);
+  const int y = min(lane, owns - 1), s = a.per_head ? quotient(y, one_heads) : y;
+  const int told = told_len(pg, s, a.per_head ? y - s * pg.Hkv : 0);
+  const NewRows nr = new_rows(pg, s);
+  const int want = max(a.shared[quotient(s, one_beams)], 0), room = !nr.n ? -1 : pg.causal ? max(told - nr.n, 0) : told;
+  const bool is_front = lane < a.fronts;
+  const int x = is_front ? lane : min(quotient(lane - a.fronts, __builtin_amdgcn_rcpf((float)a.own_blocks)), owns - 1);
+  // first sequence (and head) of the part's group
+  const int step = a.per_head ? pg.Hkv : 1, of = a.per_head ? quotient(x, one_heads) : x, h = x - of * step;
+  const int group = is_front ? of : quotient(of, one_beams);
+  const int seq0 = group * a.n_beams * step + h;
+  int least = 0x7FFFFFFF;
 #pragma unroll 4
-    for (int b = 0; b < a.n_beams; ++b) {
-      const int r = __shfl(room, seq0 + b * step);
-      least = r >= 0 ? min(least, r) : least;
-    }
-    const int shared = (int)min((int64_t)__shfl(want, seq0) << pg.lg_ps, (int64_t)pg.max_len);
-    const int tiles = least == 0x7FFFFFFF ? 0 : min(shared, least) / ATT_TILE;
-    const int own = is_front ? 0 : x, t = __shfl(told, own), first = __shfl(nr.first, own), n = __shfl(nr.n, own);
-    Entry en = {0, 0, 0, 0};
-    if (lane < parts) {
-      if (is_front) en = {tiles * ATT_TILE, 0, a.n_beams * pg.max_new, tiles};
-      else en = {t, first, n, n ? (min(t, pg.max_len) + ATT_TILE - 1) / ATT_TILE - tiles : 0};
-    }
-    const int tile0 = is_front ? 0 : tiles;
-    // (fronts of many rows go by tiles; of very long caches 2^coarse rounds are one)
-    const uint32_t team = a.front_blocks, per = (uint32_t)(is_front ? a.front_tiles : a.c_min) << a.coarse;
-    const uint32_t rounds = ((uint32_t)en.tiles + per - 1) / per, cost = rounds ? 2 * rounds + a.part_cost : 0;
-    const uint32_t upto = (uint32_t)wave_scan((int)cost), all = __builtin_amdgcn_readlane(upto, 63);
-    const uint32_t of_fronts = __builtin_amdgcn_readlane(upto, a.fronts - 1), of_own = all - of_fronts;
-    // teams for fronts: as many as their cost asks for, and one each at least
-    const uint32_t used = __popcll(__ballot(is_front && rounds > 0)), least_teams = used + (of_own > 0);
-    const float weight = (float)of_fronts * team, every = weight + (float)of_own;      // (half rounds of all workgroups)
-    const uint32_t teams = max(least_teams, (uint32_t)fminf(a.chunks, every * __builtin_amdgcn_rcpf((float)((a.part_cost + 2u) * team))));
-    const float due = (float)teams * weight * __builtin_amdgcn_rcpf(fmaxf(every, 1.f));
-    const uint32_t most = min(max((uint32_t)(due + 0.5f), used), teams - (of_own > 0 ? 1u : 0u));
-    // the fewest rounds a team (sixteenths of them) for which those are enough
-    const uint32_t of_front = is_front ? rounds : 0, all_rounds = wave_sum(of_front);
-    uint32_t n_teams, upto_teams, front_teams;
-    for (float each = fmaxf(1.f, 16.f * (float)all_rounds * __builtin_amdgcn_rcpf((float)max(most, 1u)));; each += each * 0.0625f + 1.f) {
-      n_teams = min((uint32_t)(fmaxf(16.f * (float)of_front - 0.5f, 0.f) * __builtin_amdgcn_rcpf(each)) + (of_front > 0), of_front);
-      upto_teams = (uint32_t)wave_scan((int)n_teams);
-      front_teams = __builtin_amdgcn_readlane(upto_teams, 63);
-      if (front_teams <= most) break;
-    }
-    if ((uint32_t)o.u >= max(teams, 1u)) return false;
-    const bool at_fronts = (uint32_t)o.u < front_teams;
-    uint32_t u = at_fronts ? o.u : (o.u - front_teams) * team + rb;
-    int seg0 = 0, seg1 = 0;
-    if (at_fronts) {
-      // Of two workgroups of a compute unit the one that came first is served first, and ends first (4 bits: five rounds 23 us, then
-      // 25 us): so it takes more.  Teams in the order first, second, first, .., then those whose second is no front's.
-      const uint32_t firsts = (teams + 1) / 2, seconds = front_teams > firsts ? front_teams - firsts : 0;
-      u = u >= firsts ? 2 * (u - firsts) + 1 : u < seconds ? 2 * u : u + seconds;
-      auto upto_team = [&](uint32_t x) {
-        return x < 2 * seconds ? (float)x + (x & 1 ? a.first_more : 0.f) : (float)x + (float)(x - 2 * seconds) * (seconds ? a.first_more : 0.f);
-      };
-      const uint32_t from = upto_teams - n_teams, i = u - from;
-      if (is_front && i < n_teams) {
-        const float base = upto_team(from), unit = (float)rounds * __builtin_amdgcn_rcpf(upto_team(from + n_teams) - base);
-        // (of few rounds each takes as many, so that none is without)
-        auto cut = [&](uint32_t k) {
-          return k == n_teams ? rounds : rounds < 2 * n_teams ? (uint32_t)(((float)(k * rounds) + 0.5f) * __builtin_amdgcn_rcpf((float)n_teams)) : (uint32_t)((upto_team(from + k) - base) * unit);
-        };
-        seg0 = (int)min(cut(i) * per, (uint32_t)en.tiles);
-        seg1 = (int)min(cut(i + 1) * per, (uint32_t)en.tiles);
-      }
-    } else if (!is_front && of_own) {
-      // (a share of two half rounds at least: no workgroup between others of a part is without a tile of it)
-      const uint32_t groups = max(1u, min((teams - front_teams) * team, of_own / 2)), q = of_own / groups, r = of_own % groups;
-      const uint32_t at = u * q + min(u, r), end = at + q + (u < r ? 1 : 0), ends = upto - of_fronts, begins = ends - cost + a.part_cost;
-      auto tile_of = [&](uint32_t c) { return c >= ends ? en.tiles : c <= begins ? 0 : (int)min((c - begins) / 2 * per, (uint32_t)en.tiles); };
-      seg0 = tile_of(at);
-      seg1 = tile_of(end);
-    }
-    const bool some = seg1 > seg0;
-    o.todo = __ballot(some);
-    o.slot0 = u + (at_fronts ? rb * a.front_slots : 0);
-    if (hy == 0 && threadIdx.x < 64 && lane < parts) {
-      int2* const plan = a.plan + (is_front ? lane * a.front_blocks + rb : all_fronts + lane - a.fronts);
-      if (some && seg0 == 0) plan->x = o.slot0 + lane;
-      if (some && seg1 == en.tiles) plan->y = o.slot0 + lane;
-      if (o.u == 0 && en.tiles == 0 && (is_front || rb == 0)) *plan = make_int2(1, 0);
-    }
-    if (threadIdx.x < 64) {
-      *(int4*)s_parts[lane] = make_int4(en.told, en.first, en.n, tile0 + seg0);
-      s_parts[lane][4] = tile0 + seg1;
-    }
-    __syncthreads();
-    return true;
+  for (int b = 0; b < a.n_beams; ++b) {
+    const int r = __shfl(room, seq0 + b * step);
+    least = r >= 0 ? min(least, r) : least;
   }
+  const int shared = (int)min((int64_t)__shfl(want, seq0) << pg.lg_ps, (int64_t)pg.max_len);
+  const int tiles = least == 0x7FFFFFFF ? 0 : min(shared, least) / ATT_TILE;
+  const int own = is_front ? 0 : x, t = __shfl(told, own), first = __shfl(nr.first, own), n = __shfl(nr.n, own);
+  Entry en = {0, 0, 0, 0};
+  if (lane < parts) {
+    if (is_front) en = {tiles * ATT_TILE, 0, a.n_beams * pg.max_new, tiles};
+    else en = {t, first, n, n ? (min(t, pg.max_len) + ATT_TILE - 1) / ATT_TILE - tiles : 0};
+  }
+  const int tile0 = is_front ? 0 : tiles;
+  // (fronts of many rows go by tiles; of very long caches 2^coarse rounds are one)
+  const uint32_t team = a.front_blocks, per = (uint32_t)(is_front ? a.front_tiles : a.c_min) << a.coarse;
+  const uint32_t rounds = ((uint32_t)en.tiles + per - 1) / per, cost = rounds ? 2 * rounds + a.part_cost : 0;
+  const uint32_t upto = (uint32_t)wave_scan((int)cost), all = __builtin_amdgcn_readlane(upto, 63);
+  const uint32_t of_fronts = __builtin_amdgcn_readlane(upto, a.fronts - 1), of_own = all - of_fronts;
+  // teams for fronts: as many as their cost asks for, and one each at least
+  const uint32_t used = __popcll(__ballot(is_front && rounds > 0)), least_teams = used + (of_own > 0);
+  const float weight = (float)of_fronts * team, every = weight + (float)of_own;      // (half rounds of all workgroups)
+  const uint32_t teams = max(least_teams, (uint32_t)fminf(a.chunks, every * __builtin_amdgcn_rcpf((float)((a.part_cost + 2u) * team))));
+  const float due = (float)teams * weight * __builtin_amdgcn_rcpf(fmaxf(every, 1.f));
+  const uint32_t most = min(max((uint32_t)(due + 0.5f), used), teams - (of_own > 0 ? 1u : 0u));
+  // the fewest rounds a team (sixteenths of them) for which those are enough
+  const uint32_t of_front = is_front ? rounds : 0, all_rounds = wave_sum(of_front);
+  uint32_t n_teams, upto_teams, front_teams;
+  for (float each = fmaxf(1.f, 16.f * (float)all_rounds * __builtin_amdgcn_rcpf((float)max(most, 1u)));; each += each * 0.0625f + 1.f) {
+    n_teams = min((uint32_t)(fmaxf(16.f * (float)of_front - 0.5f, 0.f) * __builtin_amdgcn_rcpf(each)) + (of_front > 0), of_front);
+    upto_teams = (uint32_t)wave_scan((int)n_teams);
+    front_teams = __builtin_amdgcn_readlane(upto_teams, 63);
+    if (front_teams <= most) break;
+  }
+  if ((uint32_t)o.u >= max(teams, 1u)) return false;
+  const bool at_fronts = (uint32_t)o.u < front_teams;
+  uint32_t u = at_fronts ? o.u : (o.u - front_teams) * team + rb;
+  int seg0 = 0, seg1 = 0;
+  if (at_fronts) {
+    // Of two workgroups of a compute unit the one that came first is served first, and ends first (4 bits: five rounds 23 us, then
+    // 25 us): so it takes more.  Teams in the order first, second, first, .., then those whose second is no front's.
+    const uint32_t firsts = (teams + 1) / 2, seconds = front_teams > firsts ? front_teams - firsts : 0;
+    u = u >= firsts ? 2 * (u - firsts) + 1 : u < seconds ? 2 * u : u + seconds;
+    auto upto_team = [&](uint32_t x) {
+      return x < 2 * seconds ? (float)x + (x & 1 ? a.first_more : 0.f) : (float)x + (float)(x - 2 * seconds) * (seconds ? a.first_more : 0.f);
+    };
+    const uint32_t from = upto_teams - n_teams, i = u - from;
+    if (is_front && i < n_teams) {
+      const float base = upto_team(from), unit = (float)rounds * __builtin_amdgcn_rcpf(upto_team(from + n_teams) - base);
+      // (of few rounds each takes as many, so that none is without)
+      auto cut = [&](uint32_t k) {
+        return k == n_teams ? rounds : rounds < 2 * n_teams ? (uint32_t)(((float)(k * rounds) + 0.5f) * __builtin_amdgcn_rcpf((float)n_teams)) : (uint32_t)((upto_team(from + k) - base) * unit);
+      };
+      seg0 = (int)min(cut(i) * per, (uint32_t)en.tiles);
+      seg1 = (int)min(cut(i + 1) * per, (uint32_t)en.tiles);
+    }
+  } else if (!is_front && of_own) {
+    // (a share of two half rounds at least: no workgroup between others of a part is without a tile of it)
+    const uint32_t groups = max(1u, min((teams - front_teams) * team, of_own / 2)), q = of_own / groups, r = of_own % groups;
+    const uint32_t at = u * q + min(u, r), end = at + q + (u < r ? 1 : 0), ends = upto - of_fronts, begins = ends - cost + a.part_cost;
+    auto tile_of = [&](uint32_t c) { return c >= ends ? en.tiles : c <= begins ? 0 : (int)min((c - begins) / 2 * per, (uint32_t)en.tiles); };
+    seg0 = tile_of(at);
+    seg1 = tile_of(end);
+  }
+  const bool some = seg1 > seg0;
+  o.todo = __ballot(some);
+  o.slot0 = u + (at_fronts ? rb * a.front_slots : 0);
+  if (hy == 0 && threadIdx.x < 64 && lane < parts) {
+    int2* const plan = a.plan + (is_front ? lane * a.front_blocks + rb : all_fronts + lane - a.fronts);
+    if (some && seg0 == 0) plan->x = o.slot0 + lane;
+    if (some && seg1 == en.tiles) plan->y = o.slot0 + lane;
+    if (o.u == 0 && en.tiles == 0 && (is_front || rb == 0)) *plan = make_int2(1, 0);
+  }
+  if (threadIdx.x < 64) {
+    *(int4*)s_parts[lane] = make_int4(en.told, en.first, en.n, tile0 + seg0);
+    s_parts[lane][4] = tile0 + seg1;
+  }
+  __syncthreads();
+  return true;
 }
 // The next part: its chunk, whether it is a front, and the slot of its sums.
-__device__ __forceinline__ void next_part(const AttendArgs& a, BeamsWork& o, bool& front, int& slot) {
-  if (a.spread) {
-    const int l = __builtin_ctzll(o.todo);
-    front = l < a.fronts;
-    const int* p = o.lds[l];
-    o.ch = {front ? l : a.fronts + (l - a.fronts) / a.own_blocks, p[3], p[4], 0, 0, 0, p[0], p[1], p[2]};
-    slot = o.slot0 + l;
-    o.rb = front ? o.team_rb : (l - a.fronts) % a.own_blocks;
-  } else {
-    front = o.ch.e < a.fronts;
-    slot = o.ch.slot0 + (front ? o.rb * a.front_slots : 0);
-  }
+__device__ __forceinline__ void next_part(const AttendArgs& a, BeamsWork& o, Chunk& ch, int& rb, bool& front, int& slot) {
+  const int l = __builtin_ctzll(o.todo);
+  front = l < a.fronts;
+  const int* p = o.lds[l];
+  ch = {front ? l : a.fronts + (l - a.fronts) / a.own_blocks, p[3], p[4], 0, 0, 0, p[0], p[1], p[2]};
+  slot = o.slot0 + l;
+  rb = front ? o.team_rb : (l - a.fronts) % a.own_blocks;
   o.todo &= o.todo - 1;
 }
+// Of a workgroup in a launch by a list: the same, the head, and whether there is anything.
+__device__ __forceinline__ bool listed_part(const AttendArgs& a, int& hy, Chunk& ch, int& rb, bool& front, int& slot) {
+  const int id = unit_of_block();
+  if (id >= a.units) return false;
+  // blocks of eight units, all row blocks of theirs after each other (so on one XCD)
+  const int front_ids = (a.front_chunks * a.Hy + 7) / 8 * 8 * a.front_blocks;
+  front = id < front_ids;
+  const int x = front ? id : id - front_ids, blocks = front ? a.front_blocks : a.own_blocks, eight = x / (8 * blocks);
+  const int unit = eight * 8 + (x & 7), u = unit / a.Hy, at = front ? u : u + a.front_chunks;
+  if (u >= (front ? a.front_chunks : a.own_chunks)) return false;
+  const int4 p = a.list[2 * at], q = a.list[2 * at + 1];
+  if (p.x < 0) return false;
+  hy = unit - u * a.Hy;
+  ch = {p.x, p.y, p.z, 0, 0, 0, q.x, q.y, q.z};
+  rb = (x - eight * 8 * blocks) >> 3;
+  slot = p.w + (front ? rb * a.front_slots : 0);
+  return true;
+}
 
-template <int FMT, typename T, int D, int NP, int R, int SP, bool BEAMS>
+template <int FMT, typename T, int D, int NP, int R, int SP, int BEAMS>
 __global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(2)))
 void k_attend(AttendArgs a) {
   extern __shared__ __align__(16) float sm[];
@@ -583,26 +578,26 @@ void k_attend(AttendArgs a) {
   bool front = false;
   Chunk ch;
   BeamsWork work;
-  if constexpr (BEAMS) {
-    if (!beams_work(a, work)) return;
+  if constexpr (BEAMS == BEAMS_PARTS) {
+    if (!cut_parts(a, work)) return;
     hy = work.hy;
+  } else if constexpr (BEAMS == BEAMS_LIST) {
+    if (!listed_part(a, hy, ch, rb, front, slot)) return;
   } else {
     if (!find_chunk(a, unit / a.Hy, (int*)sm, ch)) return;
   }
   do {
-    if constexpr (BEAMS) {
+    if constexpr (BEAMS == BEAMS_PARTS) {
       if (!work.todo) return;
-      next_part(a, work, front, slot);
-      ch = work.ch;
-      rb = work.rb;
+      next_part(a, work, ch, rb, front, slot);
     }
 #include "attend_chunk.inc"
-    if (BEAMS) __syncthreads();          // (the sums of this part are read, before the next one's scales or sums come there)
-  } while (BEAMS);
+    if (BEAMS == BEAMS_PARTS) __syncthreads();          // (the sums of this part are read, before the next one's scales or sums come there)
+  } while (BEAMS == BEAMS_PARTS);
 }
 
 // A chunk of what a beam has behind the shared positions, in a kernel that does other things too.
-template <int FMT, typename T, int D, int NP, int R, int SP, bool BEAMS>
+template <int FMT, typename T, int D, int NP, int R, int SP, int BEAMS>
 __device__ __forceinline__ void attend_own(const AttendArgs& a, const Chunk& ch, int hy, int rb, int slot, float* sm) {
   constexpr bool front = false;
   do {
@@ -610,7 +605,7 @@ __device__ __forceinline__ void attend_own(const AttendArgs& a, const Chunk& ch,
   } while (false);
 }
 
-template <int FMT, typename T, int D, int NP, int R, int SP = 1, bool BEAMS = false>
+template <int FMT, typename T, int D, int NP, int R, int SP = 1, int BEAMS = 0>
 int run_attend(const AttendArgs& a, hipStream_t st) {
   constexpr size_t join = (8 * 16 * R + (size_t)4 * 16 * R * (D + 4)) * 4, scales = FMT == FMT_Q4 ? 4 * 4 * 64 * (D / 32) * 4 : 0;
   constexpr size_t lds = join > scales ? join : scales;
@@ -620,6 +615,11 @@ int run_attend(const AttendArgs& a, hipStream_t st) {
   }
   hipLaunchKernelGGL(kern, unit_grid(a), dim3(256), lds, st, a);
   return hip_status();
+}
+
+template <int FMT, typename T, int D, int NP, int R>
+int run_attend_beams(const AttendArgs& a, hipStream_t st) {
+  return a.spread ? run_attend<FMT, T, D, NP, R, 1, BEAMS_PARTS>(a, st) : run_attend<FMT, T, D, NP, R, 1, BEAMS_LIST>(a, st);
 }
 
 // by format, and for many rows (attend_*.hip); for beams (attend_beams_*.hip)

@@ -8,8 +8,8 @@ int run_attend_beams_q4(const AttendArgs& a, int R, hipStream_t st) {
     constexpr int D = decltype(d)::value, NP = decltype(np)::value;
     using T = decltype(t);
     if constexpr (planes_of<T> == 1 || D == 64)
-      if (R == 2) return run_attend<FMT_Q4, T, D, NP, 2, 1, true>(a, st);
-    return run_attend<FMT_Q4, T, D, NP, 1, 1, true>(a, st);
+      if (R == 2) return run_attend_beams<FMT_Q4, T, D, NP, 2>(a, st);
+    return run_attend_beams<FMT_Q4, T, D, NP, 1>(a, st);
   };
   auto by_d = [&](auto np, auto t) {
     return a.pg.d == 128 ? go(std::integral_constant<int, 128>{}, np, t) : go(std::integral_constant<int, 64>{}, np, t);

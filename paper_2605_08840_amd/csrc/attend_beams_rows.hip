@@ -8,7 +8,8 @@ int run_attend_beams_rows(const AttendArgs& a, hipStream_t st) {
   auto go = [&](auto d, auto np) {
     constexpr int D = decltype(d)::value, NP = decltype(np)::value;
     constexpr size_t tiles = 2 * 2 * 64 * (size_t)D * 2, join = (8 * 16 + (size_t)4 * 16 * (D + 4)) * 4;
-    hipLaunchKernelGGL((k_attend_rows<D, NP, 1, 4, true>), unit_grid(a), dim3(256), tiles > join ? tiles : join, st, a);
+    if (a.spread) hipLaunchKernelGGL((k_attend_rows<D, NP, 1, 4, BEAMS_PARTS>), unit_grid(a), dim3(256), tiles > join ? tiles : join, st, a);
+    else hipLaunchKernelGGL((k_attend_rows<D, NP, 1, 4, BEAMS_LIST>), unit_grid(a), dim3(256), tiles > join ? tiles : join, st, a);
     return hip_status();
   };
   auto by_d = [&](auto np) {

@@ -8,7 +8,7 @@ namespace {
 template <int D, int NP, int R, int NW>
 int run_rows(const AttendArgs& a, hipStream_t st) {
   constexpr size_t lds = 2 * 2 * 64 * (size_t)D * 2;
-  hipLaunchKernelGGL((k_attend_rows<D, NP, R, NW, false>), unit_grid(a), dim3(64 * NW), lds, st, a);
+  hipLaunchKernelGGL((k_attend_rows<D, NP, R, NW, NO_BEAMS>), unit_grid(a), dim3(64 * NW), lds, st, a);
   return hip_status();
 }
 

@@ -17,7 +17,7 @@ namespace restkv {
 // and softmax follow each other (a wavefront alone takes 4500 cycles a tile, 2048 of them products); 31 chunks of up to 17 tiles stand
 // for 32 of 16, and 33 MB of chunk sums are written and read again.
 // Beams: the workgroup's parts one after the other, the fronts so, what a beam has behind them as for few rows.
-template <int D, int NP, int R, int NW, bool BEAMS>
+template <int D, int NP, int R, int NW, int BEAMS>
 __global__ __attribute__((amdgpu_flat_work_group_size(64 * NW, 64 * NW), amdgpu_waves_per_eu(2)))
 void k_attend_rows(AttendArgs a) {
   constexpr int UN = D / 16, QC = D / 32, ROWB = D * 2, TK = 64, NB = 4, CH = ROWB / 16, TILE = TK * ROWB;
@@ -32,21 +32,23 @@ void k_attend_rows(AttendArgs a) {
   int hy = BEAMS ? 0 : unit % a.Hy;
   Chunk ch;
   BeamsWork work;
-  if constexpr (BEAMS) {
-    if (!beams_work(a, work)) return;
+  bool front = false;
+  if constexpr (BEAMS == BEAMS_PARTS) {
+    if (!cut_parts(a, work)) return;
     hy = work.hy;
+  } else if constexpr (BEAMS == BEAMS_LIST) {
+    if (!listed_part(a, hy, ch, rb, front, slot)) return;
   } else {
     if (!find_chunk<NW>(a, unit / a.Hy, (int*)lds, ch)) return;
   }
   do {
-  if constexpr (BEAMS) {
+  if constexpr (BEAMS == BEAMS_PARTS) {
     if (!work.todo) return;
-    bool front;
-    next_part(a, work, front, slot);
-    ch = work.ch;
-    rb = work.rb;
+    next_part(a, work, ch, rb, front, slot);
+  }
+  if constexpr (BEAMS != NO_BEAMS) {
     if (!front) {
-      attend_own<FMT_BF16, bf16_t, D, NP, 1, 1, true>(a, ch, hy, rb, slot, (float*)lds);
+      attend_own<FMT_BF16, bf16_t, D, NP, 1, 1, BEAMS>(a, ch, hy, rb, slot, (float*)lds);
       __syncthreads();
       continue;
     }
@@ -322,8 +324,8 @@ void k_attend_rows(AttendArgs a) {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
-  if (BEAMS) __syncthreads();          // (the next part's tiles come where these rows were)
-  } while (BEAMS);
+  if (BEAMS == BEAMS_PARTS) __syncthreads();          // (the next part's tiles come where these rows were)
+  } while (BEAMS == BEAMS_PARTS);
 }
 
 }  // namespace restkv
