@@ -298,7 +298,7 @@ const char* restkv_strerror(int code) {
   }
 }
 
-int restkv_version(void) { return 200; }
+int restkv_version(void) { return 300; }
 
 int restkv_debug_force_fp32(int on) {
   g_force_fp32 = on != 0;
