@@ -627,9 +627,9 @@ int run_attend_rows(const AttendArgs& a, int R, int waves, hipStream_t st);
 int run_attend_f32(const AttendArgs& a, int R, hipStream_t st);
 int run_attend_bf16(const AttendArgs& a, hipStream_t st);
 int run_attend_q4(const AttendArgs& a, int R, hipStream_t st);
-int run_attend_beams_f32(const AttendArgs& a, int R, hipStream_t st);
+int run_attend_beams_f32(const AttendArgs& a, hipStream_t st);
 int run_attend_beams_bf16(const AttendArgs& a, int R, hipStream_t st);
-int run_attend_beams_q4(const AttendArgs& a, int R, hipStream_t st);
+int run_attend_beams_q4(const AttendArgs& a, hipStream_t st);
 int run_attend_beams_rows(const AttendArgs& a, hipStream_t st);
 // What kernels and join share of the arguments.
 AttendArgs attend_args(const Pages& pg, const void* q, const void* k_pages, const void* v_pages, const void* k_scale,

@@ -69,7 +69,8 @@ __global__ __launch_bounds__(256) void k_beams_join(AttendArgs a) {
   }
 }
 
-constexpr int PART_ROUNDS = 2;         // what a part's beginning and end take, in rounds
+// What a part's beginning and end take, in rounds (0 / 1 / 2, us: 20 groups of four beams over 4k positions 70.9 / 71.5 / 79.7, 16 over 1k 28.0 / 27.2 / 27.2).
+constexpr int PART_ROUNDS = 1;
 
 // Sum over the workgroup; lds: 16 words, free to be written.
 template <typename V>
@@ -171,22 +172,30 @@ __global__ __launch_bounds__(1024) void k_beams_list(AttendArgs a, int at_a_time
 struct BeamsPlan { int many, R, front_rows, own_rows, c_min, target, spread, coarse; int64_t front_blocks, own_blocks, fronts, entries, parts, Hy, groups, at_a_time, slots, front_slots; };
 BeamsPlan beams_plan(const Pages& pg, int n_beams) {
   BeamsPlan p = {};
-  const int64_t rows = (int64_t)pg.G * pg.max_new;
-  const bool wide_q = pg.fmt == RESTKV_Q4 && pg.dtype == RESTKV_F32 && pg.d == 128;      // (see attend_plan)
-  p.many = pg.fmt == RESTKV_BF16 && rows * n_beams > 32;
-  p.R = p.many ? 1 : rows * n_beams <= 16 || wide_q ? 1 : 2;
-  p.front_rows = p.many ? 64 : 16 * p.R;
-  p.own_rows = p.many ? 16 : 16 * p.R;
-  p.front_blocks = (rows * n_beams + p.front_rows - 1) / p.front_rows;
-  p.own_blocks = (rows + p.own_rows - 1) / p.own_rows;
-  const bool per_head = pg.lens_sh != 0;
+  const int64_t rows = (int64_t)pg.G * pg.max_new, of_group = rows * n_beams;
+  const bool per_head = pg.lens_sh != 0, bf16 = pg.fmt == RESTKV_BF16;
   p.Hy = per_head ? 1 : pg.Hkv;
   p.fronts = (int64_t)(pg.n_seqs / n_beams) * (per_head ? pg.Hkv : 1);
   p.entries = p.fronts + (int64_t)pg.n_seqs * (per_head ? pg.Hkv : 1);
-  p.parts = p.fronts * p.front_blocks + (p.entries - p.fronts) * p.own_blocks;
-  p.c_min = pg.fmt == RESTKV_Q4 ? 4 : pg.fmt == RESTKV_BF16 ? 2 : 1;      // (tiles of a round: one of the keys of each wavefront)
+  p.c_min = pg.fmt == RESTKV_Q4 ? 4 : bf16 ? 2 : 1;      // (tiles of a round: one of the keys of each wavefront)
   p.target = n_cu() * 2;
-  p.spread = p.fronts + (p.entries - p.fronts) * p.own_blocks <= 64 && (p.fronts + 1) * p.Hy * p.front_blocks <= p.target;
+  // Fronts of bf16 pages by tiles in LDS for 64 rows (many), or from memory for 16 R rows a wavefront; us, 32 query and 8 KV heads of 128: parts
+  // cut evenly, 32 rows over two times 32k positions 62.3 (R = 2) / 67.5 (many), 48 rows over 16k 43.9 / 37.7, 64 rows 50.6 / 42.7; by a
+  // list, 32 groups of 32 rows over 1k 56.8 / 51.7; R = 1 in place of 2 39 / 35.  Blocks of 128 rows (many) spill: 43.6 -> 48.8 for 128 rows.
+  // Other pages take R = 1: their kernels have no registers left for two blocks (R = 2 / 1: float32, 32 rows over 8k 43.9 / 38.8, 256 rows
+  // 239 / 224; 4 bits, 32 rows over 16k 37.2 / 35.3, 32 groups of 64 rows over 1k 120 / 108, 256 rows over 4k 183 / 190).
+  auto blocks_of = [&](bool many) {
+    p.many = many;
+    p.R = !many && bf16 && of_group > 16 ? 2 : 1;
+    p.front_rows = many ? 64 : 16 * p.R;
+    p.own_rows = many ? 16 : 16 * p.R;
+    p.front_blocks = (of_group + p.front_rows - 1) / p.front_rows;
+    p.own_blocks = (rows + p.own_rows - 1) / p.own_rows;
+    p.parts = p.fronts * p.front_blocks + (p.entries - p.fronts) * p.own_blocks;
+    p.spread = p.fronts + (p.entries - p.fronts) * p.own_blocks <= 64 && (p.fronts + 1) * p.Hy * p.front_blocks <= p.target;
+  };
+  blocks_of(bf16 && of_group > 32);
+  if (!p.spread && p.R == 2) blocks_of(true);
   p.coarse = 0;
   if (p.spread) {
     p.groups = p.target / (p.Hy * p.front_blocks);
@@ -265,7 +274,7 @@ int launch_attend_beams(const Pages& pg, int n_beams, const int32_t* shared, con
     const int64_t lanes = p.fronts << (32 - __builtin_clz(n_beams - 1)), threads = std::min<int64_t>(1024, (std::max(lanes, p.entries - p.fronts) + 63) / 64 * 64);
     hipLaunchKernelGGL(k_beams_list, dim3(1), dim3(threads), 0, st, a, (int)p.at_a_time);
   }
-  const int rc = p.many ? run_attend_beams_rows(a, st) : pg.fmt == RESTKV_F32 ? run_attend_beams_f32(a, p.R, st) : pg.fmt == RESTKV_BF16 ? run_attend_beams_bf16(a, p.R, st) : run_attend_beams_q4(a, p.R, st);
+  const int rc = p.many ? run_attend_beams_rows(a, st) : pg.fmt == RESTKV_F32 ? run_attend_beams_f32(a, st) : pg.fmt == RESTKV_BF16 ? run_attend_beams_bf16(a, p.R, st) : run_attend_beams_q4(a, st);
   if (rc) return rc;
   const int each = p.spread ? 1 : 1024 / pg.d;
   const dim3 grid((pg.max_new * pg.Hq + each - 1) / each, pg.n_seqs);

@@ -307,7 +307,7 @@ __global__ __launch_bounds__(SEL_THREADS) void k_select_rows(SelectArgs a) {
       uint32_t hits = 0;
 #pragma unroll
       for (int i = 0; i < VEC; ++i) hits |= x[c][i] >= limit ? 1u << i : 0u;
-      const bool several = __ballot(hits & (hits - 1)) != 0;       // (mostly a lane has one, its largest: select of 16 rows of 16 beams 33.9 -> 33.4 us)
+      const bool several = __ballot(hits & (hits - 1)) != 0;       // (mostly a lane has one, its largest: 256 rows of 131072 logits, 32 out, 33.9 -> 33.4 us)
       while (__ballot(hits)) {         // one of each lane's at a time
         const int which = __builtin_ctz(hits | 1u << VEC);
         float y = top[c];
