@@ -37,7 +37,7 @@ struct AttendArgs {
   // for a block of rows, and k_beams_list has written which: list[2 u], [2 u + 1] {entry (-1: none), tiles from, to, slot}, {positions, first
   // row, new tokens}, of up to front_chunks chunks of fronts, then up to own_chunks of the rest.
   const int32_t* shared;
-  int4* list; int* front_tiles_of;
+  int4* list; int* tiles_of;
   int front_chunks, own_chunks;
   int n_beams, fronts, front_blocks, own_blocks, front_slots, spread, front_rows, own_rows, front_tiles, coarse;
   uint32_t part_cost;

@@ -86,9 +86,11 @@ __device__ __forceinline__ V block_sum(V x, V* lds) {
 }
 
 // Where there are many parts, or many rows: which workgroup takes what, worked out once, by one workgroup.  Entries are cut into chunks of at
-// most C tiles, C being an even share of all rounds with what parts cost beside them, but more where the chunks of fronts would be
-// more than run at a time.  Fronts come first: they are the long ones, and what the beams have of their own fills the end.
-// (Each workgroup for itself, as restkv_attend has it, looks at all beams of all groups: 256 groups of four beams 472 us in place of 312.)
+// most C tiles, C being an even share of all rounds with what parts cost beside them, but more where the chunks would be more than
+// run at a time (seven groups of eight beams, lengths per head, 536 chunks for 512 workgroups: 77 us, then 59); where the parts alone are more,
+// the chunks of fronts.  Fronts come first: they are the long ones, and what the beams have of their own fills the end.
+// (Each workgroup for itself, as restkv_attend has it, looks at all beams of all groups: 256 groups of four beams 472 us in place of 316.)
+// 5 us for 16 groups of four beams, 8 for 256, 29 for 2048.
 __global__ __launch_bounds__(1024) void k_beams_list(AttendArgs a, int at_a_time) {
   __shared__ long long s_sum[16];
   __shared__ int s_count[16];
@@ -97,6 +99,7 @@ __global__ __launch_bounds__(1024) void k_beams_list(AttendArgs a, int at_a_time
   // tiles that a group (and head) shares: `seg` lanes each, one a beam
   const int seg = 1 << (32 - __clz(a.n_beams - 1)), b = tid & (seg - 1);
   long long cost = 0;
+  int parts = 0;
   auto cost_of = [&](int tiles, int blocks) { return tiles ? (long long)((tiles + a.c_min - 1) / a.c_min + PART_ROUNDS) * blocks : 0; };
   for (int base = 0; base < a.fronts; base += T / seg) {
     const int x = base + tid / seg, y = min(x, a.fronts - 1), g = y / heads, h = y - g * heads, s = g * a.n_beams + min(b, a.n_beams - 1);
@@ -107,20 +110,28 @@ __global__ __launch_bounds__(1024) void k_beams_list(AttendArgs a, int at_a_time
     const int tiles = least == 0x7FFFFFFF ? 0 : min(shared, least) / ATT_TILE;
     if (x >= a.fronts || b >= a.n_beams) continue;
     if (b == 0) {
-      a.front_tiles_of[x] = tiles;
+      a.tiles_of[x] = tiles;
       cost += cost_of(tiles, a.front_blocks);
+      parts += tiles ? a.front_blocks : 0;
     }
-    if (n) cost += cost_of((min(told, pg.max_len) + ATT_TILE - 1) / ATT_TILE - tiles, a.own_blocks);
+    const int own = n ? (min(told, pg.max_len) + ATT_TILE - 1) / ATT_TILE - tiles : 0;
+    a.tiles_of[a.fronts + s * heads + h] = own;
+    cost += cost_of(own, a.own_blocks);
+    parts += own ? a.own_blocks : 0;
   }
-  cost = block_sum(cost, s_sum);       // (and front_tiles_of is there for the whole workgroup)
-  long long rounds = max((cost + at_a_time - 1) / at_a_time, 1ll);
-  for (int i = 0; i < 16 && (int64_t)a.fronts * a.front_blocks < at_a_time; ++i) {
+  cost = block_sum(cost, s_sum);       // (and tiles_of is there for the whole workgroup)
+  const int active = block_sum(parts, s_count);
+  int rounds = (int)min(max((cost + at_a_time - 1) / at_a_time, 1ll), (long long)1 << 23);
+  // chunks that are to fit: all, or of more parts than that the fronts'
+  const int fit = active <= at_a_time ? a.entries : (int64_t)a.fronts * a.front_blocks < at_a_time ? a.fronts : 0;
+  for (int i = 0; i < 16 && fit; ++i) {
     int chunks = 0;
-    for (int x = tid; x < a.fronts; x += T) chunks += (int)((a.front_tiles_of[x] + rounds * a.c_min - 1) / (rounds * a.c_min)) * a.front_blocks;
+    const int C = rounds * a.c_min;
+    for (int x = tid; x < fit; x += T) chunks += (a.tiles_of[x] + C - 1) / C * (x < a.fronts ? a.front_blocks : a.own_blocks);
     if (block_sum(chunks, s_count) <= at_a_time) break;
     rounds += rounds / 16 + 1;
   }
-  const int C = (int)min((long long)1 << 25, rounds * a.c_min);
+  const int C = rounds * a.c_min;
   auto list = [&](bool front) {
     const int count = front ? a.fronts : a.entries - a.fronts, blocks = front ? a.front_blocks : a.own_blocks;
     int2* const plan = a.plan + (front ? 0 : (int64_t)a.fronts * a.front_blocks);
@@ -132,13 +143,12 @@ __global__ __launch_bounds__(1024) void k_beams_list(AttendArgs a, int at_a_time
       NewRows nr = {0, a.n_beams * pg.max_new};
       if (x < count) {
         const int s = a.per_head ? x / pg.Hkv : x, h = a.per_head ? x - s * pg.Hkv : 0;
-        tiles = a.front_tiles_of[front ? x : s / a.n_beams * heads + h];
+        tiles = a.tiles_of[front ? x : a.fronts + x];
         told = tiles * ATT_TILE;
         if (!front) {
-          tile0 = tiles;
+          tile0 = a.tiles_of[s / a.n_beams * heads + h];
           told = told_len(pg, s, h);
           nr = new_rows(pg, s);
-          tiles = nr.n ? (min(told, pg.max_len) + ATT_TILE - 1) / ATT_TILE - tile0 : 0;
         }
         cnt = (tiles + C - 1) / C;
       }
@@ -220,7 +230,7 @@ BeamsWs beams_ws(const Pages& pg, const BeamsPlan& p) {
   const size_t front = (size_t)p.front_slots * p.front_blocks * p.Hy * p.front_rows;
   w.plan = take((size_t)p.parts * 8);
   w.list = take(p.spread ? 0 : (size_t)(p.front_slots + p.slots) * 32);
-  w.tiles = take(p.spread ? 0 : (size_t)p.fronts * 4);
+  w.tiles = take(p.spread ? 0 : (size_t)p.entries * 4);
   w.m = take(rows * 4);
   w.l = take(rows * 4);
   w.o = take(rows * pg.d * 4);
@@ -257,7 +267,7 @@ int launch_attend_beams(const Pages& pg, int n_beams, const int32_t* shared, con
   if (ids > (int64_t)1 << 30 || p.front_slots * p.front_blocks > (int64_t)1 << 30 || std::max(p.front_blocks, p.own_blocks) > (1 << 20) || (int64_t)pg.max_new * pg.Hq >= (1 << 24)) return RESTKV_EUNSUPPORTED;
   AttendArgs a = attend_args(pg, q, k_pages, v_pages, k_scale, v_scale, out, lse);
   a.plan = (int2*)(ws + lay.plan);
-  a.list = (int4*)(ws + lay.list); a.front_tiles_of = (int*)(ws + lay.tiles);
+  a.list = (int4*)(ws + lay.list); a.tiles_of = (int*)(ws + lay.tiles);
   a.part_m = (float*)(ws + lay.m); a.part_l = (float*)(ws + lay.l); a.part_o = (float*)(ws + lay.o);
   a.front_m = (float*)(ws + lay.fm); a.front_l = (float*)(ws + lay.fl); a.front_o = (float*)(ws + lay.fo);
   a.entries = (int)p.entries; a.Hy = (int)p.Hy;
