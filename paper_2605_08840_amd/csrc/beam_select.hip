@@ -593,9 +593,14 @@ int launch_beam_select(const Beams& b, const void* logits, const float* scores, 
   const dim3 grid = wide_grid((int64_t)b.n_groups * b.n_beams * a.pieces);
   if (b.dtype == RESTKV_F32) hipLaunchKernelGGL(k_select_rows<float>, grid, dim3(SEL_THREADS), 0, st, a);
   else hipLaunchKernelGGL(k_select_rows<bf16_t>, grid, dim3(SEL_THREADS), 0, st, a);
-  // (four / sixteen wavefronts, us a call: 112 continuations left by the pieces 11.8 / 13.4, 504 of them 22.1 / 23.2, 2048 39.5 / 33.9)
-  if ((int64_t)b.n_beams * a.pieces * b.n_out <= 1024) hipLaunchKernelGGL(k_select_join<4>, dim3(b.n_groups), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(k_select_join<16>, dim3(b.n_groups), dim3(1024), 0, st, a);
+  // Wavefronts of a request: its beams go round them, and a barrier takes longer the more there are.  Four / eight / sixteen, us a call: 4 beams,
+  // 112 continuations left by the pieces 11.9 / 12.0 / 13.3, 896 of them 15.5 / 13.9 / 14.5; 6 beams, 504 22.6 / 23.0 / 23.6; 8 beams, 256
+  // 13.9 / 12.6 / 13.5; 16 beams, 256 20.1 / 16.8 / 16.9, 512 16.6 / 13.8 / 13.3, 1024 25.5 / 22.0 / 22.0; 12 beams, 1152 - / 17.3 / 15.7; 64 beams - / 55.2 / 37.8.
+  const int64_t left = (int64_t)b.n_beams * a.pieces * b.n_out;
+  auto join = [&](auto kern, int waves) { hipLaunchKernelGGL(kern, dim3(b.n_groups), dim3(64 * waves), 0, st, a); };
+  if (left > 1024) join(k_select_join<16>, 16);
+  else if (left > 512 || b.n_beams >= 8) join(k_select_join<8>, 8);
+  else join(k_select_join<4>, 4);
   return hip_status();
 }
 
