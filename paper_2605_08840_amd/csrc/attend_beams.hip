@@ -90,7 +90,7 @@ __device__ __forceinline__ V block_sum(V x, V* lds) {
 // run at a time (seven groups of eight beams, lengths per head, 536 chunks for 512 workgroups: 77 us, then 59); where the parts alone are more,
 // the chunks of fronts.  Fronts come first: they are the long ones, and what the beams have of their own fills the end.
 // (Each workgroup for itself, as restkv_attend has it, looks at all beams of all groups: 256 groups of four beams 472 us in place of 316.)
-// 5 us for 16 groups of four beams, 8 for 256, 29 for 2048.
+// 6 us for 16 groups of four beams, 10 for 256, 30 for 2048.
 __global__ __launch_bounds__(1024) void k_beams_list(AttendArgs a, int at_a_time) {
   __shared__ long long s_sum[16];
   __shared__ int s_count[16];
