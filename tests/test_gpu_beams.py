@@ -568,6 +568,74 @@ def test_attend_beams_two_calls_at_once_and_on_another_stream(shared_once):
     assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[2])
 
 
+MANY = dict(lens=[300 + 11 * i for i in range(72)], new=[1] * 72, hq=8, hkv=2, d=128)          # more parts than a wavefront has lanes
+
+
+@pytest.mark.parametrize("fmt", [None, "q4"])
+@pytest.mark.parametrize("n_beams", [3, 24])
+def test_attend_of_many_beams_at_once_and_replayed(n_beams, fmt, shared_once):
+    """Calls by a list: two at a time, and captured, with other lengths and counts of shared pages at each replay."""
+    p = Plain(rk, fmt=fmt, **MANY)
+    sh = share(p, n_beams, [18] * (72 // n_beams))
+    q, t = p.normal(p.tokens, 8, 128).bfloat16().cuda(), p.tensors
+    outs, ws = [torch.empty_like(q) for _ in range(4)], [rk.alloc_attend_beams_workspace(p.c, n_beams) for _ in range(3)]
+    call = lambda i, w, **k: rk.restkv_attend_beams(p.c, n_beams, sh, q, p.pages, t["table"], t["lens"], outs[i], None, w, **k)  # noqa: E731
+    call(2, ws[0])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            call(i, ws[i], stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[2])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(3, ws[2])
+    lens = t["lens"].clone()
+    for i in range(5):
+        t["lens"].copy_((lens - 37 * i * (torch.arange(72, device="cuda") % 3)).clamp_min(0))
+        sh.copy_(torch.arange(72 // n_beams, device="cuda") * i % 18)
+        outs[3].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        call(2, ws[0])
+        torch.cuda.synchronize()
+        assert torch.equal(outs[3], outs[2]), i
+
+
+def test_workspaces_are_not_exceeded(shared_once):
+    """Bytes behind a workspace of just the size that is asked for stay as they are."""
+    def guarded(n):
+        x = torch.full((n + 4096 + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+        off = -x.data_ptr() % 256
+        return x, x[off:off + n], x[off + n:]
+
+    cases = [(MANY, 3, 18), (MANY, 24, 18), (dict(lens=[700, 720, 650, 900], new=[2, 1, 1, 3], hq=8, hkv=2, d=128), 2, 39),
+             (dict(lens=[333] * 20, new=[1] * 20, hq=14, hkv=2, d=64), 20, 20),
+             (dict(lens=[[90 + i, 300 - 3 * i] for i in range(40)], new=[5] * 40, hq=16, hkv=2, head_lens=True), 5, 5)]
+    for fmt in (None, "q4"):
+        for kw, n_beams, shared in cases:
+            p = Plain(rk, fmt=fmt, **kw)
+            sh = share(p, n_beams, [shared] * (len(p.new) // n_beams))
+            need = rk.restkv_attend_beams_workspace_bytes(p.c, n_beams)
+            _, ws, rest = guarded(need)
+            q = p.normal(p.tokens, p.hq, p.d).bfloat16().cuda()
+            want, got, t = torch.empty_like(q), torch.empty_like(q), p.tensors
+            for out, w in ((got, ws), (want, rk.alloc_attend_beams_workspace(p.c, n_beams))):
+                rk.restkv_attend_beams(p.c, n_beams, sh, q, p.pages, t["table"], t["lens"], out, None, w, new_start=t["new_start"])
+            assert (rest == 0xA5).all() and torch.equal(got, want)
+    for groups, beams, vocab, n_out in ((3, 4, 20000, 8), (2, 12, 5001, 64), (1, 1, 9, 1)):
+        for dtype in (torch.float32, torch.bfloat16):
+            b = rk.make_beams(n_groups=groups, n_beams=beams, n_vocab=vocab, n_out=n_out, dtype=dtype)
+            _, ws, rest = guarded(rk.restkv_beam_workspace_bytes(b))
+            flat = torch.randn(groups * beams * vocab + 1, device="cuda").to(dtype)
+            for at in (0, 1):                              # rows at 16-byte addresses, and not
+                i32 = lambda: torch.empty((groups, n_out), dtype=torch.int32, device="cuda")  # noqa: E731
+                rk.restkv_beam_select(b, flat[at:at + groups * beams * vocab].view(-1, vocab), torch.zeros((groups, beams), device="cuda"),
+                                      torch.empty((groups, n_out), device="cuda"), i32(), i32(), ws)
+                assert (rest == 0xA5).all()
+
+
 # ---- together -----------------------------------------------------------------------------------
 
 
