@@ -40,11 +40,12 @@ struct RowParts {
   }
 };
 
+constexpr int FEW_CHUNKS = 8;
 // A workgroup a row; or (ALONE, where there are many) as many rows as it has groups of d / 4 threads, each joined by one of these if
 // none has many chunks.  256 groups of four beams, 32 heads of 128: 50 -> 19 us.
 template <int D, bool ALONE>
 __global__ __launch_bounds__(256) void k_beams_join(AttendArgs a) {
-  constexpr int TPR = D / 4, NGR = 256 / TPR, FEW = 8;
+  constexpr int TPR = D / 4, NGR = 256 / TPR;
   const Pages& pg = a.pg;
   const int s = blockIdx.y, all = pg.max_new * pg.Hq;
   if constexpr (ALONE) {
@@ -52,7 +53,7 @@ __global__ __launch_bounds__(256) void k_beams_join(AttendArgs a) {
     const RowParts p(a, s, x / pg.Hq, x % pg.Hq);
     const NewRows nr = new_rows(pg, s);
     const bool there = (int)blockIdx.x * NGR + (int)threadIdx.x / TPR < all && x / pg.Hq < nr.n;
-    if (!__syncthreads_or(there && p.count > FEW)) {
+    if (!__syncthreads_or(there && p.count > FEW_CHUNKS)) {
       if (!there) return;
       const Sums sums = sum_chunks(0, 1, p.count, c, [&](int k) { return p.at<D>(k); });
       store_out(a, nr.first + x / pg.Hq, x % pg.Hq, c, sums.x, sums.M, sums.L);
@@ -286,11 +287,14 @@ int launch_attend_beams(const Pages& pg, int n_beams, const int32_t* shared, con
   }
   const int rc = p.many ? run_attend_beams_rows(a, st) : pg.fmt == RESTKV_F32 ? run_attend_beams_f32(a, st) : pg.fmt == RESTKV_BF16 ? run_attend_beams_bf16(a, p.R, st) : run_attend_beams_q4(a, st);
   if (rc) return rc;
-  const int each = p.spread ? 1 : 1024 / pg.d;
+  // (by the chunks that a front's row may have; one / eight rows a workgroup, bf16, us: one group of 64 beams over 16k 65.6 / 77.5, over 4k 36.6 / 34.6,
+  // two groups of 33 beams with 8 query heads over 16k 47.1 / 62.7; 256 groups of four 316 / 287 when this came)
+  const bool alone = !p.spread && p.at_a_time <= FEW_CHUNKS * p.fronts * p.front_blocks;
+  const int each = alone ? 1024 / pg.d : 1;
   const dim3 grid((pg.max_new * pg.Hq + each - 1) / each, pg.n_seqs);
   auto join = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, a); };
-  if (pg.d == 128) p.spread ? join(k_beams_join<128, false>) : join(k_beams_join<128, true>);
-  else p.spread ? join(k_beams_join<64, false>) : join(k_beams_join<64, true>);
+  if (pg.d == 128) alone ? join(k_beams_join<128, true>) : join(k_beams_join<128, false>);
+  else alone ? join(k_beams_join<64, true>) : join(k_beams_join<64, false>);
   return hip_status();
 }
 
