@@ -244,11 +244,16 @@ BeamsWs beams_ws(const Pages& pg, const BeamsPlan& p) {
 // Short caches are read as if nothing were shared: one launch where each is one chunk, and no join of two kinds of chunks.  By what all
 // caches may hold together.  So / by parts, us, 8 KV heads of 128, pages that the last call has read too: bf16, 4 beams 33 MB 14.2 / 15.7
 // and 64 MB 16.3 / 16.3, four groups of them 33 MB 13.7 / 14.8, 65 MB 16.3 / 16.4, 129 MB 23.6 / 17.4, two groups of 16 beams 66 MB 14.6 / 18.1, 130 MB
-// 19.1 / 19.6; 4 bits 40 MB 19.4 / 21.1, 80 MB 28.5 / 21.7; float32 33 MB 15.9 / 17.0, 65 MB 19.3 / 17.2.
+// 19.1 / 19.6; 4 bits 40 MB 19.4 / 21.1, 80 MB 28.5 / 21.7; float32 33 MB 15.9 / 17.0, 65 MB 19.3 / 17.2.  A list takes a launch, and 3 us
+// for each 32 beams: so / by a list, MiB that the caches may hold: bf16, 12 beams with lengths per head 99 19.5 / 20.9, 32 136 22.0 / 23.2, 64 144
+// 20.6 / 23.0 and 208 26.1 / 24.2, 80 180 25.0 / 26.4, 160 200 30.1 / 33.1 and 360 45.9 / 35.6; float32, 64 160 22.4 / 25.2 and 288 32.1 / 30.9; 4 bits,
+// 32 42 19.9 / 23.1, 64 65 21.6 / 25.1, 80 106 36.2 / 30.2, 160 62 31.0 / 39.7 and 112 42.0 / 42.4.
 std::atomic<int> g_force_shared{0};
-bool as_if_alone(const Pages& pg, int n_beams) {
+bool as_if_alone(const Pages& pg, int n_beams, const BeamsPlan& p) {
+  if (n_beams == 1 || g_force_shared) return n_beams == 1;
   const int64_t row = pg.fmt == RESTKV_Q4 ? pg.d / 2 + pg.d / 8 : pg.fmt == RESTKV_BF16 ? pg.d * 2 : pg.d * 4;
-  return n_beams == 1 || (!g_force_shared && 2 * row * pg.Hkv * pg.n_seqs <= ((int64_t)48 << 20) / pg.max_len);
+  const int64_t most = (p.spread ? 48 : 112 + (int64_t)pg.n_seqs * 3 / 4) << (!p.spread && pg.fmt == RESTKV_Q4 ? 19 : 20);
+  return 2 * row * pg.Hkv * pg.n_seqs <= most / pg.max_len;
 }
 
 }  // namespace
@@ -256,13 +261,14 @@ bool as_if_alone(const Pages& pg, int n_beams) {
 void force_shared(bool on) { g_force_shared = on; }
 
 size_t attend_beams_ws_bytes(const Pages& pg, int n_beams) {
-  return as_if_alone(pg, n_beams) ? attend_ws_bytes(pg) : beams_ws(pg, beams_plan(pg, n_beams)).bytes;
+  const BeamsPlan p = beams_plan(pg, n_beams);
+  return as_if_alone(pg, n_beams, p) ? attend_ws_bytes(pg) : beams_ws(pg, p).bytes;
 }
 
 int launch_attend_beams(const Pages& pg, int n_beams, const int32_t* shared, const void* q, const void* k_pages, const void* v_pages,
                         const void* k_scale, const void* v_scale, void* out, float* lse, char* ws, hipStream_t st) {
-  if (as_if_alone(pg, n_beams)) return launch_attend(pg, q, k_pages, v_pages, k_scale, v_scale, out, lse, ws, st);
   const BeamsPlan p = beams_plan(pg, n_beams);
+  if (as_if_alone(pg, n_beams, p)) return launch_attend(pg, q, k_pages, v_pages, k_scale, v_scale, out, lse, ws, st);
   const BeamsWs lay = beams_ws(pg, p);
   const int64_t ids = p.spread ? p.groups * p.Hy : (p.front_slots * p.Hy + 7) / 8 * 8 * p.front_blocks + (p.slots * p.Hy + 7) / 8 * 8 * p.own_blocks;
   if (ids > (int64_t)1 << 30 || p.front_slots * p.front_blocks > (int64_t)1 << 30 || std::max(p.front_blocks, p.own_blocks) > (1 << 20) || (int64_t)pg.max_new * pg.Hq >= (1 << 24)) return RESTKV_EUNSUPPORTED;
