@@ -476,6 +476,7 @@ class _Told:
         self.positions = ((c.n_tokens,), i32, "positions", None)
         self.grid = ((n_seqs, c.max_new), i32, "positions", None) if n_seqs * c.max_new == c.n_tokens else self.positions
         self.pages = None                    # the last layout of pages that was found to be the described one
+        self.n_seqs, self.shared = n_seqs, {}            # shared pages of groups, by their beams
 
 
 def _told(c: RestkvCache) -> _Told:
@@ -761,5 +762,8 @@ def restkv_attend_beams(c: RestkvCache, n_beams, shared, q, pages: CachePages, t
     are read once for all of them."""
     what, told = "restkv_attend_beams", _told(c)
     dev = _check_pages(what, c, told, pages)
-    sh = _check_flat(what, dev, shared, ((c.n_seqs // max(n_beams, 1),), torch.int32, "shared", None))
+    of = told.shared.get(n_beams)
+    if of is None:
+        of = told.shared[n_beams] = ((told.n_seqs // max(n_beams, 1),), torch.int32, "shared", None)
+    sh = _check_flat(what, dev, shared, of)
     _attend(what, lib().restkv_attend_beams, (n_beams, sh), c, told, dev, q, pages, table, lens, out, lse, workspace, new_start, stream)
