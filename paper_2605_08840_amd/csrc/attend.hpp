@@ -427,9 +427,10 @@ struct BeamsWork {
   int u, hy, team_rb, slot0;
 };
 // Parts (up to 64, a lane each; a front with all its blocks of rows is one) cut evenly: the rounds of all follow each other, with
-// a.part_cost half rounds more for each part, which is what its beginning and end take.  Workgroups come in teams of front_blocks.  Some teams take the fronts, one front each and all about as many rounds, each of a team's workgroups the same tiles for a block of rows
-// (at the same time on one XCD, whose L2 reads them once); the workgroups of the other teams cut what is left, one by one.  A round is what
-// the wavefronts of a workgroup take at a time, a.c_min tiles.
+// a.part_cost half rounds more for each part, which is what its beginning and end take.  Workgroups come in teams of front_blocks.  Some
+// teams take the fronts, one front each and all about as many rounds, each of a team's workgroups the same tiles for a block of rows
+// (at the same time on one XCD, whose L2 reads them once); the workgroups of the other teams cut what is left, one by one.  A round is
+// what the wavefronts of a workgroup take at a time, a.c_min tiles.
 // (What comes of it is in LDS, so that the loops between have the registers.)
 // Quotients of small whole numbers (below 2^15), where a division of 32 bits would take forty instructions.
 __device__ __forceinline__ int quotient(int x, float one_over) { return (int)(((float)x + 0.5f) * one_over); }

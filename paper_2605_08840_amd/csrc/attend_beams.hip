@@ -180,7 +180,10 @@ __global__ __launch_bounds__(1024) void k_beams_list(AttendArgs a, int at_a_time
   list(false);
 }
 
-struct BeamsPlan { int many, R, front_rows, own_rows, c_min, target, spread, coarse; int64_t front_blocks, own_blocks, fronts, entries, parts, Hy, groups, at_a_time, slots, front_slots; };
+struct BeamsPlan {
+  int many, R, front_rows, own_rows, c_min, target, spread, coarse;
+  int64_t front_blocks, own_blocks, fronts, entries, parts, Hy, groups, at_a_time, slots, front_slots;
+};
 BeamsPlan beams_plan(const Pages& pg, int n_beams) {
   BeamsPlan p = {};
   const int64_t rows = (int64_t)pg.G * pg.max_new, of_group = rows * n_beams;
@@ -192,21 +195,26 @@ BeamsPlan beams_plan(const Pages& pg, int n_beams) {
   p.target = n_cu() * 2;
   // Fronts of bf16 pages by tiles in LDS for 64 rows (many), or from memory for 16 R rows a wavefront; us, 32 query and 8 KV heads of 128: parts
   // cut evenly, 32 rows over two times 32k positions 62.3 (R = 2) / 67.5 (many), 48 rows over 16k 43.9 / 37.7, 64 rows 50.6 / 42.7; by a
-  // list, 32 groups of 32 rows over 1k 56.8 / 51.7; R = 1 in place of 2 39 / 35.  Blocks of 128 rows (many) spill: 43.6 -> 48.8 for 128 rows.
+  // list, 32 groups of 32 rows over 1k 56.8 / 51.7; R = 1 in place of 2 39 / 35.  Blocks of 64 / 128 rows
+  // (many): parts cut evenly, 80 rows over 8k 25.4 / 29.5, 128 over 16k 40.7 / 43.8, two times 128 53.8 / 50.7; by a list, 32 groups of 80 rows over 1k
+  // 99.4 / 89.9, 16 of 256 over 512 118 / 112, eight of 256 over 4k 130 / 96.7.
   // Other pages take R = 1: their kernels have no registers left for two blocks (R = 2 / 1: float32, 32 rows over 8k 43.9 / 38.8, 256 rows
   // 239 / 224; 4 bits, 32 rows over 16k 37.2 / 35.3, 32 groups of 64 rows over 1k 120 / 108, 256 rows over 4k 183 / 190).
-  auto blocks_of = [&](bool many) {
-    p.many = many;
+  auto blocks_of = [&](int many) {       // rows of a block that go by tiles in LDS, or 0
+    p.many = many != 0;
     p.R = !many && bf16 && of_group > 16 ? 2 : 1;
-    p.front_rows = many ? 64 : 16 * p.R;
+    p.front_rows = many ? many : 16 * p.R;
     p.own_rows = many ? 16 : 16 * p.R;
     p.front_blocks = (of_group + p.front_rows - 1) / p.front_rows;
     p.own_blocks = (rows + p.own_rows - 1) / p.own_rows;
     p.parts = p.fronts * p.front_blocks + (p.entries - p.fronts) * p.own_blocks;
     p.spread = p.fronts + (p.entries - p.fronts) * p.own_blocks <= 64 && (p.fronts + 1) * p.Hy * p.front_blocks <= p.target;
   };
-  blocks_of(bf16 && of_group > 32);
-  if (!p.spread && p.R == 2) blocks_of(true);
+  blocks_of(bf16 && of_group > 32 ? 64 : 0);
+  if (!p.spread && bf16 && of_group > 16) {
+    blocks_of(of_group > 64 ? 128 : 64);
+    p.spread = 0;
+  }
   p.coarse = 0;
   if (p.spread) {
     p.groups = p.target / (p.Hy * p.front_blocks);
@@ -271,7 +279,9 @@ int launch_attend_beams(const Pages& pg, int n_beams, const int32_t* shared, con
   if (as_if_alone(pg, n_beams, p)) return launch_attend(pg, q, k_pages, v_pages, k_scale, v_scale, out, lse, ws, st);
   const BeamsWs lay = beams_ws(pg, p);
   const int64_t ids = p.spread ? p.groups * p.Hy : (p.front_slots * p.Hy + 7) / 8 * 8 * p.front_blocks + (p.slots * p.Hy + 7) / 8 * 8 * p.own_blocks;
-  if (ids > (int64_t)1 << 30 || p.front_slots * p.front_blocks > (int64_t)1 << 30 || std::max(p.front_blocks, p.own_blocks) > (1 << 20) || (int64_t)pg.max_new * pg.Hq >= (1 << 24)) return RESTKV_EUNSUPPORTED;
+  if (ids > (int64_t)1 << 30 || p.front_slots * p.front_blocks > (int64_t)1 << 30 || std::max(p.front_blocks, p.own_blocks) > (1 << 20) ||
+      (int64_t)pg.max_new * pg.Hq >= (1 << 24))
+    return RESTKV_EUNSUPPORTED;
   AttendArgs a = attend_args(pg, q, k_pages, v_pages, k_scale, v_scale, out, lse);
   a.plan = (int2*)(ws + lay.plan);
   a.list = (int4*)(ws + lay.list); a.tiles_of = (int*)(ws + lay.tiles);
@@ -291,7 +301,8 @@ int launch_attend_beams(const Pages& pg, int n_beams, const int32_t* shared, con
     const int64_t lanes = p.fronts << (32 - __builtin_clz(n_beams - 1)), threads = std::min<int64_t>(1024, (std::max(lanes, p.entries - p.fronts) + 63) / 64 * 64);
     hipLaunchKernelGGL(k_beams_list, dim3(1), dim3(threads), 0, st, a, (int)p.at_a_time);
   }
-  const int rc = p.many ? run_attend_beams_rows(a, st) : pg.fmt == RESTKV_F32 ? run_attend_beams_f32(a, st) : pg.fmt == RESTKV_BF16 ? run_attend_beams_bf16(a, p.R, st) : run_attend_beams_q4(a, st);
+  const int rc = p.many ? run_attend_beams_rows(a, st) : pg.fmt == RESTKV_F32 ? run_attend_beams_f32(a, st) :
+                 pg.fmt == RESTKV_BF16 ? run_attend_beams_bf16(a, p.R, st) : run_attend_beams_q4(a, st);
   if (rc) return rc;
   // (by the chunks that a front's row may have; one / eight rows a workgroup, bf16, us: one group of 64 beams over 16k 65.6 / 77.5, over 4k 36.6 / 34.6,
   // two groups of 33 beams with 8 query heads over 16k 47.1 / 62.7; 256 groups of four 316 / 287 when this came)
