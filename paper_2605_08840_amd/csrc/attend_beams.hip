@@ -291,6 +291,9 @@ int launch_attend_beams(const Pages& pg, int n_beams, const int32_t* shared, con
   a.shared = shared; a.n_beams = n_beams; a.fronts = (int)p.fronts;
   a.front_blocks = (int)p.front_blocks; a.own_blocks = (int)p.own_blocks; a.front_slots = (int)p.front_slots; a.spread = p.spread;
   a.front_rows = p.front_rows; a.own_rows = p.own_rows;
+  // (half rounds that a part costs beside its own, 2 / 3 / 4, us: one group of 32 beams over 16k 46.7 / 41.8 / 40.2; two of eight over 32k 62.3 / 62.4 / 63.8;
+  // 4 bits, four of four over 8k to 32k 37.2 / 37.3 / 40.0.  What is added for those served first, 0 / 0.05 / 0.1 / 0.2: the last 39.3 / 39.2 / 37.7 / 38.0,
+  // over 32k 63.4 / 63.1 / 63.0 / 62.6)
   a.part_cost = p.many ? 4 : 3; a.front_tiles = p.many ? 1 : p.c_min; a.coarse = p.coarse;
   a.first_more = 0.1f;
   a.row_blocks = (int)(p.spread ? p.front_blocks : 1); a.units = (int)ids; a.c_min = p.c_min;
