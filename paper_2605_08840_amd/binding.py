@@ -602,19 +602,11 @@ def restkv_append(c: RestkvCache, k, v, pages: CachePages, table, lens, *, new_s
             _addr(pages.k_scale), _addr(pages.v_scale), tb, ln, ns, ps, cs, sn, _addr(q), _addr(q_out))
 
 
-def _take_workspace(what, dev, workspace):
-    """Address (aligned) and bytes of a workspace, or None and 0."""
-    if workspace is None:
-        return None, 0
-    if workspace.get_device() != dev or workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
-        raise RestkvError(-1, f"{what}: the workspace has to be contiguous uint8 on GPU {dev}")
-    at = workspace.data_ptr()
-    return at + -at % 256, max(workspace.numel() - -at % 256, 0)
-
-
-def _attend(what, f, front, c, told, dev, q, pages, table, lens, out, lse, workspace, new_start, stream):
-    """The call f(description, *front, q, ...)."""
-    ref = told.ref
+def restkv_attend(c: RestkvCache, q, pages: CachePages, table, lens, out, lse=None, workspace=None, *, new_start=None,
+                  stream=None):
+    """Attention of the newest tokens' queries q [n_tokens, Hq, d] over the pages: out [n_tokens, Hq, d], lse [n_tokens, Hq]."""
+    what, told = "restkv_attend", _told(c)
+    dev, ref = _check_pages(what, c, told, pages), told.ref
     tb, ln = _check_flat(what, dev, table, told.table), _check_flat(what, dev, lens, told.lens)
     ns = None if new_start is None else _check_flat(what, dev, new_start, told.new)
     qs = _check_rows(what, dev, told.dtype, "q", q, told.q, told.q_stride)
@@ -622,17 +614,14 @@ def _attend(what, f, front, c, told, dev, q, pages, table, lens, out, lse, works
     ls = told.lse_stride if lse is None else _check_rows(what, dev, torch.float32, "lse", lse, told.lse, told.lse_stride)
     if qs is not told.q_stride or outs is not told.out_stride or ls is not told.lse_stride:
         ref = _as_strided(c, q=qs, out=outs, lse=ls)
-    wp, wn = _take_workspace(what, dev, workspace)
-    _on_gpu(dev, stream, what, f, ref, *front, q.data_ptr(), pages.k.data_ptr(), pages.v.data_ptr(), _addr(pages.k_scale),
+    wp, wn = None, 0
+    if workspace is not None:
+        if workspace.get_device() != dev or workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
+            raise RestkvError(-1, f"{what}: the workspace has to be contiguous uint8 on GPU {dev}")
+        at = workspace.data_ptr()
+        wp, wn = at + -at % 256, max(workspace.numel() - -at % 256, 0)
+    _on_gpu(dev, stream, what, lib().restkv_attend, ref, q.data_ptr(), pages.k.data_ptr(), pages.v.data_ptr(), _addr(pages.k_scale),
             _addr(pages.v_scale), tb, ln, ns, out.data_ptr(), _addr(lse), wp, wn)
-
-
-def restkv_attend(c: RestkvCache, q, pages: CachePages, table, lens, out, lse=None, workspace=None, *, new_start=None,
-                  stream=None):
-    """Attention of the newest tokens' queries q [n_tokens, Hq, d] over the pages: out [n_tokens, Hq, d], lse [n_tokens, Hq]."""
-    what, told = "restkv_attend", _told(c)
-    dev = _check_pages(what, c, told, pages)
-    _attend(what, lib().restkv_attend, (), c, told, dev, q, pages, table, lens, out, lse, workspace, new_start, stream)
 
 
 def restkv_fetch(c: RestkvCache, pages: CachePages, table, lens, k_out, v_out, *, idx=None, first=0, stream=None):
@@ -690,6 +679,16 @@ class _BeamsTold:
             return strides[0] == self.stride or shape[0] <= 1
         return shape == self.grouped and (strides[1] == self.stride or not beams) and \
             (strides[0] == self.grouped[1] * self.stride or not groups)
+
+
+def _take_workspace(what, dev, workspace):
+    """Address (aligned) and bytes of a workspace, or None and 0."""
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != dev or workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
+        raise RestkvError(-1, f"{what}: the workspace has to be contiguous uint8 on GPU {dev}")
+    at = workspace.data_ptr()
+    return at + -at % 256, max(workspace.numel() - -at % 256, 0)
 
 
 def restkv_beam_select(b: RestkvBeams, logits, scores, new_scores, parents, tokens, workspace, *, finished=None, new_finished=None,
@@ -761,9 +760,17 @@ def restkv_attend_beams(c: RestkvCache, n_beams, shared, q, pages: CachePages, t
     """restkv_attend where the tables of each n_beams neighbouring sequences begin with the same shared[group] pages (int32), which
     are read once for all of them."""
     what, told = "restkv_attend_beams", _told(c)
-    dev = _check_pages(what, c, told, pages)
+    dev, ref = _check_pages(what, c, told, pages), told.ref
     of = told.shared.get(n_beams)
     if of is None:
         of = told.shared[n_beams] = ((told.n_seqs // max(n_beams, 1),), torch.int32, "shared", None)
-    sh = _check_flat(what, dev, shared, of)
-    _attend(what, lib().restkv_attend_beams, (n_beams, sh), c, told, dev, q, pages, table, lens, out, lse, workspace, new_start, stream)
+    sh, tb, ln = _check_flat(what, dev, shared, of), _check_flat(what, dev, table, told.table), _check_flat(what, dev, lens, told.lens)
+    ns = None if new_start is None else _check_flat(what, dev, new_start, told.new)
+    qs = _check_rows(what, dev, told.dtype, "q", q, told.q, told.q_stride)
+    outs = _check_rows(what, dev, told.out_dtype, "out", out, told.q, told.out_stride)
+    ls = told.lse_stride if lse is None else _check_rows(what, dev, torch.float32, "lse", lse, told.lse, told.lse_stride)
+    if qs is not told.q_stride or outs is not told.out_stride or ls is not told.lse_stride:
+        ref = _as_strided(c, q=qs, out=outs, lse=ls)
+    wp, wn = _take_workspace(what, dev, workspace)
+    _on_gpu(dev, stream, what, lib().restkv_attend_beams, ref, n_beams, sh, q.data_ptr(), pages.k.data_ptr(), pages.v.data_ptr(),
+            _addr(pages.k_scale), _addr(pages.v_scale), tb, ln, ns, out.data_ptr(), _addr(lse), wp, wn)
