@@ -144,7 +144,7 @@ def _select_inputs(c, seed):
     logits = torch.empty((groups * beams, vocab + c["pad"]), dtype=_value_type(c), device=DEV)
     for r in range(groups):                    # what a request's beams have in common, and each beam's own; a few likely tokens
         x = 2 * torch.randn((1, vocab), generator=g, device=DEV) + torch.randn((beams, vocab), generator=g, device=DEV)
-        likely = (torch.randint(vocab, (1,), generator=g, device=DEV) + torch.arange(40, device=DEV) * (vocab // 40)) % vocab
+        likely = torch.randint(vocab, (40,), generator=g, device=DEV)
         x[:, likely] += 6 * torch.rand((beams, 40), generator=g, device=DEV) + 2
         if c["masked"]:
             x[torch.rand((1, vocab), generator=g, device=DEV).expand(beams, vocab) < c["masked"]] = -math.inf
