@@ -517,6 +517,14 @@ int restkv_debug_fp32_plan(const restkv_params* p, int32_t* plan);
  */
 int restkv_debug_force_shared(int on);
 
+/*
+ * Debug aid: into how many chunks restkv_attend_beams would cut what these caches hold, where it works by a list of chunks
+ * (RESTKV_EUNSUPPORTED elsewhere), and how many there is room for in its workspace.  tiles: HOST array of tiles of 64 positions, 0 .. 2^24 each: what
+ * each group shares (of each KV head, with lengths per head), then what each sequence (and head) has behind it.  chunks: HOST array of 4:
+ * chunks of shared positions, room for these, chunks of the rest, room for those.
+ */
+int restkv_debug_beams_list(const restkv_cache* c, int32_t n_beams, const int32_t* tiles, int32_t* chunks);
+
 /* Static description of an error code. */
 const char* restkv_strerror(int code);
 

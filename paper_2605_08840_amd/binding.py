@@ -127,6 +127,8 @@ def lib() -> ctypes.CDLL:
         L.restkv_attend_beams_workspace_bytes.restype = sz
         L.restkv_debug_force_shared.argtypes = [ctypes.c_int]
         L.restkv_debug_force_shared.restype = ctypes.c_int
+        L.restkv_debug_beams_list.argtypes = [C, i32, vp, vp]
+        L.restkv_debug_beams_list.restype = ctypes.c_int
         L.restkv_attend_beams.argtypes = [C, i32] + [vp] * 12 + [sz, vp]
         L.restkv_attend_beams.restype = ctypes.c_int
         L.restkv_strerror.restype = ctypes.c_char_p
@@ -753,6 +755,17 @@ def alloc_attend_beams_workspace(c: RestkvCache, n_beams, device="cuda") -> Opti
 
 def restkv_debug_force_shared(on: bool):
     _chk(lib().restkv_debug_force_shared(int(bool(on))), "restkv_debug_force_shared")
+
+
+def restkv_debug_beams_list(c: RestkvCache, n_beams, tiles):
+    """(chunks of shared positions, room for them, chunks of what beams have behind them, room) for entries of so many tiles (a host list),
+    where restkv_attend_beams works by a list of chunks."""
+    tiles, chunks = (ctypes.c_int32 * len(tiles))(*tiles), (ctypes.c_int32 * 4)()
+    entries = (c.n_seqs // n_beams + c.n_seqs) * (c.n_kv_heads if c.lens_stride_h else 1) if n_beams > 0 else 0
+    if len(tiles) != entries:
+        raise RestkvError(-1, f"restkv_debug_beams_list: tiles of {entries} entries")
+    _chk(lib().restkv_debug_beams_list(ctypes.byref(c), n_beams, tiles, chunks), "restkv_debug_beams_list")
+    return tuple(chunks)
 
 
 def restkv_attend_beams(c: RestkvCache, n_beams, shared, q, pages: CachePages, table, lens, out, lse=None, workspace=None, *,

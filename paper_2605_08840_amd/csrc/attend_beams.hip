@@ -72,6 +72,10 @@ __global__ __launch_bounds__(256) void k_beams_join(AttendArgs a) {
 
 // What a part's beginning and end take, in rounds (0 / 1 / 2, us: 20 groups of four beams over 4k positions 70.9 / 71.5 / 79.7, 16 over 1k 28.0 / 27.2 / 27.2).
 constexpr int PART_ROUNDS = 1;
+// Rounds of a chunk at the most: as many as the longest cache has tiles (2^30 positions), so that an entry is one chunk then.  Fewer would cut
+// long entries into more chunks than there is room for, which is sized by even shares.
+constexpr int MOST_ROUNDS = 1 << (30 - 6);
+static_assert(ATT_TILE == 1 << 6, "");
 
 // Sum over the workgroup; lds: 16 words, free to be written.
 template <typename V>
@@ -84,6 +88,22 @@ __device__ __forceinline__ V block_sum(V x, V* lds) {
   x = lds[0];
   for (int w = 1; w < (int)blockDim.x / 64; ++w) x += lds[w];
   return x;
+}
+
+// Chunks of a list.  An entry of `tiles` tiles in `blocks` blocks of rows costs so many rounds of c_min tiles;
+__host__ __device__ __forceinline__ long long list_cost(int tiles, int blocks, int c_min) {
+  return tiles ? (long long)((tiles + c_min - 1) / c_min + PART_ROUNDS) * blocks : 0;
+}
+// a chunk has an even share of all rounds (so the chunks of entries, in all their blocks, are no more than at_a_time and one for each part)
+__host__ __device__ __forceinline__ int list_rounds(long long cost, int at_a_time) {
+  const long long even = (cost + at_a_time - 1) / at_a_time;
+  return even < 1 ? 1 : even < MOST_ROUNDS ? (int)even : MOST_ROUNDS;
+}
+__host__ __device__ __forceinline__ int more_rounds(int rounds) { return rounds + rounds / 16 + 1; }
+__host__ __device__ __forceinline__ int list_chunks(int tiles, int C) { return (tiles + C - 1) / C; }
+// What is to be no more chunks than run at a time: the first so many entries (all, or where the parts alone are more the fronts).
+__host__ __device__ __forceinline__ int list_fit(int fronts, int entries, int front_blocks, int parts, int at_a_time) {
+  return parts <= at_a_time ? entries : (int64_t)fronts * front_blocks < at_a_time ? fronts : 0;
 }
 
 // Where there are many parts, or many rows: which workgroup takes what, worked out once, by one workgroup.  Entries are cut into chunks of at
@@ -101,7 +121,6 @@ __global__ __launch_bounds__(1024) void k_beams_list(AttendArgs a, int at_a_time
   const int seg = 1 << (32 - __clz(a.n_beams - 1)), b = tid & (seg - 1);
   long long cost = 0;
   int parts = 0;
-  auto cost_of = [&](int tiles, int blocks) { return tiles ? (long long)((tiles + a.c_min - 1) / a.c_min + PART_ROUNDS) * blocks : 0; };
   for (int base = 0; base < a.fronts; base += T / seg) {
     const int x = base + tid / seg, y = min(x, a.fronts - 1), g = y / heads, h = y - g * heads, s = g * a.n_beams + min(b, a.n_beams - 1);
     const int told = told_len(pg, s, h), n = new_rows(pg, s).n;
@@ -112,25 +131,24 @@ __global__ __launch_bounds__(1024) void k_beams_list(AttendArgs a, int at_a_time
     if (x >= a.fronts || b >= a.n_beams) continue;
     if (b == 0) {
       a.tiles_of[x] = tiles;
-      cost += cost_of(tiles, a.front_blocks);
+      cost += list_cost(tiles, a.front_blocks, a.c_min);
       parts += tiles ? a.front_blocks : 0;
     }
     const int own = n ? (min(told, pg.max_len) + ATT_TILE - 1) / ATT_TILE - tiles : 0;
     a.tiles_of[a.fronts + s * heads + h] = own;
-    cost += cost_of(own, a.own_blocks);
+    cost += list_cost(own, a.own_blocks, a.c_min);
     parts += own ? a.own_blocks : 0;
   }
   cost = block_sum(cost, s_sum);       // (and tiles_of is there for the whole workgroup)
   const int active = block_sum(parts, s_count);
-  int rounds = (int)min(max((cost + at_a_time - 1) / at_a_time, 1ll), (long long)1 << 23);
-  // chunks that are to fit: all, or of more parts than that the fronts'
-  const int fit = active <= at_a_time ? a.entries : (int64_t)a.fronts * a.front_blocks < at_a_time ? a.fronts : 0;
+  int rounds = list_rounds(cost, at_a_time);
+  const int fit = list_fit(a.fronts, a.entries, a.front_blocks, active, at_a_time);
   for (int i = 0; i < 16 && fit; ++i) {
     int chunks = 0;
     const int C = rounds * a.c_min;
-    for (int x = tid; x < fit; x += T) chunks += (a.tiles_of[x] + C - 1) / C * (x < a.fronts ? a.front_blocks : a.own_blocks);
+    for (int x = tid; x < fit; x += T) chunks += list_chunks(a.tiles_of[x], C) * (x < a.fronts ? a.front_blocks : a.own_blocks);
     if (block_sum(chunks, s_count) <= at_a_time) break;
-    rounds += rounds / 16 + 1;
+    rounds = more_rounds(rounds);
   }
   const int C = rounds * a.c_min;
   auto list = [&](bool front) {
@@ -151,7 +169,7 @@ __global__ __launch_bounds__(1024) void k_beams_list(AttendArgs a, int at_a_time
           told = told_len(pg, s, h);
           nr = new_rows(pg, s);
         }
-        cnt = (tiles + C - 1) / C;
+        cnt = list_chunks(tiles, C);
       }
       const int inc = wave_scan(cnt);
       __syncthreads();
@@ -265,6 +283,34 @@ bool as_if_alone(const Pages& pg, int n_beams, const BeamsPlan& p) {
 }
 
 }  // namespace
+
+// k_beams_list's numbers, from the tiles of every entry.
+int beams_list(const Pages& pg, int n_beams, const int32_t* tiles, int32_t* chunks) {
+  const BeamsPlan p = beams_plan(pg, n_beams);
+  if (p.spread || as_if_alone(pg, n_beams, p) || p.parts > 1 << 30) return RESTKV_EUNSUPPORTED;
+  const int fronts = (int)p.fronts, entries = (int)p.entries, at_a_time = (int)p.at_a_time;
+  auto blocks = [&](int x) { return (int)(x < fronts ? p.front_blocks : p.own_blocks); };
+  long long cost = 0;
+  int parts = 0;
+  for (int x = 0; x < entries; ++x) {
+    if (tiles[x] < 0 || tiles[x] > (1 << 30) / ATT_TILE) return RESTKV_EINVAL;
+    cost += list_cost(tiles[x], blocks(x), p.c_min);
+    parts += tiles[x] ? blocks(x) : 0;
+  }
+  int rounds = list_rounds(cost, at_a_time);
+  const int fit = list_fit(fronts, entries, (int)p.front_blocks, parts, at_a_time);
+  for (int i = 0; i < 16 && fit; ++i) {
+    int n = 0;
+    for (int x = 0; x < fit; ++x) n += list_chunks(tiles[x], rounds * p.c_min) * blocks(x);
+    if (n <= at_a_time) break;
+    rounds = more_rounds(rounds);
+  }
+  chunks[0] = chunks[2] = 0;
+  for (int x = 0; x < entries; ++x) chunks[x < fronts ? 0 : 2] += list_chunks(tiles[x], rounds * p.c_min);
+  chunks[1] = (int)p.front_slots;
+  chunks[3] = (int)p.slots;
+  return RESTKV_OK;
+}
 
 void force_shared(bool on) { g_force_shared = on; }
 

@@ -17,6 +17,7 @@ int launch_beam_select(const Beams& b, const void* logits, const float* scores, 
 int launch_beam_reorder(const Pages& pg, int n_beams, const int32_t* parents, int64_t parents_stride, int32_t* table_out,
                         const restkv_layer_pages* layers, int n_layers, hipStream_t st);
 void force_shared(bool on);     // see restkv_debug_force_shared
+int beams_list(const Pages& pg, int n_beams, const int32_t* tiles, int32_t* chunks);       // see restkv_debug_beams_list
 size_t attend_beams_ws_bytes(const Pages& pg, int n_beams);
 int launch_attend_beams(const Pages& pg, int n_beams, const int32_t* shared, const void* q, const void* k_pages, const void* v_pages,
                         const void* k_scale, const void* v_scale, void* out, float* lse, char* ws, hipStream_t st);

@@ -177,6 +177,15 @@ int restkv_debug_force_shared(int on) {
   return RESTKV_OK;
 }
 
+int restkv_debug_beams_list(const restkv_cache* c, int32_t n_beams, const int32_t* tiles, int32_t* chunks) {
+  Pages pg;
+  int rc = resolve_cache(c, &pg);
+  if (!rc) rc = take_beams(pg, n_beams);
+  if (rc) return rc;
+  if (!pg.n_seqs || !tiles || !chunks) return RESTKV_EINVAL;
+  return beams_list(pg, n_beams, tiles, chunks);
+}
+
 size_t restkv_beam_workspace_bytes(const restkv_beams* b) {
   Beams o;
   return resolve_beams(b, &o) == RESTKV_OK ? beam_ws_bytes(o) : 0;
