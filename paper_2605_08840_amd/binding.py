@@ -452,10 +452,10 @@ def alloc_attend_workspace(c: RestkvCache, device="cuda") -> Optional[torch.Tens
 
 
 class _Told:
-    """What a description says of the tensors of a call, worked out once (a field that is set makes it new)."""
+    """What a description says of the tensors of a call, worked out once (a field that is set makes it new).  It hangs on the description, so
+    nothing here refers to that, not by ctypes.byref either: the two would keep each other for ever."""
 
     def __init__(self, c: RestkvCache):
-        self.ref = ctypes.byref(c)
         self.dtype, self.out_dtype = _TORCH.get(c.dtype), _TORCH.get(c.out_dtype)
         self.kv, self.q, self.lse = ((c.n_tokens, c.n_kv_heads, c.head_dim), (c.n_tokens, c.n_q_heads, c.head_dim),
                                      (c.n_tokens, c.n_q_heads))
@@ -549,13 +549,13 @@ def _check_rows(what, dev, dtype, name, t, shape, strides):
     return (along, across) + strides[2:]
 
 
-def _as_strided(c: RestkvCache, **strides) -> ctypes.c_void_p:
+def _as_strided(c: RestkvCache, **strides) -> RestkvCache:
     """A copy of the description with these strides of token tensors."""
     c = RestkvCache.from_buffer_copy(c)
     for kind, st in strides.items():
         setattr(c, kind + "_stride_t", st[0])
         setattr(c, kind + "_stride_h", st[1])
-    return ctypes.byref(c)
+    return c
 
 
 def _on_gpu(dev: int, stream, what: str, f, *args):
@@ -580,7 +580,7 @@ def restkv_append(c: RestkvCache, k, v, pages: CachePages, table, lens, *, new_s
     """New keys (rotated by their positions) and values [n_tokens, Hkv, d] into the pages, and new queries [n_tokens, Hq, d]
     rotated beside them; lens counts the new tokens already."""
     what, told = "restkv_append", _told(c)
-    dev, dt, ref = _check_pages(what, c, told, pages), told.dtype, told.ref
+    dev, dt, desc = _check_pages(what, c, told, pages), told.dtype, c
     tb, ln = _check_flat(what, dev, table, told.table), _check_flat(what, dev, lens, told.lens)
     ns = None if new_start is None else _check_flat(what, dev, new_start, told.new)
     kv = _check_rows(what, dev, dt, "k", k, told.kv, told.kv_stride)
@@ -599,8 +599,8 @@ def restkv_append(c: RestkvCache, k, v, pages: CachePages, table, lens, *, new_s
         by_row = ns is None and positions.shape == told.grid[0]
         ps = _check_flat(what, dev, positions, told.grid if by_row else told.positions)
     if kv is not told.kv_stride or qs is not told.q_stride:
-        ref = _as_strided(c, kv=kv, q=qs)
-    _on_gpu(dev, stream, what, lib().restkv_append, ref, k.data_ptr(), v.data_ptr(), pages.k.data_ptr(), pages.v.data_ptr(),
+        desc = _as_strided(c, kv=kv, q=qs)
+    _on_gpu(dev, stream, what, lib().restkv_append, desc, k.data_ptr(), v.data_ptr(), pages.k.data_ptr(), pages.v.data_ptr(),
             _addr(pages.k_scale), _addr(pages.v_scale), tb, ln, ns, ps, cs, sn, _addr(q), _addr(q_out))
 
 
@@ -608,21 +608,21 @@ def restkv_attend(c: RestkvCache, q, pages: CachePages, table, lens, out, lse=No
                   stream=None):
     """Attention of the newest tokens' queries q [n_tokens, Hq, d] over the pages: out [n_tokens, Hq, d], lse [n_tokens, Hq]."""
     what, told = "restkv_attend", _told(c)
-    dev, ref = _check_pages(what, c, told, pages), told.ref
+    dev, desc = _check_pages(what, c, told, pages), c
     tb, ln = _check_flat(what, dev, table, told.table), _check_flat(what, dev, lens, told.lens)
     ns = None if new_start is None else _check_flat(what, dev, new_start, told.new)
     qs = _check_rows(what, dev, told.dtype, "q", q, told.q, told.q_stride)
     outs = _check_rows(what, dev, told.out_dtype, "out", out, told.q, told.out_stride)
     ls = told.lse_stride if lse is None else _check_rows(what, dev, torch.float32, "lse", lse, told.lse, told.lse_stride)
     if qs is not told.q_stride or outs is not told.out_stride or ls is not told.lse_stride:
-        ref = _as_strided(c, q=qs, out=outs, lse=ls)
+        desc = _as_strided(c, q=qs, out=outs, lse=ls)
     wp, wn = None, 0
     if workspace is not None:
         if workspace.get_device() != dev or workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
             raise RestkvError(-1, f"{what}: the workspace has to be contiguous uint8 on GPU {dev}")
         at = workspace.data_ptr()
         wp, wn = at + -at % 256, max(workspace.numel() - -at % 256, 0)
-    _on_gpu(dev, stream, what, lib().restkv_attend, ref, q.data_ptr(), pages.k.data_ptr(), pages.v.data_ptr(), _addr(pages.k_scale),
+    _on_gpu(dev, stream, what, lib().restkv_attend, desc, q.data_ptr(), pages.k.data_ptr(), pages.v.data_ptr(), _addr(pages.k_scale),
             _addr(pages.v_scale), tb, ln, ns, out.data_ptr(), _addr(lse), wp, wn)
 
 
@@ -636,7 +636,7 @@ def restkv_fetch(c: RestkvCache, pages: CachePages, table, lens, k_out, v_out, *
         raise RestkvError(-1, f"{what}: k_out and v_out have to be [n_seqs, Hkv, n, d]")
     kp, vp = _check_flat(what, dev, k_out, (shape, told.dtype, "k_out", None)), _check_flat(what, dev, v_out, (shape, told.dtype, "v_out", None))
     ix = None if idx is None else _check_flat(what, dev, idx, (shape[:3], torch.int32, "idx", None))
-    _on_gpu(dev, stream, what, lib().restkv_fetch, told.ref, pages.k.data_ptr(), pages.v.data_ptr(), _addr(pages.k_scale),
+    _on_gpu(dev, stream, what, lib().restkv_fetch, c, pages.k.data_ptr(), pages.v.data_ptr(), _addr(pages.k_scale),
             _addr(pages.v_scale), tb, ln, ix, int(first), shape[2], kp, vp)
 
 
@@ -663,7 +663,7 @@ class _BeamsTold:
     """What a description says of the tensors of restkv_beam_select, worked out once (a field that is set makes it new)."""
 
     def __init__(self, b: RestkvBeams):
-        self.ref, self.dtype = ctypes.byref(b), _TORCH.get(b.dtype)
+        self.dtype = _TORCH.get(b.dtype)
         rows, stride = b.n_groups * b.n_beams, b.logit_stride or b.n_vocab
         self.flat, self.flat_strides = (rows, b.n_vocab), (stride, 1)
         self.grouped, self.stride, self.many = (b.n_groups, b.n_beams, b.n_vocab), stride, (b.n_groups > 1, b.n_beams > 1, b.n_vocab > 1)
@@ -710,7 +710,7 @@ def restkv_beam_select(b: RestkvBeams, logits, scores, new_scores, parents, toke
     fn = None if finished is None else _check_flat(what, dev, finished, told.finished)
     nf = None if new_finished is None else _check_flat(what, dev, new_finished, told.new_finished)
     wp, wn = _take_workspace(what, dev, workspace)
-    _on_gpu(dev, stream, what, lib().restkv_beam_select, told.ref, logits.data_ptr(), sc, fn, ns, ps, tk, nf, wp, wn)
+    _on_gpu(dev, stream, what, lib().restkv_beam_select, b, logits.data_ptr(), sc, fn, ns, ps, tk, nf, wp, wn)
 
 
 class CacheLayers:
@@ -739,7 +739,7 @@ def restkv_beam_reorder(c: RestkvCache, n_beams, parents, table, lens, layers, t
     if parents.dtype is not torch.int32 or parents.get_device() != dev or dev < 0 or parents.shape != (n_groups, n_beams) or \
             (st[1] != 1 and n_beams > 1) or (n_groups > 1 and st[0] < n_beams):
         raise RestkvError(-1, f"{what}: parents have to be int32 [{n_groups}, {n_beams}] on GPU {dev}, rows that do not overlap")
-    _on_gpu(dev, stream, what, lib().restkv_beam_reorder, told.ref, n_beams, parents.data_ptr(), st[0] if n_groups > 1 else 0, ln, tb, to,
+    _on_gpu(dev, stream, what, lib().restkv_beam_reorder, c, n_beams, parents.data_ptr(), st[0] if n_groups > 1 else 0, ln, tb, to,
             layers.array, len(layers.pages))
 
 
@@ -773,7 +773,7 @@ def restkv_attend_beams(c: RestkvCache, n_beams, shared, q, pages: CachePages, t
     """restkv_attend where the tables of each n_beams neighbouring sequences begin with the same shared[group] pages (int32), which
     are read once for all of them."""
     what, told = "restkv_attend_beams", _told(c)
-    dev, ref = _check_pages(what, c, told, pages), told.ref
+    dev, desc = _check_pages(what, c, told, pages), c
     of = told.shared.get(n_beams)
     if of is None:
         of = told.shared[n_beams] = ((told.n_seqs // max(n_beams, 1),), torch.int32, "shared", None)
@@ -783,7 +783,7 @@ def restkv_attend_beams(c: RestkvCache, n_beams, shared, q, pages: CachePages, t
     outs = _check_rows(what, dev, told.out_dtype, "out", out, told.q, told.out_stride)
     ls = told.lse_stride if lse is None else _check_rows(what, dev, torch.float32, "lse", lse, told.lse, told.lse_stride)
     if qs is not told.q_stride or outs is not told.out_stride or ls is not told.lse_stride:
-        ref = _as_strided(c, q=qs, out=outs, lse=ls)
+        desc = _as_strided(c, q=qs, out=outs, lse=ls)
     wp, wn = _take_workspace(what, dev, workspace)
-    _on_gpu(dev, stream, what, lib().restkv_attend_beams, ref, n_beams, sh, q.data_ptr(), pages.k.data_ptr(), pages.v.data_ptr(),
+    _on_gpu(dev, stream, what, lib().restkv_attend_beams, desc, n_beams, sh, q.data_ptr(), pages.k.data_ptr(), pages.v.data_ptr(),
             _addr(pages.k_scale), _addr(pages.v_scale), tb, ln, ns, out.data_ptr(), _addr(lse), wp, wn)
