@@ -132,26 +132,10 @@ __device__ __forceinline__ int above(const unsigned long long* list, int n, unsi
   }
   return rank;
 }
-__device__ __forceinline__ void zeros_behind(unsigned long long* list, int n) {
-  if ((threadIdx.x & 63) < 8) list[n + (threadIdx.x & 63)] = 0;
-  settle();
-}
-
-// The K best of a list of n entries, to its front; n becomes min(n, K), the answer the K-th best (0: there are fewer).
+// The K <= 64 best of a list of n > 64 entries, to its front; n becomes K, the answer the K-th best.
 template <int LOW>
 __device__ __forceinline__ unsigned long long keep_best(unsigned long long* list, int& n, int K) {
   const int lane = threadIdx.x & 63;
-  if (n < K) return 0;
-  if (n <= 64) {                       // each entry's place by counting
-    const unsigned long long e = lane < n ? list[lane] : 0;
-    zeros_behind(list, n);
-    const int rank = above(list, n, e);
-    __builtin_amdgcn_wave_barrier();
-    if (lane < n && rank < K) list[rank] = e;
-    settle();
-    n = K;
-    return list[K - 1];
-  }
   uint32_t hi[SEL_OWN], lo[SEL_OWN];
 #pragma unroll
   for (int j = 0; j < SEL_OWN; ++j) {
@@ -242,7 +226,7 @@ __global__ __launch_bounds__(SEL_THREADS) void k_select_rows(SelectArgs a) {
   __shared__ float s_max[NW];
   __shared__ int s_count;
   __shared__ __align__(16) uint32_t s_bound[132];
-  __shared__ __align__(16) unsigned long long s_list[NW][SEL_LIST + 8], s_all[SEL_THREADS + 8];
+  __shared__ __align__(16) unsigned long long s_list[NW][SEL_LIST], s_all[SEL_THREADS + 8];
   const int64_t id = wide_block();
   const int64_t row = id / a.pieces;
   const int piece = (int)(id % a.pieces), V = a.b.n_vocab, K = a.b.n_out, tid = threadIdx.x, lane = tid & 63;
@@ -339,7 +323,7 @@ __global__ __launch_bounds__(SEL_THREADS) void k_select_rows(SelectArgs a) {
       }
     }
   }
-  if (n > 64) keep_best<LOW>(list, n, K);
+  if (n > 64) keep_best<LOW>(list, n, K);        // (at most 64 go on, a lane each)
   const float wm = lanes_join<64>(m, MaxF());
   // (a thread of which everything is masked out has a sum of 0; a NaN stays one)
   sum *= m == wm ? 1.0 : (double)exp_of(m - wm);
