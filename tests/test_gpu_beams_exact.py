@@ -1,4 +1,5 @@
-"""Selection of beams on the GPU held to what the header says of its arithmetic: places, pairs and flags one by one, sums and scores in 64 bits."""
+"""Selection of beams on the GPU held to what the header says of its arithmetic: places, pairs and flags one by one, sums and scores in 64 bits, and the
+join of long lists (more continuations at the bound than it holds) for each number of its wavefronts."""
 import math
 
 import pytest
@@ -98,6 +99,42 @@ def test_every_place_of_few_values(dtype):
     for beams, vocab, n_out in ((4, 9000, 64), (16, 20000, 33), (7, 40000, 12)):
         x = torch.randint(-3, 4, (2 * beams, vocab), generator=g).to(dtype).cuda()
         check(x, -torch.rand((2, beams), generator=g), None, n_out)
+
+
+# beams, vocabulary in float32 and bfloat16, n_out, wavefronts of the join
+JOINS = [(2, 9000, 17000, 64, 4), (8, 5000, 9000, 64, 8), (16, 30000, 30000, 64, 16), (64, 700, 700, 64, 16)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("beams,vocab32,vocab16,n_out,waves", JOINS)
+def test_more_continuations_at_the_bound_than_the_join_lists(beams, vocab32, vocab16, n_out, waves, dtype):
+    vocab = vocab32 if dtype is torch.float32 else vocab16
+    pieces = -(-(vocab * dtype.itemsize // 16 + 1) // 1024)
+    left = beams * pieces * n_out
+    assert left > 64 * waves and waves == (16 if left > 1024 else 8 if left > 512 or beams >= 8 else 4)
+    same, equal = torch.zeros((2 * beams, vocab), dtype=dtype, device="cuda"), torch.zeros((2, beams))
+    want = list(range(n_out))
+    for x in (same, same - 5.5):                                   # sums that are exact: the lowest beam's lowest tokens
+        got = check(x, equal, None, n_out, end=vocab - 1, tie_exact=True)
+        assert got[1].tolist() == [[0] * n_out] * 2 and got[2].tolist() == [want] * 2
+    # half of the beams have ended: their continuations come first, in order, then the lowest of the others
+    ended = torch.arange(beams).expand(2, -1) % 2 == 0
+    got = check(same, equal, ended, n_out, end=3, tie_exact=True)
+    first = list(range(0, beams, 2))
+    assert got[1].tolist() == [(first + [1] * n_out)[:n_out]] * 2
+    # ended ones far behind: none of them, but the lowest of the others; and those all ended
+    low = torch.where(ended, torch.tensor(-100.0), torch.tensor(0.0))
+    got = check(same, low, ended, n_out, tie_exact=True)
+    assert got[1].tolist() == [[1] * n_out] * 2 and got[2].tolist() == [want] * 2
+    check(same, equal, torch.ones((2, beams)), n_out, tie_exact=True)
+    # one beam ahead of equal ones, which fill the list first or not: bounds are taken again
+    scores = equal - 50
+    scores[0, beams - 1], scores[1, beams // 2] = 0, 0
+    x = same.clone()
+    x[beams - 1].normal_(generator=torch.Generator("cuda").manual_seed(1))
+    runs = [check(x, scores, None, n_out) for _ in range(5)]
+    assert runs[0][1].tolist() == [[beams - 1] * n_out, [beams // 2] * n_out]
+    assert all(torch.equal(a, b) for r in runs[1:] for a, b in zip(r, runs[0]))       # whatever arrives first
 
 
 @pytest.mark.parametrize("dtype", TYPES)
