@@ -413,7 +413,8 @@ typedef struct restkv_beams {
  *   new_finished [n_groups, n_out] int32 out, may be NULL: 1 where the token is end_token or the beam had ended
  * new_scores may be scores, and new_finished may be finished, if n_out = n_beams.
  * Exponentials are float32, and summed in float32 up to 32 at a time (sums of these, logarithms and scores 64 bits); scores are ordered
- * in 64 bits and rounded once.  Results do not depend on timing: no atomics.
+ * in 64 bits and rounded once.  Results do not depend on timing: places follow from the order of the continuations (a counter only says where
+ * in a list one is kept until then).
  * Workspace: restkv_beam_workspace_bytes(b), 256-byte aligned, whatever it holds; calls that run at the same time need one each.
  */
 size_t restkv_beam_workspace_bytes(const restkv_beams* b);

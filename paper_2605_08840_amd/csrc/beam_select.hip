@@ -479,7 +479,8 @@ __global__ __launch_bounds__(64 * NW) void k_select_join(SelectArgs a) {
   __syncthreads();
   int n = s_count[0];
   for (int round = 1; n > 128 && round < JOIN_ROUNDS; ++round) {
-    // (of a list that has overflowed what is in it will do: as many reach the bound)
+    // (of a list that has overflowed what is in it will do: as many reach the bound.  Which ones are in it depends on who came first, and so may
+    // this bound, but not the answer: any bound that K continuations reach leaves the K best in)
     const int i = tid % NW * 64 + tid / NW;            // (neighbours to other groups)
     const Cont x = i < n ? Cont{s_scores[i], s_rests[i]} : Cont{0, 0};
     const uint32_t next = block_bound<JOIN_LIST>((uint32_t)(x.score >> 32), K, s_bound);
