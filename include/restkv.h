@@ -449,7 +449,10 @@ int restkv_beam_reorder(const restkv_cache* c, int32_t n_beams, const int32_t* p
  *          head, with tables per head).  Values below 0 count as 0; pages beyond what every beam of the group with new tokens
  *          has seen before them are each beam's own.
  * Everything else, the result too, as restkv_attend says (n_beams 1 .. 64).  Where the tables differ after all, a beam sees its own
- * pages there or the first beam's, by sizes.  Workspace: restkv_attend_beams_workspace_bytes(c, n_beams).
+ * pages there or the first beam's, by sizes.  Workspace: restkv_attend_beams_workspace_bytes(c, n_beams).  Beside caches that are read as
+ * restkv_attend does, it has room for two sums of d + 2 floats for every query row of n_seqs * max_new * n_q_heads, and some more: 1.05 GiB for
+ * 64 sequences with 512 new tokens each and 32 heads of 128 (restkv_attend: 81 MiB), so long prompts of beams go through restkv_attend.  May be refused
+ * (RESTKV_EUNSUPPORTED): n_beams * max_new * n_q_heads / n_kv_heads of 2^24 and more, n_seqs * max_new * n_q_heads of 2^29 and more.
  */
 size_t restkv_attend_beams_workspace_bytes(const restkv_cache* c, int32_t n_beams);
 int restkv_attend_beams(const restkv_cache* c, int32_t n_beams, const int32_t* shared, const void* q, const void* k_pages,
