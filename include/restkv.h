@@ -358,7 +358,8 @@ int restkv_append(const restkv_cache* c, const void* k, const void* v, void* k_p
  * (with bf16 and 4-bit pages an infinity may come out as NaN).  With out_dtype RESTKV_F32, out_stride_h = W*d, out_stride_t = d,
  * lse_stride_h = W and lse_stride_t = 1 one sequence's W queries give what restkv_score_from_attention takes.
  * Logits, statistics and sums are float32 (bf16 products are exact in it); softmax weights enter the products with
- * values to 2^-17, with float32 output to 2^-24.  Results do not depend on timing: no atomics.
+ * values to 2^-17, with float32 output to 2^-24 (of 4-bit pages with 16 + code, or code - 8, steps; what is between these and the value
+ * is added in float32).  Results do not depend on timing: no atomics.
  * Workspace: restkv_attend_workspace_bytes(c), 256-byte aligned, whatever it holds; none where that returns 0.  Calls, or
  * replays of captured ones, that run at the same time need one each.
  */

@@ -273,7 +273,9 @@ BeamsWs beams_ws(const Pages& pg, const BeamsPlan& p) {
 // 19.1 / 19.6; 4 bits 40 MB 19.4 / 21.1, 80 MB 28.5 / 21.7; float32 33 MB 15.9 / 17.0, 65 MB 19.3 / 17.2.  A list takes a launch, and 3 us
 // for each 32 beams: so / by a list, MiB that the caches may hold: bf16, 12 beams with lengths per head 99 19.5 / 20.9, 32 136 22.0 / 23.2, 64 144
 // 20.6 / 23.0 and 208 26.1 / 24.2, 80 180 25.0 / 26.4, 160 200 30.1 / 33.1 and 360 45.9 / 35.6; float32, 64 160 22.4 / 25.2 and 288 32.1 / 30.9; 4 bits,
-// 32 42 19.9 / 23.1, 64 65 21.6 / 25.1, 80 106 36.2 / 30.2, 160 62 31.0 / 39.7 and 112 42.0 / 42.4.
+// 32 42 19.9 / 23.1, 64 65 21.6 / 25.1, 80 106 36.2 / 30.2, 160 62 31.0 / 39.7 and 112 42.0 / 42.4.  Around the limit for 64 beams of 4 bits, 80 MiB, as
+// 16 groups of four (as 32 of two, eight of eight or four of 16 within 2 us): 75 21.8 / 26.6, 80 22.1 / 26.7, 85 24.4 / 26.9, 100 25.0 / 29.0, 115 27.6 / 29.2: it
+// is on the early side there, by up to 4 us; 160 beams 162 48.5 / 44.2.
 std::atomic<int> g_force_shared{0};
 bool as_if_alone(const Pages& pg, int n_beams, const BeamsPlan& p) {
   if (n_beams == 1 || g_force_shared) return n_beams == 1;
