@@ -238,8 +238,8 @@ BeamsPlan beams_plan(const Pages& pg, int n_beams) {
     p.groups = p.target / (p.Hy * p.front_blocks);
     p.front_slots = p.groups + 64;
     p.slots = p.groups * p.front_blocks + 64;
-    // (what 64 parts cost has to be below 2^32)
-    while (((pg.max_len / ATT_TILE >> p.coarse) + 4) * 2 * 64 * p.front_blocks > (int64_t)1 << 31) ++p.coarse;
+    // (what 64 parts cost has to be below 2^32; of 2^30 positions it passes 2^31)
+    while (((int64_t)(pg.max_len / ATT_TILE >> p.coarse) + 4) * 2 * 64 * p.front_blocks > (int64_t)1 << 31) ++p.coarse;
   } else {
     // chunks: one for each entry with tiles, and as many more as make up what runs at a time
     p.at_a_time = std::max<int64_t>(1, p.target / p.Hy);

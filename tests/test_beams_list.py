@@ -72,3 +72,13 @@ def test_refusals(rk):  # noqa: F811
     with pytest.raises(rk.RestkvError):
         rk.restkv_debug_beams_list(cache(rk, 256, max_len=64), 2, [1] * 384)       # as if each were alone
     assert rk.lib().restkv_debug_beams_list(rk.binding.ctypes.byref(c), 2, None, None) == -1
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_sizes_of_the_longest_caches_are_worked_out_in_64_bits(rk, fmt):  # noqa: F811
+    """Parts cut evenly, with room for 2^30 positions a sequence: what 64 parts cost passes 2^31 (an overflow shows under the sanitizer)."""
+    for groups, n_beams, hq in ((1, 2, 1), (2, 2, 8), (1, 40, 8), (3, 20, 2)):
+        c = cache(rk, groups * n_beams, fmt, n_q_heads=hq)
+        assert rk.restkv_attend_beams_workspace_bytes(c, n_beams) > 0
+        c.max_len = (1 << 30) - 1
+        assert rk.restkv_attend_beams_workspace_bytes(c, n_beams) > 0
