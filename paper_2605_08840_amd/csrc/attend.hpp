@@ -33,7 +33,7 @@ struct AttendArgs {
   // head), the rows of all its beams for them; then each sequence's own positions behind these.  An entry times a block of rows is a
   // part: front_blocks of each of the former, own_blocks of each of the latter.  plan[part] {first, last} slot (first > last: none);
   // front_*: [slots of fronts * Hy, rows of a block], part_*: [slots * Hy, rows of a sequence].  spread: parts are cut evenly over
-  // the teams of workgroups of a head, of which there are `chunks` (beams_work); else a workgroup takes a chunk of an entry
+  // the teams of workgroups of a head, of which there are `chunks` (cut_parts); else a workgroup takes a chunk of an entry
   // for a block of rows, and k_beams_list has written which: list[2 u], [2 u + 1] {entry (-1: none), tiles from, to, slot}, {positions, first
   // row, new tokens}, of up to front_chunks chunks of fronts, then up to own_chunks of the rest.
   const int32_t* shared;
@@ -399,18 +399,6 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t x, int i, uint32_t mask, 
   return __builtin_amdgcn_perm(__float_as_uint(__uint_as_float(w & 0xFFFF0000u) - 24.f), __float_as_uint(__uint_as_float(w << 16) - 24.f), 0x07060302u);
 }
 
-// FMT: pages; T: queries; R: blocks of 16 rows of a wavefront; NP: bf16 parts of a softmax weight (products with float32 pages take
-// the weight itself).  Three hold all its bits, for float32 output.  bf16 output has two, 2^-17 beside the 2^-8 of its own rounding: 0.2 % of
-// its values (4 bits, 16 + code in place of the code: 1.5 %) are not the nearest bf16 but its neighbour, where sums in float32 leave 0.03 to 0.2 %,
-// and the error against 64 bits is the same, 1.7e-3 of the norm.  Three parts there take up to 2 % more time with few rows of bf16 pages, 12 % with
-// many, 3 to 15 % with 4 bits (and leave 0.8 %), centred codes 28 to 45 % (0.2 %).
-// Of a tile the keys are loaded anew (for the next one) as soon as the logits are there, the
-// values as soon as they are in the sums: a load has the other half's arithmetic, and other wavefronts', to come back,
-// and costs no second set of registers.
-// SP (4-bit pages, up to 16 / SP rows): the sixteen columns are SP copies of the rows, and copy x takes the 16-key blocks x,
-// SP + x, ...: its queries are zeros in the products of other blocks, which add up in one set of registers, and its weights
-// are zeros in those blocks' products with values.  The matrix pipe does as much as before, but a lane scales, exponentiates
-// and splits 1 / SP of the keys, which is what bounds this format: four rows, 128k tokens 47.7 -> 39.2 us.
 // Row of the token tensors for place `tok` of a group's new tokens, max_new for each beam from sequence s on (places that a beam does not
 // have hold another's; nobody reads what comes of them).
 __device__ __forceinline__ int front_token(const Pages& pg, int s, int tok) {
@@ -568,6 +556,18 @@ __device__ __forceinline__ bool listed_part(const AttendArgs& a, int& hy, Chunk&
   return true;
 }
 
+// FMT: pages; T: queries; R: blocks of 16 rows of a wavefront; NP: bf16 parts of a softmax weight (products with float32 pages take
+// the weight itself).  Three hold all its bits, for float32 output.  bf16 output has two, 2^-17 beside the 2^-8 of its own rounding: 0.2 % of
+// its values (4 bits, 16 + code in place of the code: 1.5 %) are not the nearest bf16 but its neighbour, where sums in float32 leave 0.03 to 0.2 %,
+// and the error against 64 bits is the same, 1.7e-3 of the norm.  Three parts there take up to 2 % more time with few rows of bf16 pages, 12 % with
+// many, 3 to 15 % with 4 bits (and leave 0.8 %), centred codes 28 to 45 % (0.2 %).
+// Of a tile the keys are loaded anew (for the next one) as soon as the logits are there, the
+// values as soon as they are in the sums: a load has the other half's arithmetic, and other wavefronts', to come back,
+// and costs no second set of registers.
+// SP (4-bit pages, up to 16 / SP rows): the sixteen columns are SP copies of the rows, and copy x takes the 16-key blocks x,
+// SP + x, ...: its queries are zeros in the products of other blocks, which add up in one set of registers, and its weights
+// are zeros in those blocks' products with values.  The matrix pipe does as much as before, but a lane scales, exponentiates
+// and splits 1 / SP of the keys, which is what bounds this format: four rows, 128k tokens 47.7 -> 39.2 us.
 template <int FMT, typename T, int D, int NP, int R, int SP, int BEAMS>
 __global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(2)))
 void k_attend(AttendArgs a) {
